@@ -86,8 +86,9 @@ enum {
                                     lists, two or four for short ones, see there) */
     SI_FLAG_SIMPLE_KERNELS = 256u, /* decode: one plain-load kernel pair per step instead of the
                                      persistent bulk-copy kernel (kept for cross-checking) */
-    SI_FLAG_PRENORM = 512u       /* si_decode_chain_forward: the FFN sees its input scaled to unit root mean
+    SI_FLAG_PRENORM = 512u,      /* si_decode_chain_forward: the FFN sees its input scaled to unit root mean
                                     square, as the FFN of a pre-norm transformer block does */
+    SI_FLAG_ACC_WEIGHT = 1024u   /* si_attn_decode: add the attention every entry receives to kv->weight */
 };
 
 /* selection modes for si_select */
@@ -415,6 +416,100 @@ int si_shard_lists(const int32_t *idx, const int32_t *idx_offsets, int k_fixed, 
                    void *stream);
 int si_shard_reduce(const float *const *parts_dev, int world, const void *x, int x_dtype, int T, int d_model,
                     void *y, int y_dtype, unsigned flags, void *stream);
+
+/* ---------------------------------------------------------------- attention over a key/value cache
+ *
+ * The other half of a decoder layer, beside the selective FFN: attention over a cache of keys and values in which
+ * -- as with the neurons -- only what matters is kept.  The cache of ONE layer is described by the caller:
+ *
+ *   k, v        device, 16-bit elements of `dtype`.  Element c of entry j of head h of sequence b lies at
+ *               b * seq_stride + h * head_stride + j * row_stride + c (elements; the same for k and v; multiples of 8,
+ *               so that every row starts on 16 bytes).  Head-major caches [n_seqs, n_kv_heads, capacity, head_dim]
+ *               and token-major ones [n_seqs, capacity, n_kv_heads, head_dim] are both plain settings of the strides.
+ *   len         device int32 [n_seqs]: entries in use, 0 .. capacity (a value outside is clamped and reported as
+ *               SI_ERR_OUT_OF_RANGE).  Entries from len[b] on are never part of a result, whatever they hold.
+ *   pos         device int32 [n_seqs, n_kv_heads, capacity]: the position in the sequence of every entry, any order,
+ *               different per head after an eviction; or NULL: entry j is at position j.
+ *   weight      device float32 [n_seqs, n_kv_heads, capacity]: the attention every entry has received so far; NULL
+ *               where no call needs it.
+ *   head_dim 64 or 128 (SI_ERR_UNSUPPORTED otherwise); n_q_heads is a multiple of n_kv_heads and query heads
+ *   h * G .. h * G + G - 1 (G = n_q_heads / n_kv_heads, at most 128) read key/value head h.
+ *
+ * An entry at position p is visible to a query at position s if
+ *       p <= s   and   ( window == 0   or   p > s - window   or   p < n_sink ),
+ * i.e. causal attention, with window > 0 restricted to the last `window` positions (the query's own included) and the
+ * first n_sink positions, which stay visible.  out = sum_j p_j v_j with p the softmax of scale * (q . k_j) over the
+ * visible entries; a query that sees no entry gets out = 0 and lse = -inf.  lse (optional) is the natural logarithm
+ * of the sum of exp(scale * (q . k_j)).  Scores, softmax and sums are fp32; p is rounded to the cache's type for the
+ * product with v; out has the cache's type. */
+typedef struct si_kv {
+    void *k, *v;
+    float *weight;
+    int32_t *pos;
+    const int32_t *len;
+    long long seq_stride, head_stride, row_stride;
+    int n_seqs, n_kv_heads, head_dim, capacity, dtype;
+} si_kv_t;
+
+/* Device scratch for the calls below on this cache with at most n_q_heads query heads and T queries per sequence
+ * (n_q_heads = 0: si_kv_evict only).  256-byte aligned, never read before it is written: it needs no clearing. */
+int si_kv_workspace_bytes(const si_kv_t *kv, int n_q_heads, int T, size_t *bytes_out);
+
+/* Prefill: the queries of the LAST T positions of every sequence (their keys and values are already in the cache;
+ * query i of sequence b is at position len[b] - T + i; a negative one -- a sequence shorter than T -- sees nothing).
+ *   q       device [n_seqs, T, n_q_heads, head_dim]; sequences and tokens q_seq_stride / q_tok_stride elements apart
+ *           (multiples of 8), the heads of a token contiguous: a slice of a fused projection's output is fine
+ *   out     device [n_seqs, T, n_q_heads, head_dim], contiguous
+ *   lse     device float32 [n_seqs, T, n_q_heads], or NULL
+ * Needs kv->pos == NULL (SI_ERR_UNSUPPORTED otherwise: a prompt is prefilled before anything is evicted).  A value
+ * that is infinite or NaN below len[b] may reach every query processed with it, also ones it is hidden from. */
+int si_attn_prefill(const si_kv_t *kv, const void *q, long long q_seq_stride, long long q_tok_stride, int T,
+                    int n_q_heads, int window, int n_sink, float scale, void *out, float *lse, void *workspace,
+                    size_t ws_bytes, int32_t *status_dev, void *stream);
+
+/* The attention every entry received from those T queries, added to kv->weight (the caller zeroes it for a new
+ * prompt): weight[b, h, j] += sum over the T queries i that see j and the G query heads of exp(scale * (q_i . k_j)
+ * - lse_i).  lse: device float32 [n_seqs, T, n_q_heads] from si_attn_prefill with the same arguments.  T may be the
+ * whole prompt or only its last few positions.  Needs kv->weight and kv->pos == NULL.  Sums are taken in a fixed
+ * order: repeated calls add the same bits. */
+int si_attn_weights(const si_kv_t *kv, const void *q, long long q_seq_stride, long long q_tok_stride, int T,
+                    int n_q_heads, int window, int n_sink, float scale, const float *lse, void *workspace,
+                    size_t ws_bytes, int32_t *status_dev, void *stream);
+
+/* Decode: one query per sequence.
+ *   q        device [n_seqs, n_q_heads, head_dim], sequences q_seq_stride elements apart
+ *   q_pos    device int32 [n_seqs]: position of the query; NULL (only with kv->pos == NULL): the last entry's
+ *   k_new, v_new   device [n_seqs, n_kv_heads, head_dim], sequences new_seq_stride elements apart, or both NULL.  Given,
+ *            they are the query's own key and value: the call stores them as entry len[b] (position q_pos[b]) and
+ *            attends to len[b] + 1 entries.  len itself is not changed -- one array serves all layers, so the caller
+ *            advances it once per token.  A full cache (len[b] == capacity) is SI_ERR_OUT_OF_RANGE in *status_dev;
+ *            nothing is stored for it.
+ *   out      device [n_seqs, n_q_heads, head_dim]; lse device float32 [n_seqs, n_q_heads] or NULL
+ *   flags    SI_FLAG_ACC_WEIGHT: weight[b, h, j] += sum over the G query heads of p_j (the new entry's weight is set
+ *            to its own sum); needs kv->weight.
+ * The bytes of the visible entries are read once; the work is split evenly over the SMs whatever the lengths. */
+int si_attn_decode(const si_kv_t *kv, const void *q, long long q_seq_stride, int n_q_heads, const int32_t *q_pos,
+                   const void *k_new, const void *v_new, long long new_seq_stride, int window, int n_sink,
+                   float scale, void *out, float *lse, unsigned flags, void *workspace, size_t ws_bytes,
+                   int32_t *status_dev, void *stream);
+
+/* Eviction: every head of every sequence keeps at most `budget` of its len[b] + n_new entries (n_new: 1 after a
+ * si_attn_decode that stored a new entry, 0 otherwise).  Kept first are the entries whose position is below n_sink or
+ * above q_pos[b] - n_recent (n_sink + n_recent <= budget), then those with the largest weight; ties go to the lower
+ * slot, NaN ranks below every number.  A kept entry in a slot below `budget` keeps its slot; the kept entries beyond
+ * fill the freed slots, both in ascending order, so that as little as possible moves (the order of entries means
+ * nothing to attention; kv->pos goes along).
+ *   src      the cache, with weight; pos may be NULL (entry j at position j)
+ *   dst      where the kept entries go, with pos and weight, capacity >= budget, the same n_seqs, n_kv_heads, head_dim
+ *            and dtype; dst->len is not read.  dst == src (or the same k) evicts in place and needs src->pos; dst may
+ *            not overlap src otherwise -- the decode cache of a prompt that was prefilled into scratch memory.
+ *   q_pos    device int32 [n_seqs]: the newest position; NULL (only with src->pos == NULL): len[b] + n_new - 1
+ *   kept     device int32 [n_seqs, n_kv_heads, budget] or NULL: the source slot of every slot of dst, -1 beyond
+ *   len_out  device int32 [n_seqs] or NULL: min(len[b] + n_new, budget); may be src->len or dst->len
+ * Integer decisions on given weights: the result is exact and unique. */
+int si_kv_evict(const si_kv_t *src, const si_kv_t *dst, const int32_t *q_pos, int n_new, int budget, int n_sink,
+                int n_recent, int32_t *kept, int32_t *len_out, void *workspace, size_t ws_bytes, int32_t *status_dev,
+                void *stream);
 
 /* Library build information: "sm_100a" etc.  Never NULL. */
 const char *si_build_info(void);

@@ -29,6 +29,7 @@ SI_FLAG_LIST_PER_LAYER = 64
 SI_FLAG_STEPS_ANY_ORDER = 128
 SI_FLAG_SIMPLE_KERNELS = 256
 SI_FLAG_PRENORM = 512
+SI_FLAG_ACC_WEIGHT = 1024
 SI_SELECT_TOPK, SI_SELECT_THRESHOLD = 0, 1
 
 EXPORTS = [
@@ -40,6 +41,7 @@ EXPORTS = [
     "si_debug_read_bandwidth", "si_prefill_vote_workspace_bytes", "si_prefill_vote", "si_prefill_forward", "si_layer_range", "si_profile_accumulate", "si_profile_merge", "si_profile_rank",
     "si_loadset", "si_shard_count", "si_shard_lists", "si_shard_reduce", "si_ffn_forward_sharded",
     "si_debug_ffn_forward_sharded_group", "si_debug_pair_plan",
+    "si_kv_workspace_bytes", "si_attn_prefill", "si_attn_weights", "si_attn_decode", "si_kv_evict",
 ]
 
 
@@ -98,6 +100,12 @@ def _load_library() -> ctypes.CDLL:
     lib.si_debug_ffn_forward_sharded_group.argtypes = [vp, ci, ci, ci, ci, vp, vp, vp, vp, ci, cu, vp, vp, cu, vp, sz,
                                                        ctypes.c_longlong, vp, vp]
     lib.si_prefill_forward.argtypes = [vp, ci, vp, ci, vp, ci, ci, ci, ci, ci, cu, vp, ci, vp, vp, vp, sz, vp, sz, vp, vp]
+    ll, cf = ctypes.c_longlong, ctypes.c_float
+    lib.si_kv_workspace_bytes.argtypes = [vp, ci, ci, psz]
+    lib.si_attn_prefill.argtypes = [vp, vp, ll, ll, ci, ci, ci, ci, cf, vp, vp, vp, sz, vp, vp]
+    lib.si_attn_weights.argtypes = [vp, vp, ll, ll, ci, ci, ci, ci, cf, vp, vp, sz, vp, vp]
+    lib.si_attn_decode.argtypes = [vp, vp, ll, ci, vp, vp, vp, ll, ci, ci, cf, vp, vp, cu, vp, sz, vp, vp]
+    lib.si_kv_evict.argtypes = [vp, vp, vp, ci, ci, ci, ci, vp, vp, vp, sz, vp, vp]
     for name in EXPORTS:
         fn = getattr(lib, name)
         if name not in ("si_strerror", "si_build_info", "si_last_cuda_error"):
@@ -416,6 +424,112 @@ def si_debug_ffn_forward_waits(handle, layer: int, x, T: int, idx, idx_offsets, 
                                            dtype_code(y.dtype), flags, _dp(workspace),
                                            workspace.numel() * workspace.element_size(), _dp(status),
                                            _stream(stream), spin_limit, withhold), "si_debug_ffn_forward_waits")
+
+
+# ------------------------------------------------------------------------- attention over a key/value cache
+
+class _KvDesc(ctypes.Structure):
+    """si_kv_t"""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("pos", ctypes.c_void_p),
+                ("len", ctypes.c_void_p), ("seq_stride", ctypes.c_longlong), ("head_stride", ctypes.c_longlong),
+                ("row_stride", ctypes.c_longlong), ("n_seqs", ctypes.c_int), ("n_kv_heads", ctypes.c_int),
+                ("head_dim", ctypes.c_int), ("capacity", ctypes.c_int), ("dtype", ctypes.c_int)]
+
+
+class KVCache:
+    """Description (si_kv_t) of one layer's cache over tensors of the caller, which it keeps alive.
+
+    k, v: [n_seqs, n_kv_heads, capacity, head_dim] views with equal strides, the last dimension contiguous (a
+    token-major cache is passed as its transpose(1, 2)); length: int32 [n_seqs]; pos (optional) int32 and weight
+    (optional) float32 [n_seqs, n_kv_heads, capacity], contiguous."""
+
+    def __init__(self, k, v, length, pos=None, weight=None):
+        if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.stride(3) != 1 or k.dtype != v.dtype:
+            raise ValueError("k and v: [n_seqs, n_kv_heads, capacity, head_dim] of one type and equal strides, the last dimension contiguous")
+        B, H, cap, D = k.shape
+        for name, t, shape, dtype in (("length", length, (B,), torch.int32), ("pos", pos, (B, H, cap), torch.int32),
+                                      ("weight", weight, (B, H, cap), torch.float32)):
+            if t is not None and (tuple(t.shape) != shape or t.dtype != dtype):
+                raise ValueError(f"{name}: expected {dtype} of shape {shape}")
+        if not (k.is_cuda and v.is_cuda):
+            raise ValueError("expected CUDA tensors")
+        self.k, self.v, self.length, self.pos, self.weight = k, v, length, pos, weight
+        self.n_seqs, self.n_kv_heads, self.capacity, self.head_dim = B, H, cap, D
+        self.desc = _KvDesc(k.data_ptr(), v.data_ptr(), _dp(weight).value, _dp(pos).value, _dp(length).value, k.stride(0),
+                            k.stride(1), k.stride(2), B, H, D, cap, dtype_code(k.dtype))
+        self.ref = ctypes.addressof(self.desc)
+
+    def workspace(self, n_q_heads: int, T: int = 1) -> torch.Tensor:
+        """Scratch for calls with at most n_q_heads query heads and T queries per sequence (0, 0: eviction only)."""
+        return torch.empty(max(si_kv_workspace_bytes(self, n_q_heads, T), 256), dtype=torch.uint8, device=self.k.device)
+
+
+def _shaped(t, name: str, shape, dtype) -> None:
+    if t is not None and (tuple(t.shape) != tuple(shape) or t.dtype != dtype):
+        raise ValueError(f"{name}: expected {dtype} of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+
+
+def _heads(t, name: str, cache, lead) -> ctypes.c_void_p:
+    """[*lead, heads, head_dim] of the cache's type, the heads of a token contiguous -> device pointer."""
+    if t.dtype != cache.k.dtype or t.dim() != len(lead) + 2 or tuple(t.shape[:-2]) != lead or t.shape[-1] != cache.head_dim:
+        raise ValueError(f"{name}: expected {cache.k.dtype} [{', '.join(map(str, lead))}, heads, {cache.head_dim}]")
+    if not t.is_cuda or t.stride(-1) != 1 or (t.shape[-2] > 1 and t.stride(-2) != t.shape[-1]):
+        raise ValueError(f"{name}: expected a CUDA tensor whose heads are contiguous")
+    return ctypes.c_void_p(t.data_ptr())
+
+
+def _ws(t):
+    return (ctypes.c_void_p(0), 0) if t is None else (_dp(t), t.numel() * t.element_size())
+
+
+def si_kv_workspace_bytes(cache: KVCache, n_q_heads: int, T: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(_lib.si_kv_workspace_bytes(cache.ref, n_q_heads, T, ctypes.byref(out)), "si_kv_workspace_bytes")
+    return out.value
+
+
+def si_attn_prefill(cache: KVCache, q, window: int, n_sink: int, scale: float, out, lse, workspace, status=None, stream=None) -> None:
+    """q, out: [n_seqs, T, n_q_heads, head_dim] (q may be strided); lse: float32 [n_seqs, T, n_q_heads] or None."""
+    T, hq = q.shape[1], q.shape[2]
+    qp = _heads(q, "q", cache, (cache.n_seqs, T))
+    _shaped(out, "out", q.shape, q.dtype); _shaped(lse, "lse", q.shape[:3], torch.float32)
+    _check(_lib.si_attn_prefill(cache.ref, qp, q.stride(0), q.stride(1), T, hq, window, n_sink, scale, _dp(out), _dp(lse),
+                                *_ws(workspace), _dp(status), _stream(stream)), "si_attn_prefill")
+
+
+def si_attn_weights(cache: KVCache, q, window: int, n_sink: int, scale: float, lse, workspace, status=None, stream=None) -> None:
+    """Adds to cache.weight; q as for si_attn_prefill, lse: float32 [n_seqs, T, n_q_heads] from it."""
+    T, hq = q.shape[1], q.shape[2]
+    qp = _heads(q, "q", cache, (cache.n_seqs, T))
+    _shaped(lse, "lse", q.shape[:3], torch.float32)
+    _check(_lib.si_attn_weights(cache.ref, qp, q.stride(0), q.stride(1), T, hq, window, n_sink, scale, _dp(lse),
+                                *_ws(workspace), _dp(status), _stream(stream)), "si_attn_weights")
+
+
+def si_attn_decode(cache: KVCache, q, q_pos, k_new, v_new, window: int, n_sink: int, scale: float, out, lse, flags: int,
+                   workspace, status=None, stream=None) -> None:
+    """q, out: [n_seqs, n_q_heads, head_dim]; k_new, v_new: [n_seqs, n_kv_heads, head_dim] of equal strides, or both None."""
+    hq = q.shape[1]
+    qp = _heads(q, "q", cache, (cache.n_seqs,))
+    _shaped(out, "out", q.shape, q.dtype); _shaped(lse, "lse", q.shape[:2], torch.float32)
+    _shaped(q_pos, "q_pos", (cache.n_seqs,), torch.int32)
+    kp = vp = ctypes.c_void_p(0)
+    new_stride = 0
+    if k_new is not None or v_new is not None:
+        if k_new is None or v_new is None or k_new.shape[1] != cache.n_kv_heads or k_new.shape != v_new.shape or k_new.stride() != v_new.stride():
+            raise ValueError("k_new and v_new: [n_seqs, n_kv_heads, head_dim] of equal strides, both or neither")
+        kp, vp, new_stride = _heads(k_new, "k_new", cache, (cache.n_seqs,)), _heads(v_new, "v_new", cache, (cache.n_seqs,)), k_new.stride(0)
+    _check(_lib.si_attn_decode(cache.ref, qp, q.stride(0), hq, _dp(q_pos), kp, vp, new_stride, window, n_sink, scale, _dp(out),
+                               _dp(lse), flags, *_ws(workspace), _dp(status), _stream(stream)), "si_attn_decode")
+
+
+def si_kv_evict(src: KVCache, dst: KVCache, q_pos, n_new: int, budget: int, n_sink: int, n_recent: int, kept, len_out,
+                workspace, status=None, stream=None) -> None:
+    """dst is src: in place.  kept: int32 [n_seqs, n_kv_heads, budget] or None; len_out: int32 [n_seqs] or None."""
+    _shaped(q_pos, "q_pos", (src.n_seqs,), torch.int32); _shaped(len_out, "len_out", (src.n_seqs,), torch.int32)
+    _shaped(kept, "kept", (src.n_seqs, src.n_kv_heads, budget), torch.int32)
+    _check(_lib.si_kv_evict(src.ref, dst.ref, _dp(q_pos), n_new, budget, n_sink, n_recent, _dp(kept), _dp(len_out),
+                            *_ws(workspace), _dp(status), _stream(stream)), "si_kv_evict")
 
 
 # ------------------------------------------------------------------------- owner object

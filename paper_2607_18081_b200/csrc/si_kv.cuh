@@ -1,0 +1,62 @@
+// The key/value cache as the kernels see it, and what the calls on it share: argument checks, which entries a query
+// sees, the status word.
+#pragma once
+#include <limits.h>
+
+#include "si_common.cuh"
+
+struct si_kv_view {
+    uint16_t *k, *v;
+    float *weight;
+    int32_t *pos;
+    const int32_t *len;
+    long long ss, hs, rs;        // element strides: sequence, head, entry
+    int B, H, D, cap;
+    __host__ __device__ long long row(int b, int h, int j) const { return b * ss + h * hs + j * rs; }
+    __host__ __device__ long long meta(int b, int h) const { return ((long long)b * H + h) * cap; }
+};
+
+inline si_kv_view si_kv_view_of(const si_kv_t *kv) {
+    return {(uint16_t *)kv->k, (uint16_t *)kv->v, kv->weight, kv->pos, kv->len, kv->seq_stride, kv->head_stride,
+            kv->row_stride, kv->n_seqs, kv->n_kv_heads, kv->head_dim, kv->capacity};
+}
+
+// Host checks common to all calls on a cache.
+inline int si_kv_check(const si_kv_t *kv) {
+    if (!kv || kv->n_seqs < 0 || kv->n_kv_heads < 1 || kv->capacity < 1 || kv->head_dim < 1) return SI_ERR_INVALID_ARG;
+    if (kv->dtype != SI_F16 && kv->dtype != SI_BF16) return SI_ERR_INVALID_ARG;
+    if (kv->n_kv_heads > 65535 || kv->n_seqs > 65535) return SI_ERR_INVALID_ARG;
+    if (kv->head_dim != 64 && kv->head_dim != 128) return SI_ERR_UNSUPPORTED;
+    if (kv->n_seqs == 0) return SI_OK;
+    if (!kv->k || !kv->v || !kv->len) return SI_ERR_INVALID_ARG;
+    if (kv->row_stride < kv->head_dim || kv->head_stride < 0 || kv->seq_stride < 0) return SI_ERR_INVALID_ARG;
+    if (!si_aligned16(kv->k) || !si_aligned16(kv->v) || ((kv->row_stride | kv->head_stride | kv->seq_stride) & 7)) return SI_ERR_ALIGNMENT;
+    return SI_OK;
+}
+
+// ... and of those that bring queries.
+inline int si_attn_check(const si_kv_t *kv, int n_q_heads, int window, int n_sink, float scale) {
+    const int rc = si_kv_check(kv);
+    if (rc) return rc;
+    if (n_q_heads < 1 || n_q_heads % kv->n_kv_heads || window < 0 || n_sink < 0) return SI_ERR_INVALID_ARG;
+    if (!(scale > -3.0e38f && scale < 3.0e38f)) return SI_ERR_INVALID_ARG;
+    if (n_q_heads / kv->n_kv_heads > 128) return SI_ERR_UNSUPPORTED;
+    return SI_OK;
+}
+
+__device__ __forceinline__ void si_report(int32_t *status, int err) { if (status) atomicCAS(status, 0, err); }
+
+// Entries in use, clamped to the capacity.
+__device__ __forceinline__ int si_kv_len(const si_kv_view &kv, int b, int32_t *status) {
+    const int n = kv.len[b];
+    if (n < 0 || n > kv.cap) { si_report(status, SI_ERR_OUT_OF_RANGE); return n < 0 ? 0 : kv.cap; }
+    return n;
+}
+
+// Visibility of an entry at position p to a query at position s: p <= s and (p > lo or p < n_sink), where lo is the
+// last position in front of the window (below every position when there is no window).
+__device__ __forceinline__ int si_window_lo(int s, int window) {
+    const long long lo = (long long)s - window;
+    return window == 0 || lo < INT_MIN ? INT_MIN : (int)lo;
+}
+__device__ __forceinline__ bool si_visible(int p, int s, int lo, int n_sink) { return p <= s && (p > lo || p < n_sink || lo == INT_MIN); }

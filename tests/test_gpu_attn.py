@@ -1,0 +1,264 @@
+"""GPU parity of attention over the key/value cache -- prefill, single token, accumulated weights -- against the float64
+oracle, within the bounds of attn_utils."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from tests import attn_utils as au
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def api():
+    from paper_2607_18081_b200 import api as _api
+    return _api
+
+
+def _prefill(api, q, k, v, length, window, n_sink, scale, weight=None):
+    cache = api.KVCache(k, v, length, None, weight)
+    B, T, Hq, D = q.shape
+    out = torch.full((B, T, Hq, D), 7.0, dtype=q.dtype, device="cuda")
+    lse = torch.full((B, T, Hq), 7.0, dtype=torch.float32, device="cuda")
+    ws = cache.workspace(Hq, T)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    api.si_attn_prefill(cache, q, window, n_sink, scale, out, lse, ws, status)
+    if weight is not None:
+        api.si_attn_weights(cache, q, window, n_sink, scale, lse, ws, status)
+    torch.cuda.synchronize()
+    assert status.item() == 0
+    return out, lse
+
+
+PREFILL = [
+    # B, T, lens, Hq, Hkv, D, window, n_sink
+    (1, 1, [1], 1, 1, 64, 0, 0),
+    (1, 1, [300], 4, 1, 128, 0, 0),
+    (2, 5, [5, 3], 8, 2, 128, 0, 0),             # the second sequence is shorter than T: rows that see nothing
+    (1, 33, [33], 3, 1, 64, 0, 0),               # three query heads to a key head
+    (2, 130, [130, 257], 6, 2, 128, 0, 0),
+    (1, 200, [333], 7, 1, 64, 17, 3),
+    (1, 129, [129], 2, 2, 128, 1, 0),            # a window of one: every query sees itself only
+    (2, 300, [300, 511], 4, 2, 64, 128, 130),    # more sinks than the window is long
+    (3, 64, [0, 64, 1000], 4, 4, 128, 100, 4),   # an empty sequence
+    (1, 515, [1027], 8, 1, 128, 256, 1),
+    (1, 700, [700], 5, 1, 64, 0, 0),
+    (1, 40, [2100], 32, 4, 128, 0, 0),           # few rows, a long axis
+    (1, 3, [1500], 128, 1, 64, 0, 0),            # 128 query heads on one key head
+    (1, 260, [900], 1, 1, 128, 300, 64),
+]
+
+
+@pytest.mark.parametrize("B,T,lens,Hq,Hkv,D,window,n_sink", PREFILL)
+@pytest.mark.parametrize("dtype,order", [("bf16", "hnd"), ("f16", "nhd")])
+def test_prefill_and_weights(api, B, T, lens, Hq, Hkv, D, window, n_sink, dtype, order):
+    scale = 1.0 / math.sqrt(D)
+    cap = max(lens) + 9
+    q, k, v, length = au.make(B, Hq, Hkv, D, cap, dtype, order, T, 11 * T + D, lens)
+    before = np.random.default_rng(T).random((B, Hkv, cap)).astype(np.float32)
+    weight = torch.from_numpy(before).cuda()
+    out, lse = _prefill(api, q, k, v, length, window, n_sink, scale, weight)
+    ref = au.reference(q, k, v, lens, window, n_sink, scale)
+    au.check_out(out, ref, dtype, D)
+    au.check_lse(lse, ref, D)
+    au.check_weight(weight, before.astype(np.float64), ref, D, T)
+
+
+def test_prefill_with_scores_far_apart_and_negative_scale(api):
+    """Scores of several hundred: the running maximum moves a lot, most weights vanish; a negative scale turns the order."""
+    for scale in (2.0, -0.7):
+        q, k, v, length = au.make(1, 4, 2, 64, 400, "bf16", "hnd", 150, 5, [390], spread=4.0)
+        k[:, :, :390] *= torch.linspace(0.1, 3.0, 390, device="cuda", dtype=k.dtype)[None, None, :, None]   # the maximum keeps growing
+        out, lse = _prefill(api, q, k, v, length, 0, 0, scale)
+        ref = au.reference(q, k, v, [390], 0, 0, scale)
+        au.check_out(out, ref, "bf16", 64)
+        au.check_lse(lse, ref, 64)
+
+
+def test_prefill_is_repeatable_and_leaves_the_cache_alone(api):
+    q, k, v, length = au.make(2, 8, 2, 128, 700, "bf16", "nhd", 400, 3, [700, 555])
+    k0, v0 = k.clone(), v.clone()
+    a, la = _prefill(api, q, k, v, length, 200, 4, 0.09)
+    for _ in range(3):
+        b, lb = _prefill(api, q, k, v, length, 200, 4, 0.09)
+        assert torch.equal(a, b) and torch.equal(la, lb)
+    assert torch.equal(k.view(torch.int16), k0.view(torch.int16)) and torch.equal(v.view(torch.int16), v0.view(torch.int16))
+
+
+DECODE = [
+    # B, lens, Hq, Hkv, D, window, n_sink, positions given, new entry
+    (1, [0], 4, 1, 128, 0, 0, False, True),        # the very first token
+    (1, [1], 1, 1, 64, 0, 0, False, False),
+    (2, [0, 5], 8, 2, 64, 0, 0, False, False),     # an empty cache: nothing to see
+    (3, [6, 16, 17], 8, 2, 128, 0, 0, False, True),
+    (4, [15, 127, 128, 129], 4, 4, 128, 0, 0, False, True),
+    (2, [1000, 31], 24, 8, 128, 0, 0, False, True),
+    (2, [777, 2500], 16, 2, 64, 100, 4, False, True),
+    (1, [5000], 32, 8, 128, 0, 0, False, True),
+    (2, [900, 901], 7, 1, 128, 64, 70, False, True),
+    (1, [600], 20, 1, 64, 0, 0, False, True),      # more query heads to a key head than one matrix tile holds
+    (2, [400, 333], 8, 2, 128, 0, 0, True, True),
+    (2, [400, 2333], 4, 2, 64, 150, 8, True, True),
+    (2, [300, 20], 8, 4, 128, 90, 2, True, False),
+    (40, [3 + 37 * i for i in range(40)], 4, 2, 64, 0, 0, False, True),
+    (1, [3000], 128, 1, 64, 0, 0, False, True),
+]
+
+
+@pytest.mark.parametrize("B,lens,Hq,Hkv,D,window,n_sink,given,new", DECODE)
+@pytest.mark.parametrize("dtype,order,acc", [("bf16", "hnd", True), ("f16", "nhd", False), ("bf16", "nhd", True)])
+def test_decode(api, B, lens, Hq, Hkv, D, window, n_sink, given, new, dtype, order, acc):
+    scale = 1.0 / math.sqrt(D)
+    cap = max(lens) + 5
+    q, k, v, length = au.make(B, Hq, Hkv, D, cap, dtype, order, 1, 7 * Hq + D, lens)
+    rng = np.random.default_rng(B + Hq)
+    before = rng.random((B, Hkv, cap)).astype(np.float32)
+    weight = torch.from_numpy(before).cuda()
+    pos = q_pos = None
+    if given:   # positions with gaps, in no order, other ones per head; the query's is the newest
+        q_pos = torch.tensor([2 * n + 1 for n in lens], dtype=torch.int32, device="cuda")
+        pos = torch.full((B, Hkv, cap), -5, dtype=torch.int32)
+        for b, n in enumerate(lens):
+            for h in range(Hkv):
+                pos[b, h, :n] = torch.from_numpy(rng.permutation(2 * n + 1)[:n].astype(np.int32))
+        pos = pos.cuda()
+    wide = torch.randn(B, 3 * Hkv * D, device="cuda").to(q.dtype)
+    kn, vn = wide[:, :Hkv * D].view(B, Hkv, D), wide[:, Hkv * D:2 * Hkv * D].view(B, Hkv, D)
+    cache = api.KVCache(k, v, length, pos, weight)
+    out = torch.full((B, Hq, D), 7.0, dtype=q.dtype, device="cuda")
+    lse = torch.full((B, Hq), 7.0, dtype=torch.float32, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    k0, v0 = k.clone(), v.clone()
+    api.si_attn_decode(cache, q[:, 0], q_pos, kn if new else None, vn if new else None, window, n_sink, scale, out, lse,
+                       api.SI_FLAG_ACC_WEIGHT if acc else 0, cache.workspace(Hq, 1), status)
+    torch.cuda.synchronize()
+    assert status.item() == 0
+    assert length.tolist() == list(lens)
+    total = [n + 1 if new else n for n in lens]
+    start = before.astype(np.float64)
+    for b, n in enumerate(lens):
+        if new:
+            k0[b, :, n], v0[b, :, n] = kn[b], vn[b]
+            if acc:
+                start[b, :, n] = 0.0
+            if given:
+                assert pos[b, :, n].tolist() == [int(q_pos[b])] * Hkv
+    assert torch.equal(k.view(torch.int16), k0.view(torch.int16)) and torch.equal(v.view(torch.int16), v0.view(torch.int16))
+    ref = au.reference(q, k, v, total, window, n_sink, scale, None if pos is None else pos.cpu().numpy(), None if q_pos is None else q_pos.tolist())
+    au.check_out(out[:, None], ref, dtype, D)
+    au.check_lse(lse[:, None], ref, D)
+    if acc:
+        au.check_weight(weight, start, ref, D, 1)
+    else:
+        assert np.array_equal(weight.cpu().numpy(), before)
+
+
+def test_decode_ignores_what_hidden_entries_hold(api):
+    """NaN and infinities in entries outside the window or after the query, and beyond the length, never reach the result."""
+    for D, Hq, Hkv in ((64, 8, 2), (128, 3, 1)):
+        n, window, n_sink = 700, 50, 3
+        q, k, v, length = au.make(1, Hq, Hkv, D, 720, "bf16", "hnd", 1, 1, [n])
+        ref = au.reference(q, k, v, [n], window, n_sink, 0.1)
+        k[:, :, n_sink:n - window], v[:, :, n_sink:n - window] = float("inf"), float("nan")
+        cache = api.KVCache(k, v, length)
+        out = torch.empty(1, Hq, D, dtype=q.dtype, device="cuda")
+        lse = torch.empty(1, Hq, dtype=torch.float32, device="cuda")
+        api.si_attn_decode(cache, q[:, 0], None, None, None, window, n_sink, 0.1, out, lse, 0, cache.workspace(Hq, 1))
+        au.check_out(out[:, None], ref, "bf16", D)
+        au.check_lse(lse[:, None], ref, D)
+        # the same with positions: every third entry lies after the query
+        pos = torch.arange(720, dtype=torch.int32, device="cuda").expand(1, Hkv, 720).contiguous()
+        pos[..., ::3] += 5000
+        q2, k2, v2, _ = au.make(1, Hq, Hkv, D, 720, "bf16", "hnd", 1, 2, [n])
+        q_pos = torch.tensor([n - 1], dtype=torch.int32, device="cuda")
+        ref = au.reference(q2, k2, v2, [n], 0, 0, 0.1, pos.cpu().numpy(), [n - 1])
+        k2[:, :, ::3], v2[:, :, ::3] = float("nan"), float("inf")
+        cache = api.KVCache(k2, v2, length, pos)
+        api.si_attn_decode(cache, q2[:, 0], q_pos, None, None, 0, 0, 0.1, out, lse, 0, cache.workspace(Hq, 1))
+        au.check_out(out[:, None], ref, "bf16", D)
+        au.check_lse(lse[:, None], ref, D)
+
+
+def test_decode_equals_prefill_of_one_token_and_is_repeatable(api):
+    q, k, v, length = au.make(3, 16, 4, 128, 1300, "f16", "nhd", 1, 9, [1300, 64, 801])
+    cache = api.KVCache(k, v, length)
+    res = []
+    for _ in range(3):
+        out = torch.empty(3, 16, 128, dtype=q.dtype, device="cuda")
+        api.si_attn_decode(cache, q[:, 0], None, None, None, 500, 2, 0.08, out, None, 0, cache.workspace(16, 1))
+        res.append(out)
+    assert torch.equal(res[0], res[1]) and torch.equal(res[0], res[2])
+    ref = au.reference(q, k, v, [1300, 64, 801], 500, 2, 0.08)
+    au.check_out(res[0][:, None], ref, "f16", 128)
+    out, _ = _prefill(api, q, k, v, length, 500, 2, 0.08)
+    au.check_out(out, ref, "f16", 128)
+
+
+def test_caches_whose_offsets_pass_32_bits(api):
+    """Entries more than 2^32 elements apart: a token-major cache of one sequence with a row stride of 2^22 elements."""
+    D, rs, n = 64, 1 << 22, 1100
+    mem = torch.zeros(2, (n - 1) * rs + 4 * D, dtype=torch.bfloat16, device="cuda") if torch.cuda.mem_get_info()[0] > 40 << 30 else None
+    if mem is None:
+        pytest.skip("needs 40 GB free")
+    k, v = (m.as_strided((1, 2, n, D), (0, 2 * D, rs, 1)) for m in mem)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    k.copy_(torch.randn(1, 2, n, D, generator=g, device="cuda")); v.copy_(torch.randn(1, 2, n, D, generator=g, device="cuda"))
+    length = torch.tensor([n], dtype=torch.int32, device="cuda")
+    q = torch.randn(1, 70, 8, D, generator=g, device="cuda").to(torch.bfloat16)
+    weight = torch.zeros(1, 2, n, device="cuda")
+    ref = au.reference(q, k, v, [n], 0, 0, 0.125)
+    out, lse = _prefill(api, q, k, v, length, 0, 0, 0.125, weight)
+    au.check_out(out, ref, "bf16", D)
+    au.check_weight(weight, np.zeros((1, 2, n)), ref, D, 70)
+    cache = api.KVCache(k, v, length)
+    o1 = torch.empty(1, 8, D, dtype=q.dtype, device="cuda")
+    api.si_attn_decode(cache, q[:, -1], None, None, None, 0, 0, 0.125, o1, None, 0, cache.workspace(8, 1))
+    last = {x: ref[x][:, -1:] for x in ("out", "reach", "lse", "size", "n")}
+    au.check_out(o1[:, None], last, "bf16", D)
+
+
+def test_lengths_outside_the_capacity_and_a_full_cache_are_reported(api):
+    q, k, v, _ = au.make(2, 4, 2, 64, 64, "bf16", "hnd", 1, 1, [64, 64])
+    out = torch.empty(2, 4, 64, dtype=q.dtype, device="cuda")
+    kn = torch.zeros(2, 2, 64, dtype=q.dtype, device="cuda")
+    for lens, new in (([65, 3], None), ([-1, 3], None), ([64, 3], kn)):
+        length = torch.tensor(lens, dtype=torch.int32, device="cuda")
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        cache = api.KVCache(k, v, length)
+        k0 = k.clone()
+        api.si_attn_decode(cache, q[:, 0], None, new, new, 0, 0, 0.1, out, None, 0, cache.workspace(4, 1), status)
+        torch.cuda.synchronize()
+        assert status.item() == api.SI_ERR_OUT_OF_RANGE
+        if new is not None:
+            assert torch.equal(k[0].view(torch.int16), k0[0].view(torch.int16)) and torch.count_nonzero(k[1, :, 3]) == 0
+        status.zero_()
+        o4 = torch.empty(2, 1, 4, 64, dtype=q.dtype, device="cuda")
+        api.si_attn_prefill(cache, q, 0, 0, 0.1, o4, None, cache.workspace(4, 1), status)
+        torch.cuda.synchronize()
+        assert status.item() == (api.SI_ERR_OUT_OF_RANGE if lens[0] != 64 else 0)
+
+
+def test_calls_run_on_the_given_stream_and_in_a_graph(api):
+    lens = [200, 90]
+    q, k, v, length = au.make(2, 8, 2, 128, 256, "bf16", "hnd", 1, 4, lens)
+    weight = torch.zeros(2, 2, 256, device="cuda")
+    cache = api.KVCache(k, v, length, None, weight)
+    ws = cache.workspace(8, 1)
+    out, lse = torch.empty(2, 8, 128, dtype=q.dtype, device="cuda"), torch.empty(2, 8, dtype=torch.float32, device="cuda")
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        api.si_attn_decode(cache, q[:, 0], None, None, None, 0, 0, 0.09, out, lse, api.SI_FLAG_ACC_WEIGHT, ws, stream=s)
+    for want in (lens, [17, 230]):               # the lengths live on the device: a captured call follows them
+        kk, vv = au.make(2, 8, 2, 128, 256, "bf16", "hnd", 1, 4, [256, 256])[1:3]
+        k.copy_(kk); v.copy_(vv)
+        length.copy_(torch.tensor(want, dtype=torch.int32))
+        weight.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        ref = au.reference(q, k, v, want, 0, 0, 0.09)
+        au.check_out(out[:, None], ref, "bf16", 128)
+        au.check_weight(weight, np.zeros((2, 2, 256)), ref, 128, 1)

@@ -38,8 +38,6 @@ struct AttnArgs {
     long long q_ss, q_ts;
     int T, Hq, window, n_sink;
     float scale;
-    const int32_t *q_pos;
-    int appended;              // decode: entry len[b] holds the query's own key and value
     uint16_t *out;
     float *lse;
     int32_t *status;
@@ -52,17 +50,14 @@ __global__ void __launch_bounds__(128) attn_rows_kernel(const AttnArgs A) {
     const long long r = (long long)blockIdx.x * 4 + warp, rows = (long long)A.kv.B * A.T * A.Hq;
     if (r >= rows) return;
     const int hq = (int)(r % A.Hq), i = (int)(r / A.Hq % A.T), b = (int)(r / A.Hq / A.T), h = hq / (A.Hq / A.kv.H);
-    int n = si_kv_len(A.kv, b, A.status);
-    if (A.appended && n < A.kv.cap) ++n;
-    const int s = A.q_pos ? A.q_pos[b] : n - A.T + i, lo = si_window_lo(s, A.window);
+    const int n = si_kv_len(A.kv, b, A.status), s = n - A.T + i, lo = si_window_lo(s, A.window);
     const uint16_t *q = A.q + b * A.q_ss + i * A.q_ts + (long long)hq * D;
     for (int c = lane; c < D; c += 32) sq[warp][c] = si_cvt<DT>::lo(q[c]);
     __syncwarp();
-    const int32_t *pos = A.kv.pos ? A.kv.pos + A.kv.meta(b, h) : nullptr;
     float m = -INFINITY, l = 0.f, o[D / 32] = {};
     for (int j0 = 0; j0 < n; j0 += 32) {
         const int j = j0 + lane;
-        const bool vis = j < n && si_visible(pos ? pos[j] : j, s, lo, A.n_sink);
+        const bool vis = j < n && si_visible(j, s, lo, A.n_sink);
         if (!__any_sync(0xFFFFFFFFu, vis)) continue;
         const float x = vis ? dot_row<DT, D>(A.kv.k + A.kv.row(b, h, j), sq[warp]) * A.scale : -INFINITY;
         const float m2 = fmaxf(m, warp_max(x)), base = m2 == -INFINITY ? 0.f : m2;
@@ -85,20 +80,6 @@ __global__ void __launch_bounds__(128) attn_rows_kernel(const AttnArgs A) {
     if (A.lse && lane == 0) A.lse[r] = l == 0.f ? -INFINITY : m + logf(l);
 }
 
-// The new token's key and value into entry len[b] of every head.
-__global__ void attn_append_kernel(si_kv_view kv, const uint16_t *kn, const uint16_t *vn, long long ns, const int32_t *q_pos, int acc, int32_t *status) {
-    const int b = blockIdx.x, h = blockIdx.y, n = si_kv_len(kv, b, status);
-    if (n >= kv.cap) { if (threadIdx.x == 0) si_report(status, SI_ERR_OUT_OF_RANGE); return; }
-    for (int c = threadIdx.x; c < kv.D; c += blockDim.x) {
-        kv.k[kv.row(b, h, n) + c] = kn[b * ns + h * kv.D + c];
-        kv.v[kv.row(b, h, n) + c] = vn[b * ns + h * kv.D + c];
-    }
-    if (threadIdx.x == 0) {
-        if (kv.pos) kv.pos[kv.meta(b, h) + n] = q_pos[b];
-        if (acc) kv.weight[kv.meta(b, h) + n] = 0.f;
-    }
-}
-
 // weight[b, h, j] += sum over queries and the group's heads of exp(scale q . k_j - lse): one warp per entry, lane =
 // query row.
 template <int DT, int D>
@@ -106,16 +87,14 @@ __global__ void __launch_bounds__(128) attn_weights_kernel(const AttnArgs A, con
     __shared__ float sk[4][D];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, G = A.Hq / A.kv.H;
     const int j = blockIdx.x * 4 + warp, h = blockIdx.y, b = blockIdx.z;
-    int n = si_kv_len(A.kv, b, A.status);
-    if (A.appended && n < A.kv.cap) ++n;
+    const int n = si_kv_len(A.kv, b, A.status);
     if (j >= n) return;
-    const int p = A.kv.pos ? A.kv.pos[A.kv.meta(b, h) + j] : j;
     for (int c = lane; c < D; c += 32) sk[warp][c] = si_cvt<DT>::lo(A.kv.k[A.kv.row(b, h, j) + c]);
     __syncwarp();
     float sum = 0.f;
     for (int r = lane; r < A.T * G; r += 32) {
-        const int i = r / G, hq = h * G + r % G, s = A.q_pos ? A.q_pos[b] : n - A.T + i;
-        if (!si_visible(p, s, si_window_lo(s, A.window), A.n_sink)) continue;
+        const int i = r / G, hq = h * G + r % G, s = n - A.T + i;
+        if (!si_visible(j, s, si_window_lo(s, A.window), A.n_sink)) continue;
         const float x = dot_row<DT, D>(A.q + b * A.q_ss + i * A.q_ts + (long long)hq * D, sk[warp]) * A.scale;
         sum += exp2f((x - lse[((long long)b * A.T + i) * A.Hq + hq]) * kLog2e);
     }
@@ -158,7 +137,7 @@ extern "C" int si_attn_prefill(const si_kv_t *kv, const void *q, long long q_seq
     if (kv->pos) return SI_ERR_UNSUPPORTED;
     if (!si_aligned16(q) || !si_aligned16(out) || ((q_seq_stride | q_tok_stride) & 7)) return SI_ERR_ALIGNMENT;
     const AttnArgs A{si_kv_view_of(kv), (const uint16_t *)q, q_seq_stride, q_tok_stride, T, n_q_heads, window, n_sink, scale,
-                     nullptr, 0, (uint16_t *)out, lse, status_dev};
+                     (uint16_t *)out, lse, status_dev};
     return by_type(kv->dtype, kv->head_dim, Rows{A, (cudaStream_t)stream});
 }
 
@@ -173,35 +152,6 @@ extern "C" int si_attn_weights(const si_kv_t *kv, const void *q, long long q_seq
     if (kv->pos) return SI_ERR_UNSUPPORTED;
     if (!si_aligned16(q) || ((q_seq_stride | q_tok_stride) & 7)) return SI_ERR_ALIGNMENT;
     const AttnArgs A{si_kv_view_of(kv), (const uint16_t *)q, q_seq_stride, q_tok_stride, T, n_q_heads, window, n_sink, scale,
-                     nullptr, 0, nullptr, nullptr, status_dev};
+                     nullptr, nullptr, status_dev};
     return by_type(kv->dtype, kv->head_dim, Weights{A, lse, (cudaStream_t)stream});
-}
-
-extern "C" int si_attn_decode(const si_kv_t *kv, const void *q, long long q_seq_stride, int n_q_heads, const int32_t *q_pos,
-                              const void *k_new, const void *v_new, long long new_seq_stride, int window, int n_sink,
-                              float scale, void *out, float *lse, unsigned flags, void *workspace, size_t ws_bytes,
-                              int32_t *status_dev, void *stream) {
-    const int rc = si_attn_check(kv, n_q_heads, window, n_sink, scale);
-    if (rc) return rc;
-    if (flags & ~(unsigned)SI_FLAG_ACC_WEIGHT) return SI_ERR_INVALID_ARG;
-    if (kv->n_seqs == 0) return SI_OK;
-    const int acc = (flags & SI_FLAG_ACC_WEIGHT) != 0;
-    if (!q || !out || q_seq_stride < 0 || !k_new != !v_new || new_seq_stride < 0) return SI_ERR_INVALID_ARG;
-    if ((kv->pos && !q_pos) || (acc && !kv->weight)) return SI_ERR_INVALID_ARG;
-    if (!si_aligned16(q) || !si_aligned16(out) || !si_aligned16(k_new) || !si_aligned16(v_new) || ((q_seq_stride | new_seq_stride) & 7))
-        return SI_ERR_ALIGNMENT;
-    size_t need = 0;
-    si_kv_workspace_bytes(kv, n_q_heads, 1, &need);
-    if (need > ws_bytes) return SI_ERR_NOMEM;
-    if (need && !workspace) return SI_ERR_INVALID_ARG;
-    const cudaStream_t st = (cudaStream_t)stream;
-    float *row_lse = lse ? lse : (float *)workspace;
-    const AttnArgs A{si_kv_view_of(kv), (const uint16_t *)q, q_seq_stride, 0, 1, n_q_heads, window, n_sink, scale,
-                     q_pos, k_new != nullptr, (uint16_t *)out, row_lse, status_dev};
-    if (k_new) {
-        attn_append_kernel<<<dim3(kv->n_seqs, kv->n_kv_heads), 128, 0, st>>>(A.kv, (const uint16_t *)k_new, (const uint16_t *)v_new, new_seq_stride, q_pos, acc, status_dev);
-        SI_CUDA_TRY(cudaGetLastError());
-    }
-    const int r = by_type(kv->dtype, kv->head_dim, Rows{A, st});
-    return r || !acc ? r : by_type(kv->dtype, kv->head_dim, Weights{A, row_lse, st});
 }

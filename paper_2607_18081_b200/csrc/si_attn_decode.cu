@@ -1,0 +1,601 @@
+// Single-token attention over the key/value cache.
+//
+//   out_q = sum_j p_qj v_j,  p_q = softmax over the visible entries j of scale q . k_j,   q = the G query heads of a key head
+//
+// Bound by HBM: every visible key and value is read once, 2 G flops per byte.  So the kernel is a stream: each warp keeps
+// two chunks of 4 KB of keys and 4 KB of values in flight (cp.async into a ring of its own, 128 KB per SM) while it works
+// on a third.  The G heads make the second dimension of two small matrix products per chunk,
+//   S^T [keys x heads] = K Q^T        O^T [head_dim x heads] += V^T P^T,
+// with the keys on the long side of the m16n8k16 fragment, so that eight heads fill it (heads-first would waste half of
+// it), K and V come from shared memory by ldmatrix as they lie there, and P^T gets from the accumulator layout to the
+// operand layout by a transposing register move.  At 23 bytes per SM and clock the warp-level products are a tenth busy:
+// a tcgen05 tile of 128 rows would be filled with G of them and gains nothing.
+//
+// Work is split in chunks, not in sequences: the chunks of all (sequence, head) items in one row, cut into equal runs, one
+// per CTA, whatever the lengths.  An item that crosses CTAs leaves partial sums (one maximum, one sum and head_dim fp32
+// values per head and CTA) that a second kernel joins in the order of the CTAs -- no atomics, the same bits every time.
+// With weights wanted the scores go to the workspace (4 bytes per head beside 4 * head_dim bytes per key) and the second
+// kernel, which knows the sums, adds exp(score - lse).
+#include "si_kv.cuh"
+#include "si_tc.cuh"
+
+namespace {
+
+constexpr int kWarps = 8, kThreads = kWarps * 32;
+constexpr int kStages = 3;
+constexpr int kMinChunks = kWarps;         // a CTA's run: at least one chunk per warp
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLazy = 8.f;               // the running maximum moves only when a score exceeds it by 2^8: p stays below 2^8, exact to fp32 all the same
+
+template <int D, int NT> struct Cfg {
+    static constexpr int CH = 2048 / D;                  // keys per chunk: 4 KB of keys, 4 KB of values
+    static constexpr int kStage = 8192 + CH * 4;         // ... and the entries' positions
+    static constexpr int kRow = D + 4;                   // padded row of the merge buffer: conflict-free fragment writes
+    static constexpr int kMerge = 8 * kRow;              // floats per warp: eight heads at a time
+    static constexpr int kSmem = kWarps * kStages * kStage + kWarps / 2 * kMerge * 4 + kWarps * 8 * NT * 2 * 4;
+};
+
+struct DecodeArgs {
+    si_kv_view kv;
+    const uint16_t *q, *kn, *vn;
+    const int32_t *q_pos;
+    long long q_ss, new_ss;
+    int Hq, G, GB, GS, window, n_sink;   // GB: blocks of 8 * NT heads per key head; GS: heads per key in `scores`
+    float scale2;                        // scale * log2(e)
+    uint16_t *out;
+    float *lse;
+    int32_t *status;
+    int acc, n_cta;
+    float *part_o, *part_ml;             // [n_cta][2][8 NT][D], [n_cta][2][8 NT][2]
+    float *lse2;                         // [B][H * GB * 8 NT]: base-2 lse of finished items (weights only)
+    float *scores;                       // [B][H][GB][cap][GS]
+};
+
+// The chunks of sequence b that hold visible entries: c_sink chunks from the front, then those from c_win to c_end.
+struct SeqWork { int n, n_old, s, lo, c_sink, c_win, nc; };
+template <int D> __device__ __forceinline__ SeqWork seq_work(const DecodeArgs &A, int b, int32_t *status) {
+    constexpr int CH = 2048 / D;
+    SeqWork w;
+    w.n = si_kv_len(A.kv, b, status);
+    w.n_old = INT_MAX;
+    if (A.kn) {
+        if (w.n < A.kv.cap) w.n_old = w.n++;
+        else si_report(status, SI_ERR_OUT_OF_RANGE);
+    }
+    w.s = A.q_pos ? A.q_pos[b] : w.n - 1;
+    w.lo = si_window_lo(w.s, A.window);
+    w.c_sink = 0; w.c_win = 0;
+    int end = w.n;
+    if (!A.kv.pos) {                               // entry j is at position j
+        end = max(0, min(w.n, w.s >= INT_MAX - 1 ? w.n : w.s + 1));
+        if (w.lo >= 0) {
+            const int first = min(w.lo + 1, end);
+            w.c_win = first / CH;
+            w.c_sink = min((min(A.n_sink, first) + CH - 1) / CH, w.c_win);
+        }
+    }
+    w.nc = w.c_sink + (end + CH - 1) / CH - w.c_win;
+    return w;
+}
+
+__device__ __forceinline__ float ex2(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+__device__ __forceinline__ void ldm4(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldm4t(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ uint32_t mov_trans(uint32_t x) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+    return r;
+}
+template <int DT> __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    uint32_t r;
+    if (DT == SI_BF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+template <int DT> __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    if (DT == SI_BF16)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// Position in the row of all chunks: item = (sequence, head block), its first chunk and its number of chunks.
+struct Cursor {
+    long long start;     // global number of the item's first chunk
+    int b, hh;           // hh = head * GB + head block
+    SeqWork w;
+};
+template <int D> __device__ __forceinline__ bool next_item(const DecodeArgs &A, Cursor &c) {   // false: past the last one
+    c.start += c.w.nc;
+    if (++c.hh < A.kv.H * A.GB && c.w.nc > 0) return true;
+    c.hh = 0;
+    do {
+        if (++c.b >= A.kv.B) { c.w.nc = 0; return false; }
+        c.w = seq_work<D>(A, c.b, nullptr);
+    } while (c.w.nc == 0);
+    return true;
+}
+
+// Thread t of the block stands for sequences t * per .. : sh[t] = chunks in front of them; returns the total.
+template <int D> __device__ __forceinline__ long long scan_work(const DecodeArgs &A, long long *sh, int32_t *status) {
+    const int tid = threadIdx.x, per = (A.kv.B + kThreads - 1) / kThreads, items = A.kv.H * A.GB;
+    const int b0 = min(A.kv.B, tid * per), b1 = min(A.kv.B, b0 + per);
+    long long sum = 0;
+    for (int b = b0; b < b1; ++b) sum += (long long)seq_work<D>(A, b, status).nc * items;
+    sh[tid] = sum;
+    __syncthreads();
+    if (tid < 32) {
+        constexpr int N = kThreads / 32;
+        long long v[N], run = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) { v[i] = run; run += sh[tid * N + i]; }
+        long long inc = run;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long t = __shfl_up_sync(0xFFFFFFFFu, inc, o);
+            if (tid >= o) inc += t;
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) sh[tid * N + i] = inc - run + v[i];
+        if (tid == 31) sh[kThreads] = inc;
+    }
+    __syncthreads();
+    return sh[kThreads];
+}
+// The item that holds chunk `target` (< total).
+template <int D> __device__ __forceinline__ Cursor find_item(const DecodeArgs &A, long long target, const long long *sh) {
+    const int per = (A.kv.B + kThreads - 1) / kThreads, items = A.kv.H * A.GB;
+    int lo = 0, hi = kThreads - 1;                   // last thread whose first chunk is <= target
+    while (lo < hi) { const int mid = (lo + hi + 1) / 2; if (sh[mid] <= target) lo = mid; else hi = mid - 1; }
+    long long start = sh[lo];
+    Cursor c;
+    c.b = lo * per;
+    c.w = seq_work<D>(A, c.b, nullptr);
+    while (start + (long long)c.w.nc * items <= target) { start += (long long)c.w.nc * items; c.w = seq_work<D>(A, ++c.b, nullptr); }
+    c.hh = (int)((target - start) / c.w.nc);
+    c.start = start + (long long)c.hh * c.w.nc;
+    return c;
+}
+__device__ __forceinline__ long long run_length(long long total, int n_cta) {
+    const long long per = (total + n_cta - 1) / n_cta;
+    return per < kMinChunks ? kMinChunks : per;
+}
+
+template <int DT, int D, int NT>
+__global__ void __launch_bounds__(kThreads, 1) decode_kernel(const DecodeArgs A) {
+    using C = Cfg<D, NT>;
+    constexpr int CH = C::CH, HB = 8 * NT, PIECES = D / 8, SUB = CH / 16;
+    extern __shared__ __align__(128) char smem[];
+    __shared__ long long sh_scan[kThreads + 1];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    char *ring = smem + warp * kStages * C::kStage;
+    float *merge_o = (float *)(smem + kWarps * kStages * C::kStage);
+    float *ml = merge_o + kWarps / 2 * C::kMerge;
+    si_tc::pdl_launch();
+
+    // the new entries: stored for later calls; this one reads them from where they are
+    if (A.kn)
+        for (int r = blockIdx.x; r < A.kv.B * A.kv.H; r += gridDim.x) {
+            const int b = r / A.kv.H, h = r % A.kv.H, n = si_kv_len(A.kv, b, nullptr);
+            if (n >= A.kv.cap) continue;
+            const long long to = A.kv.row(b, h, n), from = b * A.new_ss + (long long)h * D;
+            if (tid < PIECES) *reinterpret_cast<uint4 *>(A.kv.k + to + tid * 8) = *reinterpret_cast<const uint4 *>(A.kn + from + tid * 8);
+            else if (tid < 2 * PIECES) *reinterpret_cast<uint4 *>(A.kv.v + to + (tid - PIECES) * 8) = *reinterpret_cast<const uint4 *>(A.vn + from + (tid - PIECES) * 8);
+            else if (tid == 2 * PIECES && A.kv.pos) A.kv.pos[A.kv.meta(b, h) + n] = A.q_pos[b];
+        }
+
+    // this CTA's run of chunks
+    Cursor cons;
+    long long g0, g1;
+    {
+        const long long total = scan_work<D>(A, sh_scan, blockIdx.x == 0 ? A.status : nullptr), per = run_length(total, A.n_cta);
+        g0 = blockIdx.x * per;
+        g1 = min(total, g0 + per);
+        // sequences without a visible entry have no chunk: their rows are zero
+        for (int b = blockIdx.x; b < A.kv.B; b += gridDim.x) {
+            if (seq_work<D>(A, b, nullptr).nc) continue;
+            for (int i = tid; i < A.Hq * D; i += kThreads) A.out[(long long)b * A.Hq * D + i] = 0;
+            if (A.lse) for (int i = tid; i < A.Hq; i += kThreads) A.lse[(long long)b * A.Hq + i] = -INFINITY;
+        }
+        if (g0 >= g1) return;
+        cons = find_item<D>(A, g0, sh_scan);
+    }
+
+    // ---- loader side: chunk ids g0 + warp, + kWarps, ...
+    Cursor load = cons;
+    long long load_id = g0 + warp;
+    int load_stage = 0;
+    const uint32_t ring_addr = si_tc::smem_u32(ring);
+    auto issue = [&]() {
+        if (load_id < g1) {
+            while (load_id >= load.start + load.w.nc) next_item<D>(A, load);
+            const int t = (int)(load_id - load.start), c = t < load.w.c_sink ? t : load.w.c_win + t - load.w.c_sink;
+            const int h = load.hh / A.GB, j0 = c * CH;
+            const uint32_t kdst = ring_addr + load_stage * C::kStage, vdst = kdst + 4096;
+            const int piece = lane % PIECES, r0 = lane / PIECES;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int r = r0 + i * (32 / PIECES), j = j0 + r;
+                const bool fresh = j == load.w.n_old;
+                const long long off = fresh ? load.b * A.new_ss + (long long)h * D + piece * 8 : A.kv.row(load.b, h, j < load.w.n ? j : 0) + piece * 8;
+                const uint16_t *ks = (fresh ? A.kn : A.kv.k) + off, *vs = (fresh ? A.vn : A.kv.v) + off;
+                const int bytes = j < load.w.n ? 16 : 0;     // past the end: zeros, nothing is read
+                const uint32_t at = r * (D * 2) + (((piece & 8) | ((piece ^ r) & 7)) << 4);
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(kdst + at), "l"(ks), "r"(bytes) : "memory");
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(vdst + at), "l"(vs), "r"(bytes) : "memory");
+            }
+            if (A.kv.pos && lane < CH) {
+                const int j = j0 + lane;
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(vdst + 4096 + lane * 4),
+                             "l"(A.kv.pos + A.kv.meta(load.b, h) + (j < load.w.n ? j : 0)), "r"(j < load.w.n ? 4 : 0) : "memory");
+            }
+            load_id += kWarps;
+            load_stage = load_stage + 1 == kStages ? 0 : load_stage + 1;
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    issue();
+    issue();
+
+    // ---- consumer side
+    long long id = g0 + warp;
+    int stage = 0;
+    bool first_segment = true;
+    while (true) {
+        const long long seg_end = min(g1, cons.start + cons.w.nc);
+        const int h = cons.hh / A.GB, gb = cons.hh % A.GB, head0 = gb * HB, heads = min(HB, A.G - head0);
+        const SeqWork w = cons.w;
+        uint32_t qf[NT][D / 16][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int head = nt * 8 + (lane >> 2);
+            const uint16_t *q = A.q + cons.b * A.q_ss + (long long)(h * A.G + head0 + head) * D + 2 * (lane & 3);
+#pragma unroll
+            for (int s = 0; s < D / 16; ++s) {
+                qf[nt][s][0] = head < heads ? *reinterpret_cast<const uint32_t *>(q + s * 16) : 0u;
+                qf[nt][s][1] = head < heads ? *reinterpret_cast<const uint32_t *>(q + s * 16 + 8) : 0u;
+            }
+        }
+        float o[NT][D / 16][4] = {};
+        float m[NT][2], l[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) { m[nt][0] = m[nt][1] = -INFINITY; l[nt][0] = l[nt][1] = 0.f; }
+        for (; id < seg_end; id += kWarps) {
+            asm volatile("cp.async.wait_group 1;" ::: "memory");
+            __syncwarp();
+            issue();
+            const uint32_t kbase = ring_addr + stage * C::kStage, vbase = kbase + 4096;
+            const int t = (int)(id - cons.start), j0 = (t < w.c_sink ? t : w.c_win + t - w.c_sink) * CH;
+            // which keys of the chunk are visible; the values of the others must not meet the product (0 * NaN)
+            uint32_t vis;
+            {
+                const int j = j0 + lane;
+                int p = j;
+                if (A.kv.pos) p = j == w.n_old ? w.s : *reinterpret_cast<const int *>(ring + stage * C::kStage + 8192 + (lane & (CH - 1)) * 4);
+                vis = __ballot_sync(0xFFFFFFFFu, lane < CH && j < w.n && si_visible(p, w.s, w.lo, A.n_sink));
+            }
+            constexpr uint32_t kAll = CH == 32 ? 0xFFFFFFFFu : (1u << (CH & 31)) - 1;
+            if (vis != kAll) {
+                for (int i = lane; i < CH * PIECES; i += 32)
+                    if (!(vis >> (i / PIECES) & 1)) *reinterpret_cast<uint4 *>(ring + stage * C::kStage + 4096 + i * 16) = make_uint4(0, 0, 0, 0);
+                __syncwarp();
+            }
+            float x[SUB][NT][4] = {};
+#pragma unroll
+            for (int u = 0; u < SUB; ++u) {
+                const int r = u * 16 + (lane & 15);
+#pragma unroll
+                for (int s = 0; s < D / 16; ++s) {
+                    const int piece = s * 2 + (lane >> 4);
+                    uint32_t a[4];
+                    ldm4(a, kbase + r * (D * 2) + (((piece & 8) | ((piece ^ r) & 7)) << 4));
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mma<DT>(x[u][nt], a, qf[nt][s][0], qf[nt][s][1]);
+                }
+            }
+            bool grow = false;
+#pragma unroll
+            for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int key = u * 16 + (lane >> 2) + (e >> 1) * 8;
+                        x[u][nt][e] = (vis >> key & 1) ? x[u][nt][e] * A.scale2 : -INFINITY;
+                        grow |= x[u][nt][e] > m[nt][e & 1] + kLazy;
+                    }
+            if (A.acc) {
+                float *sc = A.scores + ((((long long)cons.b * A.kv.H + h) * A.GB + gb) * A.kv.cap + j0) * A.GS;
+#pragma unroll
+                for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int e = 0; e < 4; e += 2) {
+                            const int key = u * 16 + (lane >> 2) + (e >> 1) * 8, head = nt * 8 + 2 * (lane & 3);
+                            if (head < A.GS && j0 + key < w.n)
+                                *reinterpret_cast<float2 *>(sc + (long long)key * A.GS + head) = make_float2(x[u][nt][e], x[u][nt][e + 1]);
+                        }
+            }
+            if (__any_sync(0xFFFFFFFFu, grow)) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        float mx = m[nt][c];
+#pragma unroll
+                        for (int u = 0; u < SUB; ++u) mx = fmaxf(mx, fmaxf(x[u][nt][c], x[u][nt][c + 2]));
+                        mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 4));
+                        mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 8));
+                        mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 16));
+                        const float f = mx == -INFINITY ? 1.f : ex2(m[nt][c] - mx);
+                        m[nt][c] = mx;
+                        l[nt][c] *= f;
+#pragma unroll
+                        for (int s = 0; s < D / 16; ++s) { o[nt][s][c] *= f; o[nt][s][c + 2] *= f; }
+                    }
+            }
+#pragma unroll
+            for (int u = 0; u < SUB; ++u) {
+                uint32_t pb[NT][2];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float base = m[nt][e & 1] == -INFINITY ? 0.f : m[nt][e & 1];
+                        x[u][nt][e] = ex2(x[u][nt][e] - base);
+                        l[nt][e & 1] += x[u][nt][e];
+                    }
+                    pb[nt][0] = mov_trans(pack2<DT>(x[u][nt][0], x[u][nt][1]));
+                    pb[nt][1] = mov_trans(pack2<DT>(x[u][nt][2], x[u][nt][3]));
+                }
+                const int r = u * 16 + (lane & 7) + ((lane >> 4) << 3);
+#pragma unroll
+                for (int s = 0; s < D / 16; ++s) {
+                    const int piece = s * 2 + ((lane >> 3) & 1);
+                    uint32_t a[4];
+                    ldm4t(a, vbase + r * (D * 2) + (((piece & 8) | ((piece ^ r) & 7)) << 4));
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mma<DT>(o[nt][s], a, pb[nt][0], pb[nt][1]);
+                }
+            }
+            __syncwarp();                      // the stage may be loaded again
+            stage = stage + 1 == kStages ? 0 : stage + 1;
+        }
+        // ---- the segment's warps joined: rows scaled to the common maximum, summed in warp order
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                l[nt][c] += __shfl_xor_sync(0xFFFFFFFFu, l[nt][c], 4);
+                l[nt][c] += __shfl_xor_sync(0xFFFFFFFFu, l[nt][c], 8);
+                l[nt][c] += __shfl_xor_sync(0xFFFFFFFFu, l[nt][c], 16);
+                if (lane < 4) {
+                    ml[(warp * HB + nt * 8 + 2 * lane + c) * 2] = m[nt][c];
+                    ml[(warp * HB + nt * 8 + 2 * lane + c) * 2 + 1] = l[nt][c];
+                }
+            }
+        __syncthreads();
+        const bool whole = cons.start >= g0 && cons.start + w.nc <= g1;
+        float *po = A.part_o + ((long long)blockIdx.x * 2 + (first_segment ? 0 : 1)) * HB * D;
+        float *pml = A.part_ml + ((long long)blockIdx.x * 2 + (first_segment ? 0 : 1)) * HB * 2;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            // eight heads at a time: the upper four warps through the buffer to the lower four, those to the threads that finish
+            float f[2];
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const int head = nt * 8 + 2 * (lane & 3) + c;
+                float top = -INFINITY;
+#pragma unroll
+                for (int v = 0; v < kWarps; ++v) top = fmaxf(top, ml[(v * HB + head) * 2]);
+                f[c] = m[nt][c] == -INFINITY ? 0.f : ex2(m[nt][c] - top);
+            }
+            float *mine = merge_o + (warp & 3) * C::kMerge + 2 * (lane & 3) * C::kRow + (lane >> 2);
+#pragma unroll
+            for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[nt][s][e] *= f[e & 1];
+            if (warp >= 4) {
+#pragma unroll
+                for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) mine[(e & 1) * C::kRow + s * 16 + (e >> 1) * 8] = o[nt][s][e];
+            }
+            __syncthreads();
+            if (warp < 4) {
+#pragma unroll
+                for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) mine[(e & 1) * C::kRow + s * 16 + (e >> 1) * 8] += o[nt][s][e];
+            }
+            __syncthreads();
+            for (int i = tid; i < 8 * (D / 2); i += kThreads) {
+                const int hd = i / (D / 2), d = i % (D / 2) * 2, head = nt * 8 + hd;
+                if (head >= heads) continue;
+                float top = -INFINITY, sum = 0.f;
+#pragma unroll
+                for (int v = 0; v < kWarps; ++v) top = fmaxf(top, ml[(v * HB + head) * 2]);
+                float2 acc = make_float2(0.f, 0.f);
+#pragma unroll
+                for (int v = 0; v < kWarps; ++v) {
+                    const float mv = ml[(v * HB + head) * 2];
+                    sum += mv == -INFINITY ? 0.f : ml[(v * HB + head) * 2 + 1] * ex2(mv - top);
+                }
+#pragma unroll
+                for (int v = 0; v < kWarps / 2; ++v) {
+                    const float2 t = *reinterpret_cast<const float2 *>(merge_o + v * C::kMerge + hd * C::kRow + d);
+                    acc.x += t.x; acc.y += t.y;
+                }
+                const long long row = (long long)cons.b * A.Hq + h * A.G + head0 + head;
+                if (whole) {
+                    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                    *reinterpret_cast<uint32_t *>(A.out + row * D + d) = pack2<DT>(acc.x * inv, acc.y * inv);
+                    if (d == 0) {
+                        const float l2 = sum == 0.f ? -INFINITY : top + log2f(sum);
+                        if (A.lse) A.lse[row] = l2 / kLog2e;
+                        if (A.acc) A.lse2[row] = l2;
+                    }
+                } else {
+                    *reinterpret_cast<float2 *>(po + head * D + d) = acc;
+                    if (d == 0) { pml[head * 2] = top; pml[head * 2 + 1] = sum; }
+                }
+            }
+            __syncthreads();
+        }
+        first_segment = false;
+        if (seg_end >= g1) return;
+        next_item<D>(A, cons);
+    }
+}
+
+// Joins the parts of items that crossed CTAs and, where weights are wanted, adds them up.  One CTA per (sequence, key head)
+// and range of keys.
+template <int DT, int D, int NT>
+__global__ void __launch_bounds__(kThreads) decode_join_kernel(const DecodeArgs A, int keys_per_cta) {
+    constexpr int HB = 8 * NT;
+    __shared__ long long sh_scan[kThreads + 1];
+    __shared__ float sh_lse2[128];
+    const int tid = threadIdx.x, h = blockIdx.y, b = blockIdx.z;
+    si_tc::pdl_wait();
+    const SeqWork w = seq_work<D>(A, b, nullptr);
+    if (w.nc == 0 && !A.acc) return;
+    const long long total = scan_work<D>(A, sh_scan, nullptr), per = run_length(total, A.n_cta);
+    // the first chunk of this sequence: the scan has it for the first sequence of each thread's run
+    const int per_thread = (A.kv.B + kThreads - 1) / kThreads;
+    long long start = sh_scan[b / per_thread];
+    for (int c = b / per_thread * per_thread; c < b; ++c) start += (long long)seq_work<D>(A, c, nullptr).nc * A.kv.H * A.GB;
+    for (int gb = 0; gb < A.GB; ++gb) {
+        const long long s0 = start + (long long)(h * A.GB + gb) * w.nc, s1 = s0 + w.nc;
+        const int head0 = gb * HB, heads = min(HB, A.G - head0);
+        const long long row0 = (long long)b * A.Hq + h * A.G + head0;
+        if (w.nc == 0) break;
+        const int x0 = (int)(s0 / per), x1 = (int)((s1 - 1) / per);
+        if (x0 == x1) {                                // finished by one CTA
+            if (A.acc && tid < heads) sh_lse2[head0 + tid] = A.lse2[row0 + tid];
+            continue;
+        }
+        for (int i = tid; i < heads * (D / 2); i += kThreads) {
+            const int head = i / (D / 2), d = i % (D / 2) * 2;
+            if (blockIdx.x > 0 && d > 0) continue;     // the other key ranges need the sums only
+            float top = -INFINITY, sum = 0.f;
+            float2 acc = make_float2(0.f, 0.f);
+            for (int x = x0; x <= x1; ++x) top = fmaxf(top, A.part_ml[(((long long)x * 2 + (s0 <= x * per ? 0 : 1)) * HB + head) * 2]);
+            for (int x = x0; x <= x1; ++x) {
+                const long long slot = (long long)x * 2 + (s0 <= x * per ? 0 : 1);
+                const float mv = A.part_ml[(slot * HB + head) * 2], f = mv == -INFINITY ? 0.f : ex2(mv - top);
+                sum += A.part_ml[(slot * HB + head) * 2 + 1] * f;
+                const float2 t = *reinterpret_cast<const float2 *>(A.part_o + (slot * HB + head) * D + d);
+                acc.x += t.x * f; acc.y += t.y * f;
+            }
+            const float l2 = sum == 0.f ? -INFINITY : top + log2f(sum), inv = sum == 0.f ? 0.f : 1.f / sum;
+            if (blockIdx.x == 0) {
+                *reinterpret_cast<uint32_t *>(A.out + (row0 + head) * D + d) = pack2<DT>(acc.x * inv, acc.y * inv);
+                if (d == 0 && A.lse) A.lse[row0 + head] = l2 / kLog2e;
+            }
+            if (d == 0) sh_lse2[head0 + head] = l2;
+        }
+    }
+    if (!A.acc) return;
+    __syncthreads();
+    constexpr int CH = 2048 / D;
+    float *weight = A.kv.weight + A.kv.meta(b, h);
+    const float *sc = A.scores + ((long long)b * A.kv.H + h) * A.GB * A.kv.cap * A.GS;
+    const int j0 = blockIdx.x * keys_per_cta, j1 = min(w.n, j0 + keys_per_cta);
+    for (int j = j0 + tid; j < j1; j += kThreads) {
+        const int c = j / CH;
+        float sum = 0.f;
+        const bool worked = c < w.c_sink || (c >= w.c_win && c < w.c_win + w.nc - w.c_sink);
+        if (worked)
+            for (int g = 0; g < A.G; ++g) {
+                const float x = sc[((long long)(g / HB) * A.kv.cap + j) * A.GS + g % HB];
+                if (x != -INFINITY) sum += ex2(x - sh_lse2[g]);
+            }
+        if (j == w.n_old) weight[j] = sum;
+        else if (worked) weight[j] += sum;
+    }
+}
+
+struct Layout { int n_cta, NT, GB, GS; size_t o, ml, lse2, scores, total; };
+Layout layout_of(const si_kv_t *kv, int n_q_heads, bool acc) {
+    Layout L;
+    static int sms = 0;
+    if (!sms) {
+        int dev = 0, n = 0;
+        if (cudaGetDevice(&dev) == cudaSuccess && cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess && n > 0) sms = n;
+        else (void)cudaGetLastError();
+    }
+    L.n_cta = sms ? sms : SI_NUM_SMS_FALLBACK;
+    const int G = n_q_heads / kv->n_kv_heads;
+    L.NT = G <= 8 ? 1 : 2;
+    L.GB = (G + 8 * L.NT - 1) / (8 * L.NT);
+    L.GS = G >= 8 * L.NT ? 8 * L.NT : (G + 1) / 2 * 2;
+    size_t off = 0;
+    auto take = [&](size_t bytes) { const size_t at = off; off += si_align_up(bytes, 256); return at; };
+    L.o = take((size_t)L.n_cta * 2 * 8 * L.NT * kv->head_dim * 4);
+    L.ml = take((size_t)L.n_cta * 2 * 8 * L.NT * 2 * 4);
+    L.lse2 = take(acc ? (size_t)kv->n_seqs * n_q_heads * 4 : 0);
+    L.scores = take(acc ? (size_t)kv->n_seqs * kv->n_kv_heads * L.GB * kv->capacity * L.GS * 4 : 0);
+    L.total = off;
+    return L;
+}
+
+template <int DT, int D, int NT> int launch(const DecodeArgs &A, cudaStream_t st) {
+    static std::atomic<int> ready{0};
+    if (!ready.load()) {
+        SI_CUDA_TRY(cudaFuncSetAttribute(decode_kernel<DT, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (Cfg<D, NT>::kSmem)));
+        ready.store(1);
+    }
+    decode_kernel<DT, D, NT><<<A.n_cta, kThreads, (Cfg<D, NT>::kSmem), st>>>(A);
+    SI_CUDA_TRY(cudaGetLastError());
+    const int keys = 2048;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(A.acc ? (A.kv.cap + keys - 1) / keys : 1, A.kv.H, A.kv.B);
+    cfg.blockDim = dim3(kThreads);
+    cfg.stream = st;
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &at; cfg.numAttrs = 1;
+    SI_CUDA_TRY(cudaLaunchKernelEx(&cfg, decode_join_kernel<DT, D, NT>, A, keys));
+    return SI_OK;
+}
+template <int DT> int launch_t(const DecodeArgs &A, int NT, cudaStream_t st) {
+    if (A.kv.D == 128) return NT == 1 ? launch<DT, 128, 1>(A, st) : launch<DT, 128, 2>(A, st);
+    return NT == 1 ? launch<DT, 64, 1>(A, st) : launch<DT, 64, 2>(A, st);
+}
+
+}  // namespace
+
+size_t si_attn_decode_ws_bytes(const si_kv_t *kv, int n_q_heads) { return layout_of(kv, n_q_heads, kv->weight != nullptr).total; }
+
+extern "C" int si_attn_decode(const si_kv_t *kv, const void *q, long long q_seq_stride, int n_q_heads, const int32_t *q_pos,
+                              const void *k_new, const void *v_new, long long new_seq_stride, int window, int n_sink,
+                              float scale, void *out, float *lse, unsigned flags, void *workspace, size_t ws_bytes,
+                              int32_t *status_dev, void *stream) {
+    const int rc = si_attn_check(kv, n_q_heads, window, n_sink, scale);
+    if (rc) return rc;
+    if (flags & ~(unsigned)SI_FLAG_ACC_WEIGHT) return SI_ERR_INVALID_ARG;
+    if (kv->n_seqs == 0) return SI_OK;
+    const int acc = (flags & SI_FLAG_ACC_WEIGHT) != 0;
+    if (!q || !out || q_seq_stride < 0 || !k_new != !v_new || new_seq_stride < 0) return SI_ERR_INVALID_ARG;
+    if ((kv->pos && !q_pos) || (acc && !kv->weight)) return SI_ERR_INVALID_ARG;
+    if (!si_aligned16(q) || !si_aligned16(out) || !si_aligned16(k_new) || !si_aligned16(v_new) || ((q_seq_stride | new_seq_stride) & 7))
+        return SI_ERR_ALIGNMENT;
+    const Layout L = layout_of(kv, n_q_heads, acc);
+    if (ws_bytes < L.total) return SI_ERR_NOMEM;
+    if (!workspace) return SI_ERR_INVALID_ARG;
+    if ((uintptr_t)workspace & 255) return SI_ERR_ALIGNMENT;
+    char *ws = (char *)workspace;
+    const DecodeArgs A{si_kv_view_of(kv), (const uint16_t *)q, (const uint16_t *)k_new, (const uint16_t *)v_new, q_pos, q_seq_stride,
+                       new_seq_stride, n_q_heads, n_q_heads / kv->n_kv_heads, L.GB, L.GS, window, n_sink, scale * kLog2e,
+                       (uint16_t *)out, lse, status_dev, acc, L.n_cta, (float *)(ws + L.o), (float *)(ws + L.ml),
+                       (float *)(ws + L.lse2), (float *)(ws + L.scores)};
+    return kv->dtype == SI_BF16 ? launch_t<SI_BF16>(A, L.NT, (cudaStream_t)stream) : launch_t<SI_F16>(A, L.NT, (cudaStream_t)stream);
+}

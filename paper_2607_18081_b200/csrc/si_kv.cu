@@ -157,7 +157,7 @@ extern "C" int si_kv_workspace_bytes(const si_kv_t *kv, int n_q_heads, int T, si
     const int rc = si_kv_check(kv);
     if (rc) return rc;
     if (!bytes_out || n_q_heads < 0 || T < 0 || n_q_heads % kv->n_kv_heads) return SI_ERR_INVALID_ARG;
-    const size_t attn = si_align_up((size_t)kv->n_seqs * n_q_heads * 4, 256), ev = evict_ws_bytes(kv);
+    const size_t attn = n_q_heads && T ? si_attn_decode_ws_bytes(kv, n_q_heads) : 0, ev = kv->weight ? evict_ws_bytes(kv) : 0;
     *bytes_out = attn > ev ? attn : ev;
     return SI_OK;
 }

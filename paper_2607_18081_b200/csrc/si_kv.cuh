@@ -44,6 +44,9 @@ inline int si_attn_check(const si_kv_t *kv, int n_q_heads, int window, int n_sin
     return SI_OK;
 }
 
+// implemented in si_attn_decode.cu
+size_t si_attn_decode_ws_bytes(const si_kv_t *kv, int n_q_heads);
+
 __device__ __forceinline__ void si_report(int32_t *status, int err) { if (status) atomicCAS(status, 0, err); }
 
 // Entries in use, clamped to the capacity.

@@ -454,7 +454,7 @@ class KVCache:
         if not (k.is_cuda and v.is_cuda):
             raise ValueError("expected CUDA tensors")
         self.k, self.v, self.length, self.pos, self.weight = k, v, length, pos, weight
-        self.n_seqs, self.n_kv_heads, self.capacity, self.head_dim = B, H, cap, D
+        self.n_seqs, self.n_kv_heads, self.capacity, self.head_dim, self.dtype = B, H, cap, D, k.dtype
         self.desc = _KvDesc(k.data_ptr(), v.data_ptr(), _dp(weight).value, _dp(pos).value, _dp(length).value, k.stride(0),
                             k.stride(1), k.stride(2), B, H, D, cap, dtype_code(k.dtype))
         self.ref = ctypes.addressof(self.desc)
@@ -464,22 +464,36 @@ class KVCache:
         return torch.empty(max(si_kv_workspace_bytes(self, n_q_heads, T), 256), dtype=torch.uint8, device=self.k.device)
 
 
-def _shaped(t, name: str, shape, dtype) -> None:
-    if t is not None and (tuple(t.shape) != tuple(shape) or t.dtype != dtype):
-        raise ValueError(f"{name}: expected {dtype} of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+def _ptr(t, name: str, shape, dtype):
+    """Address of a contiguous CUDA tensor of this shape and type (None -> NULL)."""
+    if t is None:
+        return None
+    if t.shape != shape or t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous CUDA tensor, {dtype} of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    return t.data_ptr()
 
 
-def _heads(t, name: str, cache, lead) -> ctypes.c_void_p:
-    """[*lead, heads, head_dim] of the cache's type, the heads of a token contiguous -> device pointer."""
-    if t.dtype != cache.k.dtype or t.dim() != len(lead) + 2 or tuple(t.shape[:-2]) != lead or t.shape[-1] != cache.head_dim:
-        raise ValueError(f"{name}: expected {cache.k.dtype} [{', '.join(map(str, lead))}, heads, {cache.head_dim}]")
-    if not t.is_cuda or t.stride(-1) != 1 or (t.shape[-2] > 1 and t.stride(-2) != t.shape[-1]):
+def _heads(t, name: str, cache, heads: int):
+    """Address of [n_seqs, ..., heads, head_dim] of the cache's type whose heads of a token are contiguous."""
+    shape, stride = t.shape, t.stride()
+    if t.dtype != cache.dtype or shape[0] != cache.n_seqs or shape[-2] != heads or shape[-1] != cache.head_dim:
+        raise ValueError(f"{name}: expected {cache.dtype} [{cache.n_seqs}, ..., {heads}, {cache.head_dim}], got {t.dtype} {tuple(shape)}")
+    if not t.is_cuda or stride[-1] != 1 or (stride[-2] != cache.head_dim and heads > 1):
         raise ValueError(f"{name}: expected a CUDA tensor whose heads are contiguous")
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
 def _ws(t):
-    return (ctypes.c_void_p(0), 0) if t is None else (_dp(t), t.numel() * t.element_size())
+    if t is None:
+        return None, 0
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError("expected a contiguous CUDA tensor")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def _on(stream):
+    # the raw handle of the current stream: building a Stream object takes 3 us of a 15 us call
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) if stream is None else stream.cuda_stream
 
 
 def si_kv_workspace_bytes(cache: KVCache, n_q_heads: int, T: int) -> int:
@@ -490,46 +504,49 @@ def si_kv_workspace_bytes(cache: KVCache, n_q_heads: int, T: int) -> int:
 
 def si_attn_prefill(cache: KVCache, q, window: int, n_sink: int, scale: float, out, lse, workspace, status=None, stream=None) -> None:
     """q, out: [n_seqs, T, n_q_heads, head_dim] (q may be strided); lse: float32 [n_seqs, T, n_q_heads] or None."""
-    T, hq = q.shape[1], q.shape[2]
-    qp = _heads(q, "q", cache, (cache.n_seqs, T))
-    _shaped(out, "out", q.shape, q.dtype); _shaped(lse, "lse", q.shape[:3], torch.float32)
-    _check(_lib.si_attn_prefill(cache.ref, qp, q.stride(0), q.stride(1), T, hq, window, n_sink, scale, _dp(out), _dp(lse),
-                                *_ws(workspace), _dp(status), _stream(stream)), "si_attn_prefill")
+    _, T, hq, _ = shape = q.shape
+    ws, ws_bytes = _ws(workspace)
+    _check(_lib.si_attn_prefill(cache.ref, _heads(q, "q", cache, hq), q.stride(0), q.stride(1), T, hq, window, n_sink, scale,
+                                _ptr(out, "out", shape, q.dtype), _ptr(lse, "lse", shape[:3], torch.float32), ws, ws_bytes,
+                                _ptr(status, "status", (1,), torch.int32), _on(stream)), "si_attn_prefill")
 
 
 def si_attn_weights(cache: KVCache, q, window: int, n_sink: int, scale: float, lse, workspace, status=None, stream=None) -> None:
     """Adds to cache.weight; q as for si_attn_prefill, lse: float32 [n_seqs, T, n_q_heads] from it."""
-    T, hq = q.shape[1], q.shape[2]
-    qp = _heads(q, "q", cache, (cache.n_seqs, T))
-    _shaped(lse, "lse", q.shape[:3], torch.float32)
-    _check(_lib.si_attn_weights(cache.ref, qp, q.stride(0), q.stride(1), T, hq, window, n_sink, scale, _dp(lse),
-                                *_ws(workspace), _dp(status), _stream(stream)), "si_attn_weights")
+    _, T, hq, _ = shape = q.shape
+    ws, ws_bytes = _ws(workspace)
+    _check(_lib.si_attn_weights(cache.ref, _heads(q, "q", cache, hq), q.stride(0), q.stride(1), T, hq, window, n_sink, scale,
+                                _ptr(lse, "lse", shape[:3], torch.float32), ws, ws_bytes, _ptr(status, "status", (1,), torch.int32),
+                                _on(stream)), "si_attn_weights")
 
 
 def si_attn_decode(cache: KVCache, q, q_pos, k_new, v_new, window: int, n_sink: int, scale: float, out, lse, flags: int,
                    workspace, status=None, stream=None) -> None:
     """q, out: [n_seqs, n_q_heads, head_dim]; k_new, v_new: [n_seqs, n_kv_heads, head_dim] of equal strides, or both None."""
-    hq = q.shape[1]
-    qp = _heads(q, "q", cache, (cache.n_seqs,))
-    _shaped(out, "out", q.shape, q.dtype); _shaped(lse, "lse", q.shape[:2], torch.float32)
-    _shaped(q_pos, "q_pos", (cache.n_seqs,), torch.int32)
-    kp = vp = ctypes.c_void_p(0)
+    _, hq, _ = shape = q.shape
+    kp = vp = None
     new_stride = 0
     if k_new is not None or v_new is not None:
-        if k_new is None or v_new is None or k_new.shape[1] != cache.n_kv_heads or k_new.shape != v_new.shape or k_new.stride() != v_new.stride():
+        if k_new is None or v_new is None or k_new.stride() != v_new.stride():
             raise ValueError("k_new and v_new: [n_seqs, n_kv_heads, head_dim] of equal strides, both or neither")
-        kp, vp, new_stride = _heads(k_new, "k_new", cache, (cache.n_seqs,)), _heads(v_new, "v_new", cache, (cache.n_seqs,)), k_new.stride(0)
-    _check(_lib.si_attn_decode(cache.ref, qp, q.stride(0), hq, _dp(q_pos), kp, vp, new_stride, window, n_sink, scale, _dp(out),
-                               _dp(lse), flags, *_ws(workspace), _dp(status), _stream(stream)), "si_attn_decode")
+        kp, vp = _heads(k_new, "k_new", cache, cache.n_kv_heads), _heads(v_new, "v_new", cache, cache.n_kv_heads)
+        new_stride = k_new.stride(0)
+    ws, ws_bytes = _ws(workspace)
+    _check(_lib.si_attn_decode(cache.ref, _heads(q, "q", cache, hq), q.stride(0), hq, _ptr(q_pos, "q_pos", (cache.n_seqs,), torch.int32),
+                               kp, vp, new_stride, window, n_sink, scale, _ptr(out, "out", shape, q.dtype),
+                               _ptr(lse, "lse", shape[:2], torch.float32), flags, ws, ws_bytes,
+                               _ptr(status, "status", (1,), torch.int32), _on(stream)), "si_attn_decode")
 
 
 def si_kv_evict(src: KVCache, dst: KVCache, q_pos, n_new: int, budget: int, n_sink: int, n_recent: int, kept, len_out,
                 workspace, status=None, stream=None) -> None:
     """dst is src: in place.  kept: int32 [n_seqs, n_kv_heads, budget] or None; len_out: int32 [n_seqs] or None."""
-    _shaped(q_pos, "q_pos", (src.n_seqs,), torch.int32); _shaped(len_out, "len_out", (src.n_seqs,), torch.int32)
-    _shaped(kept, "kept", (src.n_seqs, src.n_kv_heads, budget), torch.int32)
-    _check(_lib.si_kv_evict(src.ref, dst.ref, _dp(q_pos), n_new, budget, n_sink, n_recent, _dp(kept), _dp(len_out),
-                            *_ws(workspace), _dp(status), _stream(stream)), "si_kv_evict")
+    seqs = (src.n_seqs,)
+    ws, ws_bytes = _ws(workspace)
+    _check(_lib.si_kv_evict(src.ref, dst.ref, _ptr(q_pos, "q_pos", seqs, torch.int32), n_new, budget, n_sink, n_recent,
+                            _ptr(kept, "kept", (src.n_seqs, src.n_kv_heads, budget), torch.int32),
+                            _ptr(len_out, "len_out", seqs, torch.int32), ws, ws_bytes,
+                            _ptr(status, "status", (1,), torch.int32), _on(stream)), "si_kv_evict")
 
 
 # ------------------------------------------------------------------------- owner object

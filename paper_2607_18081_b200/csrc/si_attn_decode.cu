@@ -23,13 +23,12 @@ namespace {
 
 constexpr int kWarps = 8, kThreads = kWarps * 32;
 constexpr int kStages = 3;
-constexpr int kMinChunks = kWarps;         // a CTA's run: at least one chunk per warp
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLazy = 8.f;               // the running maximum moves only when a score exceeds it by 2^8: p stays below 2^8, exact to fp32 all the same
 
 template <int D, int NT> struct Cfg {
     static constexpr int CH = 2048 / D;                  // keys per chunk: 4 KB of keys, 4 KB of values
-    static constexpr int kStage = 8192 + CH * 4;         // ... and the entries' positions
+    static constexpr int kStage = 8192 + 128;            // ... and the entries' positions; a multiple of 128 (swizzle)
     static constexpr int kRow = D + 4;                   // padded row of the merge buffer: conflict-free fragment writes
     static constexpr int kMerge = 8 * kRow;              // floats per warp: eight heads at a time
     static constexpr int kSmem = kWarps * kStages * kStage + kWarps / 2 * kMerge * 4 + kWarps * 8 * NT * 2 * 4;
@@ -49,6 +48,8 @@ struct DecodeArgs {
     float *part_o, *part_ml;             // [n_cta][2][8 NT][D], [n_cta][2][8 NT][2]
     float *lse2;                         // [B][H * GB * 8 NT]: base-2 lse of finished items (weights only)
     float *scores;                       // [B][H][GB][cap][GS]
+    int2 *runs;                          // [B][H][GB]: first and last CTA of an item
+    int *part_first;                     // [n_cta]: the item a CTA's run starts with
 };
 
 // The chunks of sequence b that hold visible entries: c_sink chunks from the front, then those from c_win to c_end.
@@ -107,7 +108,7 @@ template <int DT> __device__ __forceinline__ void mma(float (&c)[4], const uint3
 
 // Position in the row of all chunks: item = (sequence, head block), its first chunk and its number of chunks.
 struct Cursor {
-    long long start;     // global number of the item's first chunk
+    int start;           // number of the item's first chunk among all
     int b, hh;           // hh = head * GB + head block
     SeqWork w;
 };
@@ -123,22 +124,27 @@ template <int D> __device__ __forceinline__ bool next_item(const DecodeArgs &A, 
 }
 
 // Thread t of the block stands for sequences t * per .. : sh[t] = chunks in front of them; returns the total.
-template <int D> __device__ __forceinline__ long long scan_work(const DecodeArgs &A, long long *sh, int32_t *status) {
+template <int D> __device__ __forceinline__ int scan_work(const DecodeArgs &A, int *sh, int32_t *status) {
     const int tid = threadIdx.x, per = (A.kv.B + kThreads - 1) / kThreads, items = A.kv.H * A.GB;
     const int b0 = min(A.kv.B, tid * per), b1 = min(A.kv.B, b0 + per);
-    long long sum = 0;
-    for (int b = b0; b < b1; ++b) sum += (long long)seq_work<D>(A, b, status).nc * items;
+    int sum = 0;
+    bool empty = false;
+    for (int b = b0; b < b1; ++b) {
+        const int nc = seq_work<D>(A, b, status).nc;
+        sum += nc * items;
+        empty |= nc == 0;
+    }
     sh[tid] = sum;
-    __syncthreads();
+    sh[kThreads + 1] = __syncthreads_or(empty);      // some sequence has nothing to see
     if (tid < 32) {
         constexpr int N = kThreads / 32;
-        long long v[N], run = 0;
+        int v[N], run = 0;
 #pragma unroll
         for (int i = 0; i < N; ++i) { v[i] = run; run += sh[tid * N + i]; }
-        long long inc = run;
+        int inc = run;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const long long t = __shfl_up_sync(0xFFFFFFFFu, inc, o);
+            const int t = __shfl_up_sync(0xFFFFFFFFu, inc, o);
             if (tid >= o) inc += t;
         }
 #pragma unroll
@@ -149,22 +155,32 @@ template <int D> __device__ __forceinline__ long long scan_work(const DecodeArgs
     return sh[kThreads];
 }
 // The item that holds chunk `target` (< total).
-template <int D> __device__ __forceinline__ Cursor find_item(const DecodeArgs &A, long long target, const long long *sh) {
+template <int D> __device__ __forceinline__ Cursor find_item(const DecodeArgs &A, int target, const int *sh) {
     const int per = (A.kv.B + kThreads - 1) / kThreads, items = A.kv.H * A.GB;
     int lo = 0, hi = kThreads - 1;                   // last thread whose first chunk is <= target
     while (lo < hi) { const int mid = (lo + hi + 1) / 2; if (sh[mid] <= target) lo = mid; else hi = mid - 1; }
-    long long start = sh[lo];
+    int start = sh[lo];
     Cursor c;
     c.b = lo * per;
     c.w = seq_work<D>(A, c.b, nullptr);
-    while (start + (long long)c.w.nc * items <= target) { start += (long long)c.w.nc * items; c.w = seq_work<D>(A, ++c.b, nullptr); }
-    c.hh = (int)((target - start) / c.w.nc);
-    c.start = start + (long long)c.hh * c.w.nc;
+    while (start + c.w.nc * items <= target) { start += c.w.nc * items; c.w = seq_work<D>(A, ++c.b, nullptr); }
+    c.hh = (target - start) / c.w.nc;
+    c.start = start + c.hh * c.w.nc;
     return c;
 }
-__device__ __forceinline__ long long run_length(long long total, int n_cta) {
-    const long long per = (total + n_cta - 1) / n_cta;
-    return per < kMinChunks ? kMinChunks : per;
+// The queries of an item as B operands: head = lane / 4, two neighbouring elements per register.
+template <int D, int NT> __device__ __forceinline__ void load_q(const DecodeArgs &A, int b, int hh, uint32_t (&qf)[NT][D / 16][2]) {
+    const int lane = threadIdx.x & 31, h = hh / A.GB, head0 = hh % A.GB * 8 * NT, heads = min(8 * NT, A.G - head0);
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const int head = nt * 8 + (lane >> 2);
+        const uint16_t *q = A.q + b * A.q_ss + (long long)(h * A.G + head0 + (head < heads ? head : 0)) * D + 2 * (lane & 3);
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) {
+            qf[nt][s][0] = head < heads ? *reinterpret_cast<const uint32_t *>(q + s * 16) : 0u;
+            qf[nt][s][1] = head < heads ? *reinterpret_cast<const uint32_t *>(q + s * 16 + 8) : 0u;
+        }
+    }
 }
 
 template <int DT, int D, int NT>
@@ -172,67 +188,64 @@ __global__ void __launch_bounds__(kThreads, 1) decode_kernel(const DecodeArgs A)
     using C = Cfg<D, NT>;
     constexpr int CH = C::CH, HB = 8 * NT, PIECES = D / 8, SUB = CH / 16;
     extern __shared__ __align__(128) char smem[];
-    __shared__ long long sh_scan[kThreads + 1];
+    __shared__ int sh_scan[kThreads + 2];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     char *ring = smem + warp * kStages * C::kStage;
     float *merge_o = (float *)(smem + kWarps * kStages * C::kStage);
     float *ml = merge_o + kWarps / 2 * C::kMerge;
     si_tc::pdl_launch();
 
-    // the new entries: stored for later calls; this one reads them from where they are
-    if (A.kn)
-        for (int r = blockIdx.x; r < A.kv.B * A.kv.H; r += gridDim.x) {
-            const int b = r / A.kv.H, h = r % A.kv.H, n = si_kv_len(A.kv, b, nullptr);
-            if (n >= A.kv.cap) continue;
-            const long long to = A.kv.row(b, h, n), from = b * A.new_ss + (long long)h * D;
-            if (tid < PIECES) *reinterpret_cast<uint4 *>(A.kv.k + to + tid * 8) = *reinterpret_cast<const uint4 *>(A.kn + from + tid * 8);
-            else if (tid < 2 * PIECES) *reinterpret_cast<uint4 *>(A.kv.v + to + (tid - PIECES) * 8) = *reinterpret_cast<const uint4 *>(A.vn + from + (tid - PIECES) * 8);
-            else if (tid == 2 * PIECES && A.kv.pos) A.kv.pos[A.kv.meta(b, h) + n] = A.q_pos[b];
-        }
-
     // this CTA's run of chunks
     Cursor cons;
-    long long g0, g1;
-    {
-        const long long total = scan_work<D>(A, sh_scan, blockIdx.x == 0 ? A.status : nullptr), per = run_length(total, A.n_cta);
-        g0 = blockIdx.x * per;
-        g1 = min(total, g0 + per);
-        // sequences without a visible entry have no chunk: their rows are zero
-        for (int b = blockIdx.x; b < A.kv.B; b += gridDim.x) {
-            if (seq_work<D>(A, b, nullptr).nc) continue;
-            for (int i = tid; i < A.Hq * D; i += kThreads) A.out[(long long)b * A.Hq * D + i] = 0;
-            if (A.lse) for (int i = tid; i < A.Hq; i += kThreads) A.lse[(long long)b * A.Hq + i] = -INFINITY;
-        }
-        if (g0 >= g1) return;
+    const int total = scan_work<D>(A, sh_scan, blockIdx.x == 0 ? A.status : nullptr);
+    const int per = (total - 1) / A.n_cta + 1, g0 = min((long long)total, (long long)blockIdx.x * per), g1 = total - g0 < per ? total : g0 + per;
+    if (g0 < g1) {
         cons = find_item<D>(A, g0, sh_scan);
+        if (tid == 0) A.part_first[blockIdx.x] = cons.b * A.kv.H * A.GB + cons.hh;
     }
 
     // ---- loader side: chunk ids g0 + warp, + kWarps, ...
     Cursor load = cons;
-    long long load_id = g0 + warp;
+    int load_id = g0 + warp;
     int load_stage = 0;
     const uint32_t ring_addr = si_tc::smem_u32(ring);
+    const int load_r = lane / PIECES, load_c = lane % PIECES * 8;
+    const uint32_t load_at = load_r * (D * 2) + (((lane % PIECES) & 8) << 4) + (((lane ^ load_r) & 7) << 4);
     auto issue = [&]() {
         if (load_id < g1) {
             while (load_id >= load.start + load.w.nc) next_item<D>(A, load);
-            const int t = (int)(load_id - load.start), c = t < load.w.c_sink ? t : load.w.c_win + t - load.w.c_sink;
+            const int t = load_id - load.start, c = t < load.w.c_sink ? t : load.w.c_win + t - load.w.c_sink;
             const int h = load.hh / A.GB, j0 = c * CH;
-            const uint32_t kdst = ring_addr + load_stage * C::kStage, vdst = kdst + 4096;
-            const int piece = lane % PIECES, r0 = lane / PIECES;
+            const uint32_t kdst = ring_addr + load_stage * C::kStage;
+            // row r of the chunk, 16-byte piece c of it, lies at r * 2 D + ((c ^ r) & 7) * 16 (+ 128 for c >= 8): the eight
+            // rows of an ldmatrix tile are then in eight different banks groups.  A lane loads the same piece of rows r0, r0 + 32 / PIECES, ..
+            const uint32_t at = (kdst + load_at);
+            const long long step = (32 / PIECES) * A.kv.rs;
+            if (j0 + CH <= min(load.w.n, load.w.n_old)) {
+                const uint16_t *ks = A.kv.k + A.kv.row(load.b, h, j0 + load_r) + load_c, *vs = A.kv.v + (ks - A.kv.k);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int r = r0 + i * (32 / PIECES), j = j0 + r;
-                const bool fresh = j == load.w.n_old;
-                const long long off = fresh ? load.b * A.new_ss + (long long)h * D + piece * 8 : A.kv.row(load.b, h, j < load.w.n ? j : 0) + piece * 8;
-                const uint16_t *ks = (fresh ? A.kn : A.kv.k) + off, *vs = (fresh ? A.vn : A.kv.v) + off;
-                const int bytes = j < load.w.n ? 16 : 0;     // past the end: zeros, nothing is read
-                const uint32_t at = r * (D * 2) + (((piece & 8) | ((piece ^ r) & 7)) << 4);
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(kdst + at), "l"(ks), "r"(bytes) : "memory");
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(vdst + at), "l"(vs), "r"(bytes) : "memory");
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t to = (at ^ ((i * (32 / PIECES) & 7) << 4)) + i * 512;
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(ks) : "memory");
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + 4096), "l"(vs) : "memory");
+                    ks += step; vs += step;
+                }
+            } else {
+#pragma unroll 1
+                for (int i = 0; i < 8; ++i) {
+                    const int j = j0 + load_r + i * (32 / PIECES);
+                    const bool fresh = j == load.w.n_old;
+                    const long long off = fresh ? load.b * A.new_ss + (long long)h * D + load_c : A.kv.row(load.b, h, j < load.w.n ? j : 0) + load_c;
+                    const uint16_t *ks = (fresh ? A.kn : A.kv.k) + off, *vs = (fresh ? A.vn : A.kv.v) + off;
+                    const int bytes = j < load.w.n ? 16 : 0;     // past the end: zeros, nothing is read
+                    const uint32_t to = (at ^ ((i * (32 / PIECES) & 7) << 4)) + i * 512;
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(ks), "r"(bytes) : "memory");
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + 4096), "l"(vs), "r"(bytes) : "memory");
+                }
             }
             if (A.kv.pos && lane < CH) {
                 const int j = j0 + lane;
-                asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(vdst + 4096 + lane * 4),
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(kdst + 8192 + lane * 4),
                              "l"(A.kv.pos + A.kv.meta(load.b, h) + (j < load.w.n ? j : 0)), "r"(j < load.w.n ? 4 : 0) : "memory");
             }
             load_id += kWarps;
@@ -244,34 +257,44 @@ __global__ void __launch_bounds__(kThreads, 1) decode_kernel(const DecodeArgs A)
     issue();
 
     // ---- consumer side
-    long long id = g0 + warp;
+    int id = g0 + warp;
     int stage = 0;
     bool first_segment = true;
+    uint32_t qf[NT][D / 16][2];
+    if (g0 < g1) load_q<D, NT>(A, cons.b, cons.hh, qf);
+    // while the first chunks are on their way: the new entries are stored for later calls (this one reads them from where
+    // they are), and sequences without a visible entry, which have no chunk, get their zeros
+    if (A.kn)
+        for (int r = blockIdx.x; r < A.kv.B * A.kv.H; r += gridDim.x) {
+            const int b = r / A.kv.H, h = r % A.kv.H, n = si_kv_len(A.kv, b, nullptr);
+            if (n >= A.kv.cap) continue;
+            const long long to = A.kv.row(b, h, n), from = b * A.new_ss + (long long)h * D;
+            if (tid < PIECES) *reinterpret_cast<uint4 *>(A.kv.k + to + tid * 8) = *reinterpret_cast<const uint4 *>(A.kn + from + tid * 8);
+            else if (tid < 2 * PIECES) *reinterpret_cast<uint4 *>(A.kv.v + to + (tid - PIECES) * 8) = *reinterpret_cast<const uint4 *>(A.vn + from + (tid - PIECES) * 8);
+            else if (tid == 2 * PIECES && A.kv.pos) A.kv.pos[A.kv.meta(b, h) + n] = A.q_pos[b];
+        }
+
+    if (sh_scan[kThreads + 1])
+        for (int b = blockIdx.x; b < A.kv.B; b += gridDim.x) {
+            if (seq_work<D>(A, b, nullptr).nc) continue;
+            for (int i = tid; i < A.Hq * D; i += kThreads) A.out[(long long)b * A.Hq * D + i] = 0;
+            if (A.lse) for (int i = tid; i < A.Hq; i += kThreads) A.lse[(long long)b * A.Hq + i] = -INFINITY;
+        }
+    if (g0 >= g1) return;
     while (true) {
-        const long long seg_end = min(g1, cons.start + cons.w.nc);
+        const int seg_end = min(g1, cons.start + cons.w.nc);
         const int h = cons.hh / A.GB, gb = cons.hh % A.GB, head0 = gb * HB, heads = min(HB, A.G - head0);
         const SeqWork w = cons.w;
-        uint32_t qf[NT][D / 16][2];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const int head = nt * 8 + (lane >> 2);
-            const uint16_t *q = A.q + cons.b * A.q_ss + (long long)(h * A.G + head0 + head) * D + 2 * (lane & 3);
-#pragma unroll
-            for (int s = 0; s < D / 16; ++s) {
-                qf[nt][s][0] = head < heads ? *reinterpret_cast<const uint32_t *>(q + s * 16) : 0u;
-                qf[nt][s][1] = head < heads ? *reinterpret_cast<const uint32_t *>(q + s * 16 + 8) : 0u;
-            }
-        }
         float o[NT][D / 16][4] = {};
-        float m[NT][2], l[NT][2];
+        float m[NT][2], base[NT][2], l[NT][2];      // base: the maximum, 0 while there is none
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) { m[nt][0] = m[nt][1] = -INFINITY; l[nt][0] = l[nt][1] = 0.f; }
+        for (int nt = 0; nt < NT; ++nt) { m[nt][0] = m[nt][1] = -INFINITY; base[nt][0] = base[nt][1] = l[nt][0] = l[nt][1] = 0.f; }
         for (; id < seg_end; id += kWarps) {
             asm volatile("cp.async.wait_group 1;" ::: "memory");
             __syncwarp();
             issue();
             const uint32_t kbase = ring_addr + stage * C::kStage, vbase = kbase + 4096;
-            const int t = (int)(id - cons.start), j0 = (t < w.c_sink ? t : w.c_win + t - w.c_sink) * CH;
+            const int t = id - cons.start, j0 = (t < w.c_sink ? t : w.c_win + t - w.c_sink) * CH;
             // which keys of the chunk are visible; the values of the others must not meet the product (0 * NaN)
             uint32_t vis;
             {
@@ -289,12 +312,11 @@ __global__ void __launch_bounds__(kThreads, 1) decode_kernel(const DecodeArgs A)
             float x[SUB][NT][4] = {};
 #pragma unroll
             for (int u = 0; u < SUB; ++u) {
-                const int r = u * 16 + (lane & 15);
+                const uint32_t ka = kbase + u * 16 * D * 2 + (lane & 15) * (D * 2) + (((lane >> 4 ^ lane) & 7) << 4);
 #pragma unroll
                 for (int s = 0; s < D / 16; ++s) {
-                    const int piece = s * 2 + (lane >> 4);
                     uint32_t a[4];
-                    ldm4(a, kbase + r * (D * 2) + (((piece & 8) | ((piece ^ r) & 7)) << 4));
+                    ldm4(a, (ka ^ ((2 * s & 7) << 4)) + (s >> 2) * 128);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) mma<DT>(x[u][nt], a, qf[nt][s][0], qf[nt][s][1]);
                 }
@@ -305,11 +327,22 @@ __global__ void __launch_bounds__(kThreads, 1) decode_kernel(const DecodeArgs A)
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int key = u * 16 + (lane >> 2) + (e >> 1) * 8;
-                        x[u][nt][e] = (vis >> key & 1) ? x[u][nt][e] * A.scale2 : -INFINITY;
-                        grow |= x[u][nt][e] > m[nt][e & 1] + kLazy;
-                    }
+                    for (int e = 0; e < 4; ++e) x[u][nt][e] *= A.scale2;
+            if (vis != kAll) {
+#pragma unroll
+                for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (!(vis >> (u * 16 + (lane >> 2) + (e >> 1) * 8) & 1)) x[u][nt][e] = -INFINITY;
+            }
+#pragma unroll
+            for (int u = 0; u < SUB; ++u)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) grow |= x[u][nt][e] > m[nt][e & 1] + kLazy;
             if (A.acc) {
                 float *sc = A.scores + ((((long long)cons.b * A.kv.H + h) * A.GB + gb) * A.kv.cap + j0) * A.GS;
 #pragma unroll
@@ -336,6 +369,7 @@ __global__ void __launch_bounds__(kThreads, 1) decode_kernel(const DecodeArgs A)
                         mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 16));
                         const float f = mx == -INFINITY ? 1.f : ex2(m[nt][c] - mx);
                         m[nt][c] = mx;
+                        base[nt][c] = mx == -INFINITY ? 0.f : mx;
                         l[nt][c] *= f;
 #pragma unroll
                         for (int s = 0; s < D / 16; ++s) { o[nt][s][c] *= f; o[nt][s][c + 2] *= f; }
@@ -348,19 +382,17 @@ __global__ void __launch_bounds__(kThreads, 1) decode_kernel(const DecodeArgs A)
                 for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float base = m[nt][e & 1] == -INFINITY ? 0.f : m[nt][e & 1];
-                        x[u][nt][e] = ex2(x[u][nt][e] - base);
+                        x[u][nt][e] = ex2(x[u][nt][e] - base[nt][e & 1]);
                         l[nt][e & 1] += x[u][nt][e];
                     }
                     pb[nt][0] = mov_trans(pack2<DT>(x[u][nt][0], x[u][nt][1]));
                     pb[nt][1] = mov_trans(pack2<DT>(x[u][nt][2], x[u][nt][3]));
                 }
-                const int r = u * 16 + (lane & 7) + ((lane >> 4) << 3);
+                const uint32_t va = vbase + u * 16 * D * 2 + ((lane & 7) + ((lane >> 4) << 3)) * (D * 2) + ((((lane >> 3 & 1) ^ lane) & 7) << 4);
 #pragma unroll
                 for (int s = 0; s < D / 16; ++s) {
-                    const int piece = s * 2 + ((lane >> 3) & 1);
                     uint32_t a[4];
-                    ldm4t(a, vbase + r * (D * 2) + (((piece & 8) | ((piece ^ r) & 7)) << 4));
+                    ldm4t(a, (va ^ ((2 * s & 7) << 4)) + (s >> 2) * 128);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) mma<DT>(o[nt][s], a, pb[nt][0], pb[nt][1]);
                 }
@@ -368,6 +400,15 @@ __global__ void __launch_bounds__(kThreads, 1) decode_kernel(const DecodeArgs A)
             __syncwarp();                      // the stage may be loaded again
             stage = stage + 1 == kStages ? 0 : stage + 1;
         }
+        // the next item's queries are on their way while the warps are joined
+        const Cursor seg = cons;
+        if (seg_end < g1) {
+            next_item<D>(A, cons);
+            load_q<D, NT>(A, cons.b, cons.hh, qf);
+        }
+        // the CTAs of this item, for the joining kernel: written by the one that has its first chunk
+        if (tid == 0 && seg.start >= g0)
+            A.runs[(long long)seg.b * A.kv.H * A.GB + seg.hh] = make_int2(seg.start / per, (seg.start + w.nc - 1) / per);
         // ---- the segment's warps joined: rows scaled to the common maximum, summed in warp order
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -382,7 +423,7 @@ __global__ void __launch_bounds__(kThreads, 1) decode_kernel(const DecodeArgs A)
                 }
             }
         __syncthreads();
-        const bool whole = cons.start >= g0 && cons.start + w.nc <= g1;
+        const bool whole = seg.start >= g0 && seg.start + w.nc <= g1;
         float *po = A.part_o + ((long long)blockIdx.x * 2 + (first_segment ? 0 : 1)) * HB * D;
         float *pml = A.part_ml + ((long long)blockIdx.x * 2 + (first_segment ? 0 : 1)) * HB * 2;
 #pragma unroll
@@ -433,7 +474,7 @@ __global__ void __launch_bounds__(kThreads, 1) decode_kernel(const DecodeArgs A)
                     const float2 t = *reinterpret_cast<const float2 *>(merge_o + v * C::kMerge + hd * C::kRow + d);
                     acc.x += t.x; acc.y += t.y;
                 }
-                const long long row = (long long)cons.b * A.Hq + h * A.G + head0 + head;
+                const long long row = (long long)seg.b * A.Hq + h * A.G + head0 + head;
                 if (whole) {
                     const float inv = sum == 0.f ? 0.f : 1.f / sum;
                     *reinterpret_cast<uint32_t *>(A.out + row * D + d) = pack2<DT>(acc.x * inv, acc.y * inv);
@@ -451,78 +492,116 @@ __global__ void __launch_bounds__(kThreads, 1) decode_kernel(const DecodeArgs A)
         }
         first_segment = false;
         if (seg_end >= g1) return;
-        next_item<D>(A, cons);
     }
 }
 
 // Joins the parts of items that crossed CTAs and, where weights are wanted, adds them up.  One CTA per (sequence, key head)
-// and range of keys.
+// and range of kJoinKeys keys; the first range's writes the output.
+constexpr int kJoinKeys = 1024;
+constexpr int kMaxParts = 256;             // CTAs of the main kernel at most
 template <int DT, int D, int NT>
-__global__ void __launch_bounds__(kThreads) decode_join_kernel(const DecodeArgs A, int keys_per_cta) {
-    constexpr int HB = 8 * NT;
-    __shared__ long long sh_scan[kThreads + 1];
-    __shared__ float sh_lse2[128];
-    const int tid = threadIdx.x, h = blockIdx.y, b = blockIdx.z;
+__global__ void __launch_bounds__(kThreads) decode_join_kernel(const DecodeArgs A) {
+    constexpr int HB = 8 * NT, CH = 2048 / D;
+    __shared__ float sh_lse2[128], sh_f[HB][kMaxParts], sh_inv[HB];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, h = blockIdx.y, b = blockIdx.z;
     si_tc::pdl_wait();
     const SeqWork w = seq_work<D>(A, b, nullptr);
-    if (w.nc == 0 && !A.acc) return;
-    const long long total = scan_work<D>(A, sh_scan, nullptr), per = run_length(total, A.n_cta);
-    // the first chunk of this sequence: the scan has it for the first sequence of each thread's run
-    const int per_thread = (A.kv.B + kThreads - 1) / kThreads;
-    long long start = sh_scan[b / per_thread];
-    for (int c = b / per_thread * per_thread; c < b; ++c) start += (long long)seq_work<D>(A, c, nullptr).nc * A.kv.H * A.GB;
-    for (int gb = 0; gb < A.GB; ++gb) {
-        const long long s0 = start + (long long)(h * A.GB + gb) * w.nc, s1 = s0 + w.nc;
+    const int j0 = blockIdx.x * kJoinKeys;
+    if (j0 >= w.n && (blockIdx.x > 0 || w.nc == 0)) return;
+    // the scores and weights of this CTA's keys, on their way while the sums are joined
+    constexpr int kKeys = kJoinKeys / kThreads;
+    float *weight = A.kv.weight + A.kv.meta(b, h);
+    const float *sc = A.scores + ((long long)b * A.kv.H + h) * A.GB * A.kv.cap * A.GS;
+    auto worked = [&](int j) { const int c = j / CH; return c < w.c_sink || (c >= w.c_win && c < w.c_win + w.nc - w.c_sink); };
+    float2 x[kKeys][HB / 2];
+    float old[kKeys];
+    if (A.acc) {
+#pragma unroll
+        for (int i = 0; i < kKeys; ++i) {
+            const int j = j0 + i * kThreads + tid;
+            if (j >= w.n || !worked(j)) continue;
+            old[i] = weight[j];
+#pragma unroll
+            for (int g = 0; g < HB; g += 2)
+                if (g < A.GS) x[i][g / 2] = *reinterpret_cast<const float2 *>(sc + (long long)j * A.GS + g);
+        }
+    }
+    for (int gb = 0; gb < A.GB && w.nc > 0; ++gb) {
         const int head0 = gb * HB, heads = min(HB, A.G - head0);
         const long long row0 = (long long)b * A.Hq + h * A.G + head0;
-        if (w.nc == 0) break;
-        const int x0 = (int)(s0 / per), x1 = (int)((s1 - 1) / per);
-        if (x0 == x1) {                                // finished by one CTA
+        const int2 run = A.runs[((long long)b * A.kv.H + h) * A.GB + gb];
+        if (run.x == run.y) {                          // finished by one CTA
             if (A.acc && tid < heads) sh_lse2[head0 + tid] = A.lse2[row0 + tid];
             continue;
         }
-        for (int i = tid; i < heads * (D / 2); i += kThreads) {
-            const int head = i / (D / 2), d = i % (D / 2) * 2;
-            if (blockIdx.x > 0 && d > 0) continue;     // the other key ranges need the sums only
-            float top = -INFINITY, sum = 0.f;
-            float2 acc = make_float2(0.f, 0.f);
-            for (int x = x0; x <= x1; ++x) top = fmaxf(top, A.part_ml[(((long long)x * 2 + (s0 <= x * per ? 0 : 1)) * HB + head) * 2]);
-            for (int x = x0; x <= x1; ++x) {
-                const long long slot = (long long)x * 2 + (s0 <= x * per ? 0 : 1);
-                const float mv = A.part_ml[(slot * HB + head) * 2], f = mv == -INFINITY ? 0.f : ex2(mv - top);
-                sum += A.part_ml[(slot * HB + head) * 2 + 1] * f;
-                const float2 t = *reinterpret_cast<const float2 *>(A.part_o + (slot * HB + head) * D + d);
-                acc.x += t.x * f; acc.y += t.y * f;
+        // an item's first CTA has it as its last segment, unless its run starts with it (then nothing lies before it)
+        const bool head_first = A.part_first[run.x] == (b * A.kv.H + h) * A.GB + gb;
+        const int parts = run.y - run.x + 1;
+        auto slot = [&](int i) { return (long long)(run.x + i) * 2 + (i > 0 || head_first ? 0 : 1); };
+        __syncthreads();
+        for (int head = warp; head < heads; head += kWarps) {      // a warp per head, a lane per part: one round of loads
+            float mv[kMaxParts / 32], top = -INFINITY, sum = 0.f;
+#pragma unroll
+            for (int k = 0; k < kMaxParts / 32; ++k) {
+                const int i = k * 32 + lane;
+                mv[k] = i < parts ? A.part_ml[(slot(i) * HB + head) * 2] : -INFINITY;
+                top = fmaxf(top, mv[k]);
             }
-            const float l2 = sum == 0.f ? -INFINITY : top + log2f(sum), inv = sum == 0.f ? 0.f : 1.f / sum;
-            if (blockIdx.x == 0) {
-                *reinterpret_cast<uint32_t *>(A.out + (row0 + head) * D + d) = pack2<DT>(acc.x * inv, acc.y * inv);
-                if (d == 0 && A.lse) A.lse[row0 + head] = l2 / kLog2e;
+#pragma unroll
+            for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+#pragma unroll
+            for (int k = 0; k < kMaxParts / 32; ++k) {
+                const int i = k * 32 + lane;
+                if (i >= parts) continue;
+                const float f = mv[k] == -INFINITY ? 0.f : ex2(mv[k] - top);
+                sh_f[head][i] = f;
+                sum += A.part_ml[(slot(i) * HB + head) * 2 + 1] * f;
             }
-            if (d == 0) sh_lse2[head0 + head] = l2;
+#pragma unroll
+            for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+            if (lane == 0) {
+                const float l2 = sum == 0.f ? -INFINITY : top + log2f(sum);
+                sh_lse2[head0 + head] = l2;
+                sh_inv[head] = sum == 0.f ? 0.f : 1.f / sum;
+                if (blockIdx.x == 0 && A.lse) A.lse[row0 + head] = l2 / kLog2e;
+            }
         }
+        __syncthreads();
+        if (blockIdx.x == 0)
+            for (int i = tid; i < heads * (D / 2); i += kThreads) {
+                const int head = i / (D / 2), d = i % (D / 2) * 2;
+                float2 acc = make_float2(0.f, 0.f);
+#pragma unroll 8
+                for (int x = 0; x < parts; ++x) {
+                    const float2 t = *reinterpret_cast<const float2 *>(A.part_o + (slot(x) * HB + head) * D + d);
+                    acc.x += t.x * sh_f[head][x]; acc.y += t.y * sh_f[head][x];
+                }
+                *reinterpret_cast<uint32_t *>(A.out + (row0 + head) * D + d) = pack2<DT>(acc.x * sh_inv[head], acc.y * sh_inv[head]);
+            }
     }
     if (!A.acc) return;
     __syncthreads();
-    constexpr int CH = 2048 / D;
-    float *weight = A.kv.weight + A.kv.meta(b, h);
-    const float *sc = A.scores + ((long long)b * A.kv.H + h) * A.GB * A.kv.cap * A.GS;
-    const int j0 = blockIdx.x * keys_per_cta, j1 = min(w.n, j0 + keys_per_cta);
-    for (int j = j0 + tid; j < j1; j += kThreads) {
-        const int c = j / CH;
+#pragma unroll
+    for (int i = 0; i < kKeys; ++i) {
+        const int j = j0 + i * kThreads + tid;
+        if (j >= w.n) continue;
+        if (!worked(j)) { if (j == w.n_old) weight[j] = 0.f; continue; }
         float sum = 0.f;
-        const bool worked = c < w.c_sink || (c >= w.c_win && c < w.c_win + w.nc - w.c_sink);
-        if (worked)
-            for (int g = 0; g < A.G; ++g) {
-                const float x = sc[((long long)(g / HB) * A.kv.cap + j) * A.GS + g % HB];
-                if (x != -INFINITY) sum += ex2(x - sh_lse2[g]);
+        for (int gb = 0; gb < A.GB; ++gb) {
+            const float *row = sc + ((long long)gb * A.kv.cap + j) * A.GS;
+#pragma unroll
+            for (int g = 0; g < HB; g += 2) {
+                if (g >= A.GS || gb * HB + g >= A.G) break;
+                const float2 y = gb == 0 ? x[i][g / 2] : *reinterpret_cast<const float2 *>(row + g);
+                if (y.x != -INFINITY) sum += ex2(y.x - sh_lse2[gb * HB + g]);
+                if (gb * HB + g + 1 < A.G && y.y != -INFINITY) sum += ex2(y.y - sh_lse2[gb * HB + g + 1]);
             }
-        if (j == w.n_old) weight[j] = sum;
-        else if (worked) weight[j] += sum;
+        }
+        weight[j] = j == w.n_old ? sum : old[i] + sum;
     }
 }
 
-struct Layout { int n_cta, NT, GB, GS; size_t o, ml, lse2, scores, total; };
+struct Layout { int n_cta, NT, GB, GS; size_t o, ml, lse2, scores, runs, first, total; };
 Layout layout_of(const si_kv_t *kv, int n_q_heads, bool acc) {
     Layout L;
     static int sms = 0;
@@ -531,7 +610,7 @@ Layout layout_of(const si_kv_t *kv, int n_q_heads, bool acc) {
         if (cudaGetDevice(&dev) == cudaSuccess && cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess && n > 0) sms = n;
         else (void)cudaGetLastError();
     }
-    L.n_cta = sms ? sms : SI_NUM_SMS_FALLBACK;
+    L.n_cta = sms ? (sms < kMaxParts ? sms : kMaxParts) : SI_NUM_SMS_FALLBACK;
     const int G = n_q_heads / kv->n_kv_heads;
     L.NT = G <= 8 ? 1 : 2;
     L.GB = (G + 8 * L.NT - 1) / (8 * L.NT);
@@ -542,6 +621,8 @@ Layout layout_of(const si_kv_t *kv, int n_q_heads, bool acc) {
     L.ml = take((size_t)L.n_cta * 2 * 8 * L.NT * 2 * 4);
     L.lse2 = take(acc ? (size_t)kv->n_seqs * n_q_heads * 4 : 0);
     L.scores = take(acc ? (size_t)kv->n_seqs * kv->n_kv_heads * L.GB * kv->capacity * L.GS * 4 : 0);
+    L.runs = take((size_t)kv->n_seqs * kv->n_kv_heads * L.GB * 8);
+    L.first = take((size_t)L.n_cta * 4);
     L.total = off;
     return L;
 }
@@ -554,16 +635,15 @@ template <int DT, int D, int NT> int launch(const DecodeArgs &A, cudaStream_t st
     }
     decode_kernel<DT, D, NT><<<A.n_cta, kThreads, (Cfg<D, NT>::kSmem), st>>>(A);
     SI_CUDA_TRY(cudaGetLastError());
-    const int keys = 2048;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(A.acc ? (A.kv.cap + keys - 1) / keys : 1, A.kv.H, A.kv.B);
+    cfg.gridDim = dim3(A.acc ? (A.kv.cap + kJoinKeys - 1) / kJoinKeys : 1, A.kv.H, A.kv.B);
     cfg.blockDim = dim3(kThreads);
     cfg.stream = st;
     cudaLaunchAttribute at;
     at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at.val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = &at; cfg.numAttrs = 1;
-    SI_CUDA_TRY(cudaLaunchKernelEx(&cfg, decode_join_kernel<DT, D, NT>, A, keys));
+    SI_CUDA_TRY(cudaLaunchKernelEx(&cfg, decode_join_kernel<DT, D, NT>, A));
     return SI_OK;
 }
 template <int DT> int launch_t(const DecodeArgs &A, int NT, cudaStream_t st) {
@@ -589,6 +669,8 @@ extern "C" int si_attn_decode(const si_kv_t *kv, const void *q, long long q_seq_
     if (!si_aligned16(q) || !si_aligned16(out) || !si_aligned16(k_new) || !si_aligned16(v_new) || ((q_seq_stride | new_seq_stride) & 7))
         return SI_ERR_ALIGNMENT;
     const Layout L = layout_of(kv, n_q_heads, acc);
+    // chunks are numbered in 32 bits: 2^31 of them are 16 TB of keys and values unless sequences share memory by zero strides
+    if ((double)kv->n_seqs * kv->n_kv_heads * L.GB * (kv->capacity / (2048 / kv->head_dim) + 2) > 2.0e9) return SI_ERR_TOO_LARGE;
     if (ws_bytes < L.total) return SI_ERR_NOMEM;
     if (!workspace) return SI_ERR_INVALID_ARG;
     if ((uintptr_t)workspace & 255) return SI_ERR_ALIGNMENT;
@@ -596,6 +678,6 @@ extern "C" int si_attn_decode(const si_kv_t *kv, const void *q, long long q_seq_
     const DecodeArgs A{si_kv_view_of(kv), (const uint16_t *)q, (const uint16_t *)k_new, (const uint16_t *)v_new, q_pos, q_seq_stride,
                        new_seq_stride, n_q_heads, n_q_heads / kv->n_kv_heads, L.GB, L.GS, window, n_sink, scale * kLog2e,
                        (uint16_t *)out, lse, status_dev, acc, L.n_cta, (float *)(ws + L.o), (float *)(ws + L.ml),
-                       (float *)(ws + L.lse2), (float *)(ws + L.scores)};
+                       (float *)(ws + L.lse2), (float *)(ws + L.scores), (int2 *)(ws + L.runs), (int *)(ws + L.first)};
     return kv->dtype == SI_BF16 ? launch_t<SI_BF16>(A, L.NT, (cudaStream_t)stream) : launch_t<SI_F16>(A, L.NT, (cudaStream_t)stream);
 }

@@ -51,7 +51,7 @@ __device__ __forceinline__ void si_report(int32_t *status, int err) { if (status
 
 // Entries in use, clamped to the capacity.
 __device__ __forceinline__ int si_kv_len(const si_kv_view &kv, int b, int32_t *status) {
-    const int n = kv.len[b];
+    const int n = __ldg(kv.len + b);
     if (n < 0 || n > kv.cap) { si_report(status, SI_ERR_OUT_OF_RANGE); return n < 0 ? 0 : kv.cap; }
     return n;
 }

@@ -604,13 +604,7 @@ __global__ void __launch_bounds__(kThreads) decode_join_kernel(const DecodeArgs 
 struct Layout { int n_cta, NT, GB, GS; size_t o, ml, lse2, scores, runs, first, total; };
 Layout layout_of(const si_kv_t *kv, int n_q_heads, bool acc) {
     Layout L;
-    static int sms = 0;
-    if (!sms) {
-        int dev = 0, n = 0;
-        if (cudaGetDevice(&dev) == cudaSuccess && cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess && n > 0) sms = n;
-        else (void)cudaGetLastError();
-    }
-    L.n_cta = sms ? (sms < kMaxParts ? sms : kMaxParts) : SI_NUM_SMS_FALLBACK;
+    L.n_cta = si_sm_count() < kMaxParts ? si_sm_count() : kMaxParts;
     const int G = n_q_heads / kv->n_kv_heads;
     L.NT = G <= 8 ? 1 : 2;
     L.GB = (G + 8 * L.NT - 1) / (8 * L.NT);

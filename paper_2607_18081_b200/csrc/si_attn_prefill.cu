@@ -2,14 +2,20 @@
 // of every sequence.  One pass over the keys with the running maximum and sum of the softmax.
 //
 // A CTA owns two tiles of 128 query rows.  A row is a (query, head of the group) pair, so the G heads that read one key head
-// share its tiles, and the span of positions in a tile -- what the causal edge and the window cost -- is 128 / G.  Warps 0-3
-// and 4-7 are the softmax warpgroups of the two tiles (one row per thread), warp 8 loads tiles by TMA, warp 9 issues the
-// matrix products (10 and 11 idle: registers are handed over by whole warpgroups):
-//   S_t = Q_t K_j^T      (operands in shared memory, S in tensor memory)
-//   O_t += P_t V_j       (P in tensor memory, written over S_t by the softmax warps; V as it lies, MN-major)
+// share its tiles, and the span of positions in a tile -- what the causal edge and the window cost -- is 128 / G.
+//   warps 0-3, 4-7   softmax of the two tiles, a row per thread
+//   warp 8           loads tiles by TMA
+//   warp 9           issues the matrix products: S_t = Q_t K_j^T  (operands in shared memory, S in tensor memory)
+//                                                O_t += P_t V_j   (P in tensor memory, written over S_t; V as it lies, MN-major)
+//   warp 10          clears the values beyond the length in a sequence's last tile (11 idles)
 // The products of one tile run while the softmax of the other does.  O stays in tensor memory; it is rescaled only when a
 // row's maximum grows by more than 2^8 (then p may reach 2^8, which fp32 sums and 16-bit p carry without loss), by the
 // softmax warps themselves: S_t(j) is complete only after O_t(j-1), so nothing else touches O_t at that time.
+//
+// With few rows the keys are split over CTAs as well: each leaves its unnormalised O, maximum and sum, and a second kernel
+// joins them in order.
+#include <type_traits>
+
 #include "si_attn_tc.cuh"
 
 namespace {
@@ -17,24 +23,28 @@ namespace {
 using namespace si_attn;
 
 constexpr int kThreads = 384;
-// Registers: 384 threads start with 168 each; the four service warps give up 96 of theirs, the softmax warps take 48 more
-// (2 x 216 + 72 = 3 x 168), so that a row's 128 scores stay in registers.
-constexpr int kRegsSoft = 216, kRegsService = 72;
+// Registers: 384 threads start with 168 each; the four service warps give up 64 of theirs, the softmax warps take 32 more
+// (2 x 200 + 104 = 3 x 168), so that a row's 128 scores stay in registers.
+constexpr int kRegsSoft = 200, kRegsService = 104;
 constexpr float kLazy = 8.f;
 
 template <int D> struct Cfg {
     static constexpr int kBytes = kTile * D * 2;            // a tile of queries, keys or values
-    static constexpr int kStages = D == 128 ? 5 : 8;
+    static constexpr int kStages = 4;                       // even ones hold keys, odd ones values
     static constexpr int kSmem = (2 + kStages) * kBytes + 1024 + 256;
     static constexpr int kPanel = kTile * 128;              // 64 columns of a tile
 };
 
-struct Bars { uint64_t q, full[8], empty[8], s[2], p[2], o[2]; uint32_t tmem; int failed; };
+struct Bars { uint64_t q, full[4], empty[4], s[2], p[2][2], o[2], dirty, clean; uint32_t tmem; int failed; };
 
-template <int DT, int D>
+// Keys split over P.n CTAs per block of queries (1: not split); parts: [split][block][tile][row], values and {maximum, sum}.
+struct SplitArgs { int n, blocks; float *o; float2 *ml; };
+
+// NEG: the scale is negative; the scores are then turned around and |scale| is used.
+template <int DT, int D, bool NEG>
 __global__ void __launch_bounds__(kThreads, 1)
 prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,
-               const TcArgs A) {
+               const TcArgs A, const SplitArgs P) {
     using C = Cfg<D>;
     constexpr int NS = C::kStages;
     extern __shared__ char smem_raw[];
@@ -47,7 +57,8 @@ prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
     if (threadIdx.x == 0) {
         mbar_init(&B->q, 1);
         for (int s = 0; s < NS; ++s) { mbar_init(&B->full[s], 1); mbar_init(&B->empty[s], 1); }
-        for (int t = 0; t < 2; ++t) { mbar_init(&B->s[t], 1); mbar_init(&B->p[t], 4); mbar_init(&B->o[t], 1); }
+        for (int t = 0; t < 2; ++t) { mbar_init(&B->s[t], 1); mbar_init(&B->p[t][0], 4); mbar_init(&B->p[t][1], 4); mbar_init(&B->o[t], 1); }
+        mbar_init(&B->dirty, 1); mbar_init(&B->clean, 1);
         B->failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -62,11 +73,14 @@ prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
 
     // blocks of queries from the last (most keys) to the first, so that the long ones start first
     const int heads = A.kv.H * A.kv.B, nqb = gridDim.x / heads;
-    const int qb = nqb - 1 - blockIdx.x / heads, h = blockIdx.x % heads % A.kv.H, b = blockIdx.x % heads / A.kv.H;
+    const int split = blockIdx.y, qb = nqb - 1 - blockIdx.x / heads, h = blockIdx.x % heads % A.kv.H, b = blockIdx.x % heads / A.kv.H;
     const int n = si_kv_len(A.kv, b, A.status), i0 = qb * 2 * A.R, shift = n - A.T;       // query i is at position shift + i
     const int tiles = i0 + A.R < A.T ? 2 : 1;
-    const KeyTiles keys = key_tiles(shift + i0, shift + min(A.T, i0 + 2 * A.R) - 1, A.window, A.n_sink);
+    KeyTiles keys = key_tiles(shift + i0, shift + min(A.T, i0 + 2 * A.R) - 1, A.window, A.n_sink);
+    keys.off = (int)((long long)keys.n * split / P.n);
+    keys.n = (int)((long long)keys.n * (split + 1) / P.n) - keys.off;
 
+    const bool tail = keys.n > 0 && keys.key0(keys.n - 1) + kTile > n;     // the last tile reaches beyond the entries in use
     if (warp >= 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsService));
         if (warp == 8 && lane == 0 && keys.n > 0) {
@@ -88,64 +102,83 @@ prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
                 for (int k = max(0, it - NS); k < it; ++k) mbar_wait(&B->full[k % NS], k / NS & 1, kWait);
             }
         } else if (warp == 9 && keys.n > 0) {
-            const uint32_t id_s = make_idesc(DT == SI_BF16, 0, 0, 128, 128), id_o = make_idesc(DT == SI_BF16, 0, 1, 128, D);
-            // descriptors: a base per operand, steps added in its 16-byte address field
-            const uint64_t q_desc = make_desc(smem_u32(smem), 16, 1024), k_desc = make_desc(smem_u32(ring), 16, 1024),
-                           v_desc = make_desc(smem_u32(ring), C::kPanel, 1024);
-            auto qk = [&](int t, int st) {
-                if (lane == 0) {
-                    const uint64_t qd = q_desc + t * (C::kBytes / 16), kd = k_desc + st * (C::kBytes / 16);
+            // One elected thread issues everything, with the stages and tiles of a round of the ring unrolled: all addresses and
+            // descriptors are then fixed offsets.  (The matrix unit takes a 128 x 128 x 16 product every 64 clocks and queues few
+            // of them; address arithmetic between two products was 30 % of the time.)
+            if (elect_one()) {
+                const uint32_t id_s = make_idesc(DT == SI_BF16, 0, 0, 128, 128), id_o = make_idesc(DT == SI_BF16, 0, 1, 128, D);
+                const Desc q_desc = desc_of(smem_u32(smem), 16, 1024), k_desc = desc_of(smem_u32(ring), 16, 1024),
+                           v_desc = desc_of(smem_u32(ring), C::kPanel, 1024);
+                auto qk = [&](int t, int st) {
 #pragma unroll
                     for (int k = 0; k < D / 16; ++k) {
-                        const uint64_t off = ((k >> 2) * C::kPanel + (k & 3) * 32) / 16;
-                        umma(tmem + t * 128, qd + off, kd + off, id_s, k > 0);
+                        const uint32_t off = ((k >> 2) * C::kPanel + (k & 3) * 32) / 16;
+                        umma_ss(tmem + t * 128, q_desc, t * (C::kBytes / 16) + off, k_desc, st * (C::kBytes / 16) + off, id_s, k > 0);
                     }
                     umma_commit(&B->s[t]);
-                }
-            };
-            auto pv = [&](int t, int st, bool acc) {
-                if (lane == 0) {
-                    const uint64_t vd = v_desc + st * (C::kBytes / 16);
-#pragma unroll
-                    for (int k = 0; k < kTile / 16; ++k) umma_ts(tmem + 256 + t * D, tmem + t * 128 + k * 8, vd + k * 128, id_o, acc || k > 0);
-                }
-            };
-            auto all = [](bool v) { return __all_sync(0xFFFFFFFFu, v) != 0; };     // the whole warp goes on or stops
-            bool ok = all(mbar_wait(&B->q, 0, kWait) && mbar_wait(&B->full[0], 0, kWait));
-            if (ok) {
-                tc_fence_after();
-                for (int t = 0; t < tiles; ++t) qk(t, 0);
-                if (lane == 0) umma_commit(&B->empty[0]);
-            }
-            for (int j = 0; j < keys.n && ok; ++j) {
-                const int iv = 2 * j + 1, sv = iv % NS, ik = 2 * j + 2, sk = ik % NS;
-                const bool more = j + 1 < keys.n;
-                ok = all(mbar_wait(&B->full[sv], iv / NS & 1, kWait) && !*failed);
-                if (ok && keys.key0(j) + kTile > n) {
-                    // entries from n on may hold anything, and 0 * NaN is NaN: their values are cleared (16-byte pieces of whole rows)
-                    const int first = n - keys.key0(j);
-                    for (int i = lane; i < (kTile - first) * 8 * (D / 64); i += 32) {
-                        const int c = i / ((kTile - first) * 8), at = i % ((kTile - first) * 8);
-                        *reinterpret_cast<uint4 *>(ring + sv * C::kBytes + c * C::kPanel + first * 128 + at * 16) = make_uint4(0, 0, 0, 0);
-                    }
-                    fence_async_proxy();
-                    __syncwarp();
-                }
-                for (int t = 0; t < tiles && ok; ++t) {
-                    ok = all(mbar_wait(&B->p[t], j & 1, kWait) && !*failed);
-                    if (ok && more && t == 0) ok = all(mbar_wait(&B->full[sk], ik / NS & 1, kWait));
-                    if (!ok) break;
+                };
+                bool ok = mbar_wait(&B->q, 0, kWait) && mbar_wait(&B->full[0], 0, kWait);
+                if (ok) {
                     tc_fence_after();
-                    pv(t, sv, j > 0);
-                    if (t == tiles - 1 && lane == 0) umma_commit(&B->empty[sv]);
-                    if (more) qk(t, sk);
-                    else if (lane == 0) umma_commit(&B->o[t]);
+                    qk(0, 0);
+                    if (tiles > 1) qk(1, 0);
+                    umma_commit(&B->empty[0]);
                 }
-                if (ok && more && lane == 0) umma_commit(&B->empty[sk]);
+                constexpr int kRound = NS / 2;                // key tiles per round of the ring (keys in even stages, values in odd ones)
+                for (int j0 = 0, round = 0; j0 < keys.n && ok; j0 += kRound, round ^= 1) {
+#pragma unroll
+                    for (int u = 0; u < kRound; ++u) {
+                        const int j = j0 + u;
+                        if (j >= keys.n || !ok) break;
+                        const int sv = 2 * u + 1, sk = (2 * u + 2) % NS;
+                        const bool more = j + 1 < keys.n;
+                        ok = mbar_spin(&B->full[sv], round, kSpin);
+                        if (ok && more) ok = mbar_spin(&B->full[sk], u + 1 == kRound ? round ^ 1 : round, kSpin);
+                        if (ok && tail && !more) {            // another warp clears what lies beyond the length
+                            mbar_arrive(&B->dirty);
+                            ok = mbar_wait(&B->clean, 0, kWait);
+                        }
+#pragma unroll
+                        for (int t = 0; t < 2; ++t) {
+                            if (t >= tiles || !ok) break;
+                            ok = mbar_spin(&B->p[t][0], j & 1, kSpin);       // the first half of P
+                            if (!ok) break;
+                            tc_fence_after();
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                umma_ts(tmem + 256 + t * D, tmem + t * 128 + k * 8, v_desc, sv * (C::kBytes / 16) + k * 128, id_o, j > 0 || k > 0);
+                            ok = mbar_spin(&B->p[t][1], j & 1, kSpin);
+                            if (!ok) break;
+                            tc_fence_after();
+#pragma unroll
+                            for (int k = 4; k < 8; ++k)
+                                umma_ts(tmem + 256 + t * D, tmem + t * 128 + k * 8, v_desc, sv * (C::kBytes / 16) + k * 128, id_o, 1);
+                            if (more) qk(t, sk);
+                            else umma_commit(&B->o[t]);
+                        }
+                        if (!ok) break;
+                        umma_commit(&B->empty[sv]);
+                        if (more) umma_commit(&B->empty[sk]);
+                    }
+                }
+                if (!ok) {
+                    *failed = 1;
+                    umma_commit(&B->o[0]);       // the products already issued end before tensor memory is freed
+                    umma_commit(&B->o[1]);
+                }
             }
-            if (!ok) {
-                *failed = 1;
-                if (lane == 0) { umma_commit(&B->o[0]); umma_commit(&B->o[1]); }    // the products already issued end before tensor memory is freed
+        } else if (warp == 10 && tail) {
+            // entries from n on may hold anything, and 0 * NaN is NaN: their values in the last tile are cleared
+            const int iv = 2 * keys.n - 1, first = n - keys.key0(keys.n - 1);
+            const bool ok = __all_sync(0xFFFFFFFFu, mbar_wait(&B->dirty, 0, kWait) && !*failed);
+            if (ok) {
+                for (int i = lane; i < (kTile - first) * 8 * (D / 64); i += 32) {
+                    const int c = i / ((kTile - first) * 8), at = i % ((kTile - first) * 8);
+                    *reinterpret_cast<uint4 *>(ring + iv % NS * C::kBytes + c * C::kPanel + first * 128 + at * 16) = make_uint4(0, 0, 0, 0);
+                }
+                fence_async_proxy();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&B->clean);
             }
         }
     } else {
@@ -160,21 +193,20 @@ prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
         float m = -INFINITY, base2 = 0.f, l = 0.f;
         bool ok = true;
         if (t < tiles) {
-            for (int j = 0; j < keys.n; ++j) {
-                ok = __all_sync(0xFFFFFFFFu, mbar_wait(&B->s[t], j & 1, kWait) && !*failed);
-                if (!ok) break;
-                tc_fence_after();
+            // one key tile; MASKED: some row of the tile does not see some key of it (a template argument: joining two versions of
+            // a row's 128 registers after a branch costs more than the maximum)
+            auto step = [&](auto masked, int j, int key0) {
+                constexpr bool MASKED = decltype(masked)::value;
                 uint32_t x[4][32];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) tmem_ld32(ts + c * 32, x[c]);
 #pragma unroll
                 for (int c = 0; c < 4; ++c) tmem_wait_ld(x[c]);
-                const int key0 = keys.key0(j);
-                if (A.sign < 0.f) {
+                if (NEG) {
 #pragma unroll
                     for (int c = 0; c < 128; ++c) x[c / 32][c % 32] ^= 0x80000000u;
                 }
-                if (!(key0 + kTile - 1 <= smin && (key0 > lo_max || key0 + kTile <= A.n_sink))) {
+                if (MASKED) {
                     const int hi_c = s - key0, lo_c = lo - key0, sink_c = A.n_sink - key0;
 #pragma unroll
                     for (int c = 0; c < 128; ++c)
@@ -183,9 +215,10 @@ prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
                 float mx[4];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    mx[c] = __uint_as_float(x[c][0]);
+                    mx[c] = max3(__uint_as_float(x[c][0]), __uint_as_float(x[c][1]), __uint_as_float(x[c][2]));
 #pragma unroll
-                    for (int k = 1; k < 32; ++k) mx[c] = fmaxf(mx[c], __uint_as_float(x[c][k]));
+                    for (int k = 3; k < 31; k += 2) mx[c] = max3(mx[c], __uint_as_float(x[c][k]), __uint_as_float(x[c][k + 1]));
+                    mx[c] = fmaxf(mx[c], __uint_as_float(x[c][31]));
                 }
                 const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
                 const bool grow = top > m && (top - m) * A.scale2 > kLazy;
@@ -193,63 +226,92 @@ prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
                     const float m2 = grow ? top : m, b2 = m2 == -INFINITY ? 0.f : m2 * A.scale2, f = grow ? ex2(m == -INFINITY ? -INFINITY : base2 - b2) : 1.f;
                     m = m2; base2 = b2; l *= f;
                     if (j > 0) {
+#pragma unroll 1
+                        for (int c = 0; c < D / 16; ++c) {
+                            uint32_t o[16];
+                            tmem_ld16(to + c * 16, o);
 #pragma unroll
-                        for (int c = 0; c < D / 32; ++c) {
-                            uint32_t o[32];
-                            tmem_ld32(to + c * 32, o);
-                            tmem_wait_ld(o);
-#pragma unroll
-                            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
-                            tmem_st32(to + c * 32, o);
+                            for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+                            tmem_st16(to + c * 16, o);
                         }
                     }
                 }
-                float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                const f32x2 sc = two(A.scale2, A.scale2), bs = two(-base2, -base2);
+                f32x2 sum[4] = {};
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
                     uint32_t pk[32];
 #pragma unroll
                     for (int k = 0; k < 32; ++k) {
                         const int c = half * 64 + 2 * k;
-                        const float p0 = ex2(fmaf(__uint_as_float(x[c / 32][c % 32]), A.scale2, -base2));
-                        const float p1 = ex2(fmaf(__uint_as_float(x[c / 32][c % 32 + 1]), A.scale2, -base2));
-                        sum[k & 3] += p0 + p1;
+                        f32x2 p = fma2(two(x[c / 32][c % 32], x[c / 32][c % 32 + 1]), sc, bs);
+                        float p0, p1;
+                        untwo(p, p0, p1);
+                        p0 = ex2(p0); p1 = ex2(p1);
+                        sum[k & 3] = add2(sum[k & 3], two(p0, p1));
                         pk[k] = pack2<DT>(p0, p1);
                     }
                     tmem_st32(ts + half * 32, pk);
+                    tmem_wait_st();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&B->p[t][half]);
                 }
-                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-                tmem_wait_st();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&B->p[t]);
+                float s0, s1;
+                untwo(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])), s0, s1);
+                l += s0 + s1;
+            };
+            for (int j = 0; j < keys.n; ++j) {
+                ok = __all_sync(0xFFFFFFFFu, mbar_spin(&B->s[t], j & 1, kSpin));
+                if (!ok) break;
+                tc_fence_after();
+                const int key0 = keys.key0(j);
+                if (key0 + kTile - 1 <= smin && (key0 > lo_max || key0 + kTile <= A.n_sink)) step(std::false_type(), j, key0);
+                else step(std::true_type(), j, key0);
             }
+            pdl_launch();
             if (!ok) *failed = 1;
             if (keys.n > 0) {
-                ok = __all_sync(0xFFFFFFFFu, mbar_wait(&B->o[t], 0, kWait) && ok);
+                ok = __all_sync(0xFFFFFFFFu, mbar_wait(&B->o[t], 0, kWait) && ok && !*failed);
                 tc_fence_after();
             }
-            const float inv = l == 0.f ? 0.f : 1.f / l;
-            const long long r = ((long long)b * A.T + i) * A.Hq + hq;
+            if (P.n > 1) {
+                const long long part = (((long long)split * P.blocks + blockIdx.x) * 2 + t) * kTile + row;
 #pragma unroll
-            for (int c = 0; c < D / 32; ++c) {
-                uint32_t o[32];
-                if (keys.n > 0) { tmem_ld32(to + c * 32, o); tmem_wait_ld(o); }
-                if (!valid) continue;
+                for (int c = 0; c < D / 32; ++c) {
+                    uint32_t o[32] = {};
+                    if (keys.n > 0) { tmem_ld32(to + c * 32, o); tmem_wait_ld(o); }
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    uint4 w = make_uint4(0, 0, 0, 0);
-                    if (l != 0.f) {
-                        const uint32_t *v = o + k * 8;
-                        w.x = pack2<DT>(__uint_as_float(v[0]) * inv, __uint_as_float(v[1]) * inv);
-                        w.y = pack2<DT>(__uint_as_float(v[2]) * inv, __uint_as_float(v[3]) * inv);
-                        w.z = pack2<DT>(__uint_as_float(v[4]) * inv, __uint_as_float(v[5]) * inv);
-                        w.w = pack2<DT>(__uint_as_float(v[6]) * inv, __uint_as_float(v[7]) * inv);
-                    }
-                    *reinterpret_cast<uint4 *>(A.out + r * D + c * 32 + k * 8) = w;
+                    for (int k = 0; k < 8; ++k) *reinterpret_cast<uint4 *>(P.o + part * D + c * 32 + k * 4) = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
                 }
+                P.ml[part] = make_float2(l < 0.5f ? -INFINITY : base2, l);
+            } else {
+                // a row that sees something has its largest p at 1 or above; less than that is a row without a visible entry
+                if (l < 0.5f) l = 0.f;
+                const float inv = l == 0.f ? 0.f : 1.f / l;
+                const long long r = ((long long)b * A.T + i) * A.Hq + hq;
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) {
+                    uint32_t o[32] = {};
+                    if (keys.n > 0) { tmem_ld32(to + c * 32, o); tmem_wait_ld(o); }      // by the whole warp
+                    if (valid) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            uint4 w = make_uint4(0, 0, 0, 0);
+                            if (l != 0.f) {
+                                const uint32_t *v = o + k * 8;
+                                w.x = pack2<DT>(__uint_as_float(v[0]) * inv, __uint_as_float(v[1]) * inv);
+                                w.y = pack2<DT>(__uint_as_float(v[2]) * inv, __uint_as_float(v[3]) * inv);
+                                w.z = pack2<DT>(__uint_as_float(v[4]) * inv, __uint_as_float(v[5]) * inv);
+                                w.w = pack2<DT>(__uint_as_float(v[6]) * inv, __uint_as_float(v[7]) * inv);
+                            }
+                            *reinterpret_cast<uint4 *>(A.out + r * D + c * 32 + k * 8) = w;
+                        }
+                    }
+                    __syncwarp();
+                }
+                if (valid && A.lse) A.lse[r] = l == 0.f ? -INFINITY : (base2 + log2f(l)) / kLog2e;
             }
-            if (valid && A.lse) A.lse[r] = l == 0.f ? -INFINITY : (base2 + log2f(l)) / kLog2e;
         }
         if (!ok && lane == 0) si_report(A.status, SI_ERR_TIMEOUT);
     }
@@ -261,25 +323,91 @@ prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
     }
 }
 
-template <int DT, int D> int launch(const CUtensorMap &qm, const CUtensorMap &km, const CUtensorMap &vm, const TcArgs &A, cudaStream_t st) {
-    static std::atomic<int> ready{0};
-    if (!ready.load()) {
-        SI_CUDA_TRY(cudaFuncSetAttribute(prefill_kernel<DT, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D>::kSmem));
-        ready.store(1);
+// One warp per row: the parts of its splits, in order.
+template <int DT, int D>
+__global__ void __launch_bounds__(256) prefill_join_kernel(const TcArgs A, const SplitArgs P) {
+    const int lane = threadIdx.x & 31;
+    const long long r = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+    pdl_wait();
+    if (r >= (long long)A.kv.B * A.T * A.Hq) return;
+    const int hq = (int)(r % A.Hq), i = (int)(r / A.Hq % A.T), b = (int)(r / A.Hq / A.T), h = hq / A.G;
+    const int heads = A.kv.H * A.kv.B, nqb = P.blocks / heads, qb = i / (2 * A.R), t = i / A.R % 2;
+    const long long block = (long long)(nqb - 1 - qb) * heads + b * A.kv.H + h, row = i % A.R * A.G + hq % A.G;
+    const long long first = (block * 2 + t) * kTile + row, step = (long long)P.blocks * 2 * kTile;
+    float top = -INFINITY;
+    for (int s = lane; s < P.n; s += 32) top = fmaxf(top, P.ml[first + s * step].x);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+    float l = 0.f, acc[D / 32] = {};
+#pragma unroll 4
+    for (int s = 0; s < P.n; ++s) {
+        const float2 ml = P.ml[first + s * step];
+        if (ml.x == -INFINITY) continue;
+        const float f = ex2(ml.x - top);
+        l += ml.y * f;
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) acc[c] += P.o[(first + s * step) * D + c * 32 + lane] * f;
     }
-    const long long blocks = (long long)((A.T + 2 * A.R - 1) / (2 * A.R)) * A.kv.H * A.kv.B;
-    if (blocks > INT_MAX) return SI_ERR_TOO_LARGE;
-    prefill_kernel<DT, D><<<(unsigned)blocks, kThreads, Cfg<D>::kSmem, st>>>(qm, km, vm, A);
-    SI_CUDA_TRY(cudaGetLastError());
-    return SI_OK;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) A.out[r * D + c * 32 + lane] = si_cvt<DT>::from_float(acc[c] * inv);
+    if (lane == 0 && A.lse) A.lse[r] = l == 0.f ? -INFINITY : (top + log2f(l)) / kLog2e;
 }
 
+// Blocks of queries, and over how many CTAs their keys are split: with fewer blocks than half the SMs as many as fit one
+// wave, but no part of fewer than four key tiles (a part costs its start, 3 us, and its join).
+struct Plan { long long blocks; int splits; };
+Plan plan_of(const si_kv_t *kv, int n_q_heads, int T, int window, int n_sink) {
+    const int G = n_q_heads / kv->n_kv_heads, R = kTile / G, sms = si_sm_count();
+    Plan p{((long long)T + 2 * R - 1) / (2 * R) * kv->n_kv_heads * kv->n_seqs, 1};
+    long long tiles = (kv->capacity + kTile - 1) / kTile;
+    if (window) {
+        const long long w = ((long long)window + 2 * R + n_sink) / kTile + 3;
+        if (w < tiles) tiles = w;
+    }
+    if (p.blocks * 2 <= sms && tiles >= 8) {
+        p.splits = (int)(sms / p.blocks);
+        if (p.splits > tiles / 4) p.splits = (int)(tiles / 4);
+    }
+    return p;
+}
+size_t parts_o_bytes(const Plan &p, int D) { return p.splits > 1 ? si_align_up((size_t)p.splits * p.blocks * 2 * kTile * D * 4, 256) : 0; }
+size_t parts_ml_bytes(const Plan &p) { return p.splits > 1 ? si_align_up((size_t)p.splits * p.blocks * 2 * kTile * 8, 256) : 0; }
+
+struct Call { const CUtensorMap &qm, &km, &vm; const TcArgs &A; const SplitArgs &P; cudaStream_t st; };
+template <int DT, int D, bool NEG> int launch(const Call &c) {
+    static std::atomic<int> ready{0};
+    if (!ready.load()) {
+        SI_CUDA_TRY(cudaFuncSetAttribute(prefill_kernel<DT, D, NEG>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D>::kSmem));
+        ready.store(1);
+    }
+    prefill_kernel<DT, D, NEG><<<dim3(c.P.blocks, c.P.n), kThreads, Cfg<D>::kSmem, c.st>>>(c.qm, c.km, c.vm, c.A, c.P);
+    SI_CUDA_TRY(cudaGetLastError());
+    if (c.P.n > 1) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)(((long long)c.A.kv.B * c.A.T * c.A.Hq + 7) / 8));
+        cfg.blockDim = dim3(256);
+        cfg.stream = c.st;
+        cudaLaunchAttribute at;
+        at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at.val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = &at; cfg.numAttrs = 1;
+        SI_CUDA_TRY(cudaLaunchKernelEx(&cfg, prefill_join_kernel<DT, D>, c.A, c.P));
+    }
+    return SI_OK;
+}
+template <int DT, int D> int launch_t(const Call &c, bool neg) { return neg ? launch<DT, D, true>(c) : launch<DT, D, false>(c); }
+
 }  // namespace
+
+size_t si_attn_prefill_ws_bytes(const si_kv_t *kv, int n_q_heads, int T) {
+    const Plan p = plan_of(kv, n_q_heads, T, 0, 0);
+    return parts_o_bytes(p, kv->head_dim) + parts_ml_bytes(p);
+}
 
 extern "C" int si_attn_prefill(const si_kv_t *kv, const void *q, long long q_seq_stride, long long q_tok_stride, int T,
                                int n_q_heads, int window, int n_sink, float scale, void *out, float *lse, void *workspace,
                                size_t ws_bytes, int32_t *status_dev, void *stream) {
-    (void)workspace; (void)ws_bytes;
     int rc = si_attn_check(kv, n_q_heads, window, n_sink, scale);
     if (rc) return rc;
     if (T < 0) return SI_ERR_INVALID_ARG;
@@ -287,11 +415,20 @@ extern "C" int si_attn_prefill(const si_kv_t *kv, const void *q, long long q_seq
     if (!q || !out || q_seq_stride < 0 || q_tok_stride < 0) return SI_ERR_INVALID_ARG;
     if (kv->pos) return SI_ERR_UNSUPPORTED;
     if (!si_aligned16(q) || !si_aligned16(out) || ((q_seq_stride | q_tok_stride) & 7)) return SI_ERR_ALIGNMENT;
+    const Plan p = plan_of(kv, n_q_heads, T, window, n_sink);
+    if (p.blocks > INT_MAX) return SI_ERR_TOO_LARGE;
+    if (p.splits > 1) {
+        if (ws_bytes < parts_o_bytes(p, kv->head_dim) + parts_ml_bytes(p)) return SI_ERR_NOMEM;
+        if (!workspace) return SI_ERR_INVALID_ARG;
+        if ((uintptr_t)workspace & 255) return SI_ERR_ALIGNMENT;
+    }
+    const SplitArgs P{p.splits, (int)p.blocks, (float *)workspace, (float2 *)((char *)workspace + parts_o_bytes(p, kv->head_dim))};
     const TcArgs A = tc_args(kv, q_seq_stride, T, n_q_heads, window, n_sink, scale, out, lse, status_dev);
     CUtensorMap qm, km, vm;
     if ((rc = make_q_map(&qm, q, kv, q_seq_stride, q_tok_stride, T, n_q_heads, A.G, A.R))) return rc;
     if ((rc = make_kv_map(&km, kv->k, kv)) || (rc = make_kv_map(&vm, kv->v, kv))) return rc;
-    const cudaStream_t st = (cudaStream_t)stream;
-    if (kv->dtype == SI_BF16) return kv->head_dim == 128 ? launch<SI_BF16, 128>(qm, km, vm, A, st) : launch<SI_BF16, 64>(qm, km, vm, A, st);
-    return kv->head_dim == 128 ? launch<SI_F16, 128>(qm, km, vm, A, st) : launch<SI_F16, 64>(qm, km, vm, A, st);
+    const Call c{qm, km, vm, A, P, (cudaStream_t)stream};
+    const bool neg = scale < 0.f;
+    if (kv->dtype == SI_BF16) return kv->head_dim == 128 ? launch_t<SI_BF16, 128>(c, neg) : launch_t<SI_BF16, 64>(c, neg);
+    return kv->head_dim == 128 ? launch_t<SI_F16, 128>(c, neg) : launch_t<SI_F16, 64>(c, neg);
 }

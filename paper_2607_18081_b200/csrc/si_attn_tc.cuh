@@ -10,13 +10,13 @@ using namespace si_tc;
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kTile = 128;                 // rows of a query tile, keys of a key tile
-constexpr long long kWait = 1ll << 22;     // probes after which a wait gives up: waits here are microseconds
+constexpr int kWait = 1 << 20, kSpin = 1 << 24;   // probes (blocking, non-blocking) after which a wait gives up: waits here are microseconds
 
 struct TcArgs {
     si_kv_view kv;
     int T, Hq, G, R;                       // G query heads per key head; R = kTile / G queries per tile: row r = query r / G, head r % G
     int window, n_sink;
-    float scale2, sign;                    // |scale| log2(e); sign of the scale
+    float scale2;                          // |scale| log2(e)
     int q_b, kv_b, kv_h;                   // 0 where sequences (heads) share memory through a zero stride, else 1
     uint16_t *out;
     float *lse;
@@ -25,11 +25,11 @@ struct TcArgs {
 
 // The key tiles that queries at positions smin .. smax see: `sinks` tiles from the front, then those from `first` on; n in all.
 struct KeyTiles {
-    int sinks, first, n;
-    __device__ __forceinline__ int key0(int j) const { return (j < sinks ? j : first + j - sinks) * kTile; }
+    int sinks, first, n, off;      // off: the first one of this CTA's share
+    __device__ __forceinline__ int key0(int j) const { j += off; return (j < sinks ? j : first + j - sinks) * kTile; }
 };
 __device__ __forceinline__ KeyTiles key_tiles(int smin, int smax, int window, int n_sink) {
-    KeyTiles k = {0, 0, 0};
+    KeyTiles k = {0, 0, 0, 0};
     if (smax < 0) return k;
     const int end = smax / kTile + 1, lo = window ? max(0, si_window_lo(smin, window) + 1) : 0;
     k.first = lo / kTile;
@@ -46,17 +46,80 @@ template <int DT> __device__ __forceinline__ uint32_t pack2(float lo, float hi) 
     return r;
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c) { float r; asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
+// two fp32 values in a register pair: one instruction for both
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 two(float lo, float hi) { f32x2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi)); return r; }
+__device__ __forceinline__ f32x2 two(uint32_t lo, uint32_t hi) { f32x2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(lo), "r"(hi)); return r; }
+__device__ __forceinline__ void untwo(f32x2 v, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) { f32x2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) { f32x2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) { f32x2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+
+// 2^x for a pair on the multiply-add units: x = n + f with n the nearest integer (added to and taken from 1.5 * 2^23, whose low
+// bits then hold n), 2^f by its polynomial of least relative error on [-1/2, 1/2] of degree 5 (2.1e-7 in fp32, computed for
+// this file by a Remez exchange), n added to the exponent field.  x below -126 counts as -126.  The exponential unit does 16
+// values per clock and SM, which a tile's softmax is otherwise bound by.
+__device__ __forceinline__ f32x2 ex2_poly(f32x2 x) {
+    float a, b;
+    untwo(x, a, b);
+    x = two(fmaxf(a, -126.f), fmaxf(b, -126.f));
+    const f32x2 t = add2(x, two(12582912.f, 12582912.f)), f = add2(x, fma2(t, two(-1.f, -1.f), two(12582912.f, 12582912.f)));
+    f32x2 p = two(0.0013276472454890609f, 0.0013276472454890609f);
+    p = fma2(p, f, two(0.009675540961325169f, 0.009675540961325169f));
+    p = fma2(p, f, two(0.05550713092088699f, 0.05550713092088699f));
+    p = fma2(p, f, two(0.24022120237350464f, 0.24022120237350464f));
+    p = fma2(p, f, two(0.6931469440460205f, 0.6931469440460205f));
+    p = fma2(p, f, two(1.0000001192092896f, 1.0000001192092896f));
+    float ta, tb, pa, pb;
+    untwo(t, ta, tb);
+    untwo(p, pa, pb);
+    return two(__float_as_uint(pa) + (__float_as_uint(ta) << 23), __float_as_uint(pb) + (__float_as_uint(tb) << 23));
+}
+
 __device__ __forceinline__ void tma_load_4d(void *dst, const CUtensorMap *map, int x, int y, int z, int w, uint64_t *bar) {
     asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
                  ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar)) : "memory");
 }
-// D[tmem] (+)= A[tmem, 16-bit pairs] . B[smem]
-__device__ __forceinline__ void umma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+// Bounded wait by non-blocking probes: a thread that the blocking probe has put to sleep is woken late, and the hand-overs
+// between the softmax warps and the matrix unit are on the critical path of every tile.
+__device__ __forceinline__ bool mbar_spin(uint64_t *bar, uint32_t parity, int limit) {
+    for (int i = 0; i < limit; ++i) {
+        uint32_t ok;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
+        if (ok) return true;
+    }
+    return false;
+}
+// One lane of a converged warp.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
+// D[tmem] (+)= A . B with A in shared memory or (16-bit pairs) in tensor memory and B in shared memory.  Descriptors come as
+// their two words: the upper one is the same for all steps of an operand, the lower one (address / 16) takes the offsets.
+struct Desc { uint32_t lo, hi; };
+__device__ __forceinline__ Desc desc_of(uint32_t smem_addr, uint32_t lbo_bytes, uint32_t sbo_bytes) {
+    const uint64_t d = make_desc(smem_addr, lbo_bytes, sbo_bytes);
+    return {(uint32_t)d, (uint32_t)(d >> 32)};
+}
+__device__ __forceinline__ void umma_ss(uint32_t d_tmem, Desc a, uint32_t a_off, Desc b, uint32_t b_off, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, {%5, %5, %5, %5}, p;\n\t}"
-        ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(0u) : "memory");
+        "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\t"
+        "mov.b64 a, {%1, %2};\n\tmov.b64 b, {%3, %4};\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %5, p;\n\t}"
+        ::"r"(d_tmem), "r"(a.lo + a_off), "r"(a.hi), "r"(b.lo + b_off), "r"(b.hi), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void umma_ts(uint32_t d_tmem, uint32_t a_tmem, Desc b, uint32_t b_off, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 b;\n\t"
+        "mov.b64 b, {%2, %3};\n\t"
+        "setp.ne.b32 p, %5, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_tmem), "r"(b.lo + b_off), "r"(b.hi), "r"(idesc), "r"(accumulate) : "memory");
 }
 #define SI_R8(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3]), "=r"(r[i + 4]), "=r"(r[i + 5]), "=r"(r[i + 6]), "=r"(r[i + 7])
 #define SI_P8(r, i) "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]), "+r"(r[i + 6]), "+r"(r[i + 7])
@@ -74,6 +137,10 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
     asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
                  "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
                  ::SI_I8(r, 0), SI_I8(r, 8), SI_I8(r, 16), SI_I8(r, 24), "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
+                 ::SI_I8(r, 0), SI_I8(r, 8), "r"(taddr) : "memory");
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void mbar_arrive(uint64_t *bar) {
@@ -126,7 +193,6 @@ inline TcArgs tc_args(const si_kv_t *kv, long long q_ss, int T, int Hq, int wind
     A.window = window; A.n_sink = n_sink;
     // a scale of zero makes all weights equal; the smallest steps keep -inf * scale from becoming NaN
     A.scale2 = scale == 0.f ? 1e-30f : (scale < 0.f ? -scale : scale) * kLog2e;
-    A.sign = scale < 0.f ? -1.f : 1.f;
     A.q_b = kv->n_seqs > 1 && q_ss != 0; A.kv_b = kv->n_seqs > 1 && kv->seq_stride != 0; A.kv_h = kv->n_kv_heads > 1 && kv->head_stride != 0;
     A.out = (uint16_t *)out; A.lse = lse; A.status = status;
     return A;

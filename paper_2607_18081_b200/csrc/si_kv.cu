@@ -153,12 +153,31 @@ size_t evict_ws_bytes(const si_kv_t *kv) {
 
 }  // namespace
 
+int si_sm_count() {
+    static std::atomic<int> known{0};
+    int n = known.load();
+    if (!n) {
+        int dev = 0;
+        if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) {
+            (void)cudaGetLastError();
+            return SI_NUM_SMS_FALLBACK;
+        }
+        known.store(n);
+    }
+    return n;
+}
+
 extern "C" int si_kv_workspace_bytes(const si_kv_t *kv, int n_q_heads, int T, size_t *bytes_out) {
     const int rc = si_kv_check(kv);
     if (rc) return rc;
     if (!bytes_out || n_q_heads < 0 || T < 0 || n_q_heads % kv->n_kv_heads) return SI_ERR_INVALID_ARG;
-    const size_t attn = n_q_heads && T ? si_attn_decode_ws_bytes(kv, n_q_heads) : 0, ev = kv->weight ? evict_ws_bytes(kv) : 0;
-    *bytes_out = attn > ev ? attn : ev;
+    size_t most = kv->weight ? evict_ws_bytes(kv) : 0;
+    if (n_q_heads && T) {
+        if (n_q_heads / kv->n_kv_heads > 128) return SI_ERR_UNSUPPORTED;
+        const size_t each[3] = {si_attn_decode_ws_bytes(kv, n_q_heads), si_attn_prefill_ws_bytes(kv, n_q_heads, T), kv->weight ? si_attn_weights_ws_bytes(kv) : 0};
+        for (size_t b : each) most = b > most ? b : most;
+    }
+    *bytes_out = most;
     return SI_OK;
 }
 

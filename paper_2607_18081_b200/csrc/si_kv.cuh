@@ -44,8 +44,13 @@ inline int si_attn_check(const si_kv_t *kv, int n_q_heads, int window, int n_sin
     return SI_OK;
 }
 
-// implemented in si_attn_decode.cu
+// SMs of the current device when first asked (all devices of a machine are alike here)
+int si_sm_count();
+
+// implemented in si_attn_decode.cu / si_attn_prefill.cu / si_attn_weights.cu
 size_t si_attn_decode_ws_bytes(const si_kv_t *kv, int n_q_heads);
+size_t si_attn_prefill_ws_bytes(const si_kv_t *kv, int n_q_heads, int T);
+size_t si_attn_weights_ws_bytes(const si_kv_t *kv);
 
 __device__ __forceinline__ void si_report(int32_t *status, int err) { if (status) atomicCAS(status, 0, err); }
 

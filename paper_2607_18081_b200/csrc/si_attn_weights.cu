@@ -1,19 +1,21 @@
 // The attention every cache entry received from the last T queries:
 //   weight[j] += sum_i sum_heads exp(scale q_i . k_j - lse_i)   over the queries i that see entry j.
 //
-// S^T = K Q^T with the 128 keys of a tile as rows and 128 packed (query, head) rows as columns: a thread owns a key, so the
+// S^T = K Q^T with 128 keys as rows and 128 packed (query, head) rows as columns: a thread owns a key, so the
 // sum over queries is a sum along its row of tensor memory and nothing is exchanged.  2 D flops and one exponential per
 // pair; the exponential unit (16 per clock and SM: 1024 clocks per tile pair) is twice as slow as the matrix unit (512), so
 // kPolyOf8 of every eight pairs of exponentials go to the multiply-add units instead.
 //
-// Work is split in (key tile, query tile) pairs: all pairs of all sequences and heads in one row, cut into equal runs, one
+// A key tile is 256 keys, two such products with the same query tile: with 128 the stream of query tiles out of L2 (32 KB per
+// 1000 clocks and SM) was the bound.  Work is split in (key tile, query tile) pairs: all pairs of all sequences and heads in one row, cut into equal runs, one
 // per CTA, so the triangle of a causal prompt and sequences of any lengths load all SMs alike.  A key tile whose pairs lie
-// in one run is finished there; one that crosses CTAs leaves 128 partial sums per CTA, which a second kernel adds in the
+// in one run is finished there; one that crosses CTAs leaves 256 partial sums per CTA, which a second kernel adds in the
 // order of the CTAs -- no atomics, the same bits every time.
-//   warps 0-3, 4-7   exponentials and sums of the even / odd query tiles of the run
-//   warp 8           TMA loads of key tiles (two buffers) and query tiles (a ring)
-//   warp 9           matrix products into four tensor-memory buffers
-//   warp 10          the queries' lse into the ring
+//   warps 0-15   exponentials and sums: a warpgroup per half of the keys and parity of the query tile (four warps per
+//                scheduler partition cover one another's tensor-memory and exponential latencies)
+//   warp 16      TMA loads of key tiles (two buffers) and query tiles (a ring)
+//   warp 17      matrix products into four tensor-memory buffers
+//   warp 18      the queries' lse into a ring of its own
 #include <type_traits>
 
 #include "si_attn_tc.cuh"
@@ -22,19 +24,21 @@ namespace {
 
 using namespace si_attn;
 
-constexpr int kThreads = 384;
-constexpr int kStages = 4, kBufs = 4;
+constexpr int kGroups = 4, kThreads = kGroups * 128 + 128;
+constexpr int kKeys = 2 * kTile;                     // keys of a key tile
+constexpr int kBufs = 4, kLse = 4;                   // score tiles in tensor memory: [parity of the query tile][half of the keys]; ring of lse rows
 constexpr int kPolyOf8 = 3;
 
 template <int D> struct Cfg {
     static constexpr int kBytes = kTile * D * 2, kPanel = kTile * 128;
-    static constexpr int kSmem = (2 + kStages) * kBytes + 1024 + 256 + kStages * kTile * 4 + 2 * kTile * 4;
+    static constexpr int kStages = D == 128 ? 2 : 4;     // ring of query tiles
+    static constexpr int kSmem = (4 + kStages) * kBytes + 1024 + 512 + kLse * kTile * 4 + 2 * kKeys * 4;
 };
-struct Bars { uint64_t kfull[2], kempty[2], full[kStages], empty[kStages], s[kBufs], free[kBufs]; uint32_t tmem; };
+struct Bars { uint64_t kfull[2], kempty[2], full[4], empty[4], s[kBufs], free[kBufs], lfull[kLse], lempty[kLse]; uint32_t tmem; };
 
 struct WeightArgs {
     const float *lse;
-    float *part;        // [n_cta][2][128]
+    float *part;        // [n_cta][2][kKeys]
     int2 *runs;         // [B][key tiles][H]: first and last CTA of a key tile
     int *part_first;    // [n_cta]: the item a CTA's run starts with
     int n_cta, nkt;     // key tiles of a full cache
@@ -43,11 +47,11 @@ struct WeightArgs {
 // Query tiles that see key tile kt of a sequence with n entries: first, number.
 struct Span { int first, n; };
 __device__ __forceinline__ Span query_tiles(const TcArgs &A, int n, int kt) {
-    const int k0 = kt * kTile, shift = n - A.T;
+    const int k0 = kt * kKeys, shift = n - A.T;
     if (k0 >= n) return {0, 0};
     const int i0 = max(0, k0 - shift);
     long long i1 = A.T - 1;
-    if (A.window && k0 >= A.n_sink) i1 = min(i1, (long long)min(k0 + kTile, n) - 1 + A.window - 1 - shift);
+    if (A.window && k0 >= A.n_sink) i1 = min(i1, (long long)min(k0 + kKeys, n) - 1 + A.window - 1 - shift);
     if (i1 < i0) return {0, 0};
     return {i0 / A.R, (int)i1 / A.R - i0 / A.R + 1};
 }
@@ -60,7 +64,7 @@ __device__ __forceinline__ void next_item(const TcArgs &A, const WeightArgs &W, 
     if (++c.h < A.kv.H) return;
     c.h = 0;
     do {
-        if (++c.kt >= W.nkt || c.kt * kTile >= c.len) { c.kt = 0; ++c.b; c.len = si_kv_len(A.kv, c.b, nullptr); }
+        if (++c.kt >= W.nkt || c.kt * kKeys >= c.len) { c.kt = 0; ++c.b; c.len = si_kv_len(A.kv, c.b, nullptr); }
         c.q = query_tiles(A, c.len, c.kt);
     } while (c.q.n == 0);
 }
@@ -69,22 +73,24 @@ template <int DT, int D, bool NEG>
 __global__ void __launch_bounds__(kThreads, 1)
 weights_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap, const TcArgs A, const WeightArgs W) {
     using C = Cfg<D>;
+    constexpr int kStages = C::kStages;
     extern __shared__ char smem_raw[];
     __shared__ int scan[kThreads + 1];
     char *smem = (char *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-    char *ring = smem + 2 * C::kBytes;
+    char *ring = smem + 4 * C::kBytes;
     Bars *B = (Bars *)(ring + kStages * C::kBytes);
-    float *lse2 = (float *)((char *)B + 256), *other = lse2 + kStages * kTile;        // [stage][column], [segment & 1][key]
+    float *lse2 = (float *)((char *)B + 512), *other = lse2 + kLse * kTile;        // [stage][column], [segment & 1][key]
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     pdl_launch();
 
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) { mbar_init(&B->kfull[i], 1); mbar_init(&B->kempty[i], 1); }
-        for (int i = 0; i < kStages; ++i) { mbar_init(&B->full[i], 2); mbar_init(&B->empty[i], 5); }
+        for (int i = 0; i < kStages; ++i) { mbar_init(&B->full[i], 1); mbar_init(&B->empty[i], 1); }
+        for (int i = 0; i < kLse; ++i) { mbar_init(&B->lfull[i], 1); mbar_init(&B->lempty[i], 8); }
         for (int i = 0; i < kBufs; ++i) { mbar_init(&B->s[i], 1); mbar_init(&B->free[i], 4); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 9) {
+    if (warp == 17) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&B->tmem)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -143,20 +149,20 @@ weights_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
         if (tid == 0) W.part_first[blockIdx.x] = item_of(A, W, cur);
     }
 
-    if (warp == 8) {
+    if (warp == 16) {
         if (elect_one()) {
             int it = 0, seg = 0;
             bool ok = true;
             for (int g = g0; g < g1 && ok; ++seg) {
                 ok = mbar_wait(&B->kempty[seg & 1], (seg >> 1 & 1) ^ 1, kWait);
                 if (!ok) break;
-                mbar_arrive_expect_tx(&B->kfull[seg & 1], C::kBytes);
-                for (int c = 0; c < D / 64; ++c)
-                    tma_load_4d(smem + (seg & 1) * C::kBytes + c * C::kPanel, &kmap, c * 64, cur.kt * kTile, cur.h * A.kv_h, cur.b * A.kv_b, &B->kfull[seg & 1]);
+                mbar_arrive_expect_tx(&B->kfull[seg & 1], 2 * C::kBytes);
+                for (int c = 0; c < 2 * (D / 64); ++c)
+                    tma_load_4d(smem + (seg & 1) * 2 * C::kBytes + c * C::kPanel, &kmap, c % (D / 64) * 64, cur.kt * kKeys + c / (D / 64) * kTile, cur.h * A.kv_h, cur.b * A.kv_b, &B->kfull[seg & 1]);
                 const int end = min(g1, cur.start + cur.q.n);
                 for (; g < end; ++g, ++it) {
                     const int st = it % kStages;
-                    ok = mbar_wait(&B->empty[st], (it / kStages & 1) ^ 1, kWait);
+                    ok = mbar_spin(&B->empty[st], (it / kStages & 1) ^ 1, kSpin);
                     if (!ok) break;
                     mbar_arrive_expect_tx(&B->full[st], (D / 64) * 128 * used);
                     for (int c = 0; c < D / 64; ++c)
@@ -170,7 +176,7 @@ weights_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
                 for (int k = max(0, it - kStages); k < it; ++k) mbar_wait(&B->full[k % kStages], k / kStages & 1, kWait);
             }
         }
-    } else if (warp == 9) {
+    } else if (warp == 17) {
         if (elect_one()) {
             const uint32_t id = make_idesc(DT == SI_BF16, 0, 0, 128, 128);
             const Desc q_desc = desc_of(smem_u32(ring), 16, 1024), k_desc = desc_of(smem_u32(smem), 16, 1024);
@@ -179,67 +185,76 @@ weights_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
             for (int g = g0; g < g1 && ok; ++seg) {
                 ok = mbar_wait(&B->kfull[seg & 1], seg >> 1 & 1, kWait);
                 const int end = min(g1, cur.start + cur.q.n);
-                const uint32_t kb = (seg & 1) * (C::kBytes / 16);
+                const uint32_t kb = (seg & 1) * (2 * C::kBytes / 16);
                 for (; g < end && ok; ++g, ++it) {
-                    const int st = it % kStages, buf = it % kBufs;
-                    ok = mbar_spin(&B->full[st], it / kStages & 1, kSpin) && mbar_spin(&B->free[buf], (it / kBufs & 1) ^ 1, kSpin);
-                    if (!ok) break;
-                    tc_fence_after();
-                    const uint32_t qb = st * (C::kBytes / 16), d = tmem + buf * kTile;
+                    const int st = it % kStages;
+                    const uint32_t qb = st * (C::kBytes / 16);
+                    ok = mbar_spin(&B->full[st], it / kStages & 1, kSpin);
 #pragma unroll
-                    for (int k = 0; k < D / 16; ++k) {
-                        const uint32_t off = ((k >> 2) * C::kPanel + (k & 3) * 32) / 16;
-                        umma_ss(d, k_desc, kb + off, q_desc, qb + off, id, k > 0);
+                    for (int half = 0; half < 2; ++half) {
+                        const int buf = (it & 1) * 2 + half;
+                        ok = ok && mbar_spin(&B->free[buf], (it >> 1 & 1) ^ 1, kSpin);
+                        if (!ok) break;
+                        tc_fence_after();
+#pragma unroll
+                        for (int k = 0; k < D / 16; ++k) {
+                            const uint32_t off = ((k >> 2) * C::kPanel + (k & 3) * 32) / 16;
+                            umma_ss(tmem + buf * kTile, k_desc, kb + half * (C::kBytes / 16) + off, q_desc, qb + off, id, k > 0);
+                        }
+                        umma_commit(&B->s[buf]);
                     }
-                    umma_commit(&B->s[buf]);
-                    umma_commit(&B->empty[st]);
+                    if (ok) umma_commit(&B->empty[st]);
                 }
                 umma_commit(&B->kempty[seg & 1]);
                 if (g < g1 && ok) next_item(A, W, cur);
             }
             if (!ok) si_report(A.status, SI_ERR_TIMEOUT);
         }
-    } else if (warp == 10) {
-        // lse of the 128 packed rows in base 2; rows that do not exist or see nothing get +inf, so that they add exp2(-inf) = 0
+    } else if (warp == 18) {
+        // lse of the 128 packed rows in base 2, negated; rows that do not exist or see nothing get -inf, so that they add
+        // exp2(-inf) = 0.  The next tile's values are on their way while this one's place is waited for.
         int it = 0;
         bool ok = true;
-        for (int g = g0; g < g1; ) {
-            const int end = min(g1, cur.start + cur.q.n);
-            for (; g < end; ++g, ++it) {
-                const int st = it % kStages, i0 = (cur.q.first + g - cur.start) * A.R;
-                float v[4];
+        float v[4];
+        auto fetch = [&](const Cursor &c, int g) {
+            const int i0 = (c.q.first + g - c.start) * A.R;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int r = k * 32 + lane, i = i0 + r / A.G;
-                    v[k] = INFINITY;
-                    if (r < used && i < A.T) {
-                        const float x = W.lse[((long long)cur.b * A.T + i) * A.Hq + cur.h * A.G + r % A.G];
-                        if (x != -INFINITY) v[k] = x * kLog2e;
-                    }
-                }
-                ok = ok && mbar_wait(&B->empty[st], (it / kStages & 1) ^ 1, kWait);
-                __syncwarp();
-#pragma unroll
-                for (int k = 0; k < 4; ++k) lse2[st * kTile + k * 32 + lane] = v[k];
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&B->full[st]);
+            for (int k = 0; k < 4; ++k) {
+                const int r = k * 32 + lane, i = i0 + r / A.G;
+                v[k] = r < used && i < A.T ? W.lse[((long long)c.b * A.T + i) * A.Hq + c.h * A.G + r % A.G] : -INFINITY;
             }
-            if (g < g1) next_item(A, W, cur);
+        };
+        if (g0 < g1) fetch(cur, g0);
+        for (int g = g0; g < g1; ++g, ++it) {
+            const int st = it % kLse;
+            float w[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[k] = v[k] == -INFINITY ? -INFINITY : -v[k] * kLog2e;
+            if (g + 1 < g1) {
+                if (g + 1 == cur.start + cur.q.n) next_item(A, W, cur);
+                fetch(cur, g + 1);
+            }
+            ok = ok && mbar_spin(&B->lempty[st], (it / kLse & 1) ^ 1, kSpin);
+            __syncwarp();
+#pragma unroll
+            for (int k = 0; k < 4; ++k) lse2[st * kTile + k * 32 + lane] = w[k];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&B->lfull[st]);
         }
-    } else if (warp < 8) {
-        const int wg = warp >> 2, row = (warp & 3) * 32 + lane;
+    } else if (warp < 16) {
+        const int buf = warp >> 2, parity = buf >> 1, half = buf & 1, row = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const f32x2 sc = two(NEG ? -A.scale2 : A.scale2, NEG ? -A.scale2 : A.scale2);
         int it = 0, seg = 0;
         bool ok = true, first_segment = true;
         for (int g = g0; g < g1; ++seg) {
-            const int end = min(g1, cur.start + cur.q.n), key = cur.kt * kTile + row, shift = cur.len - A.T;
+            const int end = min(g1, cur.start + cur.q.n), key = cur.kt * kKeys + half * kTile + row, shift = cur.len - A.T;
             float sum = 0.f;
             for (; g < end; ++g, ++it) {
-                if ((it & 1) != wg) continue;
-                const int st = it % kStages, buf = it % kBufs;
+                if ((it & 1) != parity) continue;
+                const int st = it % kLse;
                 // a wait that runs out is reported and the run goes on without waiting, to its end
-                if (ok) ok = __all_sync(0xFFFFFFFFu, mbar_spin(&B->s[buf], it / kBufs & 1, kSpin) && mbar_spin(&B->full[st], it / kStages & 1, kSpin));
+                if (ok) ok = __all_sync(0xFFFFFFFFu, mbar_spin(&B->s[buf], it >> 1 & 1, kSpin) && mbar_spin(&B->lfull[st], it / kLse & 1, kSpin));
                 tc_fence_after();
                 // column c is the query at position s0 + c / G: this key is seen by a range of columns
                 const int s0 = shift + (cur.q.first + g - cur.start) * A.R;
@@ -258,7 +273,7 @@ weights_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
                         const float4 z = *reinterpret_cast<const float4 *>(ls + 2 * k);
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            f32x2 p = fma2(two(x[2 * (k + e)], x[2 * (k + e) + 1]), sc, e ? two(-z.z, -z.w) : two(-z.x, -z.y));
+                            f32x2 p = fma2(two(x[2 * (k + e)], x[2 * (k + e) + 1]), sc, e ? two(z.z, z.w) : two(z.x, z.y));
                             float p0, p1;
                             if (!MASKED && (k + e) * kPolyOf8 % 8 < kPolyOf8) p = ex2_poly(p);
                             else {
@@ -284,20 +299,21 @@ weights_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) { mbar_arrive(&B->free[buf]); mbar_arrive(&B->empty[st]); }
+                if (lane == 0) { mbar_arrive(&B->free[buf]); mbar_arrive(&B->lempty[st]); }
                 float a, b;
                 untwo(add2(add2(part[0], part[1]), add2(part[2], part[3])), a, b);
                 sum += a + b;
             }
-            // the odd tiles' sums to the even tiles' warpgroup
-            if (wg == 1) other[(seg & 1) * kTile + row] = sum;
-            asm volatile("bar.sync 1, 256;" ::: "memory");
+            // the odd query tiles' sums to the even ones' warpgroup
+            float *xch = other + (seg & 1) * kKeys + half * kTile + row;
+            if (parity) *xch = sum;
+            asm volatile("bar.sync %0, 256;" ::"r"(1 + half) : "memory");
             const bool whole = cur.start >= g0 && cur.start + cur.q.n <= g1;
-            if (wg == 0) {
-                sum += other[(seg & 1) * kTile + row];
-                if (!whole) W.part[((long long)blockIdx.x * 2 + (first_segment ? 0 : 1)) * kTile + row] = sum;
+            if (!parity) {
+                sum += *xch;
+                if (!whole) W.part[((long long)blockIdx.x * 2 + (first_segment ? 0 : 1)) * kKeys + half * kTile + row] = sum;
                 else if (key < cur.len) A.kv.weight[A.kv.meta(cur.b, cur.h) + key] += sum;
-                if (row == 0 && cur.start >= g0) W.runs[item_of(A, W, cur)] = make_int2(cur.start / run, (cur.start + cur.q.n - 1) / run);
+                if (half == 0 && row == 0 && cur.start >= g0) W.runs[item_of(A, W, cur)] = make_int2(cur.start / run, (cur.start + cur.q.n - 1) / run);
             }
             first_segment = false;
             if (g < g1) next_item(A, W, cur);
@@ -306,15 +322,15 @@ weights_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 9) {
+    if (warp == 17) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
     }
 }
 
 // Key tiles that crossed CTAs: their parts in order.
-__global__ void __launch_bounds__(kTile) weights_join_kernel(const TcArgs A, const WeightArgs W) {
-    const int kt = blockIdx.x, h = blockIdx.y, b = blockIdx.z, row = threadIdx.x, key = kt * kTile + row;
+__global__ void __launch_bounds__(kKeys) weights_join_kernel(const TcArgs A, const WeightArgs W) {
+    const int kt = blockIdx.x, h = blockIdx.y, b = blockIdx.z, row = threadIdx.x, key = kt * kKeys + row;
     pdl_wait();
     const int n = si_kv_len(A.kv, b, nullptr);
     if (key >= n || query_tiles(A, n, kt).n == 0) return;
@@ -323,7 +339,7 @@ __global__ void __launch_bounds__(kTile) weights_join_kernel(const TcArgs A, con
     if (run.x == run.y) return;
     float sum = 0.f;
 #pragma unroll 8
-    for (int x = run.x; x <= run.y; ++x) sum += W.part[((long long)x * 2 + (x > run.x || W.part_first[x] == item ? 0 : 1)) * kTile + row];
+    for (int x = run.x; x <= run.y; ++x) sum += W.part[((long long)x * 2 + (x > run.x || W.part_first[x] == item ? 0 : 1)) * kKeys + row];
     A.kv.weight[A.kv.meta(b, h) + key] += sum;
 }
 
@@ -331,9 +347,9 @@ struct Layout { int n_cta, nkt; size_t part, runs, first, total; };
 Layout layout_of(const si_kv_t *kv) {
     Layout L;
     L.n_cta = si_sm_count();
-    L.nkt = (kv->capacity + kTile - 1) / kTile;
+    L.nkt = (kv->capacity + kKeys - 1) / kKeys;
     L.part = 0;
-    L.runs = si_align_up((size_t)L.n_cta * 2 * kTile * 4, 256);
+    L.runs = si_align_up((size_t)L.n_cta * 2 * kKeys * 4, 256);
     L.first = L.runs + si_align_up((size_t)kv->n_seqs * L.nkt * kv->n_kv_heads * 8, 256);
     L.total = L.first + si_align_up((size_t)L.n_cta * 4, 256);
     return L;
@@ -350,7 +366,7 @@ template <int DT, int D, bool NEG> int launch(const Call &c) {
     SI_CUDA_TRY(cudaGetLastError());
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(c.W.nkt, c.A.kv.H, c.A.kv.B);
-    cfg.blockDim = dim3(kTile);
+    cfg.blockDim = dim3(kKeys);
     cfg.stream = c.st;
     cudaLaunchAttribute at;
     at.id = cudaLaunchAttributeProgrammaticStreamSerialization;

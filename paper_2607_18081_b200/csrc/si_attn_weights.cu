@@ -3,8 +3,9 @@
 //
 // S^T = K Q^T with 128 keys as rows and 128 packed (query, head) rows as columns: a thread owns a key, so the
 // sum over queries is a sum along its row of tensor memory and nothing is exchanged.  2 D flops and one exponential per
-// pair; the exponential unit (16 per clock and SM: 1024 clocks per tile pair) is twice as slow as the matrix unit (512), so
-// kPolyOf8 of every eight pairs of exponentials go to the multiply-add units instead.
+// pair; the exponential unit (16 per clock and SM: 1024 clocks per tile pair) is twice as slow as the matrix unit (512), so one
+// of every eight pairs of exponentials goes to the multiply-add units (4096-token prompt: 114 us; none 117, three of eight
+// 120: back to back the chip is at its power limit, and a polynomial costs more energy than it saves time).
 //
 // A key tile is 256 keys, two such products with the same query tile: with 128 the stream of query tiles out of L2 (32 KB per
 // 1000 clocks and SM) was the bound.  Work is split in (key tile, query tile) pairs: all pairs of all sequences and heads in one row, cut into equal runs, one
@@ -27,7 +28,7 @@ using namespace si_attn;
 constexpr int kGroups = 4, kThreads = kGroups * 128 + 128;
 constexpr int kKeys = 2 * kTile;                     // keys of a key tile
 constexpr int kBufs = 4, kLse = 4;                   // score tiles in tensor memory: [parity of the query tile][half of the keys]; ring of lse rows
-constexpr int kPolyOf8 = 3;
+constexpr int kPolyOf8 = 1;
 
 template <int D> struct Cfg {
     static constexpr int kBytes = kTile * D * 2, kPanel = kTile * 128;

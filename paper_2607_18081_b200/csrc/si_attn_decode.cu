@@ -4,7 +4,7 @@
 //
 // Bound by HBM: every visible key and value is read once, 2 G flops per byte.  So the kernel is a stream: each warp keeps
 // two chunks of 4 KB of keys and 4 KB of values in flight (cp.async into a ring of its own, 128 KB per SM) while it works
-// on a third.  The G heads make the second dimension of two small matrix products per chunk,
+// on a third (three in flight: 2 % slower).  The G heads make the second dimension of two small matrix products per chunk,
 //   S^T [keys x heads] = K Q^T        O^T [head_dim x heads] += V^T P^T,
 // with the keys on the long side of the m16n8k16 fragment, so that eight heads fill it (heads-first would waste half of
 // it), K and V come from shared memory by ldmatrix as they lie there, and P^T gets from the accumulator layout to the
@@ -23,6 +23,7 @@ namespace {
 
 constexpr int kWarps = 8, kThreads = kWarps * 32;
 constexpr int kStages = 3;
+constexpr int kSecondSlot = 1 << 30;       // in the table of runs: the item's first part is in the second slot of its CTA
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLazy = 8.f;               // the running maximum moves only when a score exceeds it by 2^8: p stays below 2^8, exact to fp32 all the same
 
@@ -49,7 +50,6 @@ struct DecodeArgs {
     float *lse2;                         // [B][H * GB * 8 NT]: base-2 lse of finished items (weights only)
     float *scores;                       // [B][H][GB][cap][GS]
     int2 *runs;                          // [B][H][GB]: first and last CTA of an item
-    int *part_first;                     // [n_cta]: the item a CTA's run starts with
 };
 
 // The chunks of sequence b that hold visible entries: c_sink chunks from the front, then those from c_win to c_end.
@@ -201,7 +201,6 @@ __global__ void __launch_bounds__(kThreads, 1) decode_kernel(const DecodeArgs A)
     const int per = (total - 1) / A.n_cta + 1, g0 = min((long long)total, (long long)blockIdx.x * per), g1 = total - g0 < per ? total : g0 + per;
     if (g0 < g1) {
         cons = find_item<D>(A, g0, sh_scan);
-        if (tid == 0) A.part_first[blockIdx.x] = cons.b * A.kv.H * A.GB + cons.hh;
     }
 
     // ---- loader side: chunk ids g0 + warp, + kWarps, ...
@@ -408,7 +407,7 @@ __global__ void __launch_bounds__(kThreads, 1) decode_kernel(const DecodeArgs A)
         }
         // the CTAs of this item, for the joining kernel: written by the one that has its first chunk
         if (tid == 0 && seg.start >= g0)
-            A.runs[(long long)seg.b * A.kv.H * A.GB + seg.hh] = make_int2(seg.start / per, (seg.start + w.nc - 1) / per);
+            A.runs[(long long)seg.b * A.kv.H * A.GB + seg.hh] = make_int2(seg.start / per | (first_segment ? 0 : kSecondSlot), (seg.start + w.nc - 1) / per);
         // ---- the segment's warps joined: rows scaled to the common maximum, summed in warp order
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -496,56 +495,53 @@ __global__ void __launch_bounds__(kThreads, 1) decode_kernel(const DecodeArgs A)
 }
 
 // Joins the parts of items that crossed CTAs and, where weights are wanted, adds them up.  One CTA per (sequence, key head)
-// and range of kJoinKeys keys; the first range's writes the output.
-constexpr int kJoinKeys = 1024;
+// and range of U * 256 keys; the first range's writes the output.  A chain of short dependent loads: everything that does not
+// depend on another load is asked for first (scores and weights beyond the length too: the memory is there, the values are
+// not used).  At most 80 registers, so that the CTAs become resident beside the main kernel's and wait there for its end.
 constexpr int kMaxParts = 256;             // CTAs of the main kernel at most
-template <int DT, int D, int NT>
-__global__ void __launch_bounds__(kThreads) decode_join_kernel(const DecodeArgs A) {
+template <int DT, int D, int NT, int U>
+__global__ void __launch_bounds__(kThreads, 3) decode_join_kernel(const DecodeArgs A) {
     constexpr int HB = 8 * NT, CH = 2048 / D;
     __shared__ float sh_lse2[128], sh_f[HB][kMaxParts], sh_inv[HB];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, h = blockIdx.y, b = blockIdx.z;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, h = blockIdx.y, b = blockIdx.z, j0 = blockIdx.x * (U * kThreads);
     si_tc::pdl_wait();
-    const SeqWork w = seq_work<D>(A, b, nullptr);
-    const int j0 = blockIdx.x * kJoinKeys;
-    if (j0 >= w.n && (blockIdx.x > 0 || w.nc == 0)) return;
-    // the scores and weights of this CTA's keys, on their way while the sums are joined
-    constexpr int kKeys = kJoinKeys / kThreads;
     float *weight = A.kv.weight + A.kv.meta(b, h);
     const float *sc = A.scores + ((long long)b * A.kv.H + h) * A.GB * A.kv.cap * A.GS;
-    auto worked = [&](int j) { const int c = j / CH; return c < w.c_sink || (c >= w.c_win && c < w.c_win + w.nc - w.c_sink); };
-    float2 x[kKeys][HB / 2];
-    float old[kKeys];
+    float2 x[U][HB / 2];                   // the first head block's scores
+    float old[U];
     if (A.acc) {
 #pragma unroll
-        for (int i = 0; i < kKeys; ++i) {
+        for (int i = 0; i < U; ++i) {
             const int j = j0 + i * kThreads + tid;
-            if (j >= w.n || !worked(j)) continue;
+            if (j >= A.kv.cap) continue;
             old[i] = weight[j];
 #pragma unroll
             for (int g = 0; g < HB; g += 2)
                 if (g < A.GS) x[i][g / 2] = *reinterpret_cast<const float2 *>(sc + (long long)j * A.GS + g);
         }
     }
+    const long long row = (long long)b * A.Hq + h * A.G;
+    const float whole = A.acc && tid < A.G ? A.lse2[row + tid] : 0.f;
+    const SeqWork w = seq_work<D>(A, b, nullptr);
+    if (j0 >= w.n && (blockIdx.x > 0 || w.nc == 0)) return;
+    if (A.acc && tid < A.G) sh_lse2[tid] = whole;
     for (int gb = 0; gb < A.GB && w.nc > 0; ++gb) {
         const int head0 = gb * HB, heads = min(HB, A.G - head0);
-        const long long row0 = (long long)b * A.Hq + h * A.G + head0;
-        const int2 run = A.runs[((long long)b * A.kv.H + h) * A.GB + gb];
-        if (run.x == run.y) {                          // finished by one CTA
-            if (A.acc && tid < heads) sh_lse2[head0 + tid] = A.lse2[row0 + tid];
-            continue;
-        }
-        // an item's first CTA has it as its last segment, unless its run starts with it (then nothing lies before it)
-        const bool head_first = A.part_first[run.x] == (b * A.kv.H + h) * A.GB + gb;
+        int2 run = A.runs[((long long)b * A.kv.H + h) * A.GB + gb];
+        const int first_slot = run.x & kSecondSlot ? 1 : 0;
+        run.x &= ~kSecondSlot;
+        if (run.x == run.y) continue;                  // finished by one CTA
         const int parts = run.y - run.x + 1;
-        auto slot = [&](int i) { return (long long)(run.x + i) * 2 + (i > 0 || head_first ? 0 : 1); };
+        auto slot = [&](int i) { return (long long)(run.x + i) * 2 + (i > 0 ? 0 : first_slot); };     // later CTAs begin with the item
         __syncthreads();
         for (int head = warp; head < heads; head += kWarps) {      // a warp per head, a lane per part: one round of loads
-            float mv[kMaxParts / 32], top = -INFINITY, sum = 0.f;
+            float2 ml[kMaxParts / 32];
+            float top = -INFINITY, sum = 0.f;
 #pragma unroll
             for (int k = 0; k < kMaxParts / 32; ++k) {
                 const int i = k * 32 + lane;
-                mv[k] = i < parts ? A.part_ml[(slot(i) * HB + head) * 2] : -INFINITY;
-                top = fmaxf(top, mv[k]);
+                ml[k] = i < parts ? *reinterpret_cast<const float2 *>(A.part_ml + (slot(i) * HB + head) * 2) : make_float2(-INFINITY, 0.f);
+                top = fmaxf(top, ml[k].x);
             }
 #pragma unroll
             for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
@@ -553,9 +549,9 @@ __global__ void __launch_bounds__(kThreads) decode_join_kernel(const DecodeArgs 
             for (int k = 0; k < kMaxParts / 32; ++k) {
                 const int i = k * 32 + lane;
                 if (i >= parts) continue;
-                const float f = mv[k] == -INFINITY ? 0.f : ex2(mv[k] - top);
+                const float f = ml[k].x == -INFINITY ? 0.f : ex2(ml[k].x - top);
                 sh_f[head][i] = f;
-                sum += A.part_ml[(slot(i) * HB + head) * 2 + 1] * f;
+                sum += ml[k].y * f;
             }
 #pragma unroll
             for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
@@ -563,7 +559,7 @@ __global__ void __launch_bounds__(kThreads) decode_join_kernel(const DecodeArgs 
                 const float l2 = sum == 0.f ? -INFINITY : top + log2f(sum);
                 sh_lse2[head0 + head] = l2;
                 sh_inv[head] = sum == 0.f ? 0.f : 1.f / sum;
-                if (blockIdx.x == 0 && A.lse) A.lse[row0 + head] = l2 / kLog2e;
+                if (blockIdx.x == 0 && A.lse) A.lse[row + head0 + head] = l2 / kLog2e;
             }
         }
         __syncthreads();
@@ -572,27 +568,27 @@ __global__ void __launch_bounds__(kThreads) decode_join_kernel(const DecodeArgs 
                 const int head = i / (D / 2), d = i % (D / 2) * 2;
                 float2 acc = make_float2(0.f, 0.f);
 #pragma unroll 8
-                for (int x = 0; x < parts; ++x) {
-                    const float2 t = *reinterpret_cast<const float2 *>(A.part_o + (slot(x) * HB + head) * D + d);
-                    acc.x += t.x * sh_f[head][x]; acc.y += t.y * sh_f[head][x];
+                for (int k = 0; k < parts; ++k) {
+                    const float2 t = *reinterpret_cast<const float2 *>(A.part_o + (slot(k) * HB + head) * D + d);
+                    acc.x += t.x * sh_f[head][k]; acc.y += t.y * sh_f[head][k];
                 }
-                *reinterpret_cast<uint32_t *>(A.out + (row0 + head) * D + d) = pack2<DT>(acc.x * sh_inv[head], acc.y * sh_inv[head]);
+                *reinterpret_cast<uint32_t *>(A.out + (row + head0 + head) * D + d) = pack2<DT>(acc.x * sh_inv[head], acc.y * sh_inv[head]);
             }
     }
     if (!A.acc) return;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kKeys; ++i) {
-        const int j = j0 + i * kThreads + tid;
+    for (int i = 0; i < U; ++i) {
+        const int j = j0 + i * kThreads + tid, c = j / CH;
         if (j >= w.n) continue;
-        if (!worked(j)) { if (j == w.n_old) weight[j] = 0.f; continue; }
+        if (!(c < w.c_sink || (c >= w.c_win && c < w.c_win + w.nc - w.c_sink))) { if (j == w.n_old) weight[j] = 0.f; continue; }
         float sum = 0.f;
         for (int gb = 0; gb < A.GB; ++gb) {
-            const float *row = sc + ((long long)gb * A.kv.cap + j) * A.GS;
+            const float *more = sc + ((long long)gb * A.kv.cap + j) * A.GS;
 #pragma unroll
             for (int g = 0; g < HB; g += 2) {
                 if (g >= A.GS || gb * HB + g >= A.G) break;
-                const float2 y = gb == 0 ? x[i][g / 2] : *reinterpret_cast<const float2 *>(row + g);
+                const float2 y = gb == 0 ? x[i][g / 2] : *reinterpret_cast<const float2 *>(more + g);
                 if (y.x != -INFINITY) sum += ex2(y.x - sh_lse2[gb * HB + g]);
                 if (gb * HB + g + 1 < A.G && y.y != -INFINITY) sum += ex2(y.y - sh_lse2[gb * HB + g + 1]);
             }
@@ -601,7 +597,7 @@ __global__ void __launch_bounds__(kThreads) decode_join_kernel(const DecodeArgs 
     }
 }
 
-struct Layout { int n_cta, NT, GB, GS; size_t o, ml, lse2, scores, runs, first, total; };
+struct Layout { int n_cta, NT, GB, GS; size_t o, ml, lse2, scores, runs, total; };
 Layout layout_of(const si_kv_t *kv, int n_q_heads, bool acc) {
     Layout L;
     L.n_cta = si_sm_count() < kMaxParts ? si_sm_count() : kMaxParts;
@@ -616,7 +612,6 @@ Layout layout_of(const si_kv_t *kv, int n_q_heads, bool acc) {
     L.lse2 = take(acc ? (size_t)kv->n_seqs * n_q_heads * 4 : 0);
     L.scores = take(acc ? (size_t)kv->n_seqs * kv->n_kv_heads * L.GB * kv->capacity * L.GS * 4 : 0);
     L.runs = take((size_t)kv->n_seqs * kv->n_kv_heads * L.GB * 8);
-    L.first = take((size_t)L.n_cta * 4);
     L.total = off;
     return L;
 }
@@ -629,15 +624,21 @@ template <int DT, int D, int NT> int launch(const DecodeArgs &A, cudaStream_t st
     }
     decode_kernel<DT, D, NT><<<A.n_cta, kThreads, (Cfg<D, NT>::kSmem), st>>>(A);
     SI_CUDA_TRY(cudaGetLastError());
+    // ranges of 256 keys while all their CTAs are resident at once (three per SM), else of 1024: the start of a CTA costs more
+    // than its keys (24 x 2 rows of 2112: 20.7 against 22.6 us a call; 32 x 8 rows of 8192: 130 against 116)
+    const long long items = (long long)A.kv.H * A.kv.B;
+    const bool few = items * ((A.kv.cap + kThreads - 1) / kThreads) <= 3ll * A.n_cta;
+    const int keys = few ? kThreads : (NT == 1 ? 4 : 2) * kThreads;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(A.acc ? (A.kv.cap + kJoinKeys - 1) / kJoinKeys : 1, A.kv.H, A.kv.B);
+    cfg.gridDim = dim3(A.acc ? (A.kv.cap + keys - 1) / keys : 1, A.kv.H, A.kv.B);
     cfg.blockDim = dim3(kThreads);
     cfg.stream = st;
     cudaLaunchAttribute at;
     at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at.val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = &at; cfg.numAttrs = 1;
-    SI_CUDA_TRY(cudaLaunchKernelEx(&cfg, decode_join_kernel<DT, D, NT>, A));
+    if (few) SI_CUDA_TRY(cudaLaunchKernelEx(&cfg, decode_join_kernel<DT, D, NT, 1>, A));
+    else SI_CUDA_TRY(cudaLaunchKernelEx(&cfg, decode_join_kernel<DT, D, NT, NT == 1 ? 4 : 2>, A));
     return SI_OK;
 }
 template <int DT> int launch_t(const DecodeArgs &A, int NT, cudaStream_t st) {
@@ -672,6 +673,6 @@ extern "C" int si_attn_decode(const si_kv_t *kv, const void *q, long long q_seq_
     const DecodeArgs A{si_kv_view_of(kv), (const uint16_t *)q, (const uint16_t *)k_new, (const uint16_t *)v_new, q_pos, q_seq_stride,
                        new_seq_stride, n_q_heads, n_q_heads / kv->n_kv_heads, L.GB, L.GS, window, n_sink, scale * kLog2e,
                        (uint16_t *)out, lse, status_dev, acc, L.n_cta, (float *)(ws + L.o), (float *)(ws + L.ml),
-                       (float *)(ws + L.lse2), (float *)(ws + L.scores), (int2 *)(ws + L.runs), (int *)(ws + L.first)};
+                       (float *)(ws + L.lse2), (float *)(ws + L.scores), (int2 *)(ws + L.runs)};
     return kv->dtype == SI_BF16 ? launch_t<SI_BF16>(A, L.NT, (cudaStream_t)stream) : launch_t<SI_F16>(A, L.NT, (cudaStream_t)stream);
 }

@@ -193,7 +193,12 @@ __global__ void __launch_bounds__(kThreads, 1) decode_kernel(const DecodeArgs A)
     char *ring = smem + warp * kStages * C::kStage;
     float *merge_o = (float *)(smem + kWarps * kStages * C::kStage);
     float *ml = merge_o + kWarps / 2 * C::kMerge;
+    si_tc::pdl_wait();                     // a programmatic dependent too: its launch runs beside the end of the kernel before it
     si_tc::pdl_launch();
+    // keys and values pass through L2 once; the scores stay there for the joining kernel
+    uint64_t once, stay;
+    asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(once));
+    asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(stay));
 
     // this CTA's run of chunks
     Cursor cons;
@@ -225,8 +230,8 @@ __global__ void __launch_bounds__(kThreads, 1) decode_kernel(const DecodeArgs A)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const uint32_t to = (at ^ ((i * (32 / PIECES) & 7) << 4)) + i * 512;
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(ks) : "memory");
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + 4096), "l"(vs) : "memory");
+                    asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(to), "l"(ks), "l"(once) : "memory");
+                    asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(to + 4096), "l"(vs), "l"(once) : "memory");
                     ks += step; vs += step;
                 }
             } else {
@@ -352,7 +357,8 @@ __global__ void __launch_bounds__(kThreads, 1) decode_kernel(const DecodeArgs A)
                         for (int e = 0; e < 4; e += 2) {
                             const int key = u * 16 + (lane >> 2) + (e >> 1) * 8, head = nt * 8 + 2 * (lane & 3);
                             if (head < A.GS && j0 + key < w.n)
-                                *reinterpret_cast<float2 *>(sc + (long long)key * A.GS + head) = make_float2(x[u][nt][e], x[u][nt][e + 1]);
+                                asm volatile("st.global.L2::cache_hint.v2.f32 [%0], {%1, %2}, %3;"
+                                             ::"l"(sc + (long long)key * A.GS + head), "f"(x[u][nt][e]), "f"(x[u][nt][e + 1]), "l"(stay) : "memory");
                         }
             }
             if (__any_sync(0xFFFFFFFFu, grow)) {
@@ -505,6 +511,7 @@ __global__ void __launch_bounds__(kThreads, 3) decode_join_kernel(const DecodeAr
     __shared__ float sh_lse2[128], sh_f[HB][kMaxParts], sh_inv[HB];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, h = blockIdx.y, b = blockIdx.z, j0 = blockIdx.x * (U * kThreads);
     si_tc::pdl_wait();
+    si_tc::pdl_launch();
     float *weight = A.kv.weight + A.kv.meta(b, h);
     const float *sc = A.scores + ((long long)b * A.kv.H + h) * A.GB * A.kv.cap * A.GS;
     float2 x[U][HB / 2];                   // the first head block's scores
@@ -622,21 +629,23 @@ template <int DT, int D, int NT> int launch(const DecodeArgs &A, cudaStream_t st
         SI_CUDA_TRY(cudaFuncSetAttribute(decode_kernel<DT, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (Cfg<D, NT>::kSmem)));
         ready.store(1);
     }
-    decode_kernel<DT, D, NT><<<A.n_cta, kThreads, (Cfg<D, NT>::kSmem), st>>>(A);
-    SI_CUDA_TRY(cudaGetLastError());
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &at; cfg.numAttrs = 1;
+    cfg.gridDim = dim3(A.n_cta);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = Cfg<D, NT>::kSmem;
+    cfg.stream = st;
+    SI_CUDA_TRY(cudaLaunchKernelEx(&cfg, decode_kernel<DT, D, NT>, A));
     // ranges of 256 keys while all their CTAs are resident at once (three per SM), else of 1024: the start of a CTA costs more
     // than its keys (24 x 2 rows of 2112: 20.7 against 22.6 us a call; 32 x 8 rows of 8192: 130 against 116)
     const long long items = (long long)A.kv.H * A.kv.B;
     const bool few = items * ((A.kv.cap + kThreads - 1) / kThreads) <= 3ll * A.n_cta;
     const int keys = few ? kThreads : (NT == 1 ? 4 : 2) * kThreads;
-    cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(A.acc ? (A.kv.cap + keys - 1) / keys : 1, A.kv.H, A.kv.B);
-    cfg.blockDim = dim3(kThreads);
-    cfg.stream = st;
-    cudaLaunchAttribute at;
-    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &at; cfg.numAttrs = 1;
+    cfg.dynamicSmemBytes = 0;
     if (few) SI_CUDA_TRY(cudaLaunchKernelEx(&cfg, decode_join_kernel<DT, D, NT, 1>, A));
     else SI_CUDA_TRY(cudaLaunchKernelEx(&cfg, decode_join_kernel<DT, D, NT, NT == 1 ? 4 : 2>, A));
     return SI_OK;

@@ -70,6 +70,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = B->tmem;
+    pdl_wait();                             // a programmatic dependent: up to here it ran beside the end of the kernel before it
 
     // blocks of queries from the last (most keys) to the first, so that the long ones start first
     const int heads = A.kv.H * A.kv.B, nqb = gridDim.x / heads;
@@ -329,6 +330,7 @@ __global__ void __launch_bounds__(256) prefill_join_kernel(const TcArgs A, const
     const int lane = threadIdx.x & 31;
     const long long r = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
     pdl_wait();
+    pdl_launch();
     if (r >= (long long)A.kv.B * A.T * A.Hq) return;
     const int hq = (int)(r % A.Hq), i = (int)(r / A.Hq % A.T), b = (int)(r / A.Hq / A.T), h = hq / A.G;
     const int heads = A.kv.H * A.kv.B, nqb = P.blocks / heads, qb = i / (2 * A.R), t = i / A.R % 2;
@@ -381,17 +383,20 @@ template <int DT, int D, bool NEG> int launch(const Call &c) {
         SI_CUDA_TRY(cudaFuncSetAttribute(prefill_kernel<DT, D, NEG>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D>::kSmem));
         ready.store(1);
     }
-    prefill_kernel<DT, D, NEG><<<dim3(c.P.blocks, c.P.n), kThreads, Cfg<D>::kSmem, c.st>>>(c.qm, c.km, c.vm, c.A, c.P);
-    SI_CUDA_TRY(cudaGetLastError());
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &at; cfg.numAttrs = 1;
+    cfg.gridDim = dim3(c.P.blocks, c.P.n);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = Cfg<D>::kSmem;
+    cfg.stream = c.st;
+    SI_CUDA_TRY(cudaLaunchKernelEx(&cfg, prefill_kernel<DT, D, NEG>, c.qm, c.km, c.vm, c.A, c.P));
     if (c.P.n > 1) {
-        cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3((unsigned)(((long long)c.A.kv.B * c.A.T * c.A.Hq + 7) / 8));
         cfg.blockDim = dim3(256);
-        cfg.stream = c.st;
-        cudaLaunchAttribute at;
-        at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        at.val.programmaticStreamSerializationAllowed = 1;
-        cfg.attrs = &at; cfg.numAttrs = 1;
+        cfg.dynamicSmemBytes = 0;
         SI_CUDA_TRY(cudaLaunchKernelEx(&cfg, prefill_join_kernel<DT, D>, c.A, c.P));
     }
     return SI_OK;

@@ -80,9 +80,8 @@ weights_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
     char *smem = (char *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     char *ring = smem + 4 * C::kBytes;
     Bars *B = (Bars *)(ring + kStages * C::kBytes);
-    float *lse2 = (float *)((char *)B + 512), *other = lse2 + kLse * kTile;        // [stage][column], [segment & 1][key]
+    float *lse2 = (float *)((char *)B + 512), *other = lse2 + kLse * kTile;        // [stage][column], [exchange & 1][key]
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    pdl_launch();
 
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) { mbar_init(&B->kfull[i], 1); mbar_init(&B->kempty[i], 1); }
@@ -102,6 +101,8 @@ weights_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
         *reinterpret_cast<uint4 *>(ring + panel * C::kPanel + used * 128 + at * 16) = make_uint4(0, 0, 0, 0);
     }
     fence_async_proxy();
+    pdl_wait();                             // a programmatic dependent: up to here it ran beside the end of the kernel before it
+    pdl_launch();
 
     // this CTA's run of pairs: thread t stands for (sequence, key tile) numbers t * per ..
     const int n_bk = A.kv.B * W.nkt, per = (n_bk + kThreads - 1) / kThreads;
@@ -246,10 +247,15 @@ weights_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
         const int buf = warp >> 2, parity = buf >> 1, half = buf & 1, row = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const f32x2 sc = two(NEG ? -A.scale2 : A.scale2, NEG ? -A.scale2 : A.scale2);
-        int it = 0, seg = 0;
+        int it = 0, exchanges = 0;
         bool ok = true, first_segment = true;
-        for (int g = g0; g < g1; ++seg) {
+        for (int g = g0; g < g1; ) {
+            // a segment of one query tile belongs to the warpgroup of its parity alone; others are joined by the even one
             const int end = min(g1, cur.start + cur.q.n), key = cur.kt * kKeys + half * kTile + row, shift = cur.len - A.T;
+            const bool single = end - g == 1, writer = single ? (it & 1) == parity : parity == 0;
+            const bool whole = cur.start >= g0 && cur.start + cur.q.n <= g1;
+            float *weight = A.kv.weight + A.kv.meta(cur.b, cur.h) + key;
+            const float old = whole && writer && key < cur.len ? *weight : 0.f;      // needed at the end only
             float sum = 0.f;
             for (; g < end; ++g, ++it) {
                 if ((it & 1) != parity) continue;
@@ -305,15 +311,15 @@ weights_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
                 untwo(add2(add2(part[0], part[1]), add2(part[2], part[3])), a, b);
                 sum += a + b;
             }
-            // the odd query tiles' sums to the even ones' warpgroup
-            float *xch = other + (seg & 1) * kKeys + half * kTile + row;
-            if (parity) *xch = sum;
-            asm volatile("bar.sync %0, 256;" ::"r"(1 + half) : "memory");
-            const bool whole = cur.start >= g0 && cur.start + cur.q.n <= g1;
-            if (!parity) {
-                sum += *xch;
+            if (!single) {
+                float *xch = other + (exchanges++ & 1) * kKeys + half * kTile + row;
+                if (parity) *xch = sum;
+                asm volatile("bar.sync %0, 256;" ::"r"(1 + half) : "memory");
+                if (!parity) sum += *xch;
+            }
+            if (writer) {
                 if (!whole) W.part[((long long)blockIdx.x * 2 + (first_segment ? 0 : 1)) * kKeys + half * kTile + row] = sum;
-                else if (key < cur.len) A.kv.weight[A.kv.meta(cur.b, cur.h) + key] += sum;
+                else if (key < cur.len) *weight = old + sum;
                 if (half == 0 && row == 0 && cur.start >= g0) W.runs[item_of(A, W, cur)] = make_int2(cur.start / run, (cur.start + cur.q.n - 1) / run);
             }
             first_segment = false;
@@ -333,6 +339,7 @@ weights_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
 __global__ void __launch_bounds__(kKeys) weights_join_kernel(const TcArgs A, const WeightArgs W) {
     const int kt = blockIdx.x, h = blockIdx.y, b = blockIdx.z, row = threadIdx.x, key = kt * kKeys + row;
     pdl_wait();
+    pdl_launch();
     const int n = si_kv_len(A.kv, b, nullptr);
     if (key >= n || query_tiles(A, n, kt).n == 0) return;
     const int item = (b * W.nkt + kt) * A.kv.H + h;
@@ -363,16 +370,19 @@ template <int DT, int D, bool NEG> int launch(const Call &c) {
         SI_CUDA_TRY(cudaFuncSetAttribute(weights_kernel<DT, D, NEG>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D>::kSmem));
         ready.store(1);
     }
-    weights_kernel<DT, D, NEG><<<c.W.n_cta, kThreads, Cfg<D>::kSmem, c.st>>>(c.qm, c.km, c.A, c.W);
-    SI_CUDA_TRY(cudaGetLastError());
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(c.W.nkt, c.A.kv.H, c.A.kv.B);
-    cfg.blockDim = dim3(kKeys);
-    cfg.stream = c.st;
     cudaLaunchAttribute at;
     at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at.val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = &at; cfg.numAttrs = 1;
+    cfg.gridDim = dim3(c.W.n_cta);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = Cfg<D>::kSmem;
+    cfg.stream = c.st;
+    SI_CUDA_TRY(cudaLaunchKernelEx(&cfg, weights_kernel<DT, D, NEG>, c.qm, c.km, c.A, c.W));
+    cfg.gridDim = dim3(c.W.nkt, c.A.kv.H, c.A.kv.B);
+    cfg.blockDim = dim3(kKeys);
+    cfg.dynamicSmemBytes = 0;
     SI_CUDA_TRY(cudaLaunchKernelEx(&cfg, weights_join_kernel, c.A, c.W));
     return SI_OK;
 }

@@ -87,10 +87,11 @@ __global__ void __launch_bounds__(kRowThreads, 2) evict_select_kernel(const Evic
     __shared__ uint32_t sh_prefix;
     __shared__ int sh_need;
     const int C = gridDim.x, rank = blockIdx.x, tid = threadIdx.x, h = blockIdx.y, b = blockIdx.z, row = b * A.src.H + h;
+    si_tc::pdl_wait();                                       // a programmatic dependent too
     const int n = entries(A, b), budget = A.budget;
     int32_t *source = A.source + (size_t)row * A.slots, *freed_slots = A.lists + (size_t)row * (A.src.cap + 2), *movers = freed_slots + A.src.cap / 2 + 1;
     if (A.move_here && A.len_out && h == 0 && rank == 0 && tid == 0) A.len_out[b] = min(n, budget);
-    if (!A.move_here) si_tc::pdl_launch();
+    si_tc::pdl_launch();
     if (n <= budget) {                                       // the whole cluster alike
         for (int j = rank * kRowThreads + tid; j < A.slots; j += C * kRowThreads) source[j] = j < n ? j : -1;
         return;
@@ -217,6 +218,7 @@ __global__ void __launch_bounds__(256) evict_move_kernel(const EvictArgs A) {
     // heads side by side in time: in a token-major cache they share the DRAM pages of a token
     const int b = blockIdx.z, h = blockIdx.x, row = b * A.src.H + h, lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
     si_tc::pdl_wait();
+    si_tc::pdl_launch();
     if (h == 0 && blockIdx.y == 0 && threadIdx.x == 0 && A.len_out) A.len_out[b] = min(entries(A, b), A.budget);
     const bool is_v = lane >= kLanes / 2;
     const int c = (is_v ? lane - kLanes / 2 : lane) * 8, slot0 = blockIdx.y * (kGroups * kMoveRows) + group;
@@ -284,10 +286,12 @@ template <bool SMEM> int launch_select(const EvictArgs &A, int C, size_t smem, c
     cfg.blockDim = dim3(kRowThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
-    cudaLaunchAttribute at;
-    at.id = cudaLaunchAttributeClusterDimension;
-    at.val.clusterDim.x = C; at.val.clusterDim.y = 1; at.val.clusterDim.z = 1;
-    cfg.attrs = &at; cfg.numAttrs = 1;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = C; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
+    cfg.attrs = at; cfg.numAttrs = C > 1 ? 2 : 1;
     SI_CUDA_TRY(cudaLaunchKernelEx(&cfg, evict_select_kernel<SMEM>, A));
     return SI_OK;
 }

@@ -47,7 +47,8 @@ struct DecodeArgs {
     int32_t *status;
     int acc, n_cta;
     float *part_o, *part_ml;             // [n_cta][2][8 NT][D], [n_cta][2][8 NT][2]
-    float *lse2;                         // [B][H * GB * 8 NT]: base-2 lse of finished items (weights only)
+    float2 *done;                        // [B][Hq]: maximum and 1 / sum of finished items (weights only: p = 2^(score - maximum) / sum, without
+                                         // the rounding of a logarithm)
     float *scores;                       // [B][H][GB][cap][GS]
     int2 *runs;                          // [B][H][GB]: first and last CTA of an item
 };
@@ -486,7 +487,7 @@ __global__ void __launch_bounds__(kThreads, 1) decode_kernel(const DecodeArgs A)
                     if (d == 0) {
                         const float l2 = sum == 0.f ? -INFINITY : top + log2f(sum);
                         if (A.lse) A.lse[row] = l2 / kLog2e;
-                        if (A.acc) A.lse2[row] = l2;
+                        if (A.acc) A.done[row] = make_float2(top == -INFINITY ? 0.f : top, inv);
                     }
                 } else {
                     *reinterpret_cast<float2 *>(po + head * D + d) = acc;
@@ -508,7 +509,8 @@ constexpr int kMaxParts = 256;             // CTAs of the main kernel at most
 template <int DT, int D, int NT, int U>
 __global__ void __launch_bounds__(kThreads, 3) decode_join_kernel(const DecodeArgs A) {
     constexpr int HB = 8 * NT, CH = 2048 / D;
-    __shared__ float sh_lse2[128], sh_f[HB][kMaxParts], sh_inv[HB];
+    __shared__ float sh_f[HB][kMaxParts];
+    __shared__ float2 sh_done[128];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, h = blockIdx.y, b = blockIdx.z, j0 = blockIdx.x * (U * kThreads);
     si_tc::pdl_wait();
     si_tc::pdl_launch();
@@ -528,10 +530,10 @@ __global__ void __launch_bounds__(kThreads, 3) decode_join_kernel(const DecodeAr
         }
     }
     const long long row = (long long)b * A.Hq + h * A.G;
-    const float whole = A.acc && tid < A.G ? A.lse2[row + tid] : 0.f;
+    const float2 whole = A.acc && tid < A.G ? A.done[row + tid] : make_float2(0.f, 0.f);
     const SeqWork w = seq_work<D>(A, b, nullptr);
     if (j0 >= w.n && (blockIdx.x > 0 || w.nc == 0)) return;
-    if (A.acc && tid < A.G) sh_lse2[tid] = whole;
+    if (A.acc && tid < A.G) sh_done[tid] = whole;
     for (int gb = 0; gb < A.GB && w.nc > 0; ++gb) {
         const int head0 = gb * HB, heads = min(HB, A.G - head0);
         int2 run = A.runs[((long long)b * A.kv.H + h) * A.GB + gb];
@@ -563,10 +565,8 @@ __global__ void __launch_bounds__(kThreads, 3) decode_join_kernel(const DecodeAr
 #pragma unroll
             for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
             if (lane == 0) {
-                const float l2 = sum == 0.f ? -INFINITY : top + log2f(sum);
-                sh_lse2[head0 + head] = l2;
-                sh_inv[head] = sum == 0.f ? 0.f : 1.f / sum;
-                if (blockIdx.x == 0 && A.lse) A.lse[row + head0 + head] = l2 / kLog2e;
+                sh_done[head0 + head] = make_float2(top == -INFINITY ? 0.f : top, sum == 0.f ? 0.f : 1.f / sum);
+                if (blockIdx.x == 0 && A.lse) A.lse[row + head0 + head] = sum == 0.f ? -INFINITY : (top + log2f(sum)) / kLog2e;
             }
         }
         __syncthreads();
@@ -579,7 +579,7 @@ __global__ void __launch_bounds__(kThreads, 3) decode_join_kernel(const DecodeAr
                     const float2 t = *reinterpret_cast<const float2 *>(A.part_o + (slot(k) * HB + head) * D + d);
                     acc.x += t.x * sh_f[head][k]; acc.y += t.y * sh_f[head][k];
                 }
-                *reinterpret_cast<uint32_t *>(A.out + (row + head0 + head) * D + d) = pack2<DT>(acc.x * sh_inv[head], acc.y * sh_inv[head]);
+                *reinterpret_cast<uint32_t *>(A.out + (row + head0 + head) * D + d) = pack2<DT>(acc.x * sh_done[head0 + head].y, acc.y * sh_done[head0 + head].y);
             }
     }
     if (!A.acc) return;
@@ -596,15 +596,15 @@ __global__ void __launch_bounds__(kThreads, 3) decode_join_kernel(const DecodeAr
             for (int g = 0; g < HB; g += 2) {
                 if (g >= A.GS || gb * HB + g >= A.G) break;
                 const float2 y = gb == 0 ? x[i][g / 2] : *reinterpret_cast<const float2 *>(more + g);
-                if (y.x != -INFINITY) sum += ex2(y.x - sh_lse2[gb * HB + g]);
-                if (gb * HB + g + 1 < A.G && y.y != -INFINITY) sum += ex2(y.y - sh_lse2[gb * HB + g + 1]);
+                sum += ex2(y.x - sh_done[gb * HB + g].x) * sh_done[gb * HB + g].y;         // a hidden entry's score is -inf
+                if (gb * HB + g + 1 < A.G) sum += ex2(y.y - sh_done[gb * HB + g + 1].x) * sh_done[gb * HB + g + 1].y;
             }
         }
         weight[j] = j == w.n_old ? sum : old[i] + sum;
     }
 }
 
-struct Layout { int n_cta, NT, GB, GS; size_t o, ml, lse2, scores, runs, total; };
+struct Layout { int n_cta, NT, GB, GS; size_t o, ml, done, scores, runs, total; };
 Layout layout_of(const si_kv_t *kv, int n_q_heads, bool acc) {
     Layout L;
     L.n_cta = si_sm_count() < kMaxParts ? si_sm_count() : kMaxParts;
@@ -616,7 +616,7 @@ Layout layout_of(const si_kv_t *kv, int n_q_heads, bool acc) {
     auto take = [&](size_t bytes) { const size_t at = off; off += si_align_up(bytes, 256); return at; };
     L.o = take((size_t)L.n_cta * 2 * 8 * L.NT * kv->head_dim * 4);
     L.ml = take((size_t)L.n_cta * 2 * 8 * L.NT * 2 * 4);
-    L.lse2 = take(acc ? (size_t)kv->n_seqs * n_q_heads * 4 : 0);
+    L.done = take(acc ? (size_t)kv->n_seqs * n_q_heads * 8 : 0);
     L.scores = take(acc ? (size_t)kv->n_seqs * kv->n_kv_heads * L.GB * kv->capacity * L.GS * 4 : 0);
     L.runs = take((size_t)kv->n_seqs * kv->n_kv_heads * L.GB * 8);
     L.total = off;
@@ -682,6 +682,6 @@ extern "C" int si_attn_decode(const si_kv_t *kv, const void *q, long long q_seq_
     const DecodeArgs A{si_kv_view_of(kv), (const uint16_t *)q, (const uint16_t *)k_new, (const uint16_t *)v_new, q_pos, q_seq_stride,
                        new_seq_stride, n_q_heads, n_q_heads / kv->n_kv_heads, L.GB, L.GS, window, n_sink, scale * kLog2e,
                        (uint16_t *)out, lse, status_dev, acc, L.n_cta, (float *)(ws + L.o), (float *)(ws + L.ml),
-                       (float *)(ws + L.lse2), (float *)(ws + L.scores), (int2 *)(ws + L.runs)};
+                       (float2 *)(ws + L.done), (float *)(ws + L.scores), (int2 *)(ws + L.runs)};
     return kv->dtype == SI_BF16 ? launch_t<SI_BF16>(A, L.NT, (cudaStream_t)stream) : launch_t<SI_F16>(A, L.NT, (cudaStream_t)stream);
 }

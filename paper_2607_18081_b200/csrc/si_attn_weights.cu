@@ -256,7 +256,7 @@ weights_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
             const bool whole = cur.start >= g0 && cur.start + cur.q.n <= g1;
             float *weight = A.kv.weight + A.kv.meta(cur.b, cur.h) + key;
             const float old = whole && writer && key < cur.len ? *weight : 0.f;      // needed at the end only
-            float sum = 0.f;
+            float sum = 0.f, lost = 0.f;
             for (; g < end; ++g, ++it) {
                 if ((it & 1) != parity) continue;
                 const int st = it % kLse;
@@ -309,7 +309,10 @@ weights_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
                 if (lane == 0) { mbar_arrive(&B->free[buf]); mbar_arrive(&B->lempty[st]); }
                 float a, b;
                 untwo(add2(add2(part[0], part[1]), add2(part[2], part[3])), a, b);
-                sum += a + b;
+                // a long prompt's first entries collect thousands of tiles: the sum carries what its rounding lost
+                const float add = (a + b) - lost, next = sum + add;
+                lost = (next - sum) - add;
+                sum = next;
             }
             if (!single) {
                 float *xch = other + (exchanges++ & 1) * kKeys + half * kTile + row;

@@ -35,6 +35,9 @@ template <int D> struct Cfg {
     static constexpr int kPanel = kTile * 128;              // 64 columns of a tile
 };
 
+// The lowest n bits.
+__device__ __forceinline__ uint32_t first_bits(int n) { return n >= 32 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << n) - 1; }
+
 struct Bars { uint64_t q, full[4], empty[4], s[2], p[2][2], o[2], dirty, clean; uint32_t tmem; int failed; };
 
 // Keys split over P.n CTAs per block of queries (1: not split); parts: [split][block][tile][row], values and {maximum, sum}.
@@ -208,10 +211,17 @@ prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
                     for (int c = 0; c < 128; ++c) x[c / 32][c % 32] ^= 0x80000000u;
                 }
                 if (MASKED) {
+                    // the columns this row sees, a bit each; a hidden score becomes -inf by two logical operations
                     const int hi_c = s - key0, lo_c = lo - key0, sink_c = A.n_sink - key0;
 #pragma unroll
-                    for (int c = 0; c < 128; ++c)
-                        if (!(c <= hi_c && (c > lo_c || c < sink_c))) x[c / 32][c % 32] = 0xFF800000u;
+                    for (int c = 0; c < 4; ++c) {
+                        const uint32_t seen = first_bits(hi_c + 1 - c * 32) & (~first_bits(lo_c + 1 - c * 32) | first_bits(sink_c - c * 32));
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) {
+                            const uint32_t all = (uint32_t)((int)(seen << (31 - k)) >> 31);
+                            x[c][k] = (x[c][k] & all) | (0xFF800000u & ~all);
+                        }
+                    }
                 }
                 float mx[4];
 #pragma unroll

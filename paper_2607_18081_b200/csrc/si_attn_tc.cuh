@@ -23,18 +23,18 @@ struct TcArgs {
     int32_t *status;
 };
 
-// The key tiles that queries at positions smin .. smax see: `sinks` tiles from the front, then those from `first` on; n in all.
+// The key tiles that queries at positions smin .. smax see: `sinks` tiles from the front, then tiles from entry `first` on; n in
+// all.  With a window, `first` is the first entry in it, wherever that lies: a tile may start at any entry.
 struct KeyTiles {
     int sinks, first, n, off;      // off: the first one of this CTA's share
-    __device__ __forceinline__ int key0(int j) const { j += off; return (j < sinks ? j : first + j - sinks) * kTile; }
+    __device__ __forceinline__ int key0(int j) const { j += off; return j < sinks ? j * kTile : first + (j - sinks) * kTile; }
 };
 __device__ __forceinline__ KeyTiles key_tiles(int smin, int smax, int window, int n_sink) {
     KeyTiles k = {0, 0, 0, 0};
     if (smax < 0) return k;
-    const int end = smax / kTile + 1, lo = window ? max(0, si_window_lo(smin, window) + 1) : 0;
-    k.first = lo / kTile;
-    k.sinks = min((min(n_sink, lo) + kTile - 1) / kTile, k.first);
-    k.n = k.sinks + end - k.first;
+    const int lo = window ? max(0, si_window_lo(smin, window) + 1) : 0, sinks = (min(n_sink, lo) + kTile - 1) / kTile;
+    if (lo >= sinks * kTile) { k.sinks = sinks; k.first = lo; }      // else the two would overlap: everything from the front
+    k.n = k.sinks + (smax + kTile - k.first) / kTile;
     return k;
 }
 

@@ -47,7 +47,7 @@ struct SplitArgs { int n, blocks; float *o; float2 *ml; };
 template <int DT, int D, bool NEG>
 __global__ void __launch_bounds__(kThreads, 1)
 prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,
-               const TcArgs A, const SplitArgs P) {
+               const __grid_constant__ CUtensorMap omap, const TcArgs A, const SplitArgs P) {
     using C = Cfg<D>;
     constexpr int NS = C::kStages;
     extern __shared__ char smem_raw[];
@@ -57,7 +57,14 @@ prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
     volatile int *failed = &B->failed;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
+    // blocks of queries from the last (most keys) to the first, so that the long ones start first
+    const int heads = A.kv.H * A.kv.B, nqb = gridDim.x / heads;
+    const int split = blockIdx.y, qb = nqb - 1 - blockIdx.x / heads, h = blockIdx.x % heads % A.kv.H, b = blockIdx.x % heads / A.kv.H;
+    pdl_wait();                             // a programmatic dependent: its launch runs beside the end of the kernel before it
+    const int n = si_kv_len(A.kv, b, A.status);      // on its way during the set-up
+
     if (threadIdx.x == 0) {
+        prefetch_map(&qmap); prefetch_map(&kmap); prefetch_map(&vmap); prefetch_map(&omap);
         mbar_init(&B->q, 1);
         for (int s = 0; s < NS; ++s) { mbar_init(&B->full[s], 1); mbar_init(&B->empty[s], 1); }
         for (int t = 0; t < 2; ++t) { mbar_init(&B->s[t], 1); mbar_init(&B->p[t][0], 4); mbar_init(&B->p[t][1], 4); mbar_init(&B->o[t], 1); }
@@ -73,16 +80,13 @@ prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = B->tmem;
-    pdl_wait();                             // a programmatic dependent: up to here it ran beside the end of the kernel before it
-
-    // blocks of queries from the last (most keys) to the first, so that the long ones start first
-    const int heads = A.kv.H * A.kv.B, nqb = gridDim.x / heads;
-    const int split = blockIdx.y, qb = nqb - 1 - blockIdx.x / heads, h = blockIdx.x % heads % A.kv.H, b = blockIdx.x % heads / A.kv.H;
-    const int n = si_kv_len(A.kv, b, A.status), i0 = qb * 2 * A.R, shift = n - A.T;       // query i is at position shift + i
+    const int i0 = qb * 2 * A.R, shift = n - A.T;            // query i is at position shift + i
     const int tiles = i0 + A.R < A.T ? 2 : 1;
     KeyTiles keys = key_tiles(shift + i0, shift + min(A.T, i0 + 2 * A.R) - 1, A.window, A.n_sink);
-    keys.off = (int)((long long)keys.n * split / P.n);
-    keys.n = (int)((long long)keys.n * (split + 1) / P.n) - keys.off;
+    if (P.n > 1) {                          // the tiles of this CTA's share (far fewer than 2^31 / splits)
+        keys.off = keys.n * split / P.n;
+        keys.n = keys.n * (split + 1) / P.n - keys.off;
+    }
 
     const bool tail = keys.n > 0 && keys.key0(keys.n - 1) + kTile > n;     // the last tile reaches beyond the entries in use
     if (warp >= 8) {
@@ -301,25 +305,33 @@ prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
                 if (l < 0.5f) l = 0.f;
                 const float inv = l == 0.f ? 0.f : 1.f / l;
                 const long long r = ((long long)b * A.T + i) * A.Hq + hq;
+                // through the tile's query buffer (its last product is done), in the layout of the boxes the queries came in, and
+                // out as the same boxes: rows of a thread are 2 D bytes apart, storing them directly took 4000 clocks
+                char *stage = smem + t * C::kBytes + row * 128;
 #pragma unroll
                 for (int c = 0; c < D / 32; ++c) {
                     uint32_t o[32] = {};
-                    if (keys.n > 0) { tmem_ld32(to + c * 32, o); tmem_wait_ld(o); }      // by the whole warp
-                    if (valid) {
+                    if (keys.n > 0) { tmem_ld32(to + c * 32, o); tmem_wait_ld(o); }
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            uint4 w = make_uint4(0, 0, 0, 0);
-                            if (l != 0.f) {
-                                const uint32_t *v = o + k * 8;
-                                w.x = pack2<DT>(__uint_as_float(v[0]) * inv, __uint_as_float(v[1]) * inv);
-                                w.y = pack2<DT>(__uint_as_float(v[2]) * inv, __uint_as_float(v[3]) * inv);
-                                w.z = pack2<DT>(__uint_as_float(v[4]) * inv, __uint_as_float(v[5]) * inv);
-                                w.w = pack2<DT>(__uint_as_float(v[6]) * inv, __uint_as_float(v[7]) * inv);
-                            }
-                            *reinterpret_cast<uint4 *>(A.out + r * D + c * 32 + k * 8) = w;
+                    for (int k = 0; k < 4; ++k) {
+                        uint4 w = make_uint4(0, 0, 0, 0);
+                        if (l != 0.f) {
+                            const uint32_t *v = o + k * 8;
+                            w.x = pack2<DT>(__uint_as_float(v[0]) * inv, __uint_as_float(v[1]) * inv);
+                            w.y = pack2<DT>(__uint_as_float(v[2]) * inv, __uint_as_float(v[3]) * inv);
+                            w.z = pack2<DT>(__uint_as_float(v[4]) * inv, __uint_as_float(v[5]) * inv);
+                            w.w = pack2<DT>(__uint_as_float(v[6]) * inv, __uint_as_float(v[7]) * inv);
                         }
+                        const int piece = c % 2 * 4 + k;
+                        *reinterpret_cast<uint4 *>(stage + c / 2 * C::kPanel + ((piece ^ (row & 7)) << 4)) = w;
                     }
-                    __syncwarp();
+                }
+                fence_async_proxy();
+                asm volatile("bar.sync %0, 128;" ::"r"(1 + t) : "memory");
+                if ((warp & 3) == 0 && elect_one()) {
+#pragma unroll
+                    for (int c = 0; c < D / 64; ++c) tma_store_4d(&omap, smem + t * C::kBytes + c * C::kPanel, c * 64, h * A.G, i0 + t * A.R, b);
+                    tma_store_wait();
                 }
                 if (valid && A.lse) A.lse[r] = l == 0.f ? -INFINITY : (base2 + log2f(l)) / kLog2e;
             }
@@ -334,35 +346,69 @@ prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
     }
 }
 
-// One warp per row: the parts of its splits, in order.
+// One warp per row: the parts of its splits, summed in order; four columns per lane, so that a warp reads 32 / (D / 4) splits at
+// a time.  The values do not wait for the maxima.
+constexpr int kMaxSplits = 160;
 template <int DT, int D>
 __global__ void __launch_bounds__(256) prefill_join_kernel(const TcArgs A, const SplitArgs P) {
-    const int lane = threadIdx.x & 31;
-    const long long r = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+    constexpr int kLanes = D / 4, kSide = 32 / kLanes, kAhead = 8;
+    __shared__ float sh_f[8][kMaxSplits];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, side = lane / kLanes, col = lane % kLanes * 4;
+    const long long r = (long long)blockIdx.x * 8 + warp;
     pdl_wait();
     pdl_launch();
     if (r >= (long long)A.kv.B * A.T * A.Hq) return;
-    const int hq = (int)(r % A.Hq), i = (int)(r / A.Hq % A.T), b = (int)(r / A.Hq / A.T), h = hq / A.G;
+    const unsigned rr = (unsigned)r;                          // rows of a split call are few
+    const int hq = rr % A.Hq, i = rr / A.Hq % A.T, b = rr / A.Hq / A.T, h = hq / A.G;
     const int heads = A.kv.H * A.kv.B, nqb = P.blocks / heads, qb = i / (2 * A.R), t = i / A.R % 2;
     const long long block = (long long)(nqb - 1 - qb) * heads + b * A.kv.H + h, row = i % A.R * A.G + hq % A.G;
     const long long first = (block * 2 + t) * kTile + row, step = (long long)P.blocks * 2 * kTile;
-    float top = -INFINITY;
-    for (int s = lane; s < P.n; s += 32) top = fmaxf(top, P.ml[first + s * step].x);
+    float4 v[kAhead];
+    auto fetch = [&](int s0) {
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int s = s0 + k * kSide + side;
+            v[k] = s < P.n ? *reinterpret_cast<const float4 *>(P.o + (first + s * step) * D + col) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+    };
+    fetch(0);
+    float2 ml[kMaxSplits / 32];
+    float top = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int k = 0; k < kMaxSplits / 32; ++k) {
+        const int s = k * 32 + lane;
+        ml[k] = s < P.n ? P.ml[first + s * step] : make_float2(-INFINITY, 0.f);
+        top = fmaxf(top, ml[k].x);
+    }
 #pragma unroll
     for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-    float l = 0.f, acc[D / 32] = {};
-#pragma unroll 4
-    for (int s = 0; s < P.n; ++s) {
-        const float2 ml = P.ml[first + s * step];
-        if (ml.x == -INFINITY) continue;
-        const float f = ex2(ml.x - top);
-        l += ml.y * f;
 #pragma unroll
-        for (int c = 0; c < D / 32; ++c) acc[c] += P.o[(first + s * step) * D + c * 32 + lane] * f;
+    for (int k = 0; k < kMaxSplits / 32; ++k) {
+        const float f = ml[k].x == -INFINITY ? 0.f : ex2(ml[k].x - top);
+        sh_f[warp][k * 32 + lane] = f;
+        l += ml[k].y * f;
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, o);
+    __syncwarp();
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int s0 = 0; s0 < P.n; s0 += kAhead * kSide) {
+        if (s0 > 0) fetch(s0);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int s = s0 + k * kSide + side;
+            const float f = s < P.n ? sh_f[warp][s] : 0.f;
+            if (f == 0.f) continue;                           // nothing seen in this part: its values are not used
+            acc.x += v[k].x * f; acc.y += v[k].y * f; acc.z += v[k].z * f; acc.w += v[k].w * f;
+        }
+    }
+#pragma unroll
+    for (int o = kLanes; o < 32; o *= 2) {
+        acc.x += __shfl_xor_sync(0xFFFFFFFFu, acc.x, o); acc.y += __shfl_xor_sync(0xFFFFFFFFu, acc.y, o);
+        acc.z += __shfl_xor_sync(0xFFFFFFFFu, acc.z, o); acc.w += __shfl_xor_sync(0xFFFFFFFFu, acc.w, o);
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-    for (int c = 0; c < D / 32; ++c) A.out[r * D + c * 32 + lane] = si_cvt<DT>::from_float(acc[c] * inv);
+    if (side == 0) *reinterpret_cast<uint2 *>(A.out + r * D + col) = make_uint2(pack2<DT>(acc.x * inv, acc.y * inv), pack2<DT>(acc.z * inv, acc.w * inv));
     if (lane == 0 && A.lse) A.lse[r] = l == 0.f ? -INFINITY : (top + log2f(l)) / kLog2e;
 }
 
@@ -379,6 +425,7 @@ Plan plan_of(const si_kv_t *kv, int n_q_heads, int T, int window, int n_sink) {
     }
     if (p.blocks * 2 <= sms && tiles >= 8) {
         p.splits = (int)(sms / p.blocks);
+        if (p.splits > kMaxSplits) p.splits = kMaxSplits;
         if (p.splits > tiles / 4) p.splits = (int)(tiles / 4);
     }
     return p;
@@ -386,7 +433,7 @@ Plan plan_of(const si_kv_t *kv, int n_q_heads, int T, int window, int n_sink) {
 size_t parts_o_bytes(const Plan &p, int D) { return p.splits > 1 ? si_align_up((size_t)p.splits * p.blocks * 2 * kTile * D * 4, 256) : 0; }
 size_t parts_ml_bytes(const Plan &p) { return p.splits > 1 ? si_align_up((size_t)p.splits * p.blocks * 2 * kTile * 8, 256) : 0; }
 
-struct Call { const CUtensorMap &qm, &km, &vm; const TcArgs &A; const SplitArgs &P; cudaStream_t st; };
+struct Call { const CUtensorMap &qm, &km, &vm, &om; const TcArgs &A; const SplitArgs &P; cudaStream_t st; };
 template <int DT, int D, bool NEG> int launch(const Call &c) {
     static std::atomic<int> ready{0};
     if (!ready.load()) {
@@ -402,7 +449,7 @@ template <int DT, int D, bool NEG> int launch(const Call &c) {
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = Cfg<D>::kSmem;
     cfg.stream = c.st;
-    SI_CUDA_TRY(cudaLaunchKernelEx(&cfg, prefill_kernel<DT, D, NEG>, c.qm, c.km, c.vm, c.A, c.P));
+    SI_CUDA_TRY(cudaLaunchKernelEx(&cfg, prefill_kernel<DT, D, NEG>, c.qm, c.km, c.vm, c.om, c.A, c.P));
     if (c.P.n > 1) {
         cfg.gridDim = dim3((unsigned)(((long long)c.A.kv.B * c.A.T * c.A.Hq + 7) / 8));
         cfg.blockDim = dim3(256);
@@ -439,10 +486,12 @@ extern "C" int si_attn_prefill(const si_kv_t *kv, const void *q, long long q_seq
     }
     const SplitArgs P{p.splits, (int)p.blocks, (float *)workspace, (float2 *)((char *)workspace + parts_o_bytes(p, kv->head_dim))};
     const TcArgs A = tc_args(kv, q_seq_stride, T, n_q_heads, window, n_sink, scale, out, lse, status_dev);
-    CUtensorMap qm, km, vm;
+    CUtensorMap qm, km, vm, om;
     if ((rc = make_q_map(&qm, q, kv, q_seq_stride, q_tok_stride, T, n_q_heads, A.G, A.R))) return rc;
     if ((rc = make_kv_map(&km, kv->k, kv)) || (rc = make_kv_map(&vm, kv->v, kv))) return rc;
-    const Call c{qm, km, vm, A, P, (cudaStream_t)stream};
+    const long long row = (long long)n_q_heads * kv->head_dim;
+    if ((rc = make_q_map(&om, out, kv, T * row, row, T, n_q_heads, A.G, A.R))) return rc;
+    const Call c{qm, km, vm, om, A, P, (cudaStream_t)stream};
     const bool neg = scale < 0.f;
     if (kv->dtype == SI_BF16) return kv->head_dim == 128 ? launch_t<SI_BF16, 128>(c, neg) : launch_t<SI_BF16, 64>(c, neg);
     return kv->head_dim == 128 ? launch_t<SI_F16, 128>(c, neg) : launch_t<SI_F16, 64>(c, neg);

@@ -82,8 +82,9 @@ def check_lse(lse, ref, D):
     got = f64(lse)
     empty = np.isinf(ref["lse"])
     assert np.array_equal(np.isneginf(got), empty)
-    bound = delta(ref, D) + 4 * E * (np.abs(np.where(empty, 0, ref["lse"])) + 20) + ref["n"] * E
-    assert np.all(np.abs(got - ref["lse"])[~empty] <= bound[~empty]), np.max(np.abs(got - ref["lse"])[~empty] / bound[~empty])
+    bound = (delta(ref, D) + 4 * E * (np.abs(np.where(empty, 0, ref["lse"])) + 20) + ref["n"] * E)[~empty]
+    err = np.abs(got[~empty] - ref["lse"][~empty])
+    assert np.all(err <= bound), np.max(err / bound)
 
 
 def check_weight(weight, before, ref, D, T):

@@ -48,6 +48,9 @@ PREFILL = [
     (1, 40, [2100], 32, 4, 128, 0, 0),           # few rows, a long axis
     (1, 3, [1500], 128, 1, 64, 0, 0),            # 128 query heads on one key head
     (1, 260, [900], 1, 1, 128, 300, 64),
+    (2, 30, [0, 2500], 8, 2, 128, 0, 0),         # keys split over CTAs, an empty sequence beside a long one
+    (1, 20, [3000], 8, 2, 64, 1500, 5),          # ... with a window and sinks
+    (1, 1, [5000], 12, 4, 128, 0, 0),
 ]
 
 
@@ -217,6 +220,64 @@ def test_caches_whose_offsets_pass_32_bits(api):
     api.si_attn_decode(cache, q[:, -1], None, None, None, 0, 0, 0.125, o1, None, 0, cache.workspace(8, 1))
     last = {x: ref[x][:, -1:] for x in ("out", "reach", "lse", "size", "n")}
     au.check_out(o1[:, None], last, "bf16", D)
+
+
+@pytest.mark.parametrize("D,order", [(128, "hnd"), (64, "nhd")])
+def test_sequences_that_share_one_cache_through_a_zero_stride(api, D, order):
+    """Every sequence of the batch reads the same keys and values (expand: a stride of zero), at lengths of its own."""
+    lens, Hq, Hkv, T, cap = [400, 150, 399], 8, 2, 37, 410
+    q, k, v, _ = au.make(1, Hq, Hkv, D, cap, "bf16", order, T, 8, [cap])
+    k, v = k.expand(3, -1, -1, -1), v.expand(3, -1, -1, -1)
+    q = torch.cat([q, q.flip(1), -q]).contiguous()
+    length = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    weight = torch.zeros(3, Hkv, cap, device="cuda")
+    out, lse = _prefill(api, q, k, v, length, 0, 0, 0.1, weight)
+    ref = au.reference(q, k, v, lens, 0, 0, 0.1)
+    au.check_out(out, ref, "bf16", D)
+    au.check_lse(lse, ref, D)
+    au.check_weight(weight, np.zeros(weight.shape), ref, D, T)
+    cache = api.KVCache(k, v, length)
+    o1 = torch.empty(3, Hq, D, dtype=q.dtype, device="cuda")
+    api.si_attn_decode(cache, q[:, -1], None, None, None, 0, 0, 0.1, o1, None, 0, cache.workspace(Hq, 1))
+    au.check_out(o1[:, None], {x: ref[x][:, -1:] for x in ("out", "reach", "lse", "size", "n")}, "bf16", D)
+
+
+def test_prefill_weights_and_eviction_in_one_graph(api):
+    lens = [300, 170]
+    q, k, v, length = au.make(2, 8, 2, 128, 320, "bf16", "nhd", 60, 6, lens)
+    weight = torch.zeros(2, 2, 320, device="cuda")
+    src = api.KVCache(k, v, length, None, weight)
+    dk, dv = (torch.zeros(2, 2, 64, 128, dtype=q.dtype, device="cuda") for _ in range(2))
+    dst = api.KVCache(dk, dv, torch.zeros(2, dtype=torch.int32, device="cuda"), torch.zeros(2, 2, 64, dtype=torch.int32, device="cuda"),
+                      torch.zeros(2, 2, 64, device="cuda"))
+    out, lse = torch.empty(2, 60, 8, 128, dtype=q.dtype, device="cuda"), torch.empty(2, 60, 8, device="cuda")
+    ws = src.workspace(8, 60)
+
+    def calls(stream=None):
+        weight.zero_()
+        api.si_attn_prefill(src, q, 0, 0, 0.09, out, lse, ws, stream=stream)
+        api.si_attn_weights(src, q, 0, 0, 0.09, lse, ws, stream=stream)
+        api.si_kv_evict(src, dst, None, 0, 64, 4, 8, None, dst.length, ws, stream=stream)
+
+    calls()
+    torch.cuda.synchronize()
+    first = [t.clone() for t in (out, lse, weight, dk, dv, dst.pos, dst.weight)]
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        calls(s)
+    for t in (out, lse, dk, dv, dst.pos, dst.weight):
+        t.zero_()
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert dst.length.tolist() == [64, 64]
+    for a, b in zip(first, (out, lse, weight, dk, dv, dst.pos, dst.weight)):
+        assert torch.equal(a, b)
+    ref = au.reference(q, k, v, lens, 0, 0, 0.09)
+    au.check_out(out, ref, "bf16", 128)
+    au.check_weight(weight, np.zeros(weight.shape), ref, 128, 60)
 
 
 def test_lengths_outside_the_capacity_and_a_full_cache_are_reported(api):

@@ -104,6 +104,47 @@ def test_evict_of_a_prefilled_cache_without_positions(api):
             assert torch.equal(dk[b, h], k[b, h, torch.from_numpy(want).cuda()]) and torch.equal(dv[b, h], v[b, h, torch.from_numpy(want).cuda()])
 
 
+def test_evict_into_a_cache_with_a_budget_above_the_source(api):
+    """Nothing is over the budget: every entry is copied, further slots of `kept` are -1 and of the cache untouched."""
+    B, H, D, cap, budget, lens = 2, 2, 64, 40, 100, [40, 7]
+    k, v = (torch.randn(B, H, cap, D, device="cuda").to(torch.float16) for _ in range(2))
+    w = torch.rand(B, H, cap, device="cuda")
+    length = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    for with_kept in (True, False):
+        dk, dv = (torch.zeros(B, H, budget, D, dtype=torch.float16, device="cuda") for _ in range(2))
+        dpos, dw = torch.full((B, H, budget), -9, dtype=torch.int32, device="cuda"), torch.zeros(B, H, budget, device="cuda")
+        kept = torch.full((B, H, budget), -7, dtype=torch.int32, device="cuda") if with_kept else None
+        len_out = torch.zeros(B, dtype=torch.int32, device="cuda")
+        src, dst = api.KVCache(k, v, length, None, w), api.KVCache(dk, dv, len_out, dpos, dw)
+        api.si_kv_evict(src, dst, None, 0, budget, 4, 16, kept, len_out, src.workspace(0, 0))
+        torch.cuda.synchronize()
+        assert len_out.tolist() == lens
+        for b, n in enumerate(lens):
+            assert torch.equal(dk[b, :, :n], k[b, :, :n]) and torch.equal(dv[b, :, :n], v[b, :, :n]) and torch.equal(dw[b, :, :n], w[b, :, :n])
+            assert (dpos[b, :, n:] == -9).all() and torch.count_nonzero(dk[b, :, n:]) == 0
+            if with_kept:
+                assert (kept[b, :, n:] == -1).all() and (kept[b, :, :n] == torch.arange(n, device="cuda")).all()
+
+
+@pytest.mark.parametrize("n,budget", [(400000, 150000), (393217, 393000)])
+def test_evict_of_rows_longer_than_shared_memory_holds(api, n, budget):
+    """More keys than eight CTAs keep in shared memory: the weights are read again instead, in rounds."""
+    rng = np.random.default_rng(n)
+    w = np.floor(rng.random(n) * 1000).astype(np.float32)
+    k, v = (torch.randint(-30000, 30000, (1, 1, n, 64), dtype=torch.int16, device="cuda").view(torch.bfloat16) for _ in range(2))
+    length = torch.tensor([n], dtype=torch.int32, device="cuda")
+    src = api.KVCache(k, v, length, None, torch.from_numpy(w).cuda().view(1, 1, n))
+    dk, dv = (torch.zeros(1, 1, budget, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    dst = api.KVCache(dk, dv, length, torch.zeros(1, 1, budget, dtype=torch.int32, device="cuda"), torch.zeros(1, 1, budget, device="cuda"))
+    kept = torch.zeros(1, 1, budget, dtype=torch.int32, device="cuda")
+    api.si_kv_evict(src, dst, None, 0, budget, 16, 1000, kept, None, src.workspace(0, 0))
+    torch.cuda.synchronize()
+    want = ao.evict(w, np.arange(n), n - 1, budget, 16, 1000)
+    assert np.array_equal(kept[0, 0].cpu().numpy(), want) and np.array_equal(dst.pos[0, 0].cpu().numpy(), want)
+    at = torch.from_numpy(want).cuda()
+    assert torch.equal(dk[0, 0].view(torch.int16), k[0, 0, at].view(torch.int16)) and torch.equal(dv[0, 0].view(torch.int16), v[0, 0, at].view(torch.int16))
+
+
 def test_evict_reports_lengths_outside_the_capacity(api):
     k = torch.zeros(1, 1, 16, 64, dtype=torch.float16, device="cuda")
     pos, w = torch.zeros(1, 1, 16, dtype=torch.int32, device="cuda"), torch.zeros(1, 1, 16, device="cuda")

@@ -124,51 +124,38 @@ template <int D> __device__ __forceinline__ bool next_item(const DecodeArgs &A, 
     return true;
 }
 
-// Thread t of the block stands for sequences t * per .. : sh[t] = chunks in front of them; returns the total.
-template <int D> __device__ __forceinline__ int scan_work(const DecodeArgs &A, int *sh, int32_t *status) {
-    const int tid = threadIdx.x, per = (A.kv.B + kThreads - 1) / kThreads, items = A.kv.H * A.GB;
-    const int b0 = min(A.kv.B, tid * per), b1 = min(A.kv.B, b0 + per);
+// Number of chunks of all items; the first chunk of this CTA's run is at `at` on return (of all threads, if there is one).  Thread t
+// of the block stands for sequences t * per ..; the one that holds the run's first chunk looks it up.
+struct Run { int g0, g1, per; bool empty; };
+template <int D> __device__ __forceinline__ Run find_run(const DecodeArgs &A, Cursor *at, int *sh, int32_t *status) {
+    const int tid = threadIdx.x, share = (A.kv.B + kThreads - 1) / kThreads, items = A.kv.H * A.GB;
+    const int b0 = min(A.kv.B, tid * share), b1 = min(A.kv.B, b0 + share);
     int sum = 0;
     bool empty = false;
-    for (int b = b0; b < b1; ++b) {
-        const int nc = seq_work<D>(A, b, status).nc;
-        sum += nc * items;
-        empty |= nc == 0;
-    }
-    sh[tid] = sum;
-    sh[kThreads + 1] = __syncthreads_or(empty);      // some sequence has nothing to see
-    if (tid < 32) {
-        constexpr int N = kThreads / 32;
-        int v[N], run = 0;
-#pragma unroll
-        for (int i = 0; i < N; ++i) { v[i] = run; run += sh[tid * N + i]; }
-        int inc = run;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int t = __shfl_up_sync(0xFFFFFFFFu, inc, o);
-            if (tid >= o) inc += t;
-        }
-#pragma unroll
-        for (int i = 0; i < N; ++i) sh[tid * N + i] = inc - run + v[i];
-        if (tid == 31) sh[kThreads] = inc;
-    }
-    __syncthreads();
-    return sh[kThreads];
-}
-// The item that holds chunk `target` (< total).
-template <int D> __device__ __forceinline__ Cursor find_item(const DecodeArgs &A, int target, const int *sh) {
-    const int per = (A.kv.B + kThreads - 1) / kThreads, items = A.kv.H * A.GB;
-    int lo = 0, hi = kThreads - 1;                   // last thread whose first chunk is <= target
-    while (lo < hi) { const int mid = (lo + hi + 1) / 2; if (sh[mid] <= target) lo = mid; else hi = mid - 1; }
-    int start = sh[lo];
     Cursor c;
-    c.b = lo * per;
-    c.w = seq_work<D>(A, c.b, nullptr);
-    while (start + c.w.nc * items <= target) { start += c.w.nc * items; c.w = seq_work<D>(A, ++c.b, nullptr); }
-    c.hh = (target - start) / c.w.nc;
-    c.start = start + c.hh * c.w.nc;
-    return c;
+    for (int b = b0; b < b1; ++b) {
+        c.w = seq_work<D>(A, b, status);
+        sum += c.w.nc * items;
+        empty |= c.w.nc == 0;
+    }
+    const int before = si_block_scan<kThreads>(sum, sh), total = sh[kThreads / 32];
+    Run r;
+    r.per = (total - 1) / A.n_cta + 1;
+    r.g0 = (int)min((long long)total, (long long)blockIdx.x * r.per);
+    r.g1 = total - r.g0 < r.per ? total : r.g0 + r.per;
+    if (r.g0 < r.g1 && before <= r.g0 && r.g0 - before < sum) {
+        int start = before;
+        c.b = b0;
+        if (share > 1) c.w = seq_work<D>(A, b0, nullptr);    // with one sequence per thread it is at hand
+        while (start + c.w.nc * items <= r.g0) { start += c.w.nc * items; c.w = seq_work<D>(A, ++c.b, nullptr); }
+        c.hh = (r.g0 - start) / c.w.nc;
+        c.start = start + c.hh * c.w.nc;
+        *at = c;
+    }
+    r.empty = __syncthreads_or(empty);                       // some sequence has nothing to see
+    return r;
 }
+
 // The queries of an item as B operands: head = lane / 4, two neighbouring elements per register.
 template <int D, int NT> __device__ __forceinline__ void load_q(const DecodeArgs &A, int b, int hh, uint32_t (&qf)[NT][D / 16][2]) {
     const int lane = threadIdx.x & 31, h = hh / A.GB, head0 = hh % A.GB * 8 * NT, heads = min(8 * NT, A.G - head0);
@@ -189,7 +176,8 @@ __global__ void __launch_bounds__(kThreads, 1) decode_kernel(const DecodeArgs A)
     using C = Cfg<D, NT>;
     constexpr int CH = C::CH, HB = 8 * NT, PIECES = D / 8, SUB = CH / 16;
     extern __shared__ __align__(128) char smem[];
-    __shared__ int sh_scan[kThreads + 2];
+    __shared__ int sh_scan[kThreads / 32 + 1];
+    __shared__ Cursor sh_at;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     char *ring = smem + warp * kStages * C::kStage;
     float *merge_o = (float *)(smem + kWarps * kStages * C::kStage);
@@ -202,12 +190,9 @@ __global__ void __launch_bounds__(kThreads, 1) decode_kernel(const DecodeArgs A)
     asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(stay));
 
     // this CTA's run of chunks
-    Cursor cons;
-    const int total = scan_work<D>(A, sh_scan, blockIdx.x == 0 ? A.status : nullptr);
-    const int per = (total - 1) / A.n_cta + 1, g0 = min((long long)total, (long long)blockIdx.x * per), g1 = total - g0 < per ? total : g0 + per;
-    if (g0 < g1) {
-        cons = find_item<D>(A, g0, sh_scan);
-    }
+    const Run run = find_run<D>(A, &sh_at, sh_scan, blockIdx.x == 0 ? A.status : nullptr);
+    const int per = run.per, g0 = run.g0, g1 = run.g1;
+    Cursor cons = sh_at;
 
     // ---- loader side: chunk ids g0 + warp, + kWarps, ...
     Cursor load = cons;
@@ -279,7 +264,7 @@ __global__ void __launch_bounds__(kThreads, 1) decode_kernel(const DecodeArgs A)
             else if (tid == 2 * PIECES && A.kv.pos) A.kv.pos[A.kv.meta(b, h) + n] = A.q_pos[b];
         }
 
-    if (sh_scan[kThreads + 1])
+    if (run.empty)
         for (int b = blockIdx.x; b < A.kv.B; b += gridDim.x) {
             if (seq_work<D>(A, b, nullptr).nc) continue;
             for (int i = tid; i < A.Hq * D; i += kThreads) A.out[(long long)b * A.Hq * D + i] = 0;

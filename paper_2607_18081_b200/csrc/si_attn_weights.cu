@@ -76,7 +76,8 @@ weights_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
     using C = Cfg<D>;
     constexpr int kStages = C::kStages;
     extern __shared__ char smem_raw[];
-    __shared__ int scan[kThreads + 1];
+    __shared__ int scan[kThreads / 32 + 1];
+    __shared__ Cursor found;
     char *smem = (char *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     char *ring = smem + 4 * C::kBytes;
     Bars *B = (Bars *)(ring + kStages * C::kBytes);
@@ -109,47 +110,30 @@ weights_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
     int sum = 0;
     for (int k = tid * per; k < min(n_bk, (tid + 1) * per); ++k)
         sum += query_tiles(A, si_kv_len(A.kv, k / W.nkt, blockIdx.x == 0 ? A.status : nullptr), k % W.nkt).n * A.kv.H;
-    scan[tid] = sum;
     tc_fence_before();
-    __syncthreads();
+    const int before = si_block_scan<kThreads>(sum, scan);
     tc_fence_after();
-    if (tid < 32) {
-        constexpr int N = kThreads / 32;
-        int v[N], run = 0;
-#pragma unroll
-        for (int i = 0; i < N; ++i) { v[i] = run; run += scan[tid * N + i]; }
-        int inc = run;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int t = __shfl_up_sync(0xFFFFFFFFu, inc, o);
-            if (tid >= o) inc += t;
+    const uint32_t tmem = B->tmem;
+    const int total = scan[kThreads / 32], run = (total - 1) / W.n_cta + 1;
+    const int g0 = (int)min((long long)total, (long long)blockIdx.x * run), g1 = total - g0 < run ? total : g0 + run;
+    if (g0 < g1 && before <= g0 && g0 - before < sum) {      // one thread's share holds the run's first pair: it looks it up for all
+        Cursor c;
+        int k = tid * per, start = before;
+        while (true) {
+            c.b = k / W.nkt; c.kt = k % W.nkt;
+            c.len = si_kv_len(A.kv, c.b, nullptr);
+            c.q = query_tiles(A, c.len, c.kt);
+            if (start + c.q.n * A.kv.H > g0) break;
+            start += c.q.n * A.kv.H;
+            ++k;
         }
-#pragma unroll
-        for (int i = 0; i < N; ++i) scan[tid * N + i] = inc - run + v[i];
-        if (tid == 31) scan[kThreads] = inc;
+        c.h = (g0 - start) / c.q.n;
+        c.start = start + c.h * c.q.n;
+        W.part_first[blockIdx.x] = item_of(A, W, c);
+        found = c;
     }
     __syncthreads();
-    const uint32_t tmem = B->tmem;
-    const int total = scan[kThreads], run = (total - 1) / W.n_cta + 1;
-    const int g0 = (int)min((long long)total, (long long)blockIdx.x * run), g1 = total - g0 < run ? total : g0 + run;
-    Cursor cur;
-    if (g0 < g1) {
-        int lo = 0, hi = kThreads - 1;
-        while (lo < hi) { const int mid = (lo + hi + 1) / 2; if (scan[mid] <= g0) lo = mid; else hi = mid - 1; }
-        int k = lo * per, start = scan[lo];
-        cur.len = si_kv_len(A.kv, k / W.nkt, nullptr);
-        cur.q = query_tiles(A, cur.len, k % W.nkt);
-        while (start + cur.q.n * A.kv.H <= g0) {
-            start += cur.q.n * A.kv.H;
-            ++k;
-            cur.len = si_kv_len(A.kv, k / W.nkt, nullptr);
-            cur.q = query_tiles(A, cur.len, k % W.nkt);
-        }
-        cur.b = k / W.nkt; cur.kt = k % W.nkt;
-        cur.h = (g0 - start) / cur.q.n;
-        cur.start = start + cur.h * cur.q.n;
-        if (tid == 0) W.part_first[blockIdx.x] = item_of(A, W, cur);
-    }
+    Cursor cur = found;
 
     if (warp == 16) {
         if (elect_one()) {

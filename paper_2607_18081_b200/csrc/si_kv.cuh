@@ -68,3 +68,31 @@ __device__ __forceinline__ int si_window_lo(int s, int window) {
     return window == 0 || lo < INT_MIN ? INT_MIN : (int)lo;
 }
 __device__ __forceinline__ bool si_visible(int p, int s, int lo, int n_sink) { return p <= s && (p > lo || p < n_sink || lo == INT_MIN); }
+
+// Exclusive sum over the block in thread order; `sh`: THREADS / 32 + 1 ints, the last one receives the total.
+template <int THREADS> __device__ __forceinline__ int si_block_scan(int v, int *sh) {
+    constexpr int W = THREADS / 32;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int inc = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int t = __shfl_up_sync(0xFFFFFFFFu, inc, o);
+        if (lane >= o) inc += t;
+    }
+    if (lane == 31) sh[warp] = inc;
+    __syncthreads();
+    if (warp == 0) {
+        const int w = lane < W ? sh[lane] : 0;
+        int winc = w;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int t = __shfl_up_sync(0xFFFFFFFFu, winc, o);
+            if (lane >= o) winc += t;
+        }
+        __syncwarp();
+        if (lane < W) sh[lane] = winc - w;
+        if (lane == 31) sh[W] = winc;
+    }
+    __syncthreads();
+    return sh[warp] + inc - v;
+}

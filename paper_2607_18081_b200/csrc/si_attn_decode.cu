@@ -252,18 +252,18 @@ __global__ void __launch_bounds__(kThreads, 1) decode_kernel(const DecodeArgs A)
     bool first_segment = true;
     uint32_t qf[NT][D / 16][2];
     if (g0 < g1) load_q<D, NT>(A, cons.b, cons.hh, qf);
-    // while the first chunks are on their way: the new entries are stored for later calls (this one reads them from where
-    // they are), and sequences without a visible entry, which have no chunk, get their zeros
-    if (A.kn)
+    // A new entry is stored for later calls by the warp that works on it.  One that its query does not see (entries without
+    // positions, and a query position given that lies before the entry or a window behind it) is stored here.
+    if (A.kn && A.q_pos && !A.kv.pos)
         for (int r = blockIdx.x; r < A.kv.B * A.kv.H; r += gridDim.x) {
-            const int b = r / A.kv.H, h = r % A.kv.H, n = si_kv_len(A.kv, b, nullptr);
-            if (n >= A.kv.cap) continue;
-            const long long to = A.kv.row(b, h, n), from = b * A.new_ss + (long long)h * D;
+            const int b = r / A.kv.H, h = r % A.kv.H;
+            const SeqWork w = seq_work<D>(A, b, nullptr);
+            if (w.n_old == INT_MAX || si_visible(w.n_old, w.s, w.lo, A.n_sink)) continue;
+            const long long to = A.kv.row(b, h, w.n_old), from = b * A.new_ss + (long long)h * D;
             if (tid < PIECES) *reinterpret_cast<uint4 *>(A.kv.k + to + tid * 8) = *reinterpret_cast<const uint4 *>(A.kn + from + tid * 8);
             else if (tid < 2 * PIECES) *reinterpret_cast<uint4 *>(A.kv.v + to + (tid - PIECES) * 8) = *reinterpret_cast<const uint4 *>(A.vn + from + (tid - PIECES) * 8);
-            else if (tid == 2 * PIECES && A.kv.pos) A.kv.pos[A.kv.meta(b, h) + n] = A.q_pos[b];
         }
-
+    // sequences without a visible entry have no chunk: their rows are zero
     if (run.empty)
         for (int b = blockIdx.x; b < A.kv.B; b += gridDim.x) {
             if (seq_work<D>(A, b, nullptr).nc) continue;
@@ -298,6 +298,14 @@ __global__ void __launch_bounds__(kThreads, 1) decode_kernel(const DecodeArgs A)
                 for (int i = lane; i < CH * PIECES; i += 32)
                     if (!(vis >> (i / PIECES) & 1)) *reinterpret_cast<uint4 *>(ring + stage * C::kStage + 4096 + i * 16) = make_uint4(0, 0, 0, 0);
                 __syncwarp();
+            }
+            if (w.n_old - j0 < CH && w.n_old >= j0 && gb == 0 && (vis >> (w.n_old - j0) & 1)) {       // the new entry, out of the stage
+                const int r = w.n_old - j0, piece = lane % PIECES, at = r * (D * 2) + ((piece & 8) << 4) + (((piece ^ r) & 7) << 4);
+                const char *st = ring + stage * C::kStage + at;
+                const long long to = A.kv.row(cons.b, h, w.n_old) + piece * 8;
+                if (lane < PIECES) *reinterpret_cast<uint4 *>(A.kv.k + to) = *reinterpret_cast<const uint4 *>(st);
+                if (lane >= 32 - PIECES) *reinterpret_cast<uint4 *>(A.kv.v + to) = *reinterpret_cast<const uint4 *>(st + 4096);
+                if (A.kv.pos && lane == 0) A.kv.pos[A.kv.meta(cons.b, h) + w.n_old] = w.s;
             }
             float x[SUB][NT][4] = {};
 #pragma unroll

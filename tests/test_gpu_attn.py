@@ -184,6 +184,23 @@ def test_decode_ignores_what_hidden_entries_hold(api):
         au.check_lse(lse[:, None], ref, D)
 
 
+def test_new_entries_that_their_query_does_not_see_are_stored_all_the_same(api):
+    """Entries without positions and a query position of the caller's: before the entry, far behind it (a window between), at it."""
+    lens, at, window, D = [100, 100, 100, 50], [40, 300, 100, 49], 64, 128
+    q, k, v, length = au.make(4, 4, 2, D, 120, "bf16", "nhd", 1, 12, lens)
+    kn, vn = (torch.randn(4, 2, D, device="cuda").to(q.dtype) for _ in range(2))
+    q_pos = torch.tensor(at, dtype=torch.int32, device="cuda")
+    cache = api.KVCache(k, v, length)
+    out = torch.empty(4, 4, D, dtype=q.dtype, device="cuda")
+    lse = torch.empty(4, 4, dtype=torch.float32, device="cuda")
+    api.si_attn_decode(cache, q[:, 0], q_pos, kn, vn, window, 0, 0.1, out, lse, 0, cache.workspace(4, 1))
+    for b, n in enumerate(lens):
+        assert torch.equal(k[b, :, n], kn[b]) and torch.equal(v[b, :, n], vn[b])
+    ref = au.reference(q, k, v, [n + 1 for n in lens], window, 0, 0.1, np.broadcast_to(np.arange(120), (4, 2, 120)), at)
+    au.check_out(out[:, None], ref, "bf16", D)
+    au.check_lse(lse[:, None], ref, D)
+
+
 def test_decode_equals_prefill_of_one_token_and_is_repeatable(api):
     q, k, v, length = au.make(3, 16, 4, 128, 1300, "f16", "nhd", 1, 9, [1300, 64, 801])
     cache = api.KVCache(k, v, length)

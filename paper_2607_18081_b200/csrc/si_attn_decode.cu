@@ -21,8 +21,13 @@
 
 namespace {
 
-constexpr int kWarps = 8, kThreads = kWarps * 32;
+// Two CTAs of four warps per SM rather than one of eight: while one joins its warps' sums at the end of a sequence the other
+// streams (batch of 32 ragged caches with weights 106 -> 105 us, 24 evicted caches of 2000 21.2 -> 19.7).  More runs than CTAs
+// that are resident (3 or 4 per SM) even out the SMs' shares of the bandwidth, but cost as much in starts and parts.
+constexpr int kWarps = 4, kThreads = kWarps * 32, kPerSm = 2;
+constexpr int kJoinWarps = 8, kJoinThreads = kJoinWarps * 32;
 constexpr int kStages = 3;
+constexpr int kMaxParts = 608;             // CTAs of the main kernel at most
 constexpr int kSecondSlot = 1 << 30;       // in the table of runs: the item's first part is in the second slot of its CTA
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLazy = 8.f;               // the running maximum moves only when a score exceeds it by 2^8: p stays below 2^8, exact to fp32 all the same
@@ -172,7 +177,7 @@ template <int D, int NT> __device__ __forceinline__ void load_q(const DecodeArgs
 }
 
 template <int DT, int D, int NT>
-__global__ void __launch_bounds__(kThreads, 1) decode_kernel(const DecodeArgs A) {
+__global__ void __launch_bounds__(kThreads, kPerSm) decode_kernel(const DecodeArgs A) {
     using C = Cfg<D, NT>;
     constexpr int CH = C::CH, HB = 8 * NT, PIECES = D / 8, SUB = CH / 16;
     extern __shared__ __align__(128) char smem[];
@@ -427,7 +432,7 @@ __global__ void __launch_bounds__(kThreads, 1) decode_kernel(const DecodeArgs A)
         float *pml = A.part_ml + ((long long)blockIdx.x * 2 + (first_segment ? 0 : 1)) * HB * 2;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            // eight heads at a time: the upper four warps through the buffer to the lower four, those to the threads that finish
+            // eight heads at a time: the upper half of the warps through the buffer to the lower half, those to the threads that finish
             float f[2];
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
@@ -437,19 +442,19 @@ __global__ void __launch_bounds__(kThreads, 1) decode_kernel(const DecodeArgs A)
                 for (int v = 0; v < kWarps; ++v) top = fmaxf(top, ml[(v * HB + head) * 2]);
                 f[c] = m[nt][c] == -INFINITY ? 0.f : ex2(m[nt][c] - top);
             }
-            float *mine = merge_o + (warp & 3) * C::kMerge + 2 * (lane & 3) * C::kRow + (lane >> 2);
+            float *mine = merge_o + (warp % (kWarps / 2)) * C::kMerge + 2 * (lane & 3) * C::kRow + (lane >> 2);
 #pragma unroll
             for (int s = 0; s < D / 16; ++s)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[nt][s][e] *= f[e & 1];
-            if (warp >= 4) {
+            if (warp >= kWarps / 2) {
 #pragma unroll
                 for (int s = 0; s < D / 16; ++s)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) mine[(e & 1) * C::kRow + s * 16 + (e >> 1) * 8] = o[nt][s][e];
             }
             __syncthreads();
-            if (warp < 4) {
+            if (warp < kWarps / 2) {
 #pragma unroll
                 for (int s = 0; s < D / 16; ++s)
 #pragma unroll
@@ -498,13 +503,12 @@ __global__ void __launch_bounds__(kThreads, 1) decode_kernel(const DecodeArgs A)
 // and range of U * 256 keys; the first range's writes the output.  A chain of short dependent loads: everything that does not
 // depend on another load is asked for first (scores and weights beyond the length too: the memory is there, the values are
 // not used).  At most 80 registers, so that the CTAs become resident beside the main kernel's and wait there for its end.
-constexpr int kMaxParts = 256;             // CTAs of the main kernel at most
 template <int DT, int D, int NT, int U>
-__global__ void __launch_bounds__(kThreads, 3) decode_join_kernel(const DecodeArgs A) {
+__global__ void __launch_bounds__(kJoinThreads, 3) decode_join_kernel(const DecodeArgs A) {
     constexpr int HB = 8 * NT, CH = 2048 / D;
     __shared__ float sh_f[HB][kMaxParts];
     __shared__ float2 sh_done[128];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, h = blockIdx.y, b = blockIdx.z, j0 = blockIdx.x * (U * kThreads);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, h = blockIdx.y, b = blockIdx.z, j0 = blockIdx.x * (U * kJoinThreads);
     si_tc::pdl_wait();
     si_tc::pdl_launch();
     float *weight = A.kv.weight + A.kv.meta(b, h);
@@ -514,7 +518,7 @@ __global__ void __launch_bounds__(kThreads, 3) decode_join_kernel(const DecodeAr
     if (A.acc) {
 #pragma unroll
         for (int i = 0; i < U; ++i) {
-            const int j = j0 + i * kThreads + tid;
+            const int j = j0 + i * kJoinThreads + tid;
             if (j >= A.kv.cap) continue;
             old[i] = weight[j];
 #pragma unroll
@@ -536,25 +540,24 @@ __global__ void __launch_bounds__(kThreads, 3) decode_join_kernel(const DecodeAr
         const int parts = run.y - run.x + 1;
         auto slot = [&](int i) { return (long long)(run.x + i) * 2 + (i > 0 ? 0 : first_slot); };     // later CTAs begin with the item
         __syncthreads();
-        for (int head = warp; head < heads; head += kWarps) {      // a warp per head, a lane per part: one round of loads
-            float2 ml[kMaxParts / 32];
+        for (int head = warp; head < heads; head += kJoinWarps) {      // a warp per head, a lane per part: one round of loads
+            float2 ml[4];                              // the first 128 parts stay in registers
             float top = -INFINITY, sum = 0.f;
+            auto part = [&](int i) { return i < parts ? *reinterpret_cast<const float2 *>(A.part_ml + (slot(i) * HB + head) * 2) : make_float2(-INFINITY, 0.f); };
 #pragma unroll
-            for (int k = 0; k < kMaxParts / 32; ++k) {
-                const int i = k * 32 + lane;
-                ml[k] = i < parts ? *reinterpret_cast<const float2 *>(A.part_ml + (slot(i) * HB + head) * 2) : make_float2(-INFINITY, 0.f);
-                top = fmaxf(top, ml[k].x);
-            }
+            for (int k = 0; k < 4; ++k) { ml[k] = part(k * 32 + lane); top = fmaxf(top, ml[k].x); }
+            for (int i = 128 + lane; i < parts; i += 32) top = fmaxf(top, part(i).x);
 #pragma unroll
             for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-#pragma unroll
-            for (int k = 0; k < kMaxParts / 32; ++k) {
-                const int i = k * 32 + lane;
-                if (i >= parts) continue;
-                const float f = ml[k].x == -INFINITY ? 0.f : ex2(ml[k].x - top);
+            auto add = [&](int i, float2 v) {
+                if (i >= parts) return;
+                const float f = v.x == -INFINITY ? 0.f : ex2(v.x - top);
                 sh_f[head][i] = f;
-                sum += ml[k].y * f;
-            }
+                sum += v.y * f;
+            };
+#pragma unroll
+            for (int k = 0; k < 4; ++k) add(k * 32 + lane, ml[k]);
+            for (int i = 128 + lane; i < parts; i += 32) add(i, part(i));
 #pragma unroll
             for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
             if (lane == 0) {
@@ -564,7 +567,7 @@ __global__ void __launch_bounds__(kThreads, 3) decode_join_kernel(const DecodeAr
         }
         __syncthreads();
         if (blockIdx.x == 0)
-            for (int i = tid; i < heads * (D / 2); i += kThreads) {
+            for (int i = tid; i < heads * (D / 2); i += kJoinThreads) {
                 const int head = i / (D / 2), d = i % (D / 2) * 2;
                 float2 acc = make_float2(0.f, 0.f);
 #pragma unroll 8
@@ -579,7 +582,7 @@ __global__ void __launch_bounds__(kThreads, 3) decode_join_kernel(const DecodeAr
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-        const int j = j0 + i * kThreads + tid, c = j / CH;
+        const int j = j0 + i * kJoinThreads + tid, c = j / CH;
         if (j >= w.n) continue;
         if (!(c < w.c_sink || (c >= w.c_win && c < w.c_win + w.nc - w.c_sink))) { if (j == w.n_old) weight[j] = 0.f; continue; }
         float sum = 0.f;
@@ -600,7 +603,7 @@ __global__ void __launch_bounds__(kThreads, 3) decode_join_kernel(const DecodeAr
 struct Layout { int n_cta, NT, GB, GS; size_t o, ml, done, scores, runs, total; };
 Layout layout_of(const si_kv_t *kv, int n_q_heads, bool acc) {
     Layout L;
-    L.n_cta = si_sm_count() < kMaxParts ? si_sm_count() : kMaxParts;
+    L.n_cta = kPerSm * si_sm_count() < kMaxParts ? kPerSm * si_sm_count() : kMaxParts;
     const int G = n_q_heads / kv->n_kv_heads;
     L.NT = G <= 8 ? 1 : 2;
     L.GB = (G + 8 * L.NT - 1) / (8 * L.NT);
@@ -635,9 +638,10 @@ template <int DT, int D, int NT> int launch(const DecodeArgs &A, cudaStream_t st
     // ranges of 256 keys while all their CTAs are resident at once (three per SM), else of 1024: the start of a CTA costs more
     // than its keys (24 x 2 rows of 2112: 20.7 against 22.6 us a call; 32 x 8 rows of 8192: 130 against 116)
     const long long items = (long long)A.kv.H * A.kv.B;
-    const bool few = items * ((A.kv.cap + kThreads - 1) / kThreads) <= 3ll * A.n_cta;
-    const int keys = few ? kThreads : (NT == 1 ? 4 : 2) * kThreads;
+    const bool few = items * ((A.kv.cap + kJoinThreads - 1) / kJoinThreads) <= 3ll * si_sm_count();
+    const int keys = few ? kJoinThreads : (NT == 1 ? 4 : 2) * kJoinThreads;
     cfg.gridDim = dim3(A.acc ? (A.kv.cap + keys - 1) / keys : 1, A.kv.H, A.kv.B);
+    cfg.blockDim = dim3(kJoinThreads);
     cfg.dynamicSmemBytes = 0;
     if (few) SI_CUDA_TRY(cudaLaunchKernelEx(&cfg, decode_join_kernel<DT, D, NT, 1>, A));
     else SI_CUDA_TRY(cudaLaunchKernelEx(&cfg, decode_join_kernel<DT, D, NT, NT == 1 ? 4 : 2>, A));

@@ -20,6 +20,7 @@ constexpr int kBins = 2048;
 constexpr int kMaxCluster = 8;
 constexpr int kSliceKeys = 48 * 1024;        // keys of a slice in shared memory; longer rows read their weights again instead
 constexpr int kFewMoves = 256;               // in place with at most this many entries over the budget: one kernel
+constexpr int kFewOver = 4;                  // at most this many entries over the budget are looked for one by one
 constexpr int kMoveRows = 8;                 // rows in flight per warp of the moving kernel
 
 struct EvictArgs {
@@ -29,6 +30,7 @@ struct EvictArgs {
     int slots;                           // slots that `source` describes: the budget, at most the capacity if it is scratch
     int32_t *source, *lists;             // [rows][slots]: source slot of every slot (the caller's `kept` or scratch); [rows][cap + 2]:
                                          // freed slots, then (from cap / 2 + 1) the entries that fill them, at most cap / 2 each
+    int list_source;                     // 0: nobody reads `source` (moves of this kernel only, no `kept`)
     int32_t *len_out;
     int32_t *status;
 };
@@ -93,7 +95,8 @@ __global__ void __launch_bounds__(kRowThreads, 2) evict_select_kernel(const Evic
     if (A.move_here && A.len_out && h == 0 && rank == 0 && tid == 0) A.len_out[b] = min(n, budget);
     si_tc::pdl_launch();
     if (n <= budget) {                                       // the whole cluster alike
-        for (int j = rank * kRowThreads + tid; j < A.slots; j += C * kRowThreads) source[j] = j < n ? j : -1;
+        if (A.list_source)
+            for (int j = rank * kRowThreads + tid; j < A.slots; j += C * kRowThreads) source[j] = j < n ? j : -1;
         return;
     }
     const float *w = A.src.weight + A.src.meta(b, h);
@@ -120,79 +123,143 @@ __global__ void __launch_bounds__(kRowThreads, 2) evict_select_kernel(const Evic
         }
     }
     auto key = [&](int j) -> uint32_t { return SMEM ? keys[j - s0] : key_of(pos ? pos[j] : j, w[j]); };
-    for (int i = tid; i < 3 * kBins; i += kRowThreads) hist[0][i] = 0;
-    __syncthreads();
     auto sync = [&]() { if (C > 1) si_tc::cluster_sync_all(); else __syncthreads(); };
-    // radix select of the budget-th largest key
-    uint32_t prefix = 0, mask = 0;
-    int need = budget;
+    auto list_stayers = [&]() {                              // freed slots are overwritten later
+        if (A.list_source) for (int j = s0 + tid; j < min(s1, budget); j += kRowThreads) source[j] = j;
+    };
+    int moves;
+    if (SMEM && C == 1 && n - budget <= kFewOver) {
+        // A decode step: the few that go are found one after the other, each by one maximum over the block -- the lowest key,
+        // of equal ones the highest slot (16 x 8 rows of 2049 entries: 4.8 us a step, 9.3 by histograms).
+        list_stayers();
+        unsigned long long out = 0;                          // this thread's slots that go, a bit per round of kRowThreads
+        int gone[kFewOver];
 #pragma unroll
-    for (int pass = 0; pass < 3; ++pass) {
-        constexpr int shifts[3] = {21, 10, 0}, bits[3] = {11, 11, 10};
-        for (int j = s0 + tid; j < s1; j += kRowThreads) {
-            const uint32_t k = key(j);
-            if ((k & mask) == prefix) atomicAdd(&hist[pass][(k >> shifts[pass]) & ((1u << bits[pass]) - 1)], 1u);
+        for (int r = 0; r < kFewOver; ++r) {
+            gone[r] = INT_MAX;
+            if (r >= n - budget) continue;
+            unsigned long long best = 0;
+            for (int j = tid, i = 0; j < n; j += kRowThreads, ++i)
+                if (!(out >> i & 1)) {
+                    const unsigned long long v = (unsigned long long)~keys[j] << 32 | (unsigned int)j + 1;
+                    best = v > best ? v : best;
+                }
+#pragma unroll
+            for (int o = 16; o; o >>= 1) {
+                const unsigned long long v = __shfl_xor_sync(0xFFFFFFFFu, best, o);
+                best = v > best ? v : best;
+            }
+            __syncthreads();
+            if ((tid & 31) == 0) tot[tid >> 5] = best;
+            __syncthreads();
+            best = tot[tid & 31];
+#pragma unroll
+            for (int o = 16; o; o >>= 1) {
+                const unsigned long long v = __shfl_xor_sync(0xFFFFFFFFu, best, o);
+                best = v > best ? v : best;
+            }
+            gone[r] = (int)(unsigned int)best - 1;
+            if (gone[r] % kRowThreads == tid) out |= 1ull << (gone[r] / kRowThreads);
         }
-        sync();
-        // bins from the top down: two per thread
-        const int hi = kBins - 1 - 2 * tid;
-        unsigned int c0 = 0, c1 = 0;
-        if (C == 1) { c0 = hist[pass][hi]; c1 = hist[pass][hi - 1]; }
-        else for (int r = 0; r < C; ++r) { c0 += ld_cluster(&hist[pass][hi], r); c1 += ld_cluster(&hist[pass][hi - 1], r); }
-        const int before = (int)block_scan(c0 + c1, tot, &total);
-        if (before < need && before + (int)c0 >= need) { sh_prefix = prefix | ((uint32_t)hi << shifts[pass]); sh_need = need - before; }
-        else if (before + (int)c0 < need && before + (int)(c0 + c1) >= need) { sh_prefix = prefix | ((uint32_t)(hi - 1) << shifts[pass]); sh_need = need - before - (int)c0; }
+        // freed slots in ascending order, and the entries beyond the budget that stay
+        moves = 0;
+        if (tid == 0) {
+            int m = budget;
+            while (true) {
+                int next = INT_MAX;
+#pragma unroll
+                for (int r = 0; r < kFewOver; ++r)
+                    if (gone[r] < budget && gone[r] < next && (moves == 0 || gone[r] > freed_slots[moves - 1])) next = gone[r];
+                if (next == INT_MAX) break;
+                while (true) {
+                    bool is_gone = false;
+#pragma unroll
+                    for (int r = 0; r < kFewOver; ++r) is_gone |= gone[r] == m;
+                    if (!is_gone) break;
+                    ++m;
+                }
+                freed_slots[moves] = next;
+                movers[moves++] = m++;
+            }
+            sh_need = moves;
+        }
         __syncthreads();
-        prefix = sh_prefix; need = sh_need;
-        mask |= ((1u << bits[pass]) - 1) << shifts[pass];
-    }
-    // Ordered counts.  A thread has `per` neighbouring slots (an odd number: no bank conflicts; at most 63, so that a mask of
-    // them is one register pair) of every round; slices in shared memory are one round, longer ones (one CTA) as many as it takes.
-    const int per = min((s1 - s0 + kRowThreads - 1) / kRowThreads | 1, 63), rounds = (s1 - s0 + per * kRowThreads - 1) / (per * kRowThreads);
-    auto before_me = [&](int which, unsigned int mine) {     // the sum of `mine` over the CTAs in front
-        if (C == 1) return 0u;
-        if (tid == 0) share[which] = mine;
-        sync();
-        unsigned int s = 0;
-        for (int r = 0; r < rank; ++r) s += ld_cluster(&share[which], r);
-        return s;
-    };
-    for (int j = s0 + tid; j < min(s1, budget); j += kRowThreads) source[j] = j;      // freed slots are overwritten below
-    int ties = 0, freed = 0, moved = 0;                      // so far in this row
-    // the slots of round r that are kept, ties to the lower ones; `below`: those of them under the budget
-    auto kept_of = [&](int r, int &j0, unsigned long long &valid, unsigned long long &below) {
-        j0 = s0 + r * per * kRowThreads + tid * per;
-        const int cnt = max(0, min(per, s1 - j0)), low = max(0, min(cnt, budget - j0));
-        valid = (1ull << cnt) - 1; below = (1ull << low) - 1;
-        unsigned long long keep = 0, tie = 0;
-        for (int i = 0; i < cnt; ++i) {
-            const uint32_t k = key(j0 + i);
-            keep |= (unsigned long long)(k > prefix) << i;
-            tie |= (unsigned long long)(k == prefix) << i;
+        moves = sh_need;
+    } else {
+        for (int i = tid; i < 3 * kBins; i += kRowThreads) hist[0][i] = 0;
+        __syncthreads();
+        // radix select of the budget-th largest key
+        uint32_t prefix = 0, mask = 0;
+        int need = budget;
+#pragma unroll
+        for (int pass = 0; pass < 3; ++pass) {
+            constexpr int shifts[3] = {21, 10, 0}, bits[3] = {11, 11, 10};
+            for (int j = s0 + tid; j < s1; j += kRowThreads) {
+                const uint32_t k = key(j);
+                if ((k & mask) == prefix) atomicAdd(&hist[pass][(k >> shifts[pass]) & ((1u << bits[pass]) - 1)], 1u);
+            }
+            sync();
+            // bins from the top down: two per thread
+            const int hi = kBins - 1 - 2 * tid;
+            unsigned int c0 = 0, c1 = 0;
+            if (C == 1) { c0 = hist[pass][hi]; c1 = hist[pass][hi - 1]; }
+            else for (int r = 0; r < C; ++r) { c0 += ld_cluster(&hist[pass][hi], r); c1 += ld_cluster(&hist[pass][hi - 1], r); }
+            const int before = (int)block_scan(c0 + c1, tot, &total);
+            if (before < need && before + (int)c0 >= need) { sh_prefix = prefix | ((uint32_t)hi << shifts[pass]); sh_need = need - before; }
+            else if (before + (int)c0 < need && before + (int)(c0 + c1) >= need) { sh_prefix = prefix | ((uint32_t)(hi - 1) << shifts[pass]); sh_need = need - before - (int)c0; }
+            __syncthreads();
+            prefix = sh_prefix; need = sh_need;
+            mask |= ((1u << bits[pass]) - 1) << shifts[pass];
         }
-        int t = ties + (int)block_scan((unsigned long long)__popcll(tie), tot, &total);
-        const int all = (int)total;
-        if (r == 0) { const int ahead = (int)before_me(0, all); t += ahead; ties += ahead; }
-        ties += all;
-        for (; tie && t < need; ++t) { keep |= tie & (0ull - tie); tie &= tie - 1; }
-        return keep;
-    };
-    for (int r = 0; r < rounds; ++r) {
-        int j0;
-        unsigned long long valid, below;
-        const unsigned long long keep = kept_of(r, j0, valid, below), gone = valid & below & ~keep, far = keep & ~below;
-        const unsigned long long at = block_scan((unsigned long long)__popcll(gone) << 32 | (unsigned long long)__popcll(far), tot, &total);
-        const unsigned long long all = total;
-        if (r == 0) { freed += (int)before_me(1, (unsigned int)(all >> 32)); moved += (int)before_me(2, (unsigned int)all); }
-        int f = freed + (int)(at >> 32), m = moved + (int)(at & 0xFFFFFFFFu);
-        for (unsigned long long g = gone; g; g &= g - 1) freed_slots[f++] = j0 + __ffsll(g) - 1;
-        for (unsigned long long g = far; g; g &= g - 1) movers[m++] = j0 + __ffsll(g) - 1;
-        freed += (int)(all >> 32); moved += (int)(all & 0xFFFFFFFFu);
+        // Ordered counts.  A thread has `per` neighbouring slots (an odd number: no bank conflicts; at most 63, so that a mask of
+        // them is one register pair) of every round; slices in shared memory are one round, longer ones (one CTA) as many as it takes.
+        const int per = min((s1 - s0 + kRowThreads - 1) / kRowThreads | 1, 63), rounds = (s1 - s0 + per * kRowThreads - 1) / (per * kRowThreads);
+        auto before_me = [&](int which, unsigned int mine) {     // the sum of `mine` over the CTAs in front
+            if (C == 1) return 0u;
+            if (tid == 0) share[which] = mine;
+            sync();
+            unsigned int s = 0;
+            for (int r = 0; r < rank; ++r) s += ld_cluster(&share[which], r);
+            return s;
+        };
+        list_stayers();
+        int ties = 0, freed = 0, moved = 0;                      // so far in this row
+        // the slots of round r that are kept, ties to the lower ones; `below`: those of them under the budget
+        auto kept_of = [&](int r, int &j0, unsigned long long &valid, unsigned long long &below) {
+            j0 = s0 + r * per * kRowThreads + tid * per;
+            const int cnt = max(0, min(per, s1 - j0)), low = max(0, min(cnt, budget - j0));
+            valid = (1ull << cnt) - 1; below = (1ull << low) - 1;
+            unsigned long long keep = 0, tie = 0;
+            for (int i = 0; i < cnt; ++i) {
+                const uint32_t k = key(j0 + i);
+                keep |= (unsigned long long)(k > prefix) << i;
+                tie |= (unsigned long long)(k == prefix) << i;
+            }
+            int t = ties + (int)block_scan((unsigned long long)__popcll(tie), tot, &total);
+            const int all = (int)total;
+            if (r == 0) { const int ahead = (int)before_me(0, all); t += ahead; ties += ahead; }
+            ties += all;
+            for (; tie && t < need; ++t) { keep |= tie & (0ull - tie); tie &= tie - 1; }
+            return keep;
+        };
+        for (int r = 0; r < rounds; ++r) {
+            int j0;
+            unsigned long long valid, below;
+            const unsigned long long keep = kept_of(r, j0, valid, below), gone = valid & below & ~keep, far = keep & ~below;
+            const unsigned long long at = block_scan((unsigned long long)__popcll(gone) << 32 | (unsigned long long)__popcll(far), tot, &total);
+            const unsigned long long all = total;
+            if (r == 0) { freed += (int)before_me(1, (unsigned int)(all >> 32)); moved += (int)before_me(2, (unsigned int)all); }
+            int f = freed + (int)(at >> 32), m = moved + (int)(at & 0xFFFFFFFFu);
+            for (unsigned long long g = gone; g; g &= g - 1) freed_slots[f++] = j0 + __ffsll(g) - 1;
+            for (unsigned long long g = far; g; g &= g - 1) movers[m++] = j0 + __ffsll(g) - 1;
+            freed += (int)(all >> 32); moved += (int)(all & 0xFFFFFFFFu);
+        }
+        sync();                                                   // the lists are complete (global writes included); keys and weights are no longer read
+        moves = freed;
+        if (C > 1) { moves = 0; for (int r = 0; r < C; ++r) moves += (int)ld_cluster(&share[1], r); }
     }
-    sync();                                                   // the lists are complete (global writes included); keys and weights are no longer read
-    int moves = freed;
-    if (C > 1) { moves = 0; for (int r = 0; r < C; ++r) moves += (int)ld_cluster(&share[1], r); }
-    for (int i = rank * kRowThreads + tid; i < moves; i += C * kRowThreads) source[freed_slots[i]] = movers[i];
+    if (A.list_source)
+        for (int i = rank * kRowThreads + tid; i < moves; i += C * kRowThreads) source[freed_slots[i]] = movers[i];
     if (A.move_here) {
         const int lanes = A.src.D / 4, groups = kRowThreads / lanes, lane = tid % lanes;
         const bool is_v = lane >= lanes / 2;
@@ -345,7 +412,8 @@ extern "C" int si_kv_evict(const si_kv_t *src, const si_kv_t *dst, const int32_t
     const size_t rows = (size_t)src->n_seqs * src->n_kv_heads;
     EvictArgs A{si_kv_view_of(src), si_kv_view_of(dst), q_pos, n_new, budget, n_sink, n_recent, in_place,
                 in_place && src->capacity - budget <= kFewMoves, kept || budget < src->capacity ? budget : src->capacity, kept ? kept : (int32_t *)workspace,
-                (int32_t *)((char *)workspace + si_align_up(rows * src->capacity * 4, 256)), len_out, status_dev};
+                (int32_t *)((char *)workspace + si_align_up(rows * src->capacity * 4, 256)), 0, len_out, status_dev};
+    A.list_source = kept || !A.move_here;
     const cudaStream_t st = (cudaStream_t)stream;
     const bool len_after = A.move_here && len_out == src->len;  // the rows of a sequence still read the old length
     if (len_after) A.len_out = nullptr;

@@ -458,9 +458,11 @@ int si_kv_workspace_bytes(const si_kv_t *kv, int n_q_heads, int T, size_t *bytes
 /* Prefill: the queries of the LAST T positions of every sequence (their keys and values are already in the cache;
  * query i of sequence b is at position len[b] - T + i; a negative one -- a sequence shorter than T -- sees nothing).
  *   q       device [n_seqs, T, n_q_heads, head_dim]; sequences and tokens q_seq_stride / q_tok_stride elements apart
- *           (multiples of 8), the heads of a token contiguous: a slice of a fused projection's output is fine
+ *           (multiples of 8; tokens not 0 apart, SI_ERR_UNSUPPORTED), the heads of a token contiguous: a slice of a fused
+ *           projection's output is fine
  *   out     device [n_seqs, T, n_q_heads, head_dim], contiguous
  *   lse     device float32 [n_seqs, T, n_q_heads], or NULL
+ *   workspace  si_kv_workspace_bytes (with few queries the keys are split over the SMs and the parts joined)
  * Needs kv->pos == NULL (SI_ERR_UNSUPPORTED otherwise: a prompt is prefilled before anything is evicted).  A value
  * that is infinite or NaN below len[b] may reach every query processed with it, also ones it is hidden from. */
 int si_attn_prefill(const si_kv_t *kv, const void *q, long long q_seq_stride, long long q_tok_stride, int T,

@@ -620,11 +620,9 @@ Layout layout_of(const si_kv_t *kv, int n_q_heads, bool acc) {
 }
 
 template <int DT, int D, int NT> int launch(const DecodeArgs &A, cudaStream_t st) {
-    static std::atomic<int> ready{0};
-    if (!ready.load()) {
-        SI_CUDA_TRY(cudaFuncSetAttribute(decode_kernel<DT, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (Cfg<D, NT>::kSmem)));
-        ready.store(1);
-    }
+    static std::atomic<unsigned long long> allowed{0};
+    const int rc = si_allow_smem(decode_kernel<DT, D, NT>, (Cfg<D, NT>::kSmem), allowed);
+    if (rc) return rc;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute at;
     at.id = cudaLaunchAttributeProgrammaticStreamSerialization;

@@ -435,11 +435,9 @@ size_t parts_ml_bytes(const Plan &p) { return p.splits > 1 ? si_align_up((size_t
 
 struct Call { const CUtensorMap &qm, &km, &vm, &om; const TcArgs &A; const SplitArgs &P; cudaStream_t st; };
 template <int DT, int D, bool NEG> int launch(const Call &c) {
-    static std::atomic<int> ready{0};
-    if (!ready.load()) {
-        SI_CUDA_TRY(cudaFuncSetAttribute(prefill_kernel<DT, D, NEG>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D>::kSmem));
-        ready.store(1);
-    }
+    static std::atomic<unsigned long long> allowed{0};
+    const int rc = si_allow_smem(prefill_kernel<DT, D, NEG>, Cfg<D>::kSmem, allowed);
+    if (rc) return rc;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute at;
     at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -475,7 +473,7 @@ extern "C" int si_attn_prefill(const si_kv_t *kv, const void *q, long long q_seq
     if (T < 0) return SI_ERR_INVALID_ARG;
     if (kv->n_seqs == 0 || T == 0) return SI_OK;
     if (!q || !out || q_seq_stride < 0 || q_tok_stride < 0) return SI_ERR_INVALID_ARG;
-    if (kv->pos) return SI_ERR_UNSUPPORTED;
+    if (kv->pos || (q_tok_stride == 0 && T > 1)) return SI_ERR_UNSUPPORTED;     // tensor copies have no zero stride
     if (!si_aligned16(q) || !si_aligned16(out) || ((q_seq_stride | q_tok_stride) & 7)) return SI_ERR_ALIGNMENT;
     const Plan p = plan_of(kv, n_q_heads, T, window, n_sink);
     if (p.blocks > INT_MAX) return SI_ERR_TOO_LARGE;

@@ -352,11 +352,9 @@ Layout layout_of(const si_kv_t *kv) {
 
 struct Call { const CUtensorMap &qm, &km; const TcArgs &A; const WeightArgs &W; cudaStream_t st; };
 template <int DT, int D, bool NEG> int launch(const Call &c) {
-    static std::atomic<int> ready{0};
-    if (!ready.load()) {
-        SI_CUDA_TRY(cudaFuncSetAttribute(weights_kernel<DT, D, NEG>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D>::kSmem));
-        ready.store(1);
-    }
+    static std::atomic<unsigned long long> allowed{0};
+    const int rc = si_allow_smem(weights_kernel<DT, D, NEG>, Cfg<D>::kSmem, allowed);
+    if (rc) return rc;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute at;
     at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -387,7 +385,7 @@ extern "C" int si_attn_weights(const si_kv_t *kv, const void *q, long long q_seq
     if (T < 0) return SI_ERR_INVALID_ARG;
     if (kv->n_seqs == 0 || T == 0) return SI_OK;
     if (!q || !lse || !kv->weight || q_seq_stride < 0 || q_tok_stride < 0) return SI_ERR_INVALID_ARG;
-    if (kv->pos) return SI_ERR_UNSUPPORTED;
+    if (kv->pos || (q_tok_stride == 0 && T > 1)) return SI_ERR_UNSUPPORTED;     // tensor copies have no zero stride
     if (!si_aligned16(q) || ((q_seq_stride | q_tok_stride) & 7)) return SI_ERR_ALIGNMENT;
     const Layout L = layout_of(kv);
     const TcArgs A = tc_args(kv, q_seq_stride, T, n_q_heads, window, n_sink, scale, nullptr, nullptr, status_dev);

@@ -342,11 +342,9 @@ int cluster_size(const si_kv_t *kv) {
 
 template <bool SMEM> int launch_select(const EvictArgs &A, int C, size_t smem, cudaStream_t st) {
     if (smem > 0) {
-        static std::atomic<int> ready{0};
-        if (!ready.load()) {
-            SI_CUDA_TRY(cudaFuncSetAttribute(evict_select_kernel<SMEM>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSliceKeys * 4));
-            ready.store(1);
-        }
+        static std::atomic<unsigned long long> allowed{0};
+        const int rc = si_allow_smem(evict_select_kernel<SMEM>, kSliceKeys * 4, allowed);
+        if (rc) return rc;
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(C, A.src.H, A.src.B);
@@ -399,7 +397,7 @@ extern "C" int si_kv_evict(const si_kv_t *src, const si_kv_t *dst, const int32_t
     int rc = si_kv_check(src);
     if (rc) return rc;
     if ((rc = si_kv_check(dst))) return rc;
-    if (budget < 1 || n_new < 0 || n_sink < 0 || n_recent < 0 || (long long)n_sink + n_recent > budget || budget > dst->capacity) return SI_ERR_INVALID_ARG;
+    if (budget < 1 || n_new < 0 || n_new > src->capacity || n_sink < 0 || n_recent < 0 || (long long)n_sink + n_recent > budget || budget > dst->capacity) return SI_ERR_INVALID_ARG;
     if (src->n_seqs != dst->n_seqs || src->n_kv_heads != dst->n_kv_heads || src->head_dim != dst->head_dim || src->dtype != dst->dtype) return SI_ERR_INVALID_ARG;
     if (src->n_seqs == 0) return SI_OK;
     const bool in_place = src->k == dst->k;

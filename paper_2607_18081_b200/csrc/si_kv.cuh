@@ -47,6 +47,18 @@ inline int si_attn_check(const si_kv_t *kv, int n_q_heads, int window, int n_sin
 // SMs of the current device when first asked (all devices of a machine are alike here)
 int si_sm_count();
 
+// Allows `kernel` that much dynamic shared memory, once per device (`done`: a bit per device).
+template <typename K> int si_allow_smem(K kernel, int bytes, std::atomic<unsigned long long> &done) {
+    int dev = 0;
+    SI_CUDA_TRY(cudaGetDevice(&dev));
+    const unsigned long long bit = 1ull << (dev & 63);
+    if (!(done.load() & bit)) {
+        SI_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+        done.fetch_or(bit);
+    }
+    return SI_OK;
+}
+
 // implemented in si_attn_decode.cu / si_attn_prefill.cu / si_attn_weights.cu
 size_t si_attn_decode_ws_bytes(const si_kv_t *kv, int n_q_heads);
 size_t si_attn_prefill_ws_bytes(const si_kv_t *kv, int n_q_heads, int T);

@@ -68,7 +68,7 @@ def test_bad_arguments_are_refused(api):
         assert call(api, kv, hq=8 * 129) == U and call(api, kv, q=None) == I and call(api, kv, q=FAKE + 2) == A and call(api, kv, ss=4100) == A
         assert call(api, kv, ss=-8) == I
     for call in (_prefill, _weights):
-        assert call(api, kv, T=-1) == I and call(api, kv, ts=12) == A and call(api, pos) == U
+        assert call(api, kv, T=-1) == I and call(api, kv, ts=12) == A and call(api, pos) == U and call(api, kv, ts=0) == U
         assert call(api, kv, T=0, q=None) == api.SI_OK and call(api, _kv(api, n_seqs=0, k=None, v=None, len=None)) == api.SI_OK
     assert _prefill(api, kv, out=None) == I and _prefill(api, kv, out=FAKE + 4) == A
     assert _weights(api, kv, lse=None) == I and _weights(api, _kv(api, weight=None)) == I
@@ -89,7 +89,7 @@ def test_bad_evictions_are_refused(api):
     I = api.SI_ERR_INVALID_ARG
     src, dst = _kv(api), _kv(api, k=FAKE * 8, v=FAKE * 9, pos=FAKE, weight=FAKE)
     pos = _kv(api, pos=FAKE)
-    for bad in (dict(budget=0), dict(budget=101), dict(n_new=-1), dict(n_sink=-1), dict(n_recent=-1), dict(n_sink=30, n_recent=21)):
+    for bad in (dict(budget=0), dict(budget=101), dict(n_new=-1), dict(n_new=101), dict(n_sink=-1), dict(n_recent=-1), dict(n_sink=30, n_recent=21)):
         assert _evict(api, src, dst, **bad) == I
     for change in (dict(n_seqs=1), dict(n_kv_heads=4), dict(head_dim=64), dict(dtype=api.SI_F16), dict(pos=None), dict(weight=None)):
         f = {n: getattr(dst, n) for n, _ in dst._fields_}

@@ -34,7 +34,7 @@ CASES = [
     ([100, 64, 65], 0, 128, 64, 4, 16),
     ([64, 64], 1, 70, 64, 4, 8),           # a decode step at the budget
     ([66, 67], 1, 70, 64, 4, 8),           # three and four over it
-    ([2050, 1026], 2, 2052, 2048, 2040, 8),  # only protected entries can go
+    ([2050, 1026], 2, 2052, 2048, 2040, 8),  # half of the entries are protected
     ([1030, 2049], 0, 2050, 1024, 1, 1000),
     ([5000], 0, 5001, 4999, 0, 1),
     ([3000, 777], 0, 3001, 100, 100, 0),   # only protected entries fit

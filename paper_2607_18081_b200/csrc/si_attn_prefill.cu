@@ -140,8 +140,8 @@ prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
                         if (j >= keys.n || !ok) break;
                         const int sv = 2 * u + 1, sk = (2 * u + 2) % NS;
                         const bool more = j + 1 < keys.n;
-                        ok = mbar_spin(&B->full[sv], round, kSpin);
-                        if (ok && more) ok = mbar_spin(&B->full[sk], u + 1 == kRound ? round ^ 1 : round, kSpin);
+                        ok = mbar_wait(&B->full[sv], round, kWait);
+                        if (ok && more) ok = mbar_wait(&B->full[sk], u + 1 == kRound ? round ^ 1 : round, kWait);
                         if (ok && tail && !more) {            // another warp clears what lies beyond the length
                             mbar_arrive(&B->dirty);
                             ok = mbar_wait(&B->clean, 0, kWait);
@@ -149,13 +149,13 @@ prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
 #pragma unroll
                         for (int t = 0; t < 2; ++t) {
                             if (t >= tiles || !ok) break;
-                            ok = mbar_spin(&B->p[t][0], j & 1, kSpin);       // the first half of P
+                            ok = mbar_wait(&B->p[t][0], j & 1, kWait);       // the first half of P
                             if (!ok) break;
                             tc_fence_after();
 #pragma unroll
                             for (int k = 0; k < 4; ++k)
                                 umma_ts(tmem + 256 + t * D, tmem + t * 128 + k * 8, v_desc, sv * (C::kBytes / 16) + k * 128, id_o, j > 0 || k > 0);
-                            ok = mbar_spin(&B->p[t][1], j & 1, kSpin);
+                            ok = mbar_wait(&B->p[t][1], j & 1, kWait);
                             if (!ok) break;
                             tc_fence_after();
 #pragma unroll
@@ -277,7 +277,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
                 l += s0 + s1;
             };
             for (int j = 0; j < keys.n; ++j) {
-                ok = __all_sync(0xFFFFFFFFu, mbar_spin(&B->s[t], j & 1, kSpin));
+                ok = __all_sync(0xFFFFFFFFu, mbar_wait(&B->s[t], j & 1, kWait));
                 if (!ok) break;
                 tc_fence_after();
                 const int key0 = keys.key0(j);

@@ -10,7 +10,9 @@ using namespace si_tc;
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kTile = 128;                 // rows of a query tile, keys of a key tile
-constexpr int kWait = 1 << 20, kSpin = 1 << 24;   // probes (blocking, non-blocking) after which a wait gives up: waits here are microseconds
+// Probes after which a wait gives up; waits here are microseconds.  All are the suspending kind: polling without a pause takes
+// the same time alone, but back to back the chip is at its power limit and polling warps cost 1-2 %.
+constexpr int kWait = 1 << 20;
 
 struct TcArgs {
     si_kv_view kv;
@@ -80,17 +82,6 @@ __device__ __forceinline__ f32x2 ex2_poly(f32x2 x) {
 __device__ __forceinline__ void tma_load_4d(void *dst, const CUtensorMap *map, int x, int y, int z, int w, uint64_t *bar) {
     asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
                  ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar)) : "memory");
-}
-// Bounded wait by non-blocking probes: a thread that the blocking probe has put to sleep is woken late, and the hand-overs
-// between the softmax warps and the matrix unit are on the critical path of every tile.
-__device__ __forceinline__ bool mbar_spin(uint64_t *bar, uint32_t parity, int limit) {
-    for (int i = 0; i < limit; ++i) {
-        uint32_t ok;
-        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                     : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
-        if (ok) return true;
-    }
-    return false;
 }
 // One lane of a converged warp.
 __device__ __forceinline__ bool elect_one() {

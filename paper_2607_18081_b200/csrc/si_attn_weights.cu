@@ -4,7 +4,7 @@
 // S^T = K Q^T with 128 keys as rows and 128 packed (query, head) rows as columns: a thread owns a key, so the
 // sum over queries is a sum along its row of tensor memory and nothing is exchanged.  2 D flops and one exponential per
 // pair; the exponential unit (16 per clock and SM: 1024 clocks per tile pair) is twice as slow as the matrix unit (512), so one
-// of every eight pairs of exponentials goes to the multiply-add units (4096-token prompt: 114 us; none 117, three of eight
+// of every eight pairs of exponentials goes to the multiply-add units (4096-token prompt: 112 us; none 117, three of eight
 // 120: back to back the chip is at its power limit, and a polynomial costs more energy than it saves time).
 //
 // A key tile is 256 keys, two such products with the same query tile: with 128 the stream of query tiles out of L2 (32 KB per
@@ -148,7 +148,7 @@ weights_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
                 const int end = min(g1, cur.start + cur.q.n);
                 for (; g < end; ++g, ++it) {
                     const int st = it % kStages;
-                    ok = mbar_spin(&B->empty[st], (it / kStages & 1) ^ 1, kSpin);
+                    ok = mbar_wait(&B->empty[st], (it / kStages & 1) ^ 1, kWait);
                     if (!ok) break;
                     mbar_arrive_expect_tx(&B->full[st], (D / 64) * 128 * used);
                     for (int c = 0; c < D / 64; ++c)
@@ -175,11 +175,11 @@ weights_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
                 for (; g < end && ok; ++g, ++it) {
                     const int st = it % kStages;
                     const uint32_t qb = st * (C::kBytes / 16);
-                    ok = mbar_spin(&B->full[st], it / kStages & 1, kSpin);
+                    ok = mbar_wait(&B->full[st], it / kStages & 1, kWait);
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
                         const int buf = (it & 1) * 2 + half;
-                        ok = ok && mbar_spin(&B->free[buf], (it >> 1 & 1) ^ 1, kSpin);
+                        ok = ok && mbar_wait(&B->free[buf], (it >> 1 & 1) ^ 1, kWait);
                         if (!ok) break;
                         tc_fence_after();
 #pragma unroll
@@ -220,7 +220,7 @@ weights_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
                 if (g + 1 == cur.start + cur.q.n) next_item(A, W, cur);
                 fetch(cur, g + 1);
             }
-            ok = ok && mbar_spin(&B->lempty[st], (it / kLse & 1) ^ 1, kSpin);
+            ok = ok && mbar_wait(&B->lempty[st], (it / kLse & 1) ^ 1, kWait);
             __syncwarp();
 #pragma unroll
             for (int k = 0; k < 4; ++k) lse2[st * kTile + k * 32 + lane] = w[k];
@@ -245,7 +245,7 @@ weights_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
                 if ((it & 1) != parity) continue;
                 const int st = it % kLse;
                 // a wait that runs out is reported and the run goes on without waiting, to its end
-                if (ok) ok = __all_sync(0xFFFFFFFFu, mbar_spin(&B->s[buf], it >> 1 & 1, kSpin) && mbar_spin(&B->lfull[st], it / kLse & 1, kSpin));
+                if (ok) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&B->s[buf], it >> 1 & 1, kWait) && mbar_wait(&B->lfull[st], it / kLse & 1, kWait));
                 tc_fence_after();
                 // column c is the query at position s0 + c / G: this key is seen by a range of columns
                 const int s0 = shift + (cur.q.first + g - cur.start) * A.R;

@@ -18,7 +18,9 @@ namespace {
 constexpr int kRowThreads = 1024;
 constexpr int kBins = 2048;
 constexpr int kMaxCluster = 8;
-constexpr int kSliceKeys = 48 * 1024;        // keys of a slice in shared memory; longer rows read their weights again instead
+constexpr int kSliceKeys = 48 * 1024;        // keys of a slice in shared memory; longer rows read their weights again instead,
+                                             // in rounds of so many slots
+constexpr int kCandidates = 2048;            // keys of the first digit's bin that are listed for the last pass
 constexpr int kFewMoves = 256;               // in place with at most this many entries over the budget: one kernel
 constexpr int kFewOver = 4;                  // at most this many entries over the budget are looked for one by one
 constexpr int kMoveRows = 8;                 // rows in flight per warp of the moving kernel
@@ -41,6 +43,9 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
     const uint32_t b = __float_as_uint(w);
     return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
 }
+
+// The lowest n bits.
+__device__ __forceinline__ unsigned int first_bits(int n) { return n >= 32 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << n) - 1; }
 
 __device__ __forceinline__ int entries(const EvictArgs &A, int b) {
     const int n = si_kv_len(A.src, b, A.status) + A.n_new;
@@ -85,6 +90,8 @@ template <bool SMEM>
 __global__ void __launch_bounds__(kRowThreads, 2) evict_select_kernel(const EvictArgs A) {
     extern __shared__ uint32_t keys[];
     __shared__ unsigned int hist[3][kBins], share[3];        // share: counts for the CTAs behind this one
+    __shared__ uint32_t cand[kCandidates];
+    __shared__ int scan[kRowThreads / 32 + 1], n_cand;
     __shared__ unsigned long long tot[32], total;
     __shared__ uint32_t sh_prefix;
     __shared__ int sh_need;
@@ -105,22 +112,32 @@ __global__ void __launch_bounds__(kRowThreads, 2) evict_select_kernel(const Evic
     auto key_of = [&](int p, float x) -> uint32_t {
         return p < A.n_sink || (long long)p > (long long)last - A.n_recent ? 0xFFFFFFFFu : weight_key(x);
     };
-    const int len = (n + C - 1) / C, s0 = min(n, rank * len), s1 = min(n, s0 + len);     // this CTA's slots
+    const int len = ((n + C - 1) / C + 3) & ~3, s0 = min(n, rank * len), s1 = min(n, s0 + len);     // this CTA's slots
     if (SMEM) {
-        constexpr int U = 4;                                 // loads of a thread in flight: U weights, U positions
-        for (int q = s0 + tid; q < s1; q += U * kRowThreads) {
-            float x[U];
-            int p[U];
+        if (!(((uintptr_t)w | (uintptr_t)pos) & 15)) {       // (s0 is a multiple of 4, or nothing is left)
+            constexpr int U = 2;                             // 16-byte loads of a thread in flight: U weights, U positions
+            for (int q = s0 + 4 * tid; q < s1; q += 4 * U * kRowThreads) {
+                float4 x[U];
+                int4 p[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int j = q + u * kRowThreads;
-                x[u] = j < s1 ? __ldg(w + j) : 0.f;
-                p[u] = pos && j < s1 ? __ldg(pos + j) : j;
+                for (int u = 0; u < U; ++u) {
+                    const int j = q + u * 4 * kRowThreads;
+                    const bool in = j + 3 < s1;              // the last, partial group entry by entry
+                    x[u] = in ? __ldg(reinterpret_cast<const float4 *>(w + j)) : make_float4(j < s1 ? w[j] : 0.f, j + 1 < s1 ? w[j + 1] : 0.f, j + 2 < s1 ? w[j + 2] : 0.f, 0.f);
+                    p[u] = !pos ? make_int4(j, j + 1, j + 2, j + 3) : in ? __ldg(reinterpret_cast<const int4 *>(pos + j))
+                         : make_int4(j < s1 ? pos[j] : 0, j + 1 < s1 ? pos[j + 1] : 0, j + 2 < s1 ? pos[j + 2] : 0, 0);
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int j = q + u * 4 * kRowThreads;
+                    if (j < s1)                              // the slice has room for whole groups
+                        *reinterpret_cast<uint4 *>(keys + (j - s0)) = make_uint4(key_of(p[u].x, x[u].x), key_of(p[u].y, x[u].y), key_of(p[u].z, x[u].z), key_of(p[u].w, x[u].w));
+                }
             }
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (q + u * kRowThreads < s1) keys[q + u * kRowThreads - s0] = key_of(p[u], x[u]);
+        } else {
+            for (int j = s0 + tid; j < s1; j += kRowThreads) keys[j - s0] = key_of(pos ? pos[j] : j, w[j]);
         }
+        __syncthreads();
     }
     auto key = [&](int j) -> uint32_t { return SMEM ? keys[j - s0] : key_of(pos ? pos[j] : j, w[j]); };
     auto sync = [&]() { if (C > 1) si_tc::cluster_sync_all(); else __syncthreads(); };
@@ -187,72 +204,105 @@ __global__ void __launch_bounds__(kRowThreads, 2) evict_select_kernel(const Evic
         moves = sh_need;
     } else {
         for (int i = tid; i < 3 * kBins; i += kRowThreads) hist[0][i] = 0;
+        if (tid == 0) n_cand = 0;
         __syncthreads();
-        // radix select of the budget-th largest key
-        uint32_t prefix = 0, mask = 0;
+        auto each_key = [&](auto f) {
+            if (SMEM) {
+                for (int q = 4 * tid; q < s1 - s0; q += 4 * kRowThreads) {
+                    const uint4 k = *reinterpret_cast<const uint4 *>(keys + q);
+                    f(k.x);
+                    if (q + 1 < s1 - s0) f(k.y);
+                    if (q + 2 < s1 - s0) f(k.z);
+                    if (q + 3 < s1 - s0) f(k.w);
+                }
+            } else {
+                for (int j = s0 + tid; j < s1; j += kRowThreads) f(key(j));
+            }
+        };
+        // radix select of the budget-th largest key; the second pass lists the keys of its bin for the third
+        uint32_t prefix = 0;
         int need = budget;
 #pragma unroll
         for (int pass = 0; pass < 3; ++pass) {
-            constexpr int shifts[3] = {21, 10, 0}, bits[3] = {11, 11, 10};
-            for (int j = s0 + tid; j < s1; j += kRowThreads) {
-                const uint32_t k = key(j);
-                if ((k & mask) == prefix) atomicAdd(&hist[pass][(k >> shifts[pass]) & ((1u << bits[pass]) - 1)], 1u);
+            if (pass == 0) each_key([&](uint32_t k) { atomicAdd(&hist[0][k >> 21], 1u); });
+            else if (pass == 1)
+                each_key([&](uint32_t k) {
+                    if ((k >> 21) != (prefix >> 21)) return;
+                    atomicAdd(&hist[1][k >> 10 & 2047], 1u);
+                    const int at = atomicAdd(&n_cand, 1);
+                    if (at < kCandidates) cand[at] = k;
+                });
+            else {
+                auto last_digit = [&](uint32_t k) { if ((k >> 10) == (prefix >> 10)) atomicAdd(&hist[2][k & 1023], 1u); };
+                if (n_cand <= kCandidates) for (int i = tid; i < n_cand; i += kRowThreads) last_digit(cand[i]);
+                else each_key(last_digit);
             }
             sync();
             // bins from the top down: two per thread
-            const int hi = kBins - 1 - 2 * tid;
-            unsigned int c0 = 0, c1 = 0;
+            const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, hi = kBins - 1 - 2 * tid;
+            int c0 = 0, c1 = 0;
             if (C == 1) { c0 = hist[pass][hi]; c1 = hist[pass][hi - 1]; }
             else for (int r = 0; r < C; ++r) { c0 += ld_cluster(&hist[pass][hi], r); c1 += ld_cluster(&hist[pass][hi - 1], r); }
-            const int before = (int)block_scan(c0 + c1, tot, &total);
-            if (before < need && before + (int)c0 >= need) { sh_prefix = prefix | ((uint32_t)hi << shifts[pass]); sh_need = need - before; }
-            else if (before + (int)c0 < need && before + (int)(c0 + c1) >= need) { sh_prefix = prefix | ((uint32_t)(hi - 1) << shifts[pass]); sh_need = need - before - (int)c0; }
+            const int before = si_block_scan<kRowThreads>(c0 + c1, scan);
+            if (before < need && before + c0 >= need) { sh_prefix = prefix | ((uint32_t)hi << shift); sh_need = need - before; }
+            else if (before + c0 < need && before + c0 + c1 >= need) { sh_prefix = prefix | ((uint32_t)(hi - 1) << shift); sh_need = need - before - c0; }
             __syncthreads();
             prefix = sh_prefix; need = sh_need;
-            mask |= ((1u << bits[pass]) - 1) << shifts[pass];
         }
-        // Ordered counts.  A thread has `per` neighbouring slots (an odd number: no bank conflicts; at most 63, so that a mask of
-        // them is one register pair) of every round; slices in shared memory are one round, longer ones (one CTA) as many as it takes.
-        const int per = min((s1 - s0 + kRowThreads - 1) / kRowThreads | 1, 63), rounds = (s1 - s0 + per * kRowThreads - 1) / (per * kRowThreads);
+        // Ordered counts on bit maps, a bit per slot: keys above the last kept one, keys equal to it.  Their words take the place of
+        // the first two histograms (no CTA of the cluster reads those after the last exchange).  Slices in shared memory are one
+        // round; longer ones, of one CTA, as many as it takes.
+        unsigned int *above = hist[0], *equal = hist[1];
         auto before_me = [&](int which, unsigned int mine) {     // the sum of `mine` over the CTAs in front
-            if (C == 1) return 0u;
+            if (C == 1) return 0;
             if (tid == 0) share[which] = mine;
             sync();
-            unsigned int s = 0;
-            for (int r = 0; r < rank; ++r) s += ld_cluster(&share[which], r);
-            return s;
+            int t = 0;
+            for (int r = 0; r < rank; ++r) t += (int)ld_cluster(&share[which], r);
+            return t;
         };
         list_stayers();
         int ties = 0, freed = 0, moved = 0;                      // so far in this row
-        // the slots of round r that are kept, ties to the lower ones; `below`: those of them under the budget
-        auto kept_of = [&](int r, int &j0, unsigned long long &valid, unsigned long long &below) {
-            j0 = s0 + r * per * kRowThreads + tid * per;
-            const int cnt = max(0, min(per, s1 - j0)), low = max(0, min(cnt, budget - j0));
-            valid = (1ull << cnt) - 1; below = (1ull << low) - 1;
-            unsigned long long keep = 0, tie = 0;
-            for (int i = 0; i < cnt; ++i) {
-                const uint32_t k = key(j0 + i);
-                keep |= (unsigned long long)(k > prefix) << i;
-                tie |= (unsigned long long)(k == prefix) << i;
+        for (int base = s0; base < s1 || base == s0; base += kSliceKeys) {
+            const int cnt = min(kSliceKeys, s1 - base), words = (cnt + 31) / 32, share_w = words > kRowThreads ? 2 : 1;
+            for (int i = tid; i < words * 32; i += kRowThreads) {
+                const uint32_t k = i < cnt ? key(base + i) : 0u;
+                const unsigned int a = __ballot_sync(0xFFFFFFFFu, i < cnt && k > prefix), e = __ballot_sync(0xFFFFFFFFu, i < cnt && k == prefix);
+                if ((tid & 31) == 0) { above[i / 32] = a; equal[i / 32] = e; }
             }
-            int t = ties + (int)block_scan((unsigned long long)__popcll(tie), tot, &total);
-            const int all = (int)total;
-            if (r == 0) { const int ahead = (int)before_me(0, all); t += ahead; ties += ahead; }
-            ties += all;
-            for (; tie && t < need; ++t) { keep |= tie & (0ull - tie); tie &= tie - 1; }
-            return keep;
-        };
-        for (int r = 0; r < rounds; ++r) {
-            int j0;
-            unsigned long long valid, below;
-            const unsigned long long keep = kept_of(r, j0, valid, below), gone = valid & below & ~keep, far = keep & ~below;
-            const unsigned long long at = block_scan((unsigned long long)__popcll(gone) << 32 | (unsigned long long)__popcll(far), tot, &total);
-            const unsigned long long all = total;
-            if (r == 0) { freed += (int)before_me(1, (unsigned int)(all >> 32)); moved += (int)before_me(2, (unsigned int)all); }
+            __syncthreads();
+            const int w0 = min(words, tid * share_w), w1 = min(words, w0 + share_w);
+            int mine = 0;
+            for (int q = w0; q < w1; ++q) mine += __popc(equal[q]);
+            int t = ties + si_block_scan<kRowThreads>(mine, scan);
+            const int all_ties = scan[kRowThreads / 32];
+            if (base == s0) { const int ahead = before_me(0, all_ties); t += ahead; ties += ahead; }
+            ties += all_ties;
+            unsigned int keep[2], low[2], in[2];                 // of this thread's words: kept slots, slots under the budget, slots
+            unsigned long long counts = 0;                       // freed slots above, movers below
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                keep[u] = low[u] = in[u] = 0;
+                if (w0 + u >= w1) continue;
+                const int slot = base + (w0 + u) * 32;
+                unsigned int e = equal[w0 + u];
+                in[u] = first_bits(s1 - slot); low[u] = first_bits(budget - slot);
+                keep[u] = above[w0 + u];
+                for (; e && t < need; ++t) { keep[u] |= e & (0u - e); e &= e - 1; }
+                t += __popc(e);                                  // the rest of the ties goes
+                counts += (unsigned long long)__popc(in[u] & low[u] & ~keep[u]) << 32 | (unsigned)__popc(keep[u] & ~low[u]);
+            }
+            const unsigned long long at = block_scan(counts, tot, &total), all = total;
+            if (base == s0) { freed += before_me(1, (unsigned int)(all >> 32)); moved += before_me(2, (unsigned int)all); }
             int f = freed + (int)(at >> 32), m = moved + (int)(at & 0xFFFFFFFFu);
-            for (unsigned long long g = gone; g; g &= g - 1) freed_slots[f++] = j0 + __ffsll(g) - 1;
-            for (unsigned long long g = far; g; g &= g - 1) movers[m++] = j0 + __ffsll(g) - 1;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int slot = base + (w0 + u) * 32;
+                for (unsigned int g = in[u] & low[u] & ~keep[u]; g; g &= g - 1) freed_slots[f++] = slot + __ffs(g) - 1;
+                for (unsigned int g = keep[u] & ~low[u]; g; g &= g - 1) movers[m++] = slot + __ffs(g) - 1;
+            }
             freed += (int)(all >> 32); moved += (int)(all & 0xFFFFFFFFu);
+            __syncthreads();                                     // the maps may be written again
         }
         sync();                                                   // the lists are complete (global writes included); keys and weights are no longer read
         moves = freed;
@@ -336,7 +386,7 @@ int cluster_size(const si_kv_t *kv) {
     const long long rows = (long long)kv->n_seqs * kv->n_kv_heads;
     int c = 1;
     while (c < kMaxCluster && rows * c * 2 <= si_sm_count() && kv->capacity / (c * 2) >= 4096) c *= 2;
-    while (c < kMaxCluster && (kv->capacity + c - 1) / c > kSliceKeys) c *= 2;
+    while (c < kMaxCluster && (kv->capacity + c - 1) / c + 3 > kSliceKeys) c *= 2;
     return c;
 }
 
@@ -415,8 +465,8 @@ extern "C" int si_kv_evict(const si_kv_t *src, const si_kv_t *dst, const int32_t
     const cudaStream_t st = (cudaStream_t)stream;
     const bool len_after = A.move_here && len_out == src->len;  // the rows of a sequence still read the old length
     if (len_after) A.len_out = nullptr;
-    const int C = cluster_size(src), slice = (src->capacity + C - 1) / C;
-    rc = slice <= kSliceKeys ? launch_select<true>(A, C, (size_t)slice * 4, st) : launch_select<false>(A, C, 0, st);
+    const int C = cluster_size(src), slice = ((src->capacity + C - 1) / C + 3) & ~3;
+    rc = slice <= kSliceKeys ? launch_select<true>(A, C, (size_t)slice * 4, st) : launch_select<false>(A, 1, 0, st);     // in rounds: one CTA
     if (rc) return rc;
     if (len_after) {
         A.len_out = len_out;

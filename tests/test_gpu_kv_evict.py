@@ -40,6 +40,8 @@ CASES = [
     ([3000, 777], 0, 3001, 100, 100, 0),   # only protected entries fit
     ([20000], 0, 20000, 333, 4, 100),
     ([60000], 0, 60001, 30000, 16, 128),
+    ([60000, 13], 0, 60004, 30001, 16, 128),   # an aligned row length
+    ([16384, 9000], 0, 16384, 4096, 4, 256),
 ]
 
 
@@ -128,7 +130,7 @@ def test_evict_into_a_cache_with_a_budget_above_the_source(api):
                 assert (kept[b, :, n:] == -1).all() and (kept[b, :, :n] == torch.arange(n, device="cuda")).all()
 
 
-@pytest.mark.parametrize("n,budget", [(400000, 150000), (393217, 393000)])
+@pytest.mark.parametrize("n,budget", [(400000, 150000), (393217, 393000), (700001, 300000)])
 def test_evict_of_rows_longer_than_shared_memory_holds(api, n, budget):
     """More keys than eight CTAs keep in shared memory: the weights are read again instead, in rounds."""
     rng = np.random.default_rng(n)

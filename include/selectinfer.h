@@ -426,6 +426,8 @@ int si_shard_reduce(const float *const *parts_dev, int world, const void *x, int
  *               b * seq_stride + h * head_stride + j * row_stride + c (elements; the same for k and v; multiples of 8,
  *               so that every row starts on 16 bytes).  Head-major caches [n_seqs, n_kv_heads, capacity, head_dim]
  *               and token-major ones [n_seqs, capacity, n_kv_heads, head_dim] are both plain settings of the strides.
+ *               Sequences or heads may share memory through a stride of 0 where a call only reads (k_new of
+ *               si_attn_decode and dst of si_kv_evict: SI_ERR_INVALID_ARG).
  *   len         device int32 [n_seqs]: entries in use, 0 .. capacity (a value outside is clamped and reported as
  *               SI_ERR_OUT_OF_RANGE).  Entries from len[b] on are never part of a result, whatever they hold.
  *   pos         device int32 [n_seqs, n_kv_heads, capacity]: the position in the sequence of every entry, any order,
@@ -504,7 +506,8 @@ int si_attn_decode(const si_kv_t *kv, const void *q, long long q_seq_stride, int
  *   src      the cache, with weight; pos may be NULL (entry j at position j)
  *   dst      where the kept entries go, with pos and weight, capacity >= budget, the same n_seqs, n_kv_heads, head_dim
  *            and dtype; dst->len is not read.  dst == src (or the same k) evicts in place and needs src->pos; dst may
- *            not overlap src otherwise -- the decode cache of a prompt that was prefilled into scratch memory.
+ *            not overlap src otherwise -- the decode cache of a prompt that was prefilled into scratch memory (another k
+ *            with the same v, pos or weight is SI_ERR_INVALID_ARG).
  *   q_pos    device int32 [n_seqs]: the newest position; NULL (only with src->pos == NULL): len[b] + n_new - 1
  *   kept     device int32 [n_seqs, n_kv_heads, budget] or NULL: the source slot of every slot of dst, -1 beyond
  *   len_out  device int32 [n_seqs] or NULL: min(len[b] + n_new, budget); may be src->len or dst->len

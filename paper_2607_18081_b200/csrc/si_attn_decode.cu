@@ -664,7 +664,7 @@ extern "C" int si_attn_decode(const si_kv_t *kv, const void *q, long long q_seq_
     if (kv->n_seqs == 0) return SI_OK;
     const int acc = (flags & SI_FLAG_ACC_WEIGHT) != 0;
     if (!q || !out || q_seq_stride < 0 || !k_new != !v_new || new_seq_stride < 0) return SI_ERR_INVALID_ARG;
-    if ((kv->pos && !q_pos) || (acc && !kv->weight)) return SI_ERR_INVALID_ARG;
+    if ((kv->pos && !q_pos) || (acc && !kv->weight) || (k_new && si_kv_shared(kv))) return SI_ERR_INVALID_ARG;
     if (!si_aligned16(q) || !si_aligned16(out) || !si_aligned16(k_new) || !si_aligned16(v_new) || ((q_seq_stride | new_seq_stride) & 7))
         return SI_ERR_ALIGNMENT;
     const Layout L = layout_of(kv, n_q_heads, acc);

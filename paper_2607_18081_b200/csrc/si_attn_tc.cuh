@@ -10,8 +10,8 @@ using namespace si_tc;
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kTile = 128;                 // rows of a query tile, keys of a key tile
-// Probes after which a wait gives up; waits here are microseconds.  All are the suspending kind: polling without a pause takes
-// the same time alone, but back to back the chip is at its power limit and polling warps cost 1-2 %.
+// Probes after which a wait gives up: a probe that fails takes 4 us, so after some 4 s; waits here are microseconds.  All are the
+// suspending kind: polling without a pause takes the same time alone, but back to back the chip is at its power limit and polling warps cost 1-2 %.
 constexpr int kWait = 1 << 20;
 
 struct TcArgs {

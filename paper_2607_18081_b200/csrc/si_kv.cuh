@@ -34,12 +34,17 @@ inline int si_kv_check(const si_kv_t *kv) {
     return SI_OK;
 }
 
+// Two rows of the cache share memory through a zero stride: it can be read, but not written.
+inline bool si_kv_shared(const si_kv_t *kv) {
+    return (kv->n_seqs > 1 && kv->seq_stride == 0) || (kv->n_kv_heads > 1 && kv->head_stride == 0);
+}
+
 // ... and of those that bring queries.
 inline int si_attn_check(const si_kv_t *kv, int n_q_heads, int window, int n_sink, float scale) {
     const int rc = si_kv_check(kv);
     if (rc) return rc;
     if (n_q_heads < 1 || n_q_heads % kv->n_kv_heads || window < 0 || n_sink < 0) return SI_ERR_INVALID_ARG;
-    if (!(scale > -3.0e38f && scale < 3.0e38f)) return SI_ERR_INVALID_ARG;
+    if (!(scale > -2.0e38f && scale < 2.0e38f)) return SI_ERR_INVALID_ARG;      // scale log2(e) is finite too
     if (n_q_heads / kv->n_kv_heads > 128) return SI_ERR_UNSUPPORTED;
     return SI_OK;
 }

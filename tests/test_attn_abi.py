@@ -101,6 +101,29 @@ def test_bad_evictions_are_refused(api):
     assert _evict(api, pos, _kv(api, pos=FAKE, v=FAKE * 5)) == I     # half in place
 
 
+def test_writes_to_shared_memory_are_refused(api):
+    I, N = api.SI_ERR_INVALID_ARG, api.SI_ERR_NOMEM
+    for change in (dict(seq_stride=0), dict(head_stride=0)):
+        kv = _kv(api, **change)
+        assert _decode(api, kv, kn=FAKE, vn=FAKE) == I and _decode(api, kv, ws_bytes=0) == N          # reading is fine
+        assert _evict(api, _kv(api), _kv(api, k=FAKE * 8, v=FAKE * 9, pos=FAKE, weight=FAKE, **change)) == I
+        assert _evict(api, _kv(api, pos=FAKE, **change), _kv(api, pos=FAKE, **change)) == I
+        assert _evict(api, kv, _kv(api, k=FAKE * 8, v=FAKE * 9, pos=FAKE, weight=FAKE), ws_bytes=0) == N
+        alone = _kv(api, n_seqs=1, n_kv_heads=1, **change)
+        assert _decode(api, alone, kn=FAKE, vn=FAKE, ws_bytes=0) == N
+    src = _kv(api, pos=FAKE * 7)
+    apart = dict(k=FAKE * 8, v=FAKE * 9, pos=FAKE, weight=FAKE)
+    assert _evict(api, src, _kv(api, **apart), ws_bytes=0) == N
+    for same in (dict(v=src.v), dict(pos=src.pos), dict(weight=src.weight)):
+        assert _evict(api, src, _kv(api, **{**apart, **same})) == I
+
+
+def test_scales_beyond_the_type_are_refused(api):
+    for scale in (2.5e38, -2.5e38):
+        for call in (_prefill, _weights, _decode):
+            assert call(api, _kv(api), scale=scale) == api.SI_ERR_INVALID_ARG
+
+
 def test_oracle_eviction_by_hand():
     w = np.array([5.0, 1.0, 4.0, np.nan, 4.0, 0.5, 9.0])
     # budget 4, position 5 recent (protected): kept are slots 5, 6, 0 and the lower of the tied 2 and 4

@@ -22,7 +22,9 @@
  *     si_store_t handle.
  *   - `stream` is a cudaStream_t passed as void*.  All work is enqueued on it and no
  *     call synchronises except si_store_free and si_load_neurons (which waits for the
- *     upload of its id list).  Calls sharing one workspace must be ordered on one stream.
+ *     upload of its id list).  Calls sharing one workspace must be ordered on one stream; nothing else
+ *     about them needs to match.  Kernels are launched as programmatic dependents: a kernel of the
+ *     caller's own that lets its dependents start early writes a call's lists and offsets before that.
  *   - Errors that can be seen on the host (null or misaligned pointers, sizes out of
  *     range, bad enum, layer out of range, buffers too small) are reported before
  *     anything is launched.  Errors only the device can see (an index out of range or

@@ -96,6 +96,12 @@ int si_debug_ffn_forward_waits(const si_store_t *store, int layer, const void *x
  * SI_ERR_INVALID_ARG for T <= 128, d_model not a multiple of 128, union_cap not a positive multiple of 128. */
 int si_debug_pair_plan(int d_model, int union_cap, int T, int num_sms, int out[6]);
 
+/* Host logic only: *ahead_out = 1 if a multi-token call on this store with T tokens and lists of k entries in this workspace,
+ * enqueued now on this stream, would start its union stage while the kernel ahead of it may still run, 0 if in stream order.
+ * It does so only directly behind a multi-token call with the same workspace and layout (every call of this library whose
+ * kernels let their dependents start early ends that). */
+int si_debug_union_ahead(const si_store_t *store, int T, int k, void *workspace, void *stream, int *ahead_out);
+
 /* si_ffn_forward_sharded for the ranks rank_base .. rank_base + n_here - 1 of a group that share this GPU, in ONE
  * launch (kernels of different ranks that wait on one another may not run as separate launches on one GPU): the
  * ranks' first kernels one after the other, then one cooperative launch of the finishing kernel over all of them.

@@ -40,7 +40,7 @@ EXPORTS = [
     "si_debug_decode_stack_forward", "si_debug_decode_chain_forward", "si_debug_union_masks", "si_debug_ffn_forward_waits",
     "si_debug_read_bandwidth", "si_prefill_vote_workspace_bytes", "si_prefill_vote", "si_prefill_forward", "si_layer_range", "si_profile_accumulate", "si_profile_merge", "si_profile_rank",
     "si_loadset", "si_shard_count", "si_shard_lists", "si_shard_reduce", "si_ffn_forward_sharded",
-    "si_debug_ffn_forward_sharded_group", "si_debug_pair_plan",
+    "si_debug_ffn_forward_sharded_group", "si_debug_pair_plan", "si_debug_union_ahead",
     "si_kv_workspace_bytes", "si_attn_prefill", "si_attn_weights", "si_attn_decode", "si_kv_evict",
 ]
 
@@ -86,6 +86,7 @@ def _load_library() -> ctypes.CDLL:
     lib.si_debug_ffn_forward_waits.argtypes = lib.si_ffn_forward.argtypes + [ctypes.c_longlong, ci]
     lib.si_debug_read_bandwidth.argtypes = [vp, ctypes.c_size_t, vp, vp]
     lib.si_debug_pair_plan.argtypes = [ci, ci, ci, ci, ctypes.POINTER(ctypes.c_int)]
+    lib.si_debug_union_ahead.argtypes = [vp, ci, ci, vp, vp, ctypes.POINTER(ci)]
     lib.si_prefill_vote_workspace_bytes.argtypes = [ci, ci, ci, psz]
     lib.si_prefill_vote.argtypes = [vp, ci, ci, ci, ci, ci, ci, ci, cu, vp, ci, vp, vp, vp, sz, vp]
     lib.si_profile_accumulate.argtypes = [vp, ci, ci, ci, vp, vp]
@@ -416,6 +417,12 @@ def si_debug_pair_plan(d_model: int, union_cap: int, T: int, num_sms: int) -> di
     _check(_lib.si_debug_pair_plan(d_model, union_cap, T, num_sms, out), "si_debug_pair_plan")
     return {"gateup_w": out[0], "gateup_sub": out[1], "gateup_pairs": out[2], "down_n": out[3], "down_ksplit": out[4],
             "down_ctas": out[5]}
+
+
+def si_debug_union_ahead(handle, T: int, k: int, workspace, stream=None) -> bool:
+    out = ctypes.c_int(0)
+    _check(_lib.si_debug_union_ahead(handle, T, k, _dp(workspace), _stream(stream), ctypes.byref(out)), "si_debug_union_ahead")
+    return bool(out.value)
 
 
 def si_debug_ffn_forward_waits(handle, layer: int, x, T: int, idx, idx_offsets, k_fixed: int, y, flags: int,

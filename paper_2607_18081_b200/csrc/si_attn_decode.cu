@@ -678,5 +678,6 @@ extern "C" int si_attn_decode(const si_kv_t *kv, const void *q, long long q_seq_
                        new_seq_stride, n_q_heads, n_q_heads / kv->n_kv_heads, L.GB, L.GS, window, n_sink, scale * kLog2e,
                        (uint16_t *)out, lse, status_dev, acc, L.n_cta, (float *)(ws + L.o), (float *)(ws + L.ml),
                        (float2 *)(ws + L.done), (float *)(ws + L.scores), (int2 *)(ws + L.runs)};
+    si_mt_forget();
     return kv->dtype == SI_BF16 ? launch_t<SI_BF16>(A, L.NT, (cudaStream_t)stream) : launch_t<SI_F16>(A, L.NT, (cudaStream_t)stream);
 }

@@ -491,6 +491,7 @@ extern "C" int si_attn_prefill(const si_kv_t *kv, const void *q, long long q_seq
     if ((rc = make_q_map(&om, out, kv, T * row, row, T, n_q_heads, A.G, A.R))) return rc;
     const Call c{qm, km, vm, om, A, P, (cudaStream_t)stream};
     const bool neg = scale < 0.f;
+    si_mt_forget();
     if (kv->dtype == SI_BF16) return kv->head_dim == 128 ? launch_t<SI_BF16, 128>(c, neg) : launch_t<SI_BF16, 64>(c, neg);
     return kv->head_dim == 128 ? launch_t<SI_F16, 128>(c, neg) : launch_t<SI_F16, 64>(c, neg);
 }

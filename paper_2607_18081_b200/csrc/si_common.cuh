@@ -24,8 +24,6 @@ struct si_store {
     std::vector<int> n_loaded, n_base;
     std::vector<char> loaded;              // layer packed at least once
     std::vector<size_t> rec_off, s2g_off, g2s_off;
-    // multi-token calls alternate between the two copies of the union stage's outputs (see si_ws_carve)
-    mutable std::atomic<unsigned> mt_calls{0};
     size_t record_bytes() const { return (size_t)3 * d_model * 2; }
     const uint16_t *records(int l) const { return (const uint16_t *)(mem + rec_off[l]); }
     int32_t *s2g(int l) const { return (int32_t *)(mem + s2g_off[l]); }
@@ -102,6 +100,9 @@ int si_multi_token_launch(const si_store *s, int layer, const void *x, int T, co
                           const int32_t *idx_offsets, int k_fixed, void *y, int y_dtype,
                           unsigned flags, void *workspace, size_t ws_bytes, int32_t *status_dev,
                           cudaStream_t stream, long long spin_limit = 0, int withhold = 0);
+// To be called before a launch whose kernel lets its programmatic dependents start before its own last access to memory:
+// the union stage of a multi-token call behind it then waits for it (see MtCall in si_gemm.cu).
+void si_mt_forget();
 int si_union_masks_launch(const si_store *s, int layer, int T, const int32_t *idx, const int32_t *idx_offsets,
                           int k_fixed, int32_t *union_out, int32_t *n_union_out, uint32_t *masks_out,
                           void *workspace, size_t ws_bytes, cudaStream_t stream);

@@ -311,6 +311,7 @@ int launch_simple_step(const si_store *s, int layer, const void *x, const int32_
     // Both kernels are launched as programmatic dependents: each may be scheduled while its predecessor in
     // the stream finishes and waits for that kernel's results with griddepcontrol.wait before it reads
     // anything.  After a predecessor that never triggers early this is an ordinary launch.
+    si_mt_forget();                        // (the sums read their partial rows after they have let dependents start)
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;

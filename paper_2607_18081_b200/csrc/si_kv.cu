@@ -464,6 +464,7 @@ extern "C" int si_kv_evict(const si_kv_t *src, const si_kv_t *dst, const int32_t
                 in_place && src->capacity - budget <= kFewMoves, kept || budget < src->capacity ? budget : src->capacity, kept ? kept : (int32_t *)workspace,
                 (int32_t *)((char *)workspace + si_align_up(rows * src->capacity * 4, 256)), 0, len_out, status_dev};
     A.list_source = kept || !A.move_here;
+    si_mt_forget();
     const cudaStream_t st = (cudaStream_t)stream;
     const bool len_after = A.move_here && len_out == src->len;  // the rows of a sequence still read the old length
     if (len_after) A.len_out = nullptr;

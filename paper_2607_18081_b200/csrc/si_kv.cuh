@@ -64,6 +64,9 @@ template <typename K> int si_allow_smem(K kernel, int bytes, std::atomic<unsigne
     return SI_OK;
 }
 
+// Every kernel of these calls is a programmatic dependent that waits for the kernel ahead of it before it touches memory, and
+// lets its own dependents start early; each call says so by si_mt_forget() before it launches.
+
 // implemented in si_attn_decode.cu / si_attn_prefill.cu / si_attn_weights.cu
 size_t si_attn_decode_ws_bytes(const si_kv_t *kv, int n_q_heads);
 size_t si_attn_prefill_ws_bytes(const si_kv_t *kv, int n_q_heads, int T);

@@ -373,6 +373,7 @@ int select_set_attrs() {
 int select_reg_launch(const void *scores, int src, int n_rows, int n, int row_stride, int k, int use_abs, int32_t *idx_out,
                       int out_stride, int cap, int32_t *n_out, int *vote_counts, cudaStream_t stream) {
     const int per = (n + kSelThreads - 1) / kSelThreads;
+    si_mt_forget();                        // the kernel lets its dependents start before it writes the lists
 #define SI_SELECT_REG2(P, S)                                                                                             \
     si_select_topk_reg_kernel<P, S><<<n_rows, kSelThreads, (size_t)n * 4, stream>>>(scores, n, row_stride, k, use_abs, \
                                                                                     idx_out, out_stride, cap, n_out, vote_counts)

@@ -415,19 +415,21 @@ __global__ void __launch_bounds__(256) prefill_join_kernel(const TcArgs A, const
 // Blocks of queries, and over how many CTAs their keys are split: with fewer blocks than half the SMs as many as fit one
 // wave, but no part of fewer than four key tiles (a part costs its start, 3 us, and its join).
 struct Plan { long long blocks; int splits; };
+int splits_of(long long blocks, long long tiles) {
+    const int sms = si_sm_count();
+    if (blocks * 2 > sms || tiles < 8) return 1;
+    const long long n = sms / blocks < tiles / 4 ? sms / blocks : tiles / 4;
+    return n < kMaxSplits ? (int)n : kMaxSplits;
+}
 Plan plan_of(const si_kv_t *kv, int n_q_heads, int T, int window, int n_sink) {
-    const int G = n_q_heads / kv->n_kv_heads, R = kTile / G, sms = si_sm_count();
+    const int G = n_q_heads / kv->n_kv_heads, R = kTile / G;
     Plan p{((long long)T + 2 * R - 1) / (2 * R) * kv->n_kv_heads * kv->n_seqs, 1};
-    long long tiles = (kv->capacity + kTile - 1) / kTile;
+    long long tiles = ((long long)kv->capacity + kTile - 1) / kTile;
     if (window) {
         const long long w = ((long long)window + 2 * R + n_sink) / kTile + 3;
         if (w < tiles) tiles = w;
     }
-    if (p.blocks * 2 <= sms && tiles >= 8) {
-        p.splits = (int)(sms / p.blocks);
-        if (p.splits > kMaxSplits) p.splits = kMaxSplits;
-        if (p.splits > tiles / 4) p.splits = (int)(tiles / 4);
-    }
+    p.splits = splits_of(p.blocks, tiles);
     return p;
 }
 size_t parts_o_bytes(const Plan &p, int D) { return p.splits > 1 ? si_align_up((size_t)p.splits * p.blocks * 2 * kTile * D * 4, 256) : 0; }
@@ -460,9 +462,17 @@ template <int DT, int D> int launch_t(const Call &c, bool neg) { return neg ? la
 
 }  // namespace
 
+// For all calls with that many queries and heads or fewer: fewer rows are fewer blocks of queries, whose keys are split more
+// often.  The most parts that any number of blocks leaves (a window only shortens the keys).
 size_t si_attn_prefill_ws_bytes(const si_kv_t *kv, int n_q_heads, int T) {
-    const Plan p = plan_of(kv, n_q_heads, T, 0, 0);
-    return parts_o_bytes(p, kv->head_dim) + parts_ml_bytes(p);
+    const long long per = (long long)kv->n_kv_heads * kv->n_seqs, tiles = ((long long)kv->capacity + kTile - 1) / kTile;
+    const long long blocks = plan_of(kv, n_q_heads, T, 0, 0).blocks;
+    Plan most{0, 1};
+    for (long long n = per; n > 0 && n <= blocks && n * 2 <= si_sm_count(); n += per) {
+        const Plan p{n, splits_of(n, tiles)};
+        if (p.splits > 1 && p.blocks * p.splits > most.blocks * most.splits) most = p;
+    }
+    return most.splits > 1 ? parts_o_bytes(most, kv->head_dim) + parts_ml_bytes(most) : 0;
 }
 
 extern "C" int si_attn_prefill(const si_kv_t *kv, const void *q, long long q_seq_stride, long long q_tok_stride, int T,

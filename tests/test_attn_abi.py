@@ -142,3 +142,35 @@ def test_oracle_attention_against_the_definition():
         assert np.allclose(out[i], e @ v[see] / e.sum()) and np.isclose(lse[i], np.log(e.sum())) and np.isclose(w[i].sum(), 1.0)
         assert np.array_equal(np.nonzero(w[i])[0], see)
     assert np.all(out[2] == 0) and np.isneginf(lse[2]) and np.all(w[2] == 0)
+
+
+@pytest.mark.parametrize("shape", [dict(), dict(n_seqs=3), dict(head_dim=64, row_stride=64), dict(n_kv_heads=1), dict(n_seqs=20), dict(weight=None)])
+@pytest.mark.parametrize("capacity", [100, 1200, 8192, 12288, 300001])
+def test_a_workspace_covers_fewer_queries_and_heads(api, shape, capacity):
+    """Fewer rows are split over more CTAs, so the need of one size says nothing about that of a smaller one: the size is for all."""
+    f = dict(n_seqs=1, capacity=capacity)
+    f.update(shape)
+    kv = _kv(api, **f)
+    need = ctypes.c_size_t(0)
+
+    def size(hq, T):
+        assert api.lib().si_kv_workspace_bytes(ctypes.byref(kv), hq, T, ctypes.byref(need)) == api.SI_OK
+        return need.value
+
+    heads, tokens = [kv.n_kv_heads * g for g in (1, 2, 3, 4, 7, 8, 20, 64, 128)], [1, 2, 13, 45, 64, 129, 512, 600, 2048, 8192]
+    table = [[size(hq, T) for T in tokens] for hq in heads]
+    for row in table:
+        assert row == sorted(row)
+    for col in zip(*table):
+        assert list(col) == sorted(col)
+
+
+def test_a_short_chunk_passes_with_the_workspace_of_a_long_one(api):
+    """Splits of the keys need room (a workspace of NULL is refused behind the size check): never more than the larger size gave."""
+    need = ctypes.c_size_t(0)
+    for capacity, T_max, hq_max in ((8192, 2048, 32), (12288, 8192, 32), (8192, 1024, 64)):
+        kv = _kv(api, n_seqs=1, capacity=capacity)
+        assert api.lib().si_kv_workspace_bytes(ctypes.byref(kv), hq_max, T_max, ctypes.byref(need)) == api.SI_OK
+        for T, hq in ((1, 32), (45, 32), (200, 8), (512, 32)):
+            assert _prefill(api, kv, T=T, hq=hq, ws_bytes=0) == api.SI_ERR_NOMEM           # split: it does need room
+            assert _prefill(api, kv, T=T, hq=hq, ws=None, ws_bytes=need.value) == api.SI_ERR_INVALID_ARG

@@ -340,3 +340,18 @@ def test_calls_run_on_the_given_stream_and_in_a_graph(api):
         ref = au.reference(q, k, v, want, 0, 0, 0.09)
         au.check_out(out[:, None], ref, "bf16", 128)
         au.check_weight(weight, np.zeros((2, 2, 256)), ref, 128, 1)
+
+
+def test_one_workspace_for_long_and_short_chunks_and_fewer_heads(api):
+    """A program sizes its scratch once, for its longest chunk and all heads; its last chunk is short (and split over CTAs)."""
+    n, D, Hkv = 3000, 128, 2
+    _, k, v, length = au.make(1, 32, Hkv, D, n + 8, "bf16", "nhd", 1, 4, [n])
+    cache = api.KVCache(k, v, length)
+    ws = cache.workspace(32, 2048)
+    for T, Hq in ((21, 32), (130, 8), (1, 2)):
+        q = au.make(1, Hq, Hkv, D, 8, "bf16", "hnd", T, T, [8])[0]
+        out, lse = torch.empty(1, T, Hq, D, dtype=q.dtype, device="cuda"), torch.empty(1, T, Hq, device="cuda")
+        api.si_attn_prefill(cache, q, 0, 0, 0.09, out, lse, ws)
+        ref = au.reference(q, k, v, [n], 0, 0, 0.09)
+        au.check_out(out, ref, "bf16", D)
+        au.check_lse(lse, ref, D)

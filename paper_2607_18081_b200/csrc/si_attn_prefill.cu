@@ -27,6 +27,10 @@ constexpr int kThreads = 384;
 // (2 x 200 + 104 = 3 x 168), so that a row's 128 scores stay in registers.
 constexpr int kRegsSoft = 200, kRegsService = 104;
 constexpr float kLazy = 8.f;
+// An exponent is x * scale2 - base2 in one fused step, with base2 the rounded product of the maximum: all p of a row carry the
+// same factor of 2^(what was rounded off), which cancels, and which is near 1 up to here.  Beyond, where it could reach any
+// size (2^(+-4) at 2^27), the maximum is taken from the scores first.
+constexpr float kFar = 65536.f;
 
 template <int D> struct Cfg {
     static constexpr int kBytes = kTile * D * 2;            // a tile of queries, keys or values
@@ -40,7 +44,8 @@ __device__ __forceinline__ uint32_t first_bits(int n) { return n >= 32 ? 0xFFFFF
 
 struct Bars { uint64_t q, full[4], empty[4], s[2], p[2][2], o[2], dirty, clean; uint32_t tmem; int failed; };
 
-// Keys split over P.n CTAs per block of queries (1: not split); parts: [split][block][tile][row], values and {maximum, sum}.
+// Keys split over P.n CTAs per block of queries (1: not split); parts: [split][block][tile][row], values and {maximum, sum}, the
+// maximum unscaled.
 struct SplitArgs { int n, blocks; float *o; float2 *ml; };
 
 // NEG: the scale is negative; the scores are then turned around and |scale| is used.
@@ -201,10 +206,14 @@ prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
         float m = -INFINITY, base2 = 0.f, l = 0.f;
         bool ok = true;
         if (t < tiles) {
+            // what was rounded off m * scale2, as far as the p of the row carry it
+            auto off_by = [&](float m, float base2) { return m == -INFINITY || fabsf(base2) > kFar ? 0.f : __fmaf_rn(m, A.scale2, -base2); };
             // one key tile; MASKED: some row of the tile does not see some key of it (a template argument: joining two versions of
-            // a row's 128 registers after a branch costs more than the maximum)
-            auto step = [&](auto masked, int j, int key0) {
-                constexpr bool MASKED = decltype(masked)::value;
+            // a row's 128 registers after a branch costs more than the maximum).  FAR: some row's base2 may be beyond kFar; a step
+            // of the near kind that comes to one leaves everything as it is and returns false, and the rest of the tiles is worked
+            // on in a loop of its own (the third version inside the first loop: 3 % slower, 505 -> 521 us for 8192 tokens).
+            auto step = [&](auto masked, auto farther, int j, int key0) {
+                constexpr bool MASKED = decltype(masked)::value, FAR = decltype(farther)::value;
                 uint32_t x[4][32];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) tmem_ld32(ts + c * 32, x[c]);
@@ -238,7 +247,9 @@ prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
                 const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
                 const bool grow = top > m && (top - m) * A.scale2 > kLazy;
                 if (__any_sync(0xFFFFFFFFu, grow)) {
-                    const float m2 = grow ? top : m, b2 = m2 == -INFINITY ? 0.f : m2 * A.scale2, f = grow ? ex2(m == -INFINITY ? -INFINITY : base2 - b2) : 1.f;
+                    if (!FAR && __any_sync(0xFFFFFFFFu, grow && fabsf(top * A.scale2) > kFar)) return false;
+                    const float m2 = grow ? top : m, b2 = m2 == -INFINITY ? 0.f : m2 * A.scale2;
+                    const float f = !grow ? 1.f : m == -INFINITY ? 0.f : ex2((m - m2) * A.scale2 + (off_by(m2, b2) - off_by(m, base2)));
                     m = m2; base2 = b2; l *= f;
                     if (j > 0) {
 #pragma unroll 1
@@ -251,7 +262,8 @@ prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
                         }
                     }
                 }
-                const f32x2 sc = two(A.scale2, A.scale2), bs = two(-base2, -base2);
+                const bool far = FAR && fabsf(base2) > kFar;
+                const f32x2 sc = two(A.scale2, A.scale2), bs = far ? two(0.f, 0.f) : two(-base2, -base2), top2 = far ? two(-m, -m) : two(0.f, 0.f);
                 f32x2 sum[4] = {};
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
@@ -259,7 +271,9 @@ prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
 #pragma unroll
                     for (int k = 0; k < 32; ++k) {
                         const int c = half * 64 + 2 * k;
-                        f32x2 p = fma2(two(x[c / 32][c % 32], x[c / 32][c % 32 + 1]), sc, bs);
+                        f32x2 p = two(x[c / 32][c % 32], x[c / 32][c % 32 + 1]);
+                        if (FAR) p = add2(p, top2);
+                        p = fma2(p, sc, bs);
                         float p0, p1;
                         untwo(p, p0, p1);
                         p0 = ex2(p0); p1 = ex2(p1);
@@ -275,14 +289,22 @@ prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
                 float s0, s1;
                 untwo(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])), s0, s1);
                 l += s0 + s1;
+                return true;
             };
-            for (int j = 0; j < keys.n; ++j) {
+            int j = 0;
+            auto scores_of = [&](int j) {
                 ok = __all_sync(0xFFFFFFFFu, mbar_wait(&B->s[t], j & 1, kWait));
-                if (!ok) break;
-                tc_fence_after();
+                if (ok) tc_fence_after();
+                return ok;
+            };
+            for (; j < keys.n && scores_of(j); ++j) {
                 const int key0 = keys.key0(j);
-                if (key0 + kTile - 1 <= smin && (key0 > lo_max || key0 + kTile <= A.n_sink)) step(std::false_type(), j, key0);
-                else step(std::true_type(), j, key0);
+                if (key0 + kTile - 1 <= smin && (key0 > lo_max || key0 + kTile <= A.n_sink)) { if (!step(std::false_type(), std::false_type(), j, key0)) break; }
+                else if (!step(std::true_type(), std::false_type(), j, key0)) break;
+            }
+            if (ok && j < keys.n) {
+                do step(std::true_type(), std::true_type(), j, keys.key0(j));
+                while (++j < keys.n && scores_of(j));
             }
             pdl_launch();
             if (!ok) *failed = 1;
@@ -291,18 +313,20 @@ prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
                 tc_fence_after();
             }
             if (P.n > 1) {
+                // parts are relative to the maximum itself
+                const float c0 = ex2(-off_by(m, base2));
                 const long long part = (((long long)split * P.blocks + blockIdx.x) * 2 + t) * kTile + row;
 #pragma unroll
                 for (int c = 0; c < D / 32; ++c) {
                     uint32_t o[32] = {};
                     if (keys.n > 0) { tmem_ld32(to + c * 32, o); tmem_wait_ld(o); }
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) *reinterpret_cast<uint4 *>(P.o + part * D + c * 32 + k * 4) = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+                    for (int k = 0; k < 32; k += 4)
+                        *reinterpret_cast<float4 *>(P.o + part * D + c * 32 + k) = make_float4(__uint_as_float(o[k]) * c0, __uint_as_float(o[k + 1]) * c0,
+                                                                                              __uint_as_float(o[k + 2]) * c0, __uint_as_float(o[k + 3]) * c0);
                 }
-                P.ml[part] = make_float2(l < 0.5f ? -INFINITY : base2, l);
+                P.ml[part] = make_float2(m, l * c0);
             } else {
-                // a row that sees something has its largest p at 1 or above; less than that is a row without a visible entry
-                if (l < 0.5f) l = 0.f;
                 const float inv = l == 0.f ? 0.f : 1.f / l;
                 const long long r = ((long long)b * A.T + i) * A.Hq + hq;
                 // through the tile's query buffer (its last product is done), in the layout of the boxes the queries came in, and
@@ -384,7 +408,7 @@ __global__ void __launch_bounds__(256) prefill_join_kernel(const TcArgs A, const
     for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
 #pragma unroll
     for (int k = 0; k < kMaxSplits / 32; ++k) {
-        const float f = ml[k].x == -INFINITY ? 0.f : ex2(ml[k].x - top);
+        const float f = ml[k].x == -INFINITY ? 0.f : ex2((ml[k].x - top) * A.scale2);
         sh_f[warp][k * 32 + lane] = f;
         l += ml[k].y * f;
     }
@@ -409,7 +433,7 @@ __global__ void __launch_bounds__(256) prefill_join_kernel(const TcArgs A, const
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
     if (side == 0) *reinterpret_cast<uint2 *>(A.out + r * D + col) = make_uint2(pack2<DT>(acc.x * inv, acc.y * inv), pack2<DT>(acc.z * inv, acc.w * inv));
-    if (lane == 0 && A.lse) A.lse[r] = l == 0.f ? -INFINITY : (top + log2f(l)) / kLog2e;
+    if (lane == 0 && A.lse) A.lse[r] = l == 0.f ? -INFINITY : (top * A.scale2 + log2f(l)) / kLog2e;
 }
 
 // Blocks of queries, and over how many CTAs their keys are split: with fewer blocks than half the SMs as many as fit one

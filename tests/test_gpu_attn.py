@@ -355,3 +355,56 @@ def test_one_workspace_for_long_and_short_chunks_and_fewer_heads(api):
         ref = au.reference(q, k, v, [n], 0, 0, 0.09)
         au.check_out(out, ref, "bf16", D)
         au.check_lse(lse, ref, D)
+
+
+def _whole_numbers(B, Hq, Hkv, D, n, T, dtype, seed, lift=0, step=False):
+    """Queries and keys of small whole numbers: every score is exact in fp32.  lift: a common 2^20 in all scores of all queries;
+    step: the scores also grow by one from key to key."""
+    g = torch.Generator().manual_seed(seed)
+    q, k = torch.randint(-2, 3, (B, T, Hq, D), generator=g).float(), torch.randint(-2, 3, (B, Hkv, n, D), generator=g).float()
+    if lift:
+        q[..., :3], k[..., 0] = torch.tensor([1024.0, 16.0, 1.0]), 1024.0
+        j = torch.arange(n) if step else torch.zeros(n)
+        k[..., 1], k[..., 2] = j // 16, j % 16
+    v = torch.randn(B, Hkv, n, D, generator=g)
+    dt = au.TDT[dtype]
+    return q.to(dt).cuda(), k.to(dt).cuda(), v.to(dt).cuda(), torch.full((B,), n, dtype=torch.int32, device="cuda")
+
+
+def _check_exact_scores(out, lse, ref, dtype, reach_of=60.0):
+    """Bounds where the scores carry no error: p is relative to the type (u) and to the exponent's difference (8 e * reach_of; what
+    lies further below the maximum is nothing), sums n e, the result rounded once more; lse 4 e of itself."""
+    u, E = au.U[dtype], au.E
+    rel = 8 * E * reach_of + (ref["n"] + 8) * E
+    bound = (u * np.abs(ref["out"]) + (u + rel[..., None]) * ref["reach"]) * 1.01
+    if dtype == "f16":
+        bound += (ref["n"][..., None] * 5.0 + 1.0) * 2.0 ** -25
+    assert np.all(np.abs(au.f64(out) - ref["out"]) <= bound)
+    assert np.all(np.abs(au.f64(lse) - ref["lse"]) <= 4 * E * np.abs(ref["lse"]) + (ref["n"] + 8) * E)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("D,n,T", [(128, 390, 150), (64, 3000, 20), (64, 300, 300)])     # the second: keys split over CTAs
+@pytest.mark.parametrize("scale", [1e6, -1e6, 3e9, 1e30])
+def test_scores_far_beyond_the_mantissa(api, D, n, T, scale, dtype):
+    """Scaled scores above 2^24, where neighbouring fp32 numbers are more than one apart: the softmax picks the largest scores."""
+    q, k, v, length = _whole_numbers(1, 4, 2, D, n, T, dtype, n)
+    out, lse = _prefill(api, q, k, v, length, 0, 0, scale)
+    ref = au.reference(q, k, v, [n], 0, 0, scale)
+    _check_exact_scores(out, lse, ref, dtype)
+    o1, l1 = torch.empty(1, 4, D, dtype=q.dtype, device="cuda"), torch.empty(1, 4, device="cuda")
+    cache = api.KVCache(k, v, length)
+    api.si_attn_decode(cache, q[:, -1].contiguous(), None, None, None, 0, 0, scale, o1, l1, 0, cache.workspace(4, 1))
+    last = {x: ref[x][:, -1:] for x in ("out", "reach", "lse", "n")}
+    _check_exact_scores(o1[:, None], l1[:, None], last, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("D,n,T", [(128, 700, 200), (64, 3000, 20)])
+@pytest.mark.parametrize("scale", [0.04, 0.04332, 0.05, 0.5, -0.04333])
+@pytest.mark.parametrize("step", [False, True])
+def test_scores_with_a_large_common_part(api, D, n, T, scale, step, dtype):
+    """All scores lie near 2^20 * scale; what they differ by decides.  With `step` the running maximum grows from tile to tile."""
+    q, k, v, length = _whole_numbers(1, 4, 2, D, n, T, dtype, n + 1, lift=1, step=step)
+    out, lse = _prefill(api, q, k, v, length, 0, 0, scale)
+    _check_exact_scores(out, lse, au.reference(q, k, v, [n], 0, 0, scale), dtype)

@@ -158,3 +158,39 @@ def test_evict_reports_lengths_outside_the_capacity(api):
         api.si_kv_evict(c, c, torch.zeros(1, dtype=torch.int32, device="cuda"), n_new, 4, 0, 0, None, None, c.workspace(0, 0), status)
         torch.cuda.synchronize()
         assert status.item() == api.SI_ERR_OUT_OF_RANGE
+
+
+def _evict_fast(w, budget, n_sink, n_recent):
+    """ao.evict for entry j at position j without NaN, in numpy (the oracle's own takes minutes at millions of entries)."""
+    n = len(w)
+    rank = w.astype(np.float64)
+    rank[:n_sink] = rank[n - n_recent:] = np.inf
+    kept = np.zeros(n, bool)
+    kept[np.argsort(-rank, kind="stable")[:budget]] = True
+    src = np.where(kept[:budget], np.arange(budget), -1)
+    src[src < 0] = budget + np.nonzero(kept[budget:])[0]
+    return src
+
+
+@pytest.mark.parametrize("D,n,budget", [(128, 4_400_000, 4_300_001), (64, 8_500_000, 8_400_000), (128, 3000, 777)])
+def test_evict_with_budgets_of_millions(api, D, n, budget):
+    """More slots than 65535 blocks of the moving kernel hold."""
+    rng = np.random.default_rng(budget)
+    w = np.floor(rng.random(n) * 1e5).astype(np.float32)
+    want = _evict_fast(w, budget, 16, 1000 if n > 5000 else 100)
+    if n <= 5000:
+        assert np.array_equal(want, ao.evict(w, np.arange(n), n - 1, budget, 16, 100))
+    k = torch.arange(n, dtype=torch.int32, device="cuda").view(1, 1, n, 1).expand(1, 1, n, D // 2).contiguous().view(torch.bfloat16)
+    v = (torch.arange(n, dtype=torch.int32, device="cuda") ^ 0x5A5A).view(1, 1, n, 1).expand(1, 1, n, D // 2).contiguous().view(torch.bfloat16)
+    length, len_out = torch.tensor([n], dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    src = api.KVCache(k, v, length, None, torch.from_numpy(w).cuda().view(1, 1, n))
+    dk, dv = (torch.zeros(1, 1, budget, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    dst = api.KVCache(dk, dv, len_out, torch.zeros(1, 1, budget, dtype=torch.int32, device="cuda"), torch.zeros(1, 1, budget, device="cuda"))
+    api.si_kv_evict(src, dst, None, 0, budget, 16, 1000 if n > 5000 else 100, None, len_out, src.workspace(0, 0))
+    torch.cuda.synchronize()
+    at = torch.from_numpy(want).cuda()
+    assert len_out.item() == budget and torch.equal(dst.pos[0, 0].long(), at)
+    assert torch.equal(dst.weight[0, 0], src.weight[0, 0, at])
+    for d, x in ((dk, 0), (dv, 0x5A5A)):
+        got = d[0, 0].view(torch.int32)
+        assert all(torch.equal(got[:, c].long(), at ^ x) for c in (0, 5, D // 2 - 1))

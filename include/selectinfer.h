@@ -476,7 +476,7 @@ int si_attn_prefill(const si_kv_t *kv, const void *q, long long q_seq_stride, lo
 /* The attention every entry received from those T queries, added to kv->weight (the caller zeroes it for a new
  * prompt): weight[b, h, j] += sum over the T queries i that see j and the G query heads of exp(scale * (q_i . k_j)
  * - lse_i).  lse: device float32 [n_seqs, T, n_q_heads] from si_attn_prefill with the same arguments.  T may be the
- * whole prompt or only its last few positions.  Needs kv->weight and kv->pos == NULL.  Sums are taken in a fixed
+ * whole prompt or only its last few positions.  A query whose lse is NaN makes the weight of every entry it sees NaN.  Needs kv->weight and kv->pos == NULL.  Sums are taken in a fixed
  * order: repeated calls add the same bits. */
 int si_attn_weights(const si_kv_t *kv, const void *q, long long q_seq_stride, long long q_tok_stride, int T,
                     int n_q_heads, int window, int n_sink, float scale, const float *lse, void *workspace,

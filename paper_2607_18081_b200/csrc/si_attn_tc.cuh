@@ -56,11 +56,11 @@ __device__ __forceinline__ f32x2 two(uint32_t lo, uint32_t hi) { f32x2 r; asm("m
 __device__ __forceinline__ void untwo(f32x2 v, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
 __device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) { f32x2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
 __device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) { f32x2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
-__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) { f32x2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
 
 // 2^x for a pair on the multiply-add units: x = n + f with n the nearest integer (added to and taken from 1.5 * 2^23, whose low
 // bits then hold n), 2^f by its polynomial of least relative error on [-1/2, 1/2] of degree 5 (2.1e-7 in fp32, computed for
-// this file by a Remez exchange), n added to the exponent field.  x below -126 counts as -126.  The exponential unit does 16
+// this file by a Remez exchange), n added to the exponent field.  x below -126 counts as -126, and so does NaN: it is for
+// numbers only (a form that keeps NaN, with 2^n as a factor, made the weights of a prompt 112.6 -> 114.1 us).  The exponential unit does 16
 // values per clock and SM, which a tile's softmax is otherwise bound by.
 __device__ __forceinline__ f32x2 ex2_poly(f32x2 x) {
     float a, b;

@@ -35,7 +35,7 @@ template <int D> struct Cfg {
     static constexpr int kStages = D == 128 ? 2 : 4;     // ring of query tiles
     static constexpr int kSmem = (4 + kStages) * kBytes + 1024 + 512 + kLse * kTile * 4 + 2 * kKeys * 4;
 };
-struct Bars { uint64_t kfull[2], kempty[2], full[4], empty[4], s[kBufs], free[kBufs], lfull[kLse], lempty[kLse]; uint32_t tmem; };
+struct Bars { uint64_t kfull[2], kempty[2], full[4], empty[4], s[kBufs], free[kBufs], lfull[kLse], lempty[kLse]; uint32_t tmem; int odd[kLse]; };
 
 struct WeightArgs {
     const float *lse;
@@ -198,7 +198,8 @@ weights_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
         }
     } else if (warp == 18) {
         // lse of the 128 packed rows in base 2, negated; rows that do not exist or see nothing get -inf, so that they add
-        // exp2(-inf) = 0.  The next tile's values are on their way while this one's place is waited for.
+        // exp2(-inf) = 0.  Where an lse is neither a number nor -inf (a query or a key that is not a number: the scores are not
+        // either), the tile says so and is left to the exponential unit, which keeps NaN.  The next tile's values are on their way while this one's place is waited for.
         int it = 0;
         bool ok = true;
         float v[4];
@@ -214,8 +215,13 @@ weights_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
         for (int g = g0; g < g1; ++g, ++it) {
             const int st = it % kLse;
             float w[4];
+            bool odd = false;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) w[k] = v[k] == -INFINITY ? -INFINITY : -v[k] * kLog2e;
+            for (int k = 0; k < 4; ++k) {
+                w[k] = v[k] == -INFINITY ? -INFINITY : -v[k] * kLog2e;
+                odd |= !(v[k] < INFINITY);
+            }
+            odd = __any_sync(0xFFFFFFFFu, odd);
             if (g + 1 < g1) {
                 if (g + 1 == cur.start + cur.q.n) next_item(A, W, cur);
                 fetch(cur, g + 1);
@@ -225,7 +231,7 @@ weights_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
 #pragma unroll
             for (int k = 0; k < 4; ++k) lse2[st * kTile + k * 32 + lane] = w[k];
             __syncwarp();
-            if (lane == 0) mbar_arrive(&B->lfull[st]);
+            if (lane == 0) { B->odd[st] = odd; mbar_arrive(&B->lfull[st]); }
         }
     } else if (warp < 16) {
         const int buf = warp >> 2, parity = buf >> 1, half = buf & 1, row = (warp & 3) * 32 + lane;
@@ -251,7 +257,7 @@ weights_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
                 const int s0 = shift + (cur.q.first + g - cur.start) * A.R;
                 const bool sink = key < A.n_sink || !A.window;
                 const int c_lo = min(max(key - s0, 0), kTile) * A.G, c_hi = sink ? kTile : (int)min(max((long long)key + A.window - s0, 0ll), (long long)kTile) * A.G;
-                const bool open = __all_sync(0xFFFFFFFFu, c_lo == 0 && c_hi >= kTile);
+                const bool open = __all_sync(0xFFFFFFFFu, c_lo == 0 && c_hi >= kTile) && !B->odd[st];
                 f32x2 part[4] = {};
                 auto quarter = [&](auto masked, int qq) {
                     constexpr bool MASKED = decltype(masked)::value;

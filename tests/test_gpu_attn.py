@@ -408,3 +408,22 @@ def test_scores_with_a_large_common_part(api, D, n, T, scale, step, dtype):
     q, k, v, length = _whole_numbers(1, 4, 2, D, n, T, dtype, n + 1, lift=1, step=step)
     out, lse = _prefill(api, q, k, v, length, 0, 0, scale)
     _check_exact_scores(out, lse, au.reference(q, k, v, [n], 0, 0, scale), dtype)
+
+
+@pytest.mark.parametrize("D,dtype", [(128, "bf16"), (64, "f16")])
+def test_accumulated_weights_keep_nan(api, D, dtype):
+    """A query that is not a number makes the weight of every entry it sees one too, in every tile and column alike, and of no other."""
+    B, T, Hq, Hkv, n = 1, 300, 8, 2, 700
+    q, k, v, length = au.make(B, Hq, Hkv, D, n + 3, dtype, "hnd", T, 21, [n])
+    ref = au.reference(q, k, v, [n], 0, 0, 0.1)
+    lse = torch.from_numpy(ref["lse"].astype(np.float32)).cuda()
+    for i, hq in ((64, 0), (64, 1), (68, 4), (77, 2), (299, 7), (0, 5), (192, 0), (131, 3)):
+        qb, lb = q.clone(), lse.clone()
+        qb[0, i, hq, 5], lb[0, i, hq] = float("nan"), float("nan")
+        weight = torch.zeros(B, Hkv, n + 3, device="cuda")
+        cache = api.KVCache(k, v, length, None, weight)
+        api.si_attn_weights(cache, qb, 0, 0, 0.1, lb, cache.workspace(Hq, T))
+        got, seen = weight.cpu().numpy(), n - T + i + 1
+        h = hq // (Hq // Hkv)
+        assert np.isnan(got[0, h, :seen]).all(), (i, hq, np.nonzero(~np.isnan(got[0, h, :seen]))[0][:5])
+        assert np.isfinite(got[0, h, seen:]).all() and np.isfinite(got[0, 1 - h]).all()

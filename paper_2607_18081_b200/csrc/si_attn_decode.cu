@@ -471,7 +471,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) decode_kernel(const DecodeAr
 #pragma unroll
                 for (int v = 0; v < kWarps; ++v) {
                     const float mv = ml[(v * HB + head) * 2];
-                    sum += mv == -INFINITY ? 0.f : ml[(v * HB + head) * 2 + 1] * ex2(mv - top);
+                    sum += ml[(v * HB + head) * 2 + 1] * (mv == -INFINITY ? 1.f : ex2(mv - top));     // without a maximum: 0, or NaN (NaN scores only)
                 }
 #pragma unroll
                 for (int v = 0; v < kWarps / 2; ++v) {

@@ -427,3 +427,23 @@ def test_accumulated_weights_keep_nan(api, D, dtype):
         h = hq // (Hq // Hkv)
         assert np.isnan(got[0, h, :seen]).all(), (i, hq, np.nonzero(~np.isnan(got[0, h, :seen]))[0][:5])
         assert np.isfinite(got[0, h, seen:]).all() and np.isfinite(got[0, 1 - h]).all()
+
+
+@pytest.mark.parametrize("D,Hq,Hkv", [(128, 8, 2), (64, 3, 1), (128, 20, 1)])
+@pytest.mark.parametrize("n,bad", [(1, [0]), (17, [16]), (40, list(range(16, 40))), (5000, [4999]), (5000, list(range(2000, 2600)))])
+def test_decode_keeps_nan(api, D, Hq, Hkv, n, bad):
+    """Visible keys that are not numbers: the output, lse and every weight of their head are not either; other heads as ever."""
+    q, k, v, length = au.make(2, Hq, Hkv, D, n + 2, "bf16", "hnd", 1, 31, [n, n])
+    k[1, 0, bad] = float("nan")
+    weight = torch.zeros(2, Hkv, n + 2, device="cuda")
+    cache = api.KVCache(k, v, length, None, weight)
+    out, lse = torch.empty(2, Hq, D, dtype=q.dtype, device="cuda"), torch.empty(2, Hq, device="cuda")
+    api.si_attn_decode(cache, q[:, 0], None, None, None, 0, 0, 0.1, out, lse, api.SI_FLAG_ACC_WEIGHT, cache.workspace(Hq, 1))
+    G = Hq // Hkv
+    assert torch.isnan(out[1, :G]).all() and torch.isnan(weight[1, 0, :n]).all()
+    assert torch.isnan(lse[1, :G]).all()
+    for t in (out[0], out[1, G:], lse[0], lse[1, G:], weight[0], weight[1, 1:]):
+        assert torch.isfinite(t).all()
+    o, l = _prefill(api, q, k, v, length, 0, 0, 0.1)
+    assert torch.isnan(o[1, 0, :G]).all() and torch.isnan(l[1, 0, :G]).all()
+    assert torch.isfinite(o[0]).all() and torch.isfinite(l[0]).all() and torch.isfinite(l[1, 0, G:]).all()

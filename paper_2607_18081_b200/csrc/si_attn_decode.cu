@@ -592,8 +592,9 @@ __global__ void __launch_bounds__(kJoinThreads, 3) decode_join_kernel(const Deco
             for (int g = 0; g < HB; g += 2) {
                 if (g >= A.GS || gb * HB + g >= A.G) break;
                 const float2 y = gb == 0 ? x[i][g / 2] : *reinterpret_cast<const float2 *>(more + g);
-                sum += ex2(y.x - sh_done[gb * HB + g].x) * sh_done[gb * HB + g].y;         // a hidden entry's score is -inf
-                if (gb * HB + g + 1 < A.G) sum += ex2(y.y - sh_done[gb * HB + g + 1].x) * sh_done[gb * HB + g + 1].y;
+                // a hidden entry's score is -inf: it receives nothing, from a head whose sum is NaN neither
+                if (y.x != -INFINITY) sum += ex2(y.x - sh_done[gb * HB + g].x) * sh_done[gb * HB + g].y;
+                if (gb * HB + g + 1 < A.G && y.y != -INFINITY) sum += ex2(y.y - sh_done[gb * HB + g + 1].x) * sh_done[gb * HB + g + 1].y;
             }
         }
         weight[j] = j == w.n_old ? sum : old[i] + sum;

@@ -447,3 +447,18 @@ def test_decode_keeps_nan(api, D, Hq, Hkv, n, bad):
     o, l = _prefill(api, q, k, v, length, 0, 0, 0.1)
     assert torch.isnan(o[1, 0, :G]).all() and torch.isnan(l[1, 0, :G]).all()
     assert torch.isfinite(o[0]).all() and torch.isfinite(l[0]).all() and torch.isfinite(l[1, 0, G:]).all()
+
+
+def test_decode_with_nan_adds_nothing_to_hidden_entries(api):
+    n, window, n_sink, D = 700, 50, 3, 64
+    for positions in (False, True):
+        q, k, v, length = au.make(1, 4, 1, D, n + 4, "f16", "hnd", 1, 41, [n])
+        k[0, 0, n - 7] = float("nan")
+        weight = torch.zeros(1, 1, n + 4, device="cuda")
+        pos = torch.arange(n + 4, dtype=torch.int32, device="cuda").view(1, 1, -1).contiguous() if positions else None
+        cache = api.KVCache(k, v, length, pos, weight)
+        out = torch.empty(1, 4, D, dtype=q.dtype, device="cuda")
+        api.si_attn_decode(cache, q[:, 0], length - 1, None, None, window, n_sink, 0.1, out, None, api.SI_FLAG_ACC_WEIGHT, cache.workspace(4, 1))
+        got = weight[0, 0].cpu().numpy()
+        assert np.isnan(got[:n_sink]).all() and np.isnan(got[n - window:n]).all()
+        assert (got[n_sink:n - window] == 0).all() and (got[n:] == 0).all()

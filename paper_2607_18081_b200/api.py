@@ -458,8 +458,10 @@ class KVCache:
                                       ("weight", weight, (B, H, cap), torch.float32)):
             if t is not None and (tuple(t.shape) != shape or t.dtype != dtype):
                 raise ValueError(f"{name}: expected {dtype} of shape {shape}")
-        if not (k.is_cuda and v.is_cuda):
-            raise ValueError("expected CUDA tensors")
+        self.device = k.get_device()             # the number of the CUDA device (-1: host memory)
+        for name, t in (("k", k), ("v", v), ("length", length), ("pos", pos), ("weight", weight)):
+            if t is not None and (not t.is_cuda or t.get_device() != self.device):
+                raise ValueError(f"{name}: expected a CUDA tensor on the device of k")
         self.k, self.v, self.length, self.pos, self.weight = k, v, length, pos, weight
         self.n_seqs, self.n_kv_heads, self.capacity, self.head_dim, self.dtype = B, H, cap, D, k.dtype
         self.desc = _KvDesc(k.data_ptr(), v.data_ptr(), _dp(weight).value, _dp(pos).value, _dp(length).value, k.stride(0),
@@ -471,12 +473,13 @@ class KVCache:
         return torch.empty(max(si_kv_workspace_bytes(self, n_q_heads, T), 256), dtype=torch.uint8, device=self.k.device)
 
 
-def _ptr(t, name: str, shape, dtype):
-    """Address of a contiguous CUDA tensor of this shape and type (None -> NULL)."""
+def _ptr(t, name: str, cache, shape, dtype):
+    """Address of a contiguous tensor of this shape and type on the cache's device (None -> NULL)."""
     if t is None:
         return None
-    if t.shape != shape or t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"{name}: expected a contiguous CUDA tensor, {dtype} of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    if t.shape != shape or t.dtype != dtype or t.get_device() != cache.device or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous tensor on cuda:{cache.device}, {dtype} of shape {tuple(shape)}, got {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
@@ -485,22 +488,25 @@ def _heads(t, name: str, cache, heads: int):
     shape, stride = t.shape, t.stride()
     if t.dtype != cache.dtype or shape[0] != cache.n_seqs or shape[-2] != heads or shape[-1] != cache.head_dim:
         raise ValueError(f"{name}: expected {cache.dtype} [{cache.n_seqs}, ..., {heads}, {cache.head_dim}], got {t.dtype} {tuple(shape)}")
-    if not t.is_cuda or stride[-1] != 1 or (stride[-2] != cache.head_dim and heads > 1):
-        raise ValueError(f"{name}: expected a CUDA tensor whose heads are contiguous")
+    if t.get_device() != cache.device or stride[-1] != 1 or (stride[-2] != cache.head_dim and heads > 1):
+        raise ValueError(f"{name}: expected a tensor on cuda:{cache.device} whose heads are contiguous")
     return t.data_ptr()
 
 
-def _ws(t):
+def _ws(t, cache):
     if t is None:
         return None, 0
-    if not t.is_cuda or not t.is_contiguous():
-        raise ValueError("expected a contiguous CUDA tensor")
+    if t.get_device() != cache.device or not t.is_contiguous():
+        raise ValueError(f"workspace: expected a contiguous tensor on cuda:{cache.device}")
     return t.data_ptr(), t.numel() * t.element_size()
 
 
-def _on(stream):
+def _on(stream, cache):
+    # the device of the cache has to be current, as for a store
+    if torch.cuda.current_device() != cache.device or (stream is not None and stream.device_index != cache.device):
+        raise ValueError(f"the cache is on cuda:{cache.device}: that device has to be current, and the stream one of it")
     # the raw handle of the current stream: building a Stream object takes 3 us of a 15 us call
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) if stream is None else stream.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(cache.device) if stream is None else stream.cuda_stream
 
 
 def si_kv_workspace_bytes(cache: KVCache, n_q_heads: int, T: int) -> int:
@@ -512,19 +518,19 @@ def si_kv_workspace_bytes(cache: KVCache, n_q_heads: int, T: int) -> int:
 def si_attn_prefill(cache: KVCache, q, window: int, n_sink: int, scale: float, out, lse, workspace, status=None, stream=None) -> None:
     """q, out: [n_seqs, T, n_q_heads, head_dim] (q may be strided); lse: float32 [n_seqs, T, n_q_heads] or None."""
     _, T, hq, _ = shape = q.shape
-    ws, ws_bytes = _ws(workspace)
+    ws, ws_bytes = _ws(workspace, cache)
     _check(_lib.si_attn_prefill(cache.ref, _heads(q, "q", cache, hq), q.stride(0), q.stride(1), T, hq, window, n_sink, scale,
-                                _ptr(out, "out", shape, q.dtype), _ptr(lse, "lse", shape[:3], torch.float32), ws, ws_bytes,
-                                _ptr(status, "status", (1,), torch.int32), _on(stream)), "si_attn_prefill")
+                                _ptr(out, "out", cache, shape, q.dtype), _ptr(lse, "lse", cache, shape[:3], torch.float32), ws, ws_bytes,
+                                _ptr(status, "status", cache, (1,), torch.int32), _on(stream, cache)), "si_attn_prefill")
 
 
 def si_attn_weights(cache: KVCache, q, window: int, n_sink: int, scale: float, lse, workspace, status=None, stream=None) -> None:
     """Adds to cache.weight; q as for si_attn_prefill, lse: float32 [n_seqs, T, n_q_heads] from it."""
     _, T, hq, _ = shape = q.shape
-    ws, ws_bytes = _ws(workspace)
+    ws, ws_bytes = _ws(workspace, cache)
     _check(_lib.si_attn_weights(cache.ref, _heads(q, "q", cache, hq), q.stride(0), q.stride(1), T, hq, window, n_sink, scale,
-                                _ptr(lse, "lse", shape[:3], torch.float32), ws, ws_bytes, _ptr(status, "status", (1,), torch.int32),
-                                _on(stream)), "si_attn_weights")
+                                _ptr(lse, "lse", cache, shape[:3], torch.float32), ws, ws_bytes, _ptr(status, "status", cache, (1,), torch.int32),
+                                _on(stream, cache)), "si_attn_weights")
 
 
 def si_attn_decode(cache: KVCache, q, q_pos, k_new, v_new, window: int, n_sink: int, scale: float, out, lse, flags: int,
@@ -538,22 +544,24 @@ def si_attn_decode(cache: KVCache, q, q_pos, k_new, v_new, window: int, n_sink: 
             raise ValueError("k_new and v_new: [n_seqs, n_kv_heads, head_dim] of equal strides, both or neither")
         kp, vp = _heads(k_new, "k_new", cache, cache.n_kv_heads), _heads(v_new, "v_new", cache, cache.n_kv_heads)
         new_stride = k_new.stride(0)
-    ws, ws_bytes = _ws(workspace)
-    _check(_lib.si_attn_decode(cache.ref, _heads(q, "q", cache, hq), q.stride(0), hq, _ptr(q_pos, "q_pos", (cache.n_seqs,), torch.int32),
-                               kp, vp, new_stride, window, n_sink, scale, _ptr(out, "out", shape, q.dtype),
-                               _ptr(lse, "lse", shape[:2], torch.float32), flags, ws, ws_bytes,
-                               _ptr(status, "status", (1,), torch.int32), _on(stream)), "si_attn_decode")
+    ws, ws_bytes = _ws(workspace, cache)
+    _check(_lib.si_attn_decode(cache.ref, _heads(q, "q", cache, hq), q.stride(0), hq, _ptr(q_pos, "q_pos", cache, (cache.n_seqs,), torch.int32),
+                               kp, vp, new_stride, window, n_sink, scale, _ptr(out, "out", cache, shape, q.dtype),
+                               _ptr(lse, "lse", cache, shape[:2], torch.float32), flags, ws, ws_bytes,
+                               _ptr(status, "status", cache, (1,), torch.int32), _on(stream, cache)), "si_attn_decode")
 
 
 def si_kv_evict(src: KVCache, dst: KVCache, q_pos, n_new: int, budget: int, n_sink: int, n_recent: int, kept, len_out,
                 workspace, status=None, stream=None) -> None:
     """dst is src: in place.  kept: int32 [n_seqs, n_kv_heads, budget] or None; len_out: int32 [n_seqs] or None."""
+    if dst.device != src.device:
+        raise ValueError("both caches have to be on one device")
     seqs = (src.n_seqs,)
-    ws, ws_bytes = _ws(workspace)
-    _check(_lib.si_kv_evict(src.ref, dst.ref, _ptr(q_pos, "q_pos", seqs, torch.int32), n_new, budget, n_sink, n_recent,
-                            _ptr(kept, "kept", (src.n_seqs, src.n_kv_heads, budget), torch.int32),
-                            _ptr(len_out, "len_out", seqs, torch.int32), ws, ws_bytes,
-                            _ptr(status, "status", (1,), torch.int32), _on(stream)), "si_kv_evict")
+    ws, ws_bytes = _ws(workspace, src)
+    _check(_lib.si_kv_evict(src.ref, dst.ref, _ptr(q_pos, "q_pos", src, seqs, torch.int32), n_new, budget, n_sink, n_recent,
+                            _ptr(kept, "kept", src, (src.n_seqs, src.n_kv_heads, budget), torch.int32),
+                            _ptr(len_out, "len_out", src, seqs, torch.int32), ws, ws_bytes,
+                            _ptr(status, "status", src, (1,), torch.int32), _on(stream, src)), "si_kv_evict")
 
 
 # ------------------------------------------------------------------------- owner object

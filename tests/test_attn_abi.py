@@ -174,3 +174,78 @@ def test_a_short_chunk_passes_with_the_workspace_of_a_long_one(api):
         for T, hq in ((1, 32), (45, 32), (200, 8), (512, 32)):
             assert _prefill(api, kv, T=T, hq=hq, ws_bytes=0) == api.SI_ERR_NOMEM           # split: it does need room
             assert _prefill(api, kv, T=T, hq=hq, ws=None, ws_bytes=need.value) == api.SI_ERR_INVALID_ARG
+
+
+class _On:
+    """A tensor of host memory that says it lies on a CUDA device (its address is never followed: the calls below end before a launch)."""
+
+    def __init__(self, t, device):
+        self.t, self.n, self.is_cuda, self.device = t, device, device >= 0, f"cuda:{device}"
+
+    def get_device(self):
+        return self.n
+
+    def __getattr__(self, name):
+        return getattr(self.t, name)
+
+
+def test_the_binding_refuses_tensors_of_another_device(api, monkeypatch):
+    import torch
+    B, H, cap, D, Hq = 2, 2, 16, 64, 4
+    bf16, i32, f32 = torch.bfloat16, torch.int32, torch.float32
+
+    def on(device, *shape, dtype=bf16):
+        return _On(torch.zeros(*shape, dtype=dtype), device)
+
+    def cache(device=1, **other):
+        t = dict(k=on(device, B, H, cap, D), v=on(device, B, H, cap, D), length=on(device, B, dtype=i32), pos=None, weight=on(device, B, H, cap, dtype=f32))
+        t.update(other)
+        return api.KVCache(t["k"], t["v"], t["length"], t["pos"], t["weight"])
+
+    for name, shape, dtype in (("v", (B, H, cap, D), bf16), ("length", (B,), i32), ("pos", (B, H, cap), i32), ("weight", (B, H, cap), f32)):
+        for device in (0, -1):
+            with pytest.raises(ValueError):
+                cache(**{name: on(device, *shape, dtype=dtype)})
+    with pytest.raises(ValueError):
+        cache(-1)
+    here = 1
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: here)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 0, raising=False)
+    c, elsewhere = cache(), cache(0)
+
+    class stream:
+        device_index, cuda_stream = 0, 0
+
+    def calls(c, at, T=0, **kw):          # T = 0: nothing to launch
+        q, out, lse = on(at.get("q", 1), B, T, Hq, D), on(at.get("out", 1), B, T, Hq, D), on(at.get("lse", 1), B, T, Hq, dtype=f32)
+        ws, status = on(at.get("ws", 1), 1 << 20, dtype=torch.uint8), on(at.get("status", 1), 1, dtype=i32)
+        yield lambda: api.si_attn_prefill(c, q, 0, 0, 0.1, out, lse, ws, status, **kw)
+        if "out" not in at:
+            yield lambda: api.si_attn_weights(c, q, 0, 0, 0.1, lse, ws, status, **kw)
+
+    for f in calls(c, {}):
+        f()
+    for at in (dict(q=0), dict(out=0), dict(lse=0), dict(ws=0), dict(status=0), dict(q=-1)):
+        for f in calls(c, at):
+            with pytest.raises(ValueError):
+                f()
+    for f in calls(c, {}, stream=stream):
+        with pytest.raises(ValueError):
+            f()
+    new = [on(d, B, H, D) for d in (1, 0)]
+    q1, out1, ws = on(1, B, Hq, D), on(1, B, Hq, D), on(1, 1 << 20, dtype=torch.uint8)
+    for args in ((on(0, B, Hq, D), None, None, None), (q1, on(0, B, dtype=i32), None, None), (q1, None, new[1], new[1]), (q1, None, new[0], new[1])):
+        with pytest.raises(ValueError):
+            api.si_attn_decode(c, *args, 0, 0, 0.1, out1, None, 0, ws)
+    with pytest.raises(ValueError):
+        api.si_kv_evict(c, elsewhere, None, 0, 4, 0, 0, None, None, ws)
+    with pytest.raises(ValueError):
+        api.si_kv_evict(c, c, None, 0, 4, 0, 0, on(0, B, H, 4, dtype=i32), None, ws)
+    here = 0                                # another device is current
+    for f in calls(c, {}):
+        with pytest.raises(ValueError):
+            f()
+    with pytest.raises(ValueError):
+        api.si_attn_decode(c, q1, None, None, None, 0, 0, 0.1, out1, None, 0, ws)
+    with pytest.raises(ValueError):
+        api.si_kv_evict(c, c, None, 0, 4, 0, 0, None, None, ws)

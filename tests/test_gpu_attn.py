@@ -462,3 +462,31 @@ def test_decode_with_nan_adds_nothing_to_hidden_entries(api):
         got = weight[0, 0].cpu().numpy()
         assert np.isnan(got[:n_sink]).all() and np.isnan(got[n - window:n]).all()
         assert (got[n_sink:n - window] == 0).all() and (got[n:] == 0).all()
+
+
+@pytest.mark.parametrize("T,n,Hq,Hkv,D,window,n_sink,dtype", [
+    (1500, 4000, 4, 1, 128, 0, 0, "bf16"),          # many key tiles, blocks of queries of many lengths
+    (2000, 2000, 3, 3, 64, 0, 0, "f16"),
+    (1000, 9000, 2, 1, 128, 700, 130, "bf16"),
+    (60, 12000, 8, 2, 64, 0, 0, "bf16"),            # long keys split over CTAs
+    (5, 30000, 16, 2, 128, 0, 0, "f16"),
+])
+def test_prefill_of_long_sequences(api, T, n, Hq, Hkv, D, window, n_sink, dtype):
+    q, k, v, length = au.make(1, Hq, Hkv, D, n + 1, dtype, "nhd", T, T + n, [n])
+    weight = torch.zeros(1, Hkv, n + 1, device="cuda")
+    out, lse = _prefill(api, q, k, v, length, window, n_sink, 0.1, weight)
+    # rows of every part of the range against the oracle, and all of them through the sum of what they gave
+    rows = sorted({0, 1, T // 3, T // 2, T - 2, T - 1} | set(range(0, T, max(1, T // 40))))
+    rows = [r for r in rows if 0 <= r < T]
+    G = Hq // Hkv
+    from oracle import attention_oracle as ao
+    kn, vn, qn = au.f64(k)[0, :, :n], au.f64(v)[0, :, :n], au.f64(q)[0]
+    ref = {x: np.zeros((1, len(rows), Hq) + ((D,) if x in ("out", "reach") else ())) for x in ("out", "reach", "lse", "size", "n")}
+    for h in range(Hq):
+        o, l, w, r, z = ao.attend(qn[rows, h], kn[h // G], vn[h // G], np.arange(n), n - T + np.asarray(rows), window, n_sink, 0.1)
+        for x, y in (("out", o), ("reach", r), ("lse", l), ("size", z), ("n", (w > 0).sum(-1))):
+            ref[x][0, :, h] = y
+    au.check_out(out[:, rows], ref, dtype, D)
+    au.check_lse(lse[:, rows], ref, D)
+    total = au.f64(weight)[0].sum(-1)                # every query gives each of its G heads' entries a weight of one in all
+    assert np.all(np.abs(total - T * G) <= T * G * (4 * au.delta(ref, D).max() + 3e-5))

@@ -194,3 +194,58 @@ def test_evict_with_budgets_of_millions(api, D, n, budget):
     for d, x in ((dk, 0), (dv, 0x5A5A)):
         got = d[0, 0].view(torch.int32)
         assert all(torch.equal(got[:, c].long(), at ^ x) for c in (0, 5, D // 2 - 1))
+
+
+@pytest.mark.parametrize("lens,n_new,cap,budget", [
+    ([16384], 0, 16384, 16200),             # four CTAs to a row that select and move
+    ([8300, 8299], 1, 8301, 8192),
+    ([16384, 16383], 1, 16385, 16384),      # a decode step at the budget, and one below it
+    ([50000], 0, 50003, 49999),
+    ([65536], 0, 65536, 65300),
+    ([3, 60000], 0, 60000, 59800),
+])
+@pytest.mark.parametrize("kind", ["random", "ties", "odd"])
+@pytest.mark.parametrize("with_kept", [True, False])
+def test_evict_in_place_on_rows_of_several_ctas(api, lens, n_new, cap, budget, kind, with_kept):
+    B, H, D, n_sink, n_recent = len(lens), 3, 64, 4, 100
+    rng = np.random.default_rng(cap)
+    w = _weights(kind, (B, H, cap), rng)
+    pos = np.stack([np.stack([rng.permutation(2 * cap)[:cap] for _ in range(H)]) for _ in range(B)]).astype(np.int32)
+    last = np.array([2 * cap - 1 - b for b in range(B)], np.int32)
+    k, v = (torch.randint(-30000, 30000, (B, H, cap, D), dtype=torch.int16, device="cuda").view(torch.bfloat16) for _ in range(2))
+    length = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    cache = api.KVCache(k, v, length, torch.from_numpy(pos).cuda(), torch.from_numpy(w).cuda())
+    k0, v0 = k.view(torch.int16).clone(), v.view(torch.int16).clone()
+    kept = torch.full((B, H, budget), -7, dtype=torch.int32, device="cuda") if with_kept else None
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    api.si_kv_evict(cache, cache, torch.from_numpy(last).cuda(), n_new, budget, n_sink, n_recent, kept, length, cache.workspace(0, 0), status)
+    torch.cuda.synchronize()
+    assert status.item() == 0 and length.tolist() == [min(n + n_new, budget) for n in lens]
+    got_p, got_w = cache.pos.cpu().numpy(), cache.weight.cpu().numpy()
+    for b, n in enumerate(lens):
+        n += n_new
+        for h in range(H):
+            want = ao.evict(w[b, h, :n], pos[b, h, :n].astype(np.int64), int(last[b]), budget, n_sink, n_recent)
+            if with_kept:
+                assert np.array_equal(kept[b, h].cpu().numpy(), want)
+            to = np.nonzero(want >= 0)[0]
+            d, s = torch.from_numpy(to).cuda(), torch.from_numpy(want[to]).cuda()
+            assert torch.equal(k[b, h, d].view(torch.int16), k0[b, h, s]) and torch.equal(v[b, h, d].view(torch.int16), v0[b, h, s])
+            assert np.array_equal(got_p[b, h, to], pos[b, h, want[to]])
+            assert np.array_equal(got_w[b, h, to].view(np.int32), w[b, h, want[to]].view(np.int32))
+            assert np.array_equal(got_p[b, h, len(to):], pos[b, h, len(to):])            # slots beyond are as they were
+
+
+@pytest.mark.parametrize("n,budget", [(393208, 100000), (393216, 393000), (200001, 199990)])
+def test_evict_of_rows_that_just_fit_shared_memory(api, n, budget):
+    rng = np.random.default_rng(n)
+    w = np.floor(rng.random(n) * 1000).astype(np.float32)
+    k, v = (torch.randint(-30000, 30000, (1, 1, n, 64), dtype=torch.int16, device="cuda").view(torch.bfloat16) for _ in range(2))
+    length = torch.tensor([n], dtype=torch.int32, device="cuda")
+    src = api.KVCache(k, v, length, None, torch.from_numpy(w).cuda().view(1, 1, n))
+    dk, dv = (torch.zeros(1, 1, budget, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    dst = api.KVCache(dk, dv, length, torch.zeros(1, 1, budget, dtype=torch.int32, device="cuda"), torch.zeros(1, 1, budget, device="cuda"))
+    api.si_kv_evict(src, dst, None, 0, budget, 16, 1000, None, None, src.workspace(0, 0))
+    at = torch.from_numpy(_evict_fast(w, budget, 16, 1000)).cuda()
+    assert torch.equal(dst.pos[0, 0].long(), at)
+    assert torch.equal(dk[0, 0].view(torch.int16), k[0, 0, at].view(torch.int16)) and torch.equal(dv[0, 0].view(torch.int16), v[0, 0, at].view(torch.int16))

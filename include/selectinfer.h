@@ -478,7 +478,9 @@ int si_attn_prefill(const si_kv_t *kv, const void *q, long long q_seq_stride, lo
  * prompt): weight[b, h, j] += sum over the T queries i that see j and the G query heads of exp(scale * (q_i . k_j)
  * - lse_i).  lse: device float32 [n_seqs, T, n_q_heads] from si_attn_prefill with the same arguments.  T may be the
  * whole prompt or only its last few positions.  A query whose lse is NaN makes the weight of every entry it sees NaN.  Needs kv->weight and kv->pos == NULL.  Sums are taken in a fixed
- * order: repeated calls add the same bits. */
+ * order: repeated calls add the same bits.  The matrix unit cuts its partial sums off instead of rounding them, which lowers a
+ * score by up to some 1.6e-7 of itself; si_attn_prefill's lse carries the same, so that the two cancel (error of the weights
+ * 1.4e-7 .. 5e-7), while with an exact lse they come out up to 1.5e-6 low. */
 int si_attn_weights(const si_kv_t *kv, const void *q, long long q_seq_stride, long long q_tok_stride, int T,
                     int n_q_heads, int window, int n_sink, float scale, const float *lse, void *workspace,
                     size_t ws_bytes, int32_t *status_dev, void *stream);
@@ -487,14 +489,16 @@ int si_attn_weights(const si_kv_t *kv, const void *q, long long q_seq_stride, lo
  *   q        device [n_seqs, n_q_heads, head_dim], sequences q_seq_stride elements apart
  *   q_pos    device int32 [n_seqs]: position of the query; NULL (only with kv->pos == NULL): the last entry's
  *   k_new, v_new   device [n_seqs, n_kv_heads, head_dim], sequences new_seq_stride elements apart, or both NULL.  Given,
- *            they are the query's own key and value: the call stores them as entry len[b] (position q_pos[b]) and
- *            attends to len[b] + 1 entries.  len itself is not changed -- one array serves all layers, so the caller
+ *            they are the query's own key and value: the call stores them as entry len[b] (position q_pos[b] in a cache
+ *            with positions) and attends to len[b] + 1 entries.  len itself is not changed -- one array serves all layers, so the caller
  *            advances it once per token.  A full cache (len[b] == capacity) is SI_ERR_OUT_OF_RANGE in *status_dev;
  *            nothing is stored for it.
  *   out      device [n_seqs, n_q_heads, head_dim]; lse device float32 [n_seqs, n_q_heads] or NULL
  *   flags    SI_FLAG_ACC_WEIGHT: weight[b, h, j] += sum over the G query heads of p_j (the new entry's weight is set
  *            to its own sum); needs kv->weight.
- * The bytes of the visible entries are read once; the work is split evenly over the SMs whatever the lengths. */
+ * Without positions the bytes of the visible entries are read, with positions those of all entries (which of them are visible
+ * is known only once they are on their way): once, or once per 16 query heads of a key head where there are more.  The work
+ * is split evenly over the SMs whatever the lengths. */
 int si_attn_decode(const si_kv_t *kv, const void *q, long long q_seq_stride, int n_q_heads, const int32_t *q_pos,
                    const void *k_new, const void *v_new, long long new_seq_stride, int window, int n_sink,
                    float scale, void *out, float *lse, unsigned flags, void *workspace, size_t ws_bytes,

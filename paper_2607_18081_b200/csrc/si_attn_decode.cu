@@ -2,7 +2,8 @@
 //
 //   out_q = sum_j p_qj v_j,  p_q = softmax over the visible entries j of scale q . k_j,   q = the G query heads of a key head
 //
-// Bound by HBM: every visible key and value is read once (once per 16 heads where G is larger), G flops per byte.  So the kernel is a stream: each warp keeps
+// Bound by HBM: every visible key and value is read once (once per 16 heads where G is larger; in a cache with positions every
+// one, visible or not: a chunk's positions come beside its keys), G flops per byte.  So the kernel is a stream: each warp keeps
 // two chunks of 4 KB of keys and 4 KB of values in flight (cp.async into a ring of its own, 128 KB per SM) while it works
 // on a third (three in flight: 2 % slower).  The G heads make the second dimension of two small matrix products per chunk,
 //   S^T [keys x heads] = K Q^T        O^T [head_dim x heads] += V^T P^T,
@@ -14,6 +15,8 @@
 // Work is split in chunks, not in sequences: the chunks of all (sequence, head) items in one row, cut into equal runs, one
 // per CTA, whatever the lengths.  An item that crosses CTAs leaves partial sums (one maximum, one sum and head_dim fp32
 // values per head and CTA) that a second kernel joins in the order of the CTAs -- no atomics, the same bits every time.
+// Roundings below 32 bits: p to the cache's type for the product with V (the warp-level product takes both operands in one
+// 16-bit type), the result once; everything else is fp32.
 // With weights wanted the scores go to the workspace (4 bytes per head beside 4 * head_dim bytes per key) and the second
 // kernel, which knows the sums, adds exp(score - maximum) / sum.
 #include "si_kv.cuh"

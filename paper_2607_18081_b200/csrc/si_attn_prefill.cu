@@ -12,6 +12,10 @@
 // row's maximum grows by more than 2^8 (then p may reach 2^8, which fp32 sums and 16-bit p carry without loss), by the
 // softmax warps themselves: S_t(j) is complete only after O_t(j-1), so nothing else touches O_t at that time.
 //
+// Roundings below 32 bits: p goes into the product with V in the cache's type, as V has it (the matrix unit takes both operands
+// alike; p in fp32 would be two or three products for one), the result is rounded once more; scores, the running maximum, the sum
+// (of the unrounded p) and O are fp32.  Exponentials are the hardware's (2 ulp) of a base-2 argument.
+//
 // With few rows the keys are split over CTAs as well: each leaves its unnormalised O, maximum and sum, and a second kernel
 // joins them in order.
 #include <type_traits>

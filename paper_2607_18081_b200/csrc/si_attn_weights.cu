@@ -12,6 +12,9 @@
 // per CTA, so the triangle of a causal prompt and sequences of any lengths load all SMs alike.  A key tile whose pairs lie
 // in one run is finished there; one that crosses CTAs leaves 256 partial sums per CTA, which a second kernel adds in the
 // order of the CTAs -- no atomics, the same bits every time.
+// All in fp32.  The caller's lse is rounded once more when it is turned to base 2, like the sum it is taken from; that and the scale
+// cost 1.6e-7 of a weight.  The matrix unit cuts off its D / 16 partial sums: 1.6e-7 of a score (head size 128, f16), up to
+// 1.5e-6 of a weight where the lse is exact and next to nothing where it is si_attn_prefill's, whose scores are cut off alike.
 //   warps 0-15   exponentials and sums: a warpgroup per half of the keys and parity of the query tile (four warps per
 //                scheduler partition cover one another's tensor-memory and exponential latencies)
 //   warp 16      TMA loads of key tiles (two buffers) and query tiles (a ring)

@@ -4,7 +4,7 @@
 // S^T = K Q^T with 128 keys as rows and 128 packed (query, head) rows as columns: a thread owns a key, so the
 // sum over queries is a sum along its row of tensor memory and nothing is exchanged.  2 D flops and one exponential per
 // pair; the exponential unit (16 per clock and SM: 1024 clocks per tile pair) is twice as slow as the matrix unit (512), so one
-// of every eight pairs of exponentials goes to the multiply-add units (4096-token prompt: 112 us; none 117, three of eight
+// of every eight pairs of exponentials goes to the multiply-add units (4096-token prompt: 113 us; none 117, three of eight
 // 120: back to back the chip is at its power limit, and a polynomial costs more energy than it saves time).
 //
 // A key tile is 256 keys, two such products with the same query tile: with 128 the stream of query tiles out of L2 (32 KB per

@@ -700,7 +700,7 @@ int union_blocks(const si_store *s, long long entries) {
 // if that call is the last one recorded, with the same workspace, layout, stream and capture: then the copies differ and
 // nothing else of the workspace meets.  Behind anything else -- another layout or store on the same memory, a kernel that
 // still reads scratch or writes a list after it has let its dependents start (those call si_mt_forget) -- it is launched in
-// plain stream order.  (Always waiting costs 15-20 % of back-to-back calls: 39.6 -> 45.3 us at 8 tokens, 47.6 -> 55.7 at 512.)
+// plain stream order; a graph launch between two calls is complete before the second starts.  (Always waiting costs 15-20 % of back-to-back calls: 39.6 -> 45.3 us at 8 tokens, 47.6 -> 55.7 at 512.)
 struct MtCall {
     const void *ws; cudaStream_t stream; unsigned long long capture;
     size_t union_off, union_half, mask_off, mask_half;

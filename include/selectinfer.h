@@ -436,6 +436,8 @@ int si_shard_reduce(const float *const *parts_dev, int world, const void *x, int
  *               different per head after an eviction; or NULL: entry j is at position j.
  *   weight      device float32 [n_seqs, n_kv_heads, capacity]: the attention every entry has received so far; NULL
  *               where no call needs it.
+ *   All 4-byte words (len, pos, weight and the calls' lse, q_pos, kept, len_out) lie on 4-byte boundaries, everything else on 16.
+ *   No output may overlap an input of the same call other than as said there.
  *   The device that holds the cache must be current in every call (a cache has no handle to check that by: the caller's duty).
  *   head_dim 64 or 128 (SI_ERR_UNSUPPORTED otherwise); n_q_heads is a multiple of n_kv_heads and query heads
  *   h * G .. h * G + G - 1 (G = n_q_heads / n_kv_heads, at most 128) read key/value head h.

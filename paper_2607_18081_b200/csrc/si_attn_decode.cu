@@ -669,7 +669,8 @@ extern "C" int si_attn_decode(const si_kv_t *kv, const void *q, long long q_seq_
     const int acc = (flags & SI_FLAG_ACC_WEIGHT) != 0;
     if (!q || !out || q_seq_stride < 0 || !k_new != !v_new || new_seq_stride < 0) return SI_ERR_INVALID_ARG;
     if ((kv->pos && !q_pos) || (acc && !kv->weight) || (k_new && si_kv_shared(kv))) return SI_ERR_INVALID_ARG;
-    if (!si_aligned16(q) || !si_aligned16(out) || !si_aligned16(k_new) || !si_aligned16(v_new) || ((q_seq_stride | new_seq_stride) & 7))
+    if (!si_aligned16(q) || !si_aligned16(out) || !si_aligned16(k_new) || !si_aligned16(v_new) || !si_aligned4(q_pos, lse, status_dev) ||
+        ((q_seq_stride | new_seq_stride) & 7))
         return SI_ERR_ALIGNMENT;
     const Layout L = layout_of(kv, n_q_heads, acc);
     // chunks are numbered in 32 bits: 2^31 of them are 16 TB of keys and values unless sequences share memory by zero strides

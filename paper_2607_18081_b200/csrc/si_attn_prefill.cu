@@ -512,7 +512,7 @@ extern "C" int si_attn_prefill(const si_kv_t *kv, const void *q, long long q_seq
     if (kv->n_seqs == 0 || T == 0) return SI_OK;
     if (!q || !out || q_seq_stride < 0 || q_tok_stride < 0) return SI_ERR_INVALID_ARG;
     if (kv->pos || (q_tok_stride == 0 && T > 1)) return SI_ERR_UNSUPPORTED;     // tensor copies have no zero stride
-    if (!si_aligned16(q) || !si_aligned16(out) || ((q_seq_stride | q_tok_stride) & 7)) return SI_ERR_ALIGNMENT;
+    if (!si_aligned16(q) || !si_aligned16(out) || !si_aligned4(lse, status_dev) || ((q_seq_stride | q_tok_stride) & 7)) return SI_ERR_ALIGNMENT;
     const Plan p = plan_of(kv, n_q_heads, T, window, n_sink);
     if (p.blocks > INT_MAX) return SI_ERR_TOO_LARGE;
     if (p.splits > 1) {

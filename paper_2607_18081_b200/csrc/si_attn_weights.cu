@@ -395,7 +395,7 @@ extern "C" int si_attn_weights(const si_kv_t *kv, const void *q, long long q_seq
     if (kv->n_seqs == 0 || T == 0) return SI_OK;
     if (!q || !lse || !kv->weight || q_seq_stride < 0 || q_tok_stride < 0) return SI_ERR_INVALID_ARG;
     if (kv->pos || (q_tok_stride == 0 && T > 1)) return SI_ERR_UNSUPPORTED;     // tensor copies have no zero stride
-    if (!si_aligned16(q) || ((q_seq_stride | q_tok_stride) & 7)) return SI_ERR_ALIGNMENT;
+    if (!si_aligned16(q) || !si_aligned4(lse, status_dev) || ((q_seq_stride | q_tok_stride) & 7)) return SI_ERR_ALIGNMENT;
     const Layout L = layout_of(kv);
     const TcArgs A = tc_args(kv, q_seq_stride, T, n_q_heads, window, n_sink, scale, nullptr, nullptr, status_dev);
     // pairs are numbered in 32 bits

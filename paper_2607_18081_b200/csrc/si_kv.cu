@@ -458,6 +458,7 @@ extern "C" int si_kv_evict(const si_kv_t *src, const si_kv_t *dst, const int32_t
                      src->head_stride != dst->head_stride || src->row_stride != dst->row_stride || src->capacity != dst->capacity)) return SI_ERR_INVALID_ARG;
     // one row's entries would be read while another's are written there
     if (si_kv_shared(dst) || (!in_place && (src->v == dst->v || src->weight == dst->weight || src->pos == dst->pos))) return SI_ERR_INVALID_ARG;
+    if (!si_aligned4(q_pos, kept, len_out, status_dev)) return SI_ERR_ALIGNMENT;
     if (ws_bytes < evict_ws_bytes(src)) return SI_ERR_NOMEM;
     if (!workspace) return SI_ERR_INVALID_ARG;
     if ((uintptr_t)workspace & 255) return SI_ERR_ALIGNMENT;

@@ -21,6 +21,9 @@ inline si_kv_view si_kv_view_of(const si_kv_t *kv) {
             kv->row_stride, kv->n_seqs, kv->n_kv_heads, kv->head_dim, kv->capacity};
 }
 
+// 4-byte words (lengths, positions, weights, lse, status), any of them NULL.
+template <typename... P> bool si_aligned4(const P *...p) { return (((uintptr_t)p | ...) & 3u) == 0; }
+
 // Host checks common to all calls on a cache.
 inline int si_kv_check(const si_kv_t *kv) {
     if (!kv || kv->n_seqs < 0 || kv->n_kv_heads < 1 || kv->capacity < 1 || kv->head_dim < 1) return SI_ERR_INVALID_ARG;
@@ -31,6 +34,7 @@ inline int si_kv_check(const si_kv_t *kv) {
     if (!kv->k || !kv->v || !kv->len) return SI_ERR_INVALID_ARG;
     if (kv->row_stride < kv->head_dim || kv->head_stride < 0 || kv->seq_stride < 0) return SI_ERR_INVALID_ARG;
     if (!si_aligned16(kv->k) || !si_aligned16(kv->v) || ((kv->row_stride | kv->head_stride | kv->seq_stride) & 7)) return SI_ERR_ALIGNMENT;
+    if (!si_aligned4(kv->weight, kv->pos, kv->len)) return SI_ERR_ALIGNMENT;
     return SI_OK;
 }
 

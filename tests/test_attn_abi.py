@@ -249,3 +249,26 @@ def test_the_binding_refuses_tensors_of_another_device(api, monkeypatch):
         api.si_attn_decode(c, q1, None, None, None, 0, 0, 0.1, out1, None, 0, ws)
     with pytest.raises(ValueError):
         api.si_kv_evict(c, c, None, 0, 4, 0, 0, None, None, ws)
+
+
+def test_words_off_their_boundaries_are_refused(api):
+    """Pointers that are not multiples of four would fault on the device.  (No workspace is given: without the check the calls end there.)"""
+    A, N = api.SI_ERR_ALIGNMENT, api.SI_ERR_NOMEM
+    kv, pos = _kv(api, n_seqs=1, capacity=8192), _kv(api, n_seqs=1, capacity=8192, pos=FAKE)
+    calls = (_prefill, _weights, _decode)
+    assert all(c(api, kv, ws_bytes=0) == N for c in calls) and _evict(api, pos, pos, ws_bytes=0) == N
+    for change in (dict(weight=FAKE + 2), dict(len=FAKE + 1), dict(pos=FAKE + 3)):
+        bad = _kv(api, n_seqs=1, capacity=8192, **{**dict(pos=None), **change})
+        assert _decode(api, bad, q_pos=FAKE, ws_bytes=0) == A
+        assert _evict(api, _kv(api, n_seqs=1, capacity=8192, **{**dict(pos=FAKE), **change}), pos, ws_bytes=0) == A
+        if "pos" not in change:
+            assert _prefill(api, bad, ws_bytes=0) == A and _weights(api, bad, ws_bytes=0) == A
+    assert _prefill(api, kv, lse=FAKE + 2, ws_bytes=0) == A and _weights(api, kv, lse=FAKE + 2, ws_bytes=0) == A
+    assert _decode(api, kv, lse=FAKE + 2, ws_bytes=0) == A and _decode(api, kv, q_pos=FAKE + 2, ws_bytes=0) == A
+    assert _evict(api, pos, pos, q_pos=FAKE + 2, ws_bytes=0) == A
+    lib, ref = api.lib(), ctypes.byref
+    for kept, len_out, status in ((FAKE + 1, None, None), (None, FAKE + 2, None), (None, None, FAKE + 3)):
+        assert lib.si_kv_evict(ref(pos), ref(pos), FAKE, 0, 50, 4, 4, kept, len_out, FAKE, 0, status, None) == A
+    assert lib.si_attn_prefill(ref(kv), FAKE, 4096, 4096, 4, 32, 0, 0, 0.1, FAKE, None, FAKE, 0, FAKE + 2, None) == A
+    assert lib.si_attn_weights(ref(kv), FAKE, 4096, 4096, 4, 32, 0, 0, 0.1, FAKE, FAKE, 0, FAKE + 2, None) == A
+    assert lib.si_attn_decode(ref(kv), FAKE, 4096, 32, None, None, None, 0, 0, 0, 0.1, FAKE, None, 0, FAKE, 0, FAKE + 2, None) == A

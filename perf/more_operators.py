@@ -7,7 +7,7 @@ single token over such a cache, its eviction by accumulated weight, and the two 
 The format: the head_dim values of a key (or value) are cut into groups of 32 or 64.  A group x holds its lowest value m, a
 step s and 4-bit codes c, and stands for m + s c:
     s = (max x - min x) / 15, rounded up to the cache's 16-bit type,    m = min x,    c = nearest integer of (x - m) / s
-(range, its fifteenth, the reciprocal of s and the quotient each rounded to fp32).  An entry at position p is visible to a query
+(range, its fifteenth and x - m in fp32; the quotient is the exact product with the fp32 reciprocal of s).  An entry at position p is visible to a query
 at position t if p <= t and (window == 0 or p > t - window or p < n_sink).
 """
 import math
@@ -214,7 +214,7 @@ def _quantise(x, group):
     step = (x.amax(-1, keepdim=True).float() - m.float()) * torch.tensor(1.0 / 15.0, dtype=torch.float32, device=x.device)
     s = _round_up(step, x.dtype)
     r = torch.where(s > 0, 1.0 / s.float(), 0.0)
-    c = torch.round((x.float() - m.float()) * r).clamp_(0, 15)
+    c = torch.round((x.float() - m.float()).double() * r.double()).clamp_(0, 15)     # exact: quotients halfway between two codes are common
     return c.to(torch.uint8), s, m
 
 
@@ -344,7 +344,7 @@ def run(st):
 # ------------------------------------------------------------------------------------------------ in 64 bits
 
 def _exact_cache(x, group, dt):
-    """What a 16-bit [..., D] stands for once held in 4 bits: the definition above, every fp32 rounding of it an explicit one of a 64-bit result."""
+    """What a 16-bit [..., D] stands for once held in 4 bits: the definition above, its fp32 roundings explicit ones of 64-bit results."""
     fl = lambda y: y.float().double()  # noqa: E731
     z = x.double().reshape(*x.shape[:-1], -1, min(group, x.shape[-1]))
     low, high = z.min(-1, keepdim=True).values, z.max(-1, keepdim=True).values
@@ -353,7 +353,7 @@ def _exact_cache(x, group, dt):
     bits = step.to(dt).view(torch.int16)
     step = torch.where(step < fifteenth, (bits + 1).view(dt).double(), step)
     inverse = torch.where(step > 0, fl(1.0 / step.clamp_min(1e-300)), 0.0)
-    code = fl(fl(z - low) * inverse).round().clamp(0, 15)
+    code = (fl(z - low) * inverse).round().clamp(0, 15)
     return (low + step * code).reshape(x.shape)
 
 

@@ -525,6 +525,68 @@ int si_kv_evict(const si_kv_t *src, const si_kv_t *dst, const int32_t *q_pos, in
                 int n_recent, int32_t *kept, int32_t *len_out, void *workspace, size_t ws_bytes, int32_t *status_dev,
                 void *stream);
 
+/* ---------------------------------------------------------------- a key/value cache held in 4 bits
+ *
+ * The same cache with its keys and values quantised: D + 8 * D / group bytes per entry and head (D = head_dim) instead of 4 * D.  Every
+ * `group` (32 or 64; head_dim if that is less) neighbouring values of a key or value are held as their lowest value m and a step
+ * s, both of `dtype`, and 4-bit codes c, and stand for m + s * c:
+ *       s = (largest - lowest) / 15, rounded up to dtype;  c = the nearest integer to (x - m) / s
+ * (computed in fp32, the quotient as the product with the rounded 1 / s, ties to even): |x - (m + s * c)| <= s / 2 up to those roundings.
+ * s below 2^-126 counts as 0.  A group that holds a NaN or an infinity, or whose range is beyond 2^94, stands for NaN throughout.
+ *
+ *   data        device, 16-byte aligned: tiles of 32 entries, each si_kv4_tile_bytes bytes in an order of the library's own.  Entry j of head h
+ *               of sequence b is entry j % 32 of the tile at b * seq_stride + h * head_stride + j / 32 * tile_bytes (bytes; strides
+ *               multiples of 16).  Strides of 0 share rows where a call only reads.  Needs no clearing: what lies beyond the entries in use is
+ *               never part of a result.
+ *   len, pos, weight   as in si_kv_t; pos and weight on 16-byte boundaries
+ *   capacity    entries per row, a multiple of 32
+ *   dtype       SI_F16 or SI_BF16: of the values stored, read back, queries and results
+ * The other rules of si_kv_t (alignment, overlap, current device, head counts) hold here too. */
+typedef struct si_kv4 {
+    void *data;
+    float *weight;
+    int32_t *pos;
+    const int32_t *len;
+    long long seq_stride, head_stride;
+    int n_seqs, n_kv_heads, head_dim, capacity, group, dtype;
+} si_kv4_t;
+
+/* Host functions: bytes of a tile of 32 entries; device scratch for si_kv4_attn_decode with at most n_q_heads query heads and for
+ * si_kv4_evict (n_q_heads = 0: the latter only) on this cache, 256-byte aligned, never read before it is written. */
+int si_kv4_tile_bytes(int head_dim, int group, size_t *bytes_out);
+int si_kv4_workspace_bytes(const si_kv4_t *kv, int n_q_heads, size_t *bytes_out);
+
+/* Quantise entries as they are stored: entries 0 .. src->len[b] - 1 of the 16-bit cache src become entries dst->len[b] .. of dst.  dst->len
+ * is not changed (one array serves all layers: the caller advances it).  src may be the projection's output itself, described by
+ * strides, of one token or a whole prompt.
+ *   dst->pos     (if given) receives src->pos, or, where src has none, first_pos[b] + j for entry j of src (device int32 [n_seqs]; NULL:
+ *                dst->len[b] + j)
+ *   dst->weight  (if given) receives src->weight, 0 where src has none
+ * The same n_seqs, n_kv_heads, head_dim and dtype on both sides.  Entries that do not fit dst's capacity are not stored
+ * (SI_ERR_OUT_OF_RANGE in *status_dev); no other entry of dst is touched. */
+int si_kv4_store(const si_kv_t *src, const si_kv4_t *dst, const int32_t *first_pos, int32_t *status_dev, void *stream);
+
+/* Read entries back to 16 bits: entries first[b] .. min(src->len[b], first[b] + n) - 1 of src (first: device int32 [n_seqs], NULL: 0;
+ * a negative one is SI_ERR_OUT_OF_RANGE and taken as 0) become entries 0, 1, .. of the 16-bit cache dst, rounded once to dtype (f16: at most its
+ * largest number, since s was rounded up), with their pos and weight where both sides have them.  dst->len is not read; other rows of dst stay as they were.  n <= dst->capacity.
+ *   len_out      device int32 [n_seqs] or NULL: entries read back; may be dst->len
+ * This is how the next chunk of a prompt is prefilled on such a cache: into a scratch cache, the chunk's own keys and values
+ * behind, si_attn_prefill. */
+int si_kv4_load(const si_kv4_t *src, const si_kv_t *dst, const int32_t *first, int n, int32_t *len_out, int32_t *status_dev,
+                void *stream);
+
+/* si_attn_decode on a cache in 4 bits; all arguments as there.  A new entry is quantised, stored, and attended to as it is stored.  The
+ * stored values are not rounded in between: out is the attention over m + s * c.  Scores, softmax and sums are fp32; p * s is
+ * rounded to 11 bits for the product with the codes; out has the cache's type.  A query that holds a NaN or an infinity has NaN as result. */
+int si_kv4_attn_decode(const si_kv4_t *kv, const void *q, long long q_seq_stride, int n_q_heads, const int32_t *q_pos,
+                       const void *k_new, const void *v_new, long long new_seq_stride, int window, int n_sink, float scale,
+                       void *out, float *lse, unsigned flags, void *workspace, size_t ws_bytes, int32_t *status_dev, void *stream);
+
+/* si_kv_evict on caches in 4 bits; all arguments as there (src and dst of the same group).  Codes move as they are: nothing is
+ * quantised twice. */
+int si_kv4_evict(const si_kv4_t *src, const si_kv4_t *dst, const int32_t *q_pos, int n_new, int budget, int n_sink, int n_recent,
+                 int32_t *kept, int32_t *len_out, void *workspace, size_t ws_bytes, int32_t *status_dev, void *stream);
+
 /* Library build information: "sm_100a" etc.  Never NULL. */
 const char *si_build_info(void);
 

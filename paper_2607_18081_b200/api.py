@@ -42,6 +42,7 @@ EXPORTS = [
     "si_loadset", "si_shard_count", "si_shard_lists", "si_shard_reduce", "si_ffn_forward_sharded",
     "si_debug_ffn_forward_sharded_group", "si_debug_pair_plan", "si_debug_union_ahead",
     "si_kv_workspace_bytes", "si_attn_prefill", "si_attn_weights", "si_attn_decode", "si_kv_evict",
+    "si_kv4_tile_bytes", "si_kv4_workspace_bytes", "si_kv4_store", "si_kv4_load", "si_kv4_attn_decode", "si_kv4_evict",
 ]
 
 
@@ -107,6 +108,12 @@ def _load_library() -> ctypes.CDLL:
     lib.si_attn_weights.argtypes = [vp, vp, ll, ll, ci, ci, ci, ci, cf, vp, vp, sz, vp, vp]
     lib.si_attn_decode.argtypes = [vp, vp, ll, ci, vp, vp, vp, ll, ci, ci, cf, vp, vp, cu, vp, sz, vp, vp]
     lib.si_kv_evict.argtypes = [vp, vp, vp, ci, ci, ci, ci, vp, vp, vp, sz, vp, vp]
+    lib.si_kv4_tile_bytes.argtypes = [ci, ci, psz]
+    lib.si_kv4_workspace_bytes.argtypes = [vp, ci, psz]
+    lib.si_kv4_store.argtypes = [vp, vp, vp, vp, vp]
+    lib.si_kv4_load.argtypes = [vp, vp, vp, ci, vp, vp, vp]
+    lib.si_kv4_attn_decode.argtypes = lib.si_attn_decode.argtypes
+    lib.si_kv4_evict.argtypes = lib.si_kv_evict.argtypes
     for name in EXPORTS:
         fn = getattr(lib, name)
         if name not in ("si_strerror", "si_build_info", "si_last_cuda_error"):
@@ -533,9 +540,7 @@ def si_attn_weights(cache: KVCache, q, window: int, n_sink: int, scale: float, l
                                 _on(stream, cache)), "si_attn_weights")
 
 
-def si_attn_decode(cache: KVCache, q, q_pos, k_new, v_new, window: int, n_sink: int, scale: float, out, lse, flags: int,
-                   workspace, status=None, stream=None) -> None:
-    """q, out: [n_seqs, n_q_heads, head_dim]; k_new, v_new: [n_seqs, n_kv_heads, head_dim] of equal strides, or both None."""
+def _decode(call, name, cache, q, q_pos, k_new, v_new, window, n_sink, scale, out, lse, flags, workspace, status, stream):
     _, hq, _ = shape = q.shape
     kp = vp = None
     new_stride = 0
@@ -545,23 +550,123 @@ def si_attn_decode(cache: KVCache, q, q_pos, k_new, v_new, window: int, n_sink: 
         kp, vp = _heads(k_new, "k_new", cache, cache.n_kv_heads), _heads(v_new, "v_new", cache, cache.n_kv_heads)
         new_stride = k_new.stride(0)
     ws, ws_bytes = _ws(workspace, cache)
-    _check(_lib.si_attn_decode(cache.ref, _heads(q, "q", cache, hq), q.stride(0), hq, _ptr(q_pos, "q_pos", cache, (cache.n_seqs,), torch.int32),
-                               kp, vp, new_stride, window, n_sink, scale, _ptr(out, "out", cache, shape, q.dtype),
-                               _ptr(lse, "lse", cache, shape[:2], torch.float32), flags, ws, ws_bytes,
-                               _ptr(status, "status", cache, (1,), torch.int32), _on(stream, cache)), "si_attn_decode")
+    _check(call(cache.ref, _heads(q, "q", cache, hq), q.stride(0), hq, _ptr(q_pos, "q_pos", cache, (cache.n_seqs,), torch.int32),
+                kp, vp, new_stride, window, n_sink, scale, _ptr(out, "out", cache, shape, q.dtype),
+                _ptr(lse, "lse", cache, shape[:2], torch.float32), flags, ws, ws_bytes,
+                _ptr(status, "status", cache, (1,), torch.int32), _on(stream, cache)), name)
+
+
+def si_attn_decode(cache: KVCache, q, q_pos, k_new, v_new, window: int, n_sink: int, scale: float, out, lse, flags: int,
+                   workspace, status=None, stream=None) -> None:
+    """q, out: [n_seqs, n_q_heads, head_dim]; k_new, v_new: [n_seqs, n_kv_heads, head_dim] of equal strides, or both None."""
+    _decode(_lib.si_attn_decode, "si_attn_decode", cache, q, q_pos, k_new, v_new, window, n_sink, scale, out, lse, flags, workspace, status, stream)
+
+
+def _evict(call, name, src, dst, q_pos, n_new, budget, n_sink, n_recent, kept, len_out, workspace, status, stream):
+    _one_device(src, dst)
+    seqs = (src.n_seqs,)
+    ws, ws_bytes = _ws(workspace, src)
+    _check(call(src.ref, dst.ref, _ptr(q_pos, "q_pos", src, seqs, torch.int32), n_new, budget, n_sink, n_recent,
+                _ptr(kept, "kept", src, (src.n_seqs, src.n_kv_heads, budget), torch.int32),
+                _ptr(len_out, "len_out", src, seqs, torch.int32), ws, ws_bytes,
+                _ptr(status, "status", src, (1,), torch.int32), _on(stream, src)), name)
 
 
 def si_kv_evict(src: KVCache, dst: KVCache, q_pos, n_new: int, budget: int, n_sink: int, n_recent: int, kept, len_out,
                 workspace, status=None, stream=None) -> None:
     """dst is src: in place.  kept: int32 [n_seqs, n_kv_heads, budget] or None; len_out: int32 [n_seqs] or None."""
-    if dst.device != src.device:
+    _evict(_lib.si_kv_evict, "si_kv_evict", src, dst, q_pos, n_new, budget, n_sink, n_recent, kept, len_out, workspace, status, stream)
+
+
+# ------------------------------------------------------------------------- a key/value cache held in 4 bits
+
+class _Kv4Desc(ctypes.Structure):
+    """si_kv4_t"""
+    _fields_ = [("data", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("pos", ctypes.c_void_p), ("len", ctypes.c_void_p),
+                ("seq_stride", ctypes.c_longlong), ("head_stride", ctypes.c_longlong), ("n_seqs", ctypes.c_int), ("n_kv_heads", ctypes.c_int),
+                ("head_dim", ctypes.c_int), ("capacity", ctypes.c_int), ("group", ctypes.c_int), ("dtype", ctypes.c_int)]
+
+
+class KV4Cache:
+    """Description (si_kv4_t) of one layer's cache in 4 bits over tensors of the caller, which it keeps alive.
+
+    data: uint8 [n_seqs, n_kv_heads, tiles, si_kv4_tile_bytes(head_dim, group)], a tile holds 32 entries, the last two dimensions
+    contiguous; dtype: of the values stored and read back; length, pos, weight as in KVCache.  `empty` allocates the data."""
+
+    def __init__(self, data, head_dim: int, group: int, dtype, length, pos=None, weight=None):
+        if data.dim() != 4 or data.dtype != torch.uint8 or data.shape[3] != si_kv4_tile_bytes(head_dim, group) or data.stride(3) != 1 or data.stride(2) != data.shape[3]:
+            raise ValueError("data: uint8 [n_seqs, n_kv_heads, tiles, si_kv4_tile_bytes(head_dim, group)], the last two dimensions contiguous")
+        B, H, tiles, _ = data.shape
+        cap = 32 * tiles
+        for name, t, shape, dt in (("length", length, (B,), torch.int32), ("pos", pos, (B, H, cap), torch.int32),
+                                   ("weight", weight, (B, H, cap), torch.float32)):
+            if t is not None and (tuple(t.shape) != shape or t.dtype != dt or not t.is_contiguous()):
+                raise ValueError(f"{name}: expected contiguous {dt} of shape {shape}")
+        self.device = data.get_device()
+        for name, t in (("data", data), ("length", length), ("pos", pos), ("weight", weight)):
+            if t is not None and (not t.is_cuda or t.get_device() != self.device):
+                raise ValueError(f"{name}: expected a CUDA tensor on the device of data")
+        self.data, self.length, self.pos, self.weight = data, length, pos, weight
+        self.n_seqs, self.n_kv_heads, self.capacity, self.head_dim, self.group, self.dtype = B, H, cap, head_dim, group, dtype
+        self.desc = _Kv4Desc(data.data_ptr(), _dp(weight).value, _dp(pos).value, _dp(length).value, data.stride(0), data.stride(1), B, H,
+                             head_dim, cap, group, dtype_code(dtype))
+        self.ref = ctypes.addressof(self.desc)
+
+    @classmethod
+    def empty(cls, n_seqs: int, n_kv_heads: int, capacity: int, head_dim: int, group: int, dtype, length, pos=None, weight=None) -> "KV4Cache":
+        """With memory of its own for `capacity` entries (a multiple of 32), on the device of `length`."""
+        if capacity < 32 or capacity % 32:
+            raise ValueError("capacity: a multiple of 32")
+        data = torch.empty(n_seqs, n_kv_heads, capacity // 32, si_kv4_tile_bytes(head_dim, group), dtype=torch.uint8, device=length.device)
+        return cls(data, head_dim, group, dtype, length, pos, weight)
+
+    def workspace(self, n_q_heads: int) -> torch.Tensor:
+        """Scratch for calls with at most n_q_heads query heads (0: eviction only)."""
+        return torch.empty(max(si_kv4_workspace_bytes(self, n_q_heads), 256), dtype=torch.uint8, device=self.data.device)
+
+
+def si_kv4_tile_bytes(head_dim: int, group: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(_lib.si_kv4_tile_bytes(head_dim, group, ctypes.byref(out)), "si_kv4_tile_bytes")
+    return out.value
+
+
+def si_kv4_workspace_bytes(cache: KV4Cache, n_q_heads: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(_lib.si_kv4_workspace_bytes(cache.ref, n_q_heads, ctypes.byref(out)), "si_kv4_workspace_bytes")
+    return out.value
+
+
+def _one_device(a, b):
+    if a.device != b.device:
         raise ValueError("both caches have to be on one device")
+
+
+def si_kv4_store(src: KVCache, dst: KV4Cache, first_pos=None, status=None, stream=None) -> None:
+    """Entries 0 .. src.length - 1 of src behind those of dst; first_pos: int32 [n_seqs] or None."""
+    _one_device(src, dst)
+    _check(_lib.si_kv4_store(src.ref, dst.ref, _ptr(first_pos, "first_pos", dst, (dst.n_seqs,), torch.int32),
+                             _ptr(status, "status", dst, (1,), torch.int32), _on(stream, dst)), "si_kv4_store")
+
+
+def si_kv4_load(src: KV4Cache, dst: KVCache, first, n: int, len_out, status=None, stream=None) -> None:
+    """At most n entries from first[b] on (int32 [n_seqs] or None: 0) to dst's first rows; len_out: int32 [n_seqs] or None."""
+    _one_device(src, dst)
     seqs = (src.n_seqs,)
-    ws, ws_bytes = _ws(workspace, src)
-    _check(_lib.si_kv_evict(src.ref, dst.ref, _ptr(q_pos, "q_pos", src, seqs, torch.int32), n_new, budget, n_sink, n_recent,
-                            _ptr(kept, "kept", src, (src.n_seqs, src.n_kv_heads, budget), torch.int32),
-                            _ptr(len_out, "len_out", src, seqs, torch.int32), ws, ws_bytes,
-                            _ptr(status, "status", src, (1,), torch.int32), _on(stream, src)), "si_kv_evict")
+    _check(_lib.si_kv4_load(src.ref, dst.ref, _ptr(first, "first", src, seqs, torch.int32), n, _ptr(len_out, "len_out", src, seqs, torch.int32),
+                            _ptr(status, "status", src, (1,), torch.int32), _on(stream, src)), "si_kv4_load")
+
+
+def si_kv4_attn_decode(cache: KV4Cache, q, q_pos, k_new, v_new, window: int, n_sink: int, scale: float, out, lse, flags: int,
+                       workspace, status=None, stream=None) -> None:
+    """As si_attn_decode."""
+    _decode(_lib.si_kv4_attn_decode, "si_kv4_attn_decode", cache, q, q_pos, k_new, v_new, window, n_sink, scale, out, lse, flags, workspace, status, stream)
+
+
+def si_kv4_evict(src: KV4Cache, dst: KV4Cache, q_pos, n_new: int, budget: int, n_sink: int, n_recent: int, kept, len_out,
+                 workspace, status=None, stream=None) -> None:
+    """As si_kv_evict."""
+    _evict(_lib.si_kv4_evict, "si_kv4_evict", src, dst, q_pos, n_new, budget, n_sink, n_recent, kept, len_out, workspace, status, stream)
 
 
 # ------------------------------------------------------------------------- owner object

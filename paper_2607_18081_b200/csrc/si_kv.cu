@@ -10,7 +10,7 @@
 // the CTAs add one another's histograms and counts through distributed shared memory.  Then the rows move: bound by HBM
 // (4 * head_dim bytes read and written per moved entry) in a second kernel with eight rows in flight per warp, or, in
 // place with few entries over the budget (a decode step), in the same kernel.
-#include "si_kv.cuh"
+#include "si_evict.cuh"
 #include "si_tc.cuh"
 
 namespace {
@@ -26,19 +26,6 @@ constexpr int kFewOver = 4;                  // at most this many entries over t
 constexpr int kMoveRows = 8;                 // rows in flight per warp of the moving kernel
 constexpr int kMaxGridY = 65535;
 
-struct EvictArgs {
-    si_kv_view src, dst;
-    const int32_t *q_pos;
-    int n_new, budget, n_sink, n_recent, in_place, move_here;
-    int slots;                           // slots that `source` describes: the budget, at most the capacity if it is scratch
-    int32_t *source, *lists;             // [rows][slots]: source slot of every slot (the caller's `kept` or scratch); [rows][cap + 2]:
-                                         // freed slots, then (from cap / 2 + 1) the entries that fill them, at most cap / 2 each
-    int list_source;                     // 0: nobody reads `source` (moves of this kernel only, no `kept`)
-    int32_t *len_out;
-    int32_t *status;
-    int block0;                          // moving kernel: number of the grid's first block of slots
-};
-
 __device__ __forceinline__ uint32_t weight_key(float w) {
     if (w != w) return 0u;
     if (w == 0.f) w = 0.f;
@@ -48,12 +35,6 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
 
 // The lowest n bits.
 __device__ __forceinline__ unsigned int first_bits(int n) { return n >= 32 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << n) - 1; }
-
-__device__ __forceinline__ int entries(const EvictArgs &A, int b) {
-    const int n = si_kv_len(A.src, b, A.status) + A.n_new;
-    if (n > A.src.cap) { si_report(A.status, SI_ERR_OUT_OF_RANGE); return A.src.cap; }
-    return n;
-}
 
 // exclusive scan over the block of two counters packed in 64 bits; *total gets the sum
 __device__ __forceinline__ unsigned long long block_scan(unsigned long long v, unsigned long long *tot, unsigned long long *total) {
@@ -88,7 +69,7 @@ __device__ __forceinline__ unsigned int ld_cluster(const unsigned int *smem, int
     return v;
 }
 
-template <bool SMEM>
+template <bool SMEM, bool Q4>
 __global__ void __launch_bounds__(kRowThreads, 2) evict_select_kernel(const EvictArgs A) {
     extern __shared__ uint32_t keys[];
     __shared__ unsigned int hist[3][kBins], share[3];        // share: counts for the CTAs behind this one
@@ -99,7 +80,7 @@ __global__ void __launch_bounds__(kRowThreads, 2) evict_select_kernel(const Evic
     __shared__ int sh_need;
     const int C = gridDim.x, rank = blockIdx.x, tid = threadIdx.x, h = blockIdx.y, b = blockIdx.z, row = b * A.src.H + h;
     si_tc::pdl_wait();                                       // a programmatic dependent too
-    const int n = entries(A, b), budget = A.budget;
+    const int n = si_evict_entries(A, b), budget = A.budget;
     int32_t *source = A.source + (size_t)row * A.slots, *freed_slots = A.lists + (size_t)row * (A.src.cap + 2), *movers = freed_slots + A.src.cap / 2 + 1;
     if (A.move_here && A.len_out && h == 0 && rank == 0 && tid == 0) A.len_out[b] = min(n, budget);
     si_tc::pdl_launch();
@@ -312,7 +293,10 @@ __global__ void __launch_bounds__(kRowThreads, 2) evict_select_kernel(const Evic
     }
     if (A.list_source)
         for (int i = rank * kRowThreads + tid; i < moves; i += C * kRowThreads) source[freed_slots[i]] = movers[i];
-    if (A.move_here) {
+    if (Q4 && A.move_here) {
+        for (int i = rank * (kRowThreads / kMoveLanes4) + tid / kMoveLanes4; i < moves; i += C * (kRowThreads / kMoveLanes4))
+            si_move_entry4(A, b, h, movers[i], freed_slots[i], tid % kMoveLanes4);
+    } else if (A.move_here) {
         const int lanes = A.src.D / 4, groups = kRowThreads / lanes, lane = tid % lanes;
         const bool is_v = lane >= lanes / 2;
         const int c = (is_v ? lane - lanes / 2 : lane) * 8;
@@ -338,7 +322,7 @@ __global__ void __launch_bounds__(256) evict_move_kernel(const EvictArgs A) {
     const int b = blockIdx.z, h = blockIdx.x, block = FIRST ? blockIdx.y : A.block0 + blockIdx.y, row = b * A.src.H + h, lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
     si_tc::pdl_wait();
     si_tc::pdl_launch();
-    if (FIRST && h == 0 && blockIdx.y == 0 && threadIdx.x == 0 && A.len_out) A.len_out[b] = min(entries(A, b), A.budget);
+    if (FIRST && h == 0 && blockIdx.y == 0 && threadIdx.x == 0 && A.len_out) A.len_out[b] = min(si_evict_entries(A, b), A.budget);
     const bool is_v = lane >= kLanes / 2;
     const int c = (is_v ? lane - kLanes / 2 : lane) * 8, slot0 = block * (kGroups * kMoveRows) + group;
     const uint16_t *from = (is_v ? A.src.v : A.src.k) + A.src.row(b, h, 0) + c;
@@ -374,28 +358,22 @@ __global__ void __launch_bounds__(256) evict_move_kernel(const EvictArgs A) {
 
 __global__ void evict_len_kernel(const EvictArgs A) {
     const int b = blockIdx.x * blockDim.x + threadIdx.x;
-    if (b < A.src.B) A.len_out[b] = min(entries(A, b), A.budget);
-}
-
-size_t evict_ws_bytes(const si_kv_t *kv) {
-    const size_t rows = (size_t)kv->n_seqs * kv->n_kv_heads;
-    return si_align_up(rows * kv->capacity * 4, 256) + si_align_up(rows * ((size_t)kv->capacity + 2) * 4, 256);
+    if (b < A.src.B) A.len_out[b] = min(si_evict_entries(A, b), A.budget);
 }
 
 // CTAs per row: more while the rows leave SMs idle and a slice stays long enough to be worth the exchanges (4096 keys), and
 // as many as it takes for the slices to fit shared memory.
-int cluster_size(const si_kv_t *kv) {
-    const long long rows = (long long)kv->n_seqs * kv->n_kv_heads;
+int cluster_size(long long rows, int capacity) {
     int c = 1;
-    while (c < kMaxCluster && rows * c * 2 <= si_sm_count() && kv->capacity / (c * 2) >= 4096) c *= 2;
-    while (c < kMaxCluster && (kv->capacity + c - 1) / c + 3 > kSliceKeys) c *= 2;
+    while (c < kMaxCluster && rows * c * 2 <= si_sm_count() && capacity / (c * 2) >= 4096) c *= 2;
+    while (c < kMaxCluster && (capacity + c - 1) / c + 3 > kSliceKeys) c *= 2;
     return c;
 }
 
-template <bool SMEM> int launch_select(const EvictArgs &A, int C, size_t smem, cudaStream_t st) {
+template <bool SMEM, bool Q4> int launch_select(const EvictArgs &A, int C, size_t smem, cudaStream_t st) {
     if (smem > 0) {
         static std::atomic<unsigned long long> allowed{0};
-        const int rc = si_allow_smem(evict_select_kernel<SMEM>, kSliceKeys * 4, allowed);
+        const int rc = si_allow_smem(evict_select_kernel<SMEM, Q4>, kSliceKeys * 4, allowed);
         if (rc) return rc;
     }
     cudaLaunchConfig_t cfg = {};
@@ -409,7 +387,7 @@ template <bool SMEM> int launch_select(const EvictArgs &A, int C, size_t smem, c
     at[1].id = cudaLaunchAttributeClusterDimension;
     at[1].val.clusterDim.x = C; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
     cfg.attrs = at; cfg.numAttrs = C > 1 ? 2 : 1;
-    SI_CUDA_TRY(cudaLaunchKernelEx(&cfg, evict_select_kernel<SMEM>, A));
+    SI_CUDA_TRY(cudaLaunchKernelEx(&cfg, evict_select_kernel<SMEM, Q4>, A));
     return SI_OK;
 }
 
@@ -429,11 +407,43 @@ int si_sm_count() {
     return n;
 }
 
+size_t si_evict_ws_bytes(int n_seqs, int n_kv_heads, int capacity) {
+    const size_t rows = (size_t)n_seqs * n_kv_heads;
+    return si_align_up(rows * capacity * 4, 256) + si_align_up(rows * ((size_t)capacity + 2) * 4, 256);
+}
+
+EvictArgs si_evict_args(const si_kv_view &src, const si_kv_view &dst, bool in_place, const int32_t *q_pos, int n_new, int budget, int n_sink, int n_recent,
+                        int32_t *kept, int32_t *len_out, void *workspace, int32_t *status) {
+    const size_t rows = (size_t)src.B * src.H;
+    EvictArgs A{src, dst, q_pos, n_new, budget, n_sink, n_recent, in_place, in_place && src.cap - budget <= kFewMoves,
+                kept || budget < src.cap ? budget : src.cap, kept ? kept : (int32_t *)workspace,
+                (int32_t *)((char *)workspace + si_align_up(rows * src.cap * 4, 256)), 0, len_out, status};
+    A.list_source = kept || !A.move_here;
+    return A;
+}
+
+int si_evict_select(EvictArgs &A, cudaStream_t st) {
+    int32_t *len_out = A.len_out;
+    const bool len_after = A.move_here && len_out == A.src.len;  // the rows of a sequence still read the old length
+    if (len_after) A.len_out = nullptr;
+    const int C = cluster_size((long long)A.src.B * A.src.H, A.src.cap), slice = ((A.src.cap + C - 1) / C + 3) & ~3;
+    const size_t smem = (size_t)slice * 4;
+    const bool q4 = A.src4.data != nullptr;
+    int rc;
+    if (slice <= kSliceKeys) rc = q4 ? launch_select<true, true>(A, C, smem, st) : launch_select<true, false>(A, C, smem, st);
+    else rc = q4 ? launch_select<false, true>(A, 1, 0, st) : launch_select<false, false>(A, 1, 0, st);     // in rounds: one CTA
+    if (rc || !len_after) return rc;
+    A.len_out = len_out;
+    evict_len_kernel<<<(A.src.B + 127) / 128, 128, 0, st>>>(A);
+    SI_CUDA_TRY(cudaGetLastError());
+    return SI_OK;
+}
+
 extern "C" int si_kv_workspace_bytes(const si_kv_t *kv, int n_q_heads, int T, size_t *bytes_out) {
     const int rc = si_kv_check(kv);
     if (rc) return rc;
     if (!bytes_out || n_q_heads < 0 || T < 0 || n_q_heads % kv->n_kv_heads) return SI_ERR_INVALID_ARG;
-    size_t most = kv->weight ? evict_ws_bytes(kv) : 0;
+    size_t most = kv->weight ? si_evict_ws_bytes(kv->n_seqs, kv->n_kv_heads, kv->capacity) : 0;
     if (n_q_heads && T) {
         if (n_q_heads / kv->n_kv_heads > 128) return SI_ERR_UNSUPPORTED;
         const size_t each[3] = {si_attn_decode_ws_bytes(kv, n_q_heads), si_attn_prefill_ws_bytes(kv, n_q_heads, T), kv->weight ? si_attn_weights_ws_bytes(kv) : 0};
@@ -459,26 +469,13 @@ extern "C" int si_kv_evict(const si_kv_t *src, const si_kv_t *dst, const int32_t
     // one row's entries would be read while another's are written there
     if (si_kv_shared(dst) || (!in_place && (src->v == dst->v || src->weight == dst->weight || src->pos == dst->pos))) return SI_ERR_INVALID_ARG;
     if (!si_aligned4(q_pos, kept, len_out, status_dev)) return SI_ERR_ALIGNMENT;
-    if (ws_bytes < evict_ws_bytes(src)) return SI_ERR_NOMEM;
+    if (ws_bytes < si_evict_ws_bytes(src->n_seqs, src->n_kv_heads, src->capacity)) return SI_ERR_NOMEM;
     if (!workspace) return SI_ERR_INVALID_ARG;
     if ((uintptr_t)workspace & 255) return SI_ERR_ALIGNMENT;
-    const size_t rows = (size_t)src->n_seqs * src->n_kv_heads;
-    EvictArgs A{si_kv_view_of(src), si_kv_view_of(dst), q_pos, n_new, budget, n_sink, n_recent, in_place,
-                in_place && src->capacity - budget <= kFewMoves, kept || budget < src->capacity ? budget : src->capacity, kept ? kept : (int32_t *)workspace,
-                (int32_t *)((char *)workspace + si_align_up(rows * src->capacity * 4, 256)), 0, len_out, status_dev};
-    A.list_source = kept || !A.move_here;
+    EvictArgs A = si_evict_args(si_kv_view_of(src), si_kv_view_of(dst), in_place, q_pos, n_new, budget, n_sink, n_recent, kept, len_out, workspace, status_dev);
     si_mt_forget();
     const cudaStream_t st = (cudaStream_t)stream;
-    const bool len_after = A.move_here && len_out == src->len;  // the rows of a sequence still read the old length
-    if (len_after) A.len_out = nullptr;
-    const int C = cluster_size(src), slice = ((src->capacity + C - 1) / C + 3) & ~3;
-    rc = slice <= kSliceKeys ? launch_select<true>(A, C, (size_t)slice * 4, st) : launch_select<false>(A, 1, 0, st);     // in rounds: one CTA
-    if (rc) return rc;
-    if (len_after) {
-        A.len_out = len_out;
-        evict_len_kernel<<<(src->n_seqs + 127) / 128, 128, 0, st>>>(A);
-        SI_CUDA_TRY(cudaGetLastError());
-    }
+    if ((rc = si_evict_select(A, st))) return rc;
     if (A.move_here) return SI_OK;
     const int per_block = 256 / (src->head_dim / 4) * kMoveRows, blocks = (int)(((long long)A.slots + per_block - 1) / per_block);
     cudaLaunchConfig_t cfg = {};

@@ -44,13 +44,15 @@ inline bool si_kv_shared(const si_kv_t *kv) {
 }
 
 // ... and of those that bring queries.
+inline int si_query_check(int n_kv_heads, int n_q_heads, int window, int n_sink, float scale) {
+    if (n_q_heads < 1 || n_q_heads % n_kv_heads || window < 0 || n_sink < 0) return SI_ERR_INVALID_ARG;
+    if (!(scale > -2.0e38f && scale < 2.0e38f)) return SI_ERR_INVALID_ARG;      // scale log2(e) is finite too
+    if (n_q_heads / n_kv_heads > 128) return SI_ERR_UNSUPPORTED;
+    return SI_OK;
+}
 inline int si_attn_check(const si_kv_t *kv, int n_q_heads, int window, int n_sink, float scale) {
     const int rc = si_kv_check(kv);
-    if (rc) return rc;
-    if (n_q_heads < 1 || n_q_heads % kv->n_kv_heads || window < 0 || n_sink < 0) return SI_ERR_INVALID_ARG;
-    if (!(scale > -2.0e38f && scale < 2.0e38f)) return SI_ERR_INVALID_ARG;      // scale log2(e) is finite too
-    if (n_q_heads / kv->n_kv_heads > 128) return SI_ERR_UNSUPPORTED;
-    return SI_OK;
+    return rc ? rc : si_query_check(kv->n_kv_heads, n_q_heads, window, n_sink, scale);
 }
 
 // SMs of the current device when first asked (all devices of a machine are alike here)

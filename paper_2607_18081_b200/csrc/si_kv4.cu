@@ -73,7 +73,7 @@ __global__ void __launch_bounds__(kThreads) store_kernel(const StoreArgs A) {
                 const uint32_t both = r & 1 ? __byte_perm(other, word, 0x7632) : __byte_perm(word, other, 0x5410);
                 *reinterpret_cast<uint32_t *>(sm + T::value_word(r, w, 2 * t + (r & 1))) = both;
             }
-            if (c % GL == 0) *reinterpret_cast<uint32_t *>(sm + (which ? T::kValuePar : T::kKeyPar) + (r * NG + c / GL) * 4) = par;
+            if (c % GL == 0) *reinterpret_cast<uint32_t *>(sm + (which ? T::kValuePar : T::kKeyPar) + (r * NG + T::place_of(c / GL)) * 4) = par;
         }
     }
     __syncwarp();
@@ -146,7 +146,7 @@ __global__ void __launch_bounds__(kThreads) load_kernel(const LoadArgs A) {
     const int tile = first / kTileEntries + blockIdx.x * kWarps + warp, e0 = tile * kTileEntries;
     if (e0 >= end) return;
     const uint8_t *from = A.src.row(b, h) + (long long)tile * T::kBytes;
-    const int c = lane % L, w = c / 4, t = c % 4, g = T::group_of(w);
+    const int c = lane % L, w = c / 4, t = c % 4, g = T::place_of(T::group_of(w));
 #pragma unroll 4
     for (int i = 0; i < kTileEntries; i += ROWS) {
         const int r = i + lane / L;

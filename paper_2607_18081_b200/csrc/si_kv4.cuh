@@ -14,7 +14,8 @@
 //   values   from 16 D: entries in pairs, pair r / 2 of D bytes at D (r / 2); lane g of eight has elements 32 w + 4 g + i (i < 4): D / 8
 //            bytes, word w, the even entry in its lower half, the odd one in its upper half, element i in nibble i of the half.
 //            The eight cells of a pair are permuted by an XOR of g (bank conflicts).
-//   steps    from 32 D: per entry D / group words of step (lower half) and lowest value (upper half) of the keys, then of the values
+//   steps    from 32 D: per entry D / group words of step (lower half) and lowest value (upper half) of the keys, then of the values;
+//            four groups in the order 0, 2, 1, 3 (two lanes of four work on the even groups, two on the odd ones)
 // A word masked with 0x000F000F is then a pair of f16 numbers c 2^-24 (subnormal, and exact in a product with fp32 sums): two
 // neighbouring elements of a key, or one element of two neighbouring entries; with 0x00F000F0, the next ones, times 16.
 #pragma once
@@ -31,6 +32,7 @@ template <int D, int NG> struct si_tile4 {
     // bank conflicts: the sixteen-byte (D = 64: eight-byte) cells that lanes g = 2 a, 2 a + 1 (4 a .. 4 a + 3) of all four t read
     // in one access are then in different banks
     __host__ __device__ static constexpr int swizzle(int t) { return D == 128 ? 2 * t : (t >> 1) * 4; }
+    __host__ __device__ static constexpr int place_of(int g) { return NG == 4 ? (g & 1) << 1 | g >> 1 : g; }      // its own inverse
     __host__ __device__ static constexpr int key_word(int r, int w, int t) { return r * (D / 2) + t * kCell + w * 4; }
     __host__ __device__ static constexpr int value_word(int r, int w, int g) { return kValues + (r >> 1) * D + (g ^ swizzle(r >> 1 & 3)) * kCell + w * 4; }
 };
@@ -116,7 +118,7 @@ template <int DT, int D, int NG> __device__ __forceinline__ void store_entry(con
             const int e = in % 8 + i, nibble = which ? in % 4 + i : (e >> 1) + (e & 1) * 4;
             word |= (code_bits(f[i], low, inverse) & 15u) << (4 * nibble);
         }
-        const int par_at = (which ? T::kValuePar : T::kKeyPar) + (r * NG + lane / GL) * 4;
+        const int par_at = (which ? T::kValuePar : T::kKeyPar) + (r * NG + T::place_of(lane / GL)) * 4;
         if (which == 0) {
 #pragma unroll
             for (int o = 1; o < 8 / E; o <<= 1) word |= __shfl_xor_sync(0xFFFFFFFFu, word, o);

@@ -399,7 +399,8 @@ template <int DT, int D, int NT> int launch(const DecodeArgs &A, cudaStream_t st
     return launch_join<DT, D, NT, 2048 / D>(A, st);
 }
 Layout layout_of(const si_kv_t *kv, int n_q_heads, bool acc) {
-    return layout_of(kPerSm * si_sm_count(), kv->n_seqs, kv->n_kv_heads, kv->head_dim, kv->capacity, n_q_heads, acc);
+    const int n_cta = kPerSm * si_sm_count();
+    return layout_of(n_cta < kMaxParts ? n_cta : kMaxParts, kv->n_seqs, kv->n_kv_heads, kv->head_dim, kv->capacity, n_q_heads, acc);
 }
 template <int DT> int launch_t(const DecodeArgs &A, int NT, cudaStream_t st) {
     if (A.kv.D == 128) return NT == 1 ? launch<DT, 128, 1>(A, st) : launch<DT, 128, 2>(A, st);

@@ -22,15 +22,14 @@
 
 namespace {
 
-// Three CTAs of four warps per SM (registers allow no more; two of four: 69.8 against 63.5 us for one sequence of 260001, four of
-// four with two tiles in flight: 66.8), two for sixteen heads.
-#ifndef K_PER_SM
-#define K_PER_SM 3
-#define K_STAGES 3
-#endif
-constexpr int kWarps = 4, kThreads = kWarps * 32, kMergeWarps = 2;
-template <int H> constexpr int kPerSmOf = H == 16 ? 2 : K_PER_SM;
-template <int H> constexpr int kStagesOf = H == 16 ? 4 : K_STAGES;
+// Three CTAs of four warps per SM (registers allow no more without spills: two 71 us for one sequence of 260001 entries, three 63,
+// four 66), two for sixteen heads; three (four) tiles per warp in flight.  Every warp has a run of tiles of its own: joining the
+// warps of a CTA at an item's end cost more than the additional parts do.
+constexpr int kWarps = 4, kThreads = kWarps * 32;
+template <int H> constexpr int kPerSmOf = H == 16 ? 2 : 3;
+template <int H> constexpr int kStagesOf = H == 16 ? 4 : 3;
+constexpr int kPad = 3;                // an item's start and end take about as long as so many tiles (0: 47.7 us for 512 windows of 2052, 3: 41.7, 8: 44.4)
+constexpr int kMinUnits = 2;           // of a run: fewer would leave more parts than they save time
 
 // H: query heads of a pass, 4, 8 or 16.  Eight fill the eight columns of a product; 16 are two tiles of columns beside the same
 // codes; with four the columns are two neighbouring groups side by side (a word of codes meets zeros in the columns of the
@@ -38,14 +37,62 @@ template <int H> constexpr int kStagesOf = H == 16 ? 4 : K_STAGES;
 template <int H> constexpr int kTilesOf = H == 16 ? 2 : 1;
 template <int D, int NG, int H> struct Cfg {
     static constexpr int kTile = si_tile4<D, NG>::kBytes, kStage = kTile + 128;      // ... and the entries' positions; a multiple of 128
-    static constexpr int kRow = D + 4, kMerge = 8 * kRow;                            // merge buffer of a warp: eight heads at a time, rows padded
-    static constexpr int kSmem = kWarps * kStagesOf<H> * kStage + kMergeWarps * kMerge * 4 + kWarps * 8 * kTilesOf<H> * 2 * 4;
+    static constexpr int kSmem = kWarps * kStagesOf<H> * kStage;
 };
 
 struct Decode4Args {
     DecodeArgs d;
     si_kv4_view kv;
 };
+
+// Runs: the tiles of all (sequence, head block) items in one row, in front of every item kPad units without a tile, which stand for
+// the time an item's start and end take (short items are then not crowded into one run); run i of n has units total * i / n up to
+// total * (i + 1) / n.  A.n_cta is the number of warps; there are fewer runs if they had less than kMinUnits.
+struct Runs {
+    int total, n;
+    __device__ __forceinline__ int first(int i) const { return (int)((long long)total * i / n); }
+    __device__ __forceinline__ int of(int unit) const { return (int)(((long long)n * (unit + 1) - 1) / total); }      // the run of a unit
+};
+__device__ __forceinline__ int units(const SeqWork &w) { return w.nc > 0 ? w.nc + kPad : 0; }
+__device__ __forceinline__ void next_unit_item(const DecodeArgs &A, Cursor &c) {      // there is one
+    c.start += units(c.w);
+    if (++c.hh < A.kv.H * A.GB) return;
+    c.hh = 0;
+    do c.w = seq_work<kTileEntries>(A, ++c.b, nullptr); while (c.w.nc == 0);
+}
+// The item of the first unit of every warp's run, in `at` (where there is one).  Thread t stands for sequences t * share ..; the one
+// that holds a run's first unit looks it up.
+__device__ __forceinline__ Runs find_runs(const DecodeArgs &A, Cursor *at, int *sh, int32_t *status, bool *some_empty) {
+    const int tid = threadIdx.x, share = (A.kv.B + kThreads - 1) / kThreads, items = A.kv.H * A.GB;
+    const int b0 = min(A.kv.B, tid * share), b1 = min(A.kv.B, b0 + share);
+    int sum = 0;
+    bool empty = false;
+    SeqWork w;
+    for (int b = b0; b < b1; ++b) {
+        w = seq_work<kTileEntries>(A, b, status);
+        sum += units(w) * items;
+        empty |= w.nc == 0;
+    }
+    const int before = si_block_scan<kThreads>(sum, sh);
+    const Runs r{sh[kThreads / 32], min(A.n_cta, (sh[kThreads / 32] + kMinUnits - 1) / kMinUnits)};
+    if (r.total > 0)
+        for (int i = 0; i < kWarps; ++i) {
+            const int run = i * gridDim.x + blockIdx.x;
+            if (run >= r.n) break;
+            const int g0 = r.first(run);
+            if (before > g0 || g0 - before >= sum) continue;
+            Cursor c;
+            int start = before;
+            c.b = b0;
+            c.w = share > 1 ? seq_work<kTileEntries>(A, b0, nullptr) : w;      // with one sequence per thread it is at hand
+            while (start + units(c.w) * items <= g0) { start += units(c.w) * items; c.w = seq_work<kTileEntries>(A, ++c.b, nullptr); }
+            c.hh = (g0 - start) / units(c.w);
+            c.start = start + c.hh * units(c.w);
+            at[i] = c;
+        }
+    *some_empty = __syncthreads_or(empty);
+    return r;
+}
 
 __device__ __forceinline__ float pow2(int e) { return __int_as_float((e + 127) << 23); }          // -126 .. 127
 __device__ __forceinline__ int exponent(float x) { return (int)(__float_as_uint(x) >> 23 & 255) - 127; }
@@ -56,13 +103,17 @@ template <int N> __device__ __forceinline__ void load_words(uint32_t (&r)[N], co
 }
 
 // The queries of an item as B operands (head lane / 4).  f: per word of codes the elements (0, 1), (2, 3) / 16, (4, 5), (6, 7) / 16.
-// sum: the sums of the groups' elements, for the product with the words (step, lowest value) of the keys as they lie there: 0 beside
-// the step, and beside the lowest value the sum in kParts 16-bit parts, 24 (f16: 22) bits together.  back: what a score is to be
-// multiplied with, above 0 (the sign is in the others), of the lane's heads, 2 (lane % 4) + {0, 1} (H = 4: 2 (lane % 2) + {0, 1}).
+// sum: the sums of the groups' elements, for the product with the words (lowest value, step) of the keys as they lie there: 0 beside
+// the step, and beside the lowest value the sum in kParts 16-bit parts, 24 (f16: 22) bits together.  Lane t of four has in its two
+// registers the groups whose words lie at kOwn (t / 2) and kOwn (t / 2) + 1 (one register's only where kOwn is 1), and part t % 2 of
+// them; the third part takes a product of its own, or the other register.
+// back: what a score is to be multiplied with, above 0 (the sign is in the others), and lazy: how far one may be above the
+// maximum, of the lane's heads, 2 (lane % 4) + {0, 1} (H = 4: 2 (lane % 2) + {0, 1}).
 template <int DT> constexpr int kParts = DT == SI_BF16 ? 3 : 2;
 template <int DT> constexpr float kSumScale = DT == SI_BF16 ? 0x1p-24f : 0x1p-8f;       // f16 has no room for 2^-24
-template <int DT, int NG> constexpr int kSumSteps = (kParts<DT> * NG + 7) / 8;           // products of eight words
-template <int DT, int D, int NG, int H> struct Query { uint32_t f[kTilesOf<H>][D / 32][4], sum[kTilesOf<H>][kSumSteps<DT, NG>][2]; float back[kTilesOf<H>][2]; };
+template <int DT, int NG> constexpr int kSumSteps = NG == 4 ? kParts<DT> - 1 : 1;
+template <int NG> constexpr int kOwn = NG == 4 ? 2 : 1;
+template <int DT, int D, int NG, int H> struct Query { uint32_t f[kTilesOf<H>][D / 32][4], sum[kTilesOf<H>][kSumSteps<DT, NG>][2]; float back[kTilesOf<H>][2], lazy[kTilesOf<H>][2]; };
 template <int DT, int D, int NG, int H> __device__ __forceinline__ void load_q(const DecodeArgs &A, int b, int hh, Query<DT, D, NG, H> &Q) {
     using T = si_tile4<D, NG>;
     constexpr int NT = kTilesOf<H>;
@@ -114,19 +165,29 @@ template <int DT, int D, int NG, int H> __device__ __forceinline__ void load_q(c
             float rest = sum[g] * kSumScale<DT>;
 #pragma unroll
             for (int i = 0; i < kParts<DT>; ++i) {
-                part[i][g] = (uint32_t)si_cvt<DT>::from_float(rest) << 16;
-                rest -= si_cvt<DT>::hi(part[i][g]);
+                part[i][g] = si_cvt<DT>::from_float(rest);
+                rest -= si_cvt<DT>::lo(part[i][g]);
             }
         }
-        // word t (and t + 4) of a step of eight is part i / NG of group i % NG, i its number
 #pragma unroll
-        for (int i = 0; i < kSumSteps<DT, NG> * 8; ++i)
-            if (i % 4 == 0) Q.sum[nt][i / 8][i / 4 % 2] = 0;
+        for (int i = 0; i < kSumSteps<DT, NG>; ++i)
 #pragma unroll
-        for (int i = 0; i < kParts<DT> * NG; ++i)
-            if (t == i % 4 && !(PAIR && lane >> 4)) Q.sum[nt][i / 8][i / 4 % 2] = part[i / NG][T::place_of(i % NG)];
+            for (int r = 0; r < 2; ++r) {
+                uint32_t v = 0;
+#pragma unroll
+                for (int k = 0; k < kParts<DT>; ++k)
+#pragma unroll
+                    for (int place = 0; place < NG; ++place) {
+                        // NG = 4: part 2 i + t % 2 of place 2 (t / 2) + r; NG = 2: part 2 r + t % 2 of place t / 2; NG = 1: part 2 r + t % 2, t < 2
+                        const bool here = NG == 4 ? k == 2 * i + t % 2 && place == 2 * (t / 2) + r : k == 2 * r + t % 2 && place == t / 2;
+                        if (here && !(PAIR && lane >> 4)) v = part[k][T::place_of(place)];
+                    }
+                Q.sum[nt][i][r] = v;
+            }
 #pragma unroll
         for (int c = 0; c < 2; ++c) Q.back[nt][c] = fminf(fmaxf(fabsf(A.scale2) * pow2(__shfl_sync(0xFFFFFFFFu, e, 8 * (PAIR ? t & 1 : t) + 4 * c) + 10), 1.2e-38f), 3.4e38f);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) Q.lazy[nt][c] = kLazy / Q.back[nt][c];
     }
 }
 
@@ -138,6 +199,15 @@ template <int DT> __device__ __forceinline__ void product(float (&c)[4], const u
     else
         asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
             : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// ... onto zeros.
+template <int DT> __device__ __forceinline__ void first_product(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    if (DT == SI_BF16)
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+            : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+    else
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+            : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
 }
 __device__ __forceinline__ uint32_t transposed(uint32_t x) { uint32_t r; asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x)); return r; }
 
@@ -158,13 +228,11 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
     const DecodeArgs &A = A4.d;
     extern __shared__ __align__(128) char smem[];
     __shared__ int sh_scan[kThreads / 32 + 1];
-    __shared__ Cursor sh_at;
+    __shared__ Cursor sh_item[kWarps], sh_load[kWarps];        // every warp's item to work on and to load from
     __shared__ uint64_t full[kWarps][kStages];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, lg = lane >> 2, lt = lane & 3;
     const int head_of = PAIR ? 2 * (lt & 1) : 2 * lt, par_of = PAIR ? (lt >> 1) * L * 4 : 0;      // the lane's first head, where its groups' words are
     char *ring = smem + warp * kStages * C::kStage;
-    float *merge_o = (float *)(smem + kWarps * kStages * C::kStage);
-    float *ml = merge_o + kMergeWarps * C::kMerge;
     if (lane == 0) {
 #pragma unroll
         for (int s = 0; s < kStages; ++s) si_tc::mbar_init(&full[warp][s], 1);
@@ -177,50 +245,61 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
     asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(once));
     asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(stay));
 
-    // this CTA's run of tiles
-    const Run run = find_run<CH, kThreads>(A, &sh_at, sh_scan, blockIdx.x == 0 ? A.status : nullptr);
-    const int per = run.per, g0 = run.g0, g1 = run.g1;
-    Cursor cons = sh_at;
+    // this warp's run
+    bool some_empty;
+    const Runs runs = find_runs(A, sh_item, sh_scan, blockIdx.x == 0 ? A.status : nullptr, &some_empty);
+    const int my_run = warp * gridDim.x + blockIdx.x;      // few runs: on all SMs alike
+    const bool any = my_run < runs.n;
+    const int g0 = any ? runs.first(my_run) : 0, g1 = any ? runs.first(my_run + 1) : 0;
 
-    // ---- loader side: tiles g0 + warp, + kWarps, ..; load_left of them from load_from on lie at equal distances
-    Cursor load = cons;
-    int load_id = g0 + warp, load_stage = 0, load_left = 0;
+    // ---- loader side: load_left tiles from load_from on lie one behind the other
+    int load_id = g0, load_left = 0;
     const uint8_t *load_from = nullptr;
     const int32_t *load_pos = nullptr;
+    if (lane == 0) sh_load[warp] = sh_item[warp];
+    __syncwarp();
     const uint32_t ring_addr = si_tc::smem_u32(ring);
-    auto issue = [&]() {
-        if (load_id >= g1) return;
+    auto issue = [&](int stage) {
         if (load_left == 0) {
-            while (load_id >= load.start + load.w.nc) next_item<CH>(A, load);
-            const int t = load_id - load.start, h = load.hh / A.GB;
+            if (load_id >= g1) return;
+            Cursor load = sh_load[warp];
+            if (load_id >= load.start + kPad + load.w.nc) {
+                next_unit_item(A, load);
+                __syncwarp();
+                if (lane == 0) sh_load[warp] = load;
+                __syncwarp();
+            }
+            const int first = load.start + kPad;
+            load_id = max(load_id, first);
+            if (load_id >= g1) return;
+            const int t = load_id - first, h = load.hh / A.GB;
             const bool sink = t < load.w.c_sink;
             const int c = sink ? t : load.w.c_win + t - load.w.c_sink;
-            load_left = ((sink ? load.w.c_sink : load.w.nc) - t + kWarps - 1) / kWarps;
+            load_left = min(sink ? load.w.c_sink : load.w.nc, g1 - first) - t;
             load_from = A4.kv.row(load.b, h) + (long long)c * C::kTile;
             if (A.kv.pos) load_pos = A.kv.pos + A.kv.meta(load.b, h) + c * CH;
         }
         if (lane == 0) {
-            uint64_t *bar = &full[warp][load_stage];
-            const uint32_t to = ring_addr + load_stage * C::kStage;
+            uint64_t *bar = &full[warp][stage];
+            const uint32_t to = ring_addr + stage * C::kStage;
             si_tc::mbar_arrive_expect_tx(bar, C::kTile + (A.kv.pos ? CH * 4 : 0));
             bulk_load(to, load_from, C::kTile, bar, once);
             if (A.kv.pos) bulk_load(to + C::kTile, load_pos, CH * 4, bar, once);
         }
-        load_from += kWarps * C::kTile;
-        if (A.kv.pos) load_pos += kWarps * CH;
+        load_from += C::kTile;
+        if (A.kv.pos) load_pos += CH;
         --load_left;
-        load_id += kWarps;
-        load_stage = load_stage + 1 == kStages ? 0 : load_stage + 1;
+        ++load_id;
     };
 #pragma unroll
-    for (int s = 0; s < kStages; ++s) issue();
+    for (int s = 0; s < kStages; ++s) issue(s);
 
     // ---- consumer side
-    int id = g0 + warp, stage = 0;
+    int id = g0, stage = 0;
     uint32_t parity = 0;
     bool first_segment = true;
     Query<DT, D, NG, H> Q;
-    if (g0 < g1) load_q<DT, D, NG, H>(A, cons.b, cons.hh, Q);
+    if (any) load_q<DT, D, NG, H>(A, sh_item[warp].b, sh_item[warp].hh, Q);
     // A new entry is stored by the warp that works on it.  One that its query does not see (entries without positions, and a
     // query position given that lies before the entry or a window behind it) is stored here.
     if (A.kn && A.q_pos && !A.kv.pos)
@@ -232,43 +311,52 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
             si_q4::store_entry<DT, D, NG>(A.kn + from, A.vn + from, w.n_old % CH, (char *)A4.kv.row(b, h) + (long long)(w.n_old / CH) * C::kTile, nullptr);
         }
     // sequences without a visible entry have no tile: their rows are zero
-    if (run.empty)
+    if (some_empty)
         for (int b = blockIdx.x; b < A.kv.B; b += gridDim.x) {
             if (seq_work<CH>(A, b, nullptr).nc) continue;
             for (int i = tid; i < A.Hq * D; i += kThreads) A.out[(long long)b * A.Hq * D + i] = 0;
             if (A.lse) for (int i = tid; i < A.Hq; i += kThreads) A.lse[(long long)b * A.Hq + i] = -INFINITY;
         }
-    if (g0 >= g1) return;
+    if (!any) return;
     while (true) {
-        const int seg_end = min(g1, cons.start + cons.w.nc);
-        const int h = cons.hh / A.GB, gb = cons.hh % A.GB, head0 = gb * HB, heads = min(HB, A.G - head0);
-        const SeqWork w = cons.w;
-        // o: sum p s c 2^-24.  Word i: elements 4 lg + 2 n, 4 lg + 2 n + 1 (the latter times 16) in the two halves of quad 2 i + n.  H = 4: words k of
-        // an even and an odd group, in the halves of four quads, one per element; those of the lane's own groups count.
+        const Cursor &item = sh_item[warp];
+        const int start = item.start + kPad, end = start + item.w.nc, c_sink = item.w.c_sink, c_skip = item.w.c_win - c_sink, seg_end = min(g1, end);
+        if (start >= g1) return;               // nothing of this item is in the run
+        const int h = item.hh / A.GB, gb = item.hh % A.GB, head0 = gb * HB, heads = min(HB, A.G - head0), seq = item.b;
+        // tiles numbered whole0 .. whole0 + whole_n - 1 are visible throughout and hold no new entry (without positions)
+        int whole0 = 0, whole_n = 0;
+        if (!A.kv.pos) {
+            const SeqWork &w = item.w;
+            const int from = w.lo == INT_MIN ? 0 : max(w.lo, -1) + 1, to = min(min(w.n, w.n_old), w.s >= INT_MAX - 1 ? INT_MAX : w.s + 1);
+            const int c0 = max((from + CH - 1) / CH, w.c_win);
+            whole0 = start - c_skip + c0;
+            whole_n = max(0, to / CH - c0);
+        }
+        id = max(id, start);
+        float *scores_to = A.scores + (((long long)seq * A.kv.H + h) * A.GB + gb) * A.kv.cap * A.GS;
+        // o: sum p s c 2^-24.  Word i: elements 4 lg + 2 n, 4 lg + 2 n + 1 (the latter times 16, the former plus the latter) in the two halves of
+        // quad 2 i + n.  H = 4: words k of an even and an odd group, in the halves of four quads, one per element; those of the lane's
+        // own groups count.
         // low: sum p m of this lane's entries
         float o[NT][2 * W][4] = {}, low[NT][L][2] = {};
-        // m: the maximum, raw: the same without the factor `back`, edge: the score that moves it; base: what p is relative to, 0 while there is none
-        float m[NT][2], raw[NT][2], edge[NT][2], base[NT][2], l[NT][2];
+        // the maximum and the score that moves it, both without the factor `back`; base: what p is relative to, 0 while there is none
+        float m[NT][2], edge[NT][2], base[NT][2], l[NT][2];
         int E = -1000;
-        uint32_t most = 0;                                 // 2^E in 16 bits: no step so far is above
+        uint32_t most = 0;                                 // 2^E in the place of a step: no word of a value so far is above
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) { m[nt][0] = m[nt][1] = raw[nt][0] = raw[nt][1] = edge[nt][0] = edge[nt][1] = -INFINITY; base[nt][0] = base[nt][1] = l[nt][0] = l[nt][1] = 0.f; }
-        // tiles whose first entry lies in all0 .. all1 are visible throughout and hold no new entry (without positions)
-        const int all0 = w.lo == INT_MIN ? 0 : max(w.lo, -1) + 1, all1 = A.kv.pos ? -1 : min(min(w.n, w.n_old), w.s >= INT_MAX - 1 ? INT_MAX : w.s + 1) - CH;
+        for (int nt = 0; nt < NT; ++nt) { m[nt][0] = m[nt][1] = edge[nt][0] = edge[nt][1] = -INFINITY; base[nt][0] = base[nt][1] = l[nt][0] = l[nt][1] = 0.f; }
         // The next tile in the ring: waits for it, clears the steps of hidden entries (they must not meet the products: 0 * NaN), puts the
-        // new entry in its place.  Which entries are visible, and the number of the first.
-        auto prepare = [&](int id, char *&tile, uint32_t &vis, int &j0) {
+        // new entry in its place.  Which entries are visible.
+        auto first_of = [&]() { const int t = id - start; return (t < c_sink ? t : t + c_skip) * CH; };
+        auto prepare = [&](char *tile) -> uint32_t {
             if (!si_tc::mbar_wait(&full[warp][stage], parity, si_tc::kSpinLimit)) si_report(A.status, SI_ERR_TIMEOUT);
-            tile = ring + stage * C::kStage;
-            if (++stage == kStages) { stage = 0; parity ^= 1; }
-            const int t = id - cons.start;
-            j0 = (t < w.c_sink ? t : w.c_win + t - w.c_sink) * CH;
-            vis = 0xFFFFFFFFu;
-            if (j0 >= all0 && j0 <= all1) return;
+            if ((unsigned)(id - whole0) < (unsigned)whole_n) return 0xFFFFFFFFu;
+            const int j0 = first_of();
+            const SeqWork w = item.w;
             const int j = j0 + lane;
             int p = j;
             if (A.kv.pos) p = j == w.n_old ? w.s : *reinterpret_cast<const int *>(tile + C::kTile + lane * 4);
-            vis = __ballot_sync(0xFFFFFFFFu, j < w.n && si_visible(p, w.s, w.lo, A.n_sink));
+            const uint32_t vis = __ballot_sync(0xFFFFFFFFu, j < w.n && si_visible(p, w.s, w.lo, A.n_sink));
             const bool fresh = w.n_old >= j0 && w.n_old - j0 < CH && (vis >> (w.n_old - j0) & 1);
             if (vis != 0xFFFFFFFFu) {
                 if (!(vis >> lane & 1))
@@ -280,98 +368,131 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
                 __syncwarp();
             }
             if (fresh) {                       // into the tile here and in the cache
-                const long long from = cons.b * A.new_ss + (long long)h * D;
-                si_q4::store_entry<DT, D, NG>(A.kn + from, A.vn + from, w.n_old - j0, tile, gb == 0 ? (char *)A4.kv.row(cons.b, h) + (long long)(j0 / CH) * C::kTile : nullptr);
-                if (gb == 0 && A.kv.pos && lane == 0) A.kv.pos[A.kv.meta(cons.b, h) + w.n_old] = w.s;
+                const long long from = seq * A.new_ss + (long long)h * D;
+                si_q4::store_entry<DT, D, NG>(A.kn + from, A.vn + from, w.n_old - j0, tile, gb == 0 ? (char *)A4.kv.row(seq, h) + (long long)(j0 / CH) * C::kTile : nullptr);
+                if (gb == 0 && A.kv.pos && lane == 0) A.kv.pos[A.kv.meta(seq, h) + w.n_old] = w.s;
                 __syncwarp();
             }
             if (vis != 0xFFFFFFFFu || fresh) si_tc::fence_async_proxy();      // the next copy into this stage comes behind these writes
+            return vis;
         };
-        // Scores of entries 16 u .. 16 u + 15 but for the factor `back`: rows lg and lg + 8, the lane's heads.
-        auto scores = [&](const char *tile, int u, float (&x)[NT][4]) {
-            uint32_t ka[W], kb[W], pa[L], pb[L];
-            load_words(ka, tile + u * 8 * D + lane * T::kCell);
-            load_words(kb, tile + u * 8 * D + 4 * D + lane * T::kCell);
-            load_words(pa, tile + T::kKeyPar + (u * 16 + lg) * NG * 4 + par_of);
-            load_words(pb, tile + T::kKeyPar + (u * 16 + 8 + lg) * NG * 4 + par_of);
-            const uint32_t wa = *reinterpret_cast<const uint32_t *>(tile + T::kKeyPar + ((u * 16 + lg) * NG + lt % NG) * 4);
-            const uint32_t wb = *reinterpret_cast<const uint32_t *>(tile + T::kKeyPar + ((u * 16 + 8 + lg) * NG + lt % NG) * 4);
-            float acc[NT][L][4] = {}, sum[NT][4] = {};
+        // Scores but for the factor `back`: entries 16 u + lg and 16 u + lg + 8, the lane's heads.  The products of both halves of a tile take
+        // turns: they wait for their own sums only.
+        auto scores = [&](const char *tile, float (&x)[2][NT][4]) {
+            uint32_t ka[2][W], kb[2][W], pa[2][L], pb[2][L];
+            float acc[2][NT][L][4], sum[2][NT][4];
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+            for (int u = 0; u < 2; ++u) {
+                load_words(ka[u], tile + u * 8 * D + lane * T::kCell);
+                load_words(kb[u], tile + u * 8 * D + 4 * D + lane * T::kCell);
+                load_words(pa[u], tile + T::kKeyPar + (u * 16 + lg) * NG * 4 + par_of);
+                load_words(pb[u], tile + T::kKeyPar + (u * 16 + 8 + lg) * NG * 4 + par_of);
+                uint32_t wa[kOwn<NG>], wb[kOwn<NG>];
+                if constexpr (PAIR || NG == 1) {
 #pragma unroll
-                for (int i = 0; i < kSumSteps<DT, NG>; ++i) {
-                    const uint32_t a[4] = {wa, wb, wa, wb};
-                    product<DT>(sum[nt], a, Q.sum[nt][i][0], Q.sum[nt][i][1]);
+                    for (int r = 0; r < kOwn<NG>; ++r) { wa[r] = pa[u][r]; wb[r] = pb[u][r]; }
+                } else {
+                    load_words(wa, tile + T::kKeyPar + (u * 16 + lg) * NG * 4 + (lt >> 1) * kOwn<NG> * 4);
+                    load_words(wb, tile + T::kKeyPar + (u * 16 + 8 + lg) * NG * 4 + (lt >> 1) * kOwn<NG> * 4);
                 }
+                const uint32_t a[4] = {wa[0], wb[0], wa[kOwn<NG> - 1], wb[kOwn<NG> - 1]};
 #pragma unroll
-            for (int i = 0; i < W; ++i) {
+                for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const uint32_t a[4] = {si_q4::low_codes(ka[i] >> 8 * half), si_q4::low_codes(kb[i] >> 8 * half), si_q4::high_codes(ka[i] >> 8 * half), si_q4::high_codes(kb[i] >> 8 * half)};
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) product<SI_F16>(acc[nt][PAIR ? T::group_of(i) / 2 : T::group_of(i)], a, Q.f[nt][i][2 * half], Q.f[nt][i][2 * half + 1]);
-                }
+                    for (int i = 0; i < kSumSteps<DT, NG>; ++i) {
+                        if (i == 0) first_product<DT>(sum[u][nt], a, Q.sum[nt][i][0], Q.sum[nt][i][1]);
+                        else product<DT>(sum[u][nt], a, Q.sum[nt][i][0], Q.sum[nt][i][1]);
+                    }
             }
+            constexpr int WL = W / L;          // words of a sum
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+            for (int k = 0; k < WL; ++k)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float y = sum[nt][e] * (0x1p-24f / kSumScale<DT>);
+                for (int half = 0; half < 2; ++half)
 #pragma unroll
-                    for (int g = 0; g < L; ++g) y = fmaf(acc[nt][PAIR ? g : T::place_of(g)][e], si_cvt<DT>::lo(e >> 1 ? pb[g] : pa[g]), y);
-                    x[nt][e] = PAIR ? y + __shfl_xor_sync(0xFFFFFFFFu, y, 2) : y;
-                }
+                    for (int g = 0; g < L; ++g)
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            const int i = g * WL + k;
+                            const uint32_t a[4] = {si_q4::low_codes(ka[u][i] >> 8 * half), si_q4::low_codes(kb[u][i] >> 8 * half), si_q4::high_codes(ka[u][i] >> 8 * half), si_q4::high_codes(kb[u][i] >> 8 * half)};
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) {
+                                if (k == 0 && half == 0) first_product<SI_F16>(acc[u][nt][g], a, Q.f[nt][i][0], Q.f[nt][i][1]);
+                                else product<SI_F16>(acc[u][nt][g], a, Q.f[nt][i][2 * half], Q.f[nt][i][2 * half + 1]);
+                            }
+                        }
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        float y = sum[u][nt][e] * (0x1p-24f / kSumScale<DT>);
+#pragma unroll
+                        for (int g = 0; g < L; ++g) y = fmaf(acc[u][nt][PAIR ? g : T::place_of(g)][e], si_cvt<DT>::hi(e >> 1 ? pb[u][g] : pa[u][g]), y);
+                        x[u][nt][e] = PAIR ? y + __shfl_xor_sync(0xFFFFFFFFu, y, 2) : y;
+                    }
         };
         // p of the same entries, and their share of the sums.
-        auto add = [&](const char *tile, int u, const float (&x)[NT][4], const uint32_t (&vp)[2][L]) {
-            uint32_t va[W], vb[W], pf[NT][L][2];
-            load_words(va, tile + T::kValues + u * 8 * D + lt * D + (lg ^ T::swizzle(lt)) * T::kCell);
-            load_words(vb, tile + T::kValues + u * 8 * D + 4 * D + lt * D + (lg ^ T::swizzle(lt)) * T::kCell);
+        auto add = [&](const char *tile, const float (&x)[2][NT][4], const uint32_t (&vp)[2][2][L]) {
+            uint32_t va[2][W], vb[2][W], pf[2][NT][L][2];
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                float p[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    p[e] = ex2(fmaf(x[nt][e], Q.back[nt][e & 1], -base[nt][e & 1]));
-                    l[nt][e & 1] += p[e];
-                }
-#pragma unroll
-                for (int g = 0; g < L; ++g)
-#pragma unroll
-                    for (int r = 0; r < 2; ++r) {
-                        const float s = si_cvt<DT>::lo(vp[r][g]), mn = si_cvt<DT>::hi(vp[r][g]);
-                        pf[nt][g][r] = transposed(pack2<SI_F16>(p[2 * r] * s, p[2 * r + 1] * s));
-                        low[nt][g][0] = fmaf(p[2 * r], mn, low[nt][g][0]);
-                        low[nt][g][1] = fmaf(p[2 * r + 1], mn, low[nt][g][1]);
-                    }
+            for (int u = 0; u < 2; ++u) {
+                load_words(va[u], tile + T::kValues + u * 8 * D + lt * D + (lg ^ T::swizzle(lt)) * T::kCell);
+                load_words(vb[u], tile + T::kValues + u * 8 * D + 4 * D + lt * D + (lg ^ T::swizzle(lt)) * T::kCell);
             }
-            if constexpr (PAIR) {
 #pragma unroll
-                for (int i = 0; i < W / 2; ++i) {
-                    const int even = i / GW * 2 * GW + i % GW, odd = even + GW;
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
-                    for (int n = 0; n < 4; ++n) {
-                        auto codes = [&](uint32_t w) { return n & 1 ? si_q4::high_codes(w >> 8 * (n / 2)) : si_q4::low_codes(w >> 8 * (n / 2)); };
-                        const uint32_t a[4] = {codes(va[even]), codes(va[odd]), codes(vb[even]), codes(vb[odd])};
-                        product<SI_F16>(o[0][4 * i + n], a, pf[0][i / GW][0], pf[0][i / GW][1]);
+                for (int nt = 0; nt < NT; ++nt) {
+                    float p[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        p[e] = ex2(fmaf(x[u][nt][e], Q.back[nt][e & 1], -base[nt][e & 1]));
+                        l[nt][e & 1] += p[e];
                     }
+#pragma unroll
+                    for (int g = 0; g < L; ++g)
+#pragma unroll
+                        for (int r = 0; r < 2; ++r) {
+                            const float s = si_cvt<DT>::hi(vp[u][r][g]), mn = si_cvt<DT>::lo(vp[u][r][g]);
+                            pf[u][nt][g][r] = transposed(pack2<SI_F16>(p[2 * r] * s, p[2 * r + 1] * s));
+                            low[nt][g][0] = fmaf(p[2 * r], mn, low[nt][g][0]);
+                            low[nt][g][1] = fmaf(p[2 * r + 1], mn, low[nt][g][1]);
+                        }
                 }
-            } else {
+            // A byte masked as a whole (h 16 + l) and its upper nibble: two operands by one instruction each; l is the difference at the end.
+            auto codes = [&](uint32_t w, int n) {
+                const uint32_t bytes = n < 2 ? w : __byte_perm(w, 0, 0x4341);
+                return n & 1 ? si_q4::high_codes(bytes) : n < 2 ? w & 0x00FF00FFu : bytes;
+            };
 #pragma unroll
-                for (int i = 0; i < W; ++i)
+            for (int u = 0; u < 2; ++u)
+                if constexpr (PAIR) {
 #pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        const uint32_t a[4] = {si_q4::low_codes(va[i] >> 8 * half), si_q4::high_codes(va[i] >> 8 * half), si_q4::low_codes(vb[i] >> 8 * half), si_q4::high_codes(vb[i] >> 8 * half)};
+                    for (int i = 0; i < W / 2; ++i) {
+                        const int even = i / GW * 2 * GW + i % GW, odd = even + GW;
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) product<SI_F16>(o[nt][2 * i + half], a, pf[nt][T::place_of(T::group_of(i))][0], pf[nt][T::place_of(T::group_of(i))][1]);
+                        for (int n = 0; n < 4; ++n) {
+                            const uint32_t a[4] = {codes(va[u][even], n), codes(va[u][odd], n), codes(vb[u][even], n), codes(vb[u][odd], n)};
+                            product<SI_F16>(o[0][4 * i + n], a, pf[u][0][i / GW][0], pf[u][0][i / GW][1]);
+                        }
                     }
-            }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < W; ++i)
+#pragma unroll
+                        for (int half = 0; half < 2; ++half) {
+                            const uint32_t a[4] = {codes(va[u][i], 2 * half), codes(va[u][i], 2 * half + 1), codes(vb[u][i], 2 * half), codes(vb[u][i], 2 * half + 1)};
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) product<SI_F16>(o[nt][2 * i + half], a, pf[u][nt][T::place_of(T::group_of(i))][0], pf[u][nt][T::place_of(T::group_of(i))][1]);
+                        }
+                }
         };
         float x[2][NT][4];
         uint32_t vp[2][2][L];
         // Hidden entries out of the scores; the scores out for the weights; steps of the values; whether the base has to move first.
-        auto settle = [&](const char *tile, uint32_t vis, int j0) {
+        auto settle = [&](const char *tile, uint32_t vis) {
             if (vis != 0xFFFFFFFFu) {
 #pragma unroll
                 for (int u = 0; u < 2; ++u)
@@ -381,16 +502,16 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
                         for (int e = 0; e < 4; ++e)
                             if (!(vis >> (u * 16 + lg + (e >> 1) * 8) & 1)) x[u][nt][e] = -INFINITY;
             }
-            uint32_t top16 = 0;
+            uint32_t top = 0;
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
                     load_words(vp[u][r], tile + T::kValuePar + (u * 16 + r * 8 + lg) * NG * 4 + par_of);
 #pragma unroll
-                    for (int g = 0; g < L; ++g) top16 = __vmaxu2(top16, vp[u][r][g]);
+                    for (int g = 0; g < L; ++g) top = max(top, vp[u][r][g]);
                 }
-            bool grow = (top16 & 0xFFFFu) > most;
+            bool grow = top > most;
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -398,7 +519,9 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
 #pragma unroll
                     for (int e = 0; e < 4; ++e) grow |= x[u][nt][e] > edge[nt][e & 1];
             if (A.acc) {
-                float *sc = A.scores + ((((long long)cons.b * A.kv.H + h) * A.GB + gb) * A.kv.cap + j0) * A.GS;
+                const int j0 = first_of();
+                float *sc = scores_to + (long long)j0 * A.GS;
+                const int left = vis == 0xFFFFFFFFu ? CH : item.w.n - j0;         // entries of the tile
 #pragma unroll
                 for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -406,9 +529,9 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
 #pragma unroll
                         for (int e = 0; e < 4; e += 2) {
                             const int key = u * 16 + lg + (e >> 1) * 8, head = nt * 8 + head_of;
-                            if (head < A.GS && j0 + key < w.n && !(PAIR && lt >> 1))
+                            if (head < A.GS && key < left && !(PAIR && lt >> 1))
                                 asm volatile("st.global.L2::cache_hint.v2.f32 [%0], {%1, %2}, %3;"
-                                             ::"l"(sc + (long long)key * A.GS + head), "f"(x[u][nt][e] * Q.back[nt][0]), "f"(x[u][nt][e + 1] * Q.back[nt][1]), "l"(stay) : "memory");
+                                             ::"l"(sc + key * A.GS + head), "f"(x[u][nt][e] * Q.back[nt][0]), "f"(x[u][nt][e + 1] * Q.back[nt][1]), "l"(stay) : "memory");
                         }
             }
             if (!__any_sync(0xFFFFFFFFu, grow)) return;
@@ -418,25 +541,23 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
 #pragma unroll
                 for (int r = 0; r < 2; ++r)
 #pragma unroll
-                    for (int g = 0; g < L; ++g) low16 = max(low16, vp[u][r][g] >> 16 & 0x7FFFu);
-            const uint32_t step = __reduce_max_sync(0xFFFFFFFFu, top16 & 0xFFFFu), size = __reduce_max_sync(0xFFFFFFFFu, low16);
+                    for (int g = 0; g < L; ++g) low16 = max(low16, vp[u][r][g] & 0x7FFFu);
+            const uint32_t step = __reduce_max_sync(0xFFFFFFFFu, top) >> 16, size = __reduce_max_sync(0xFFFFFFFFu, low16);
             // above every step, and p m stays in fp32
             E = max(E, min(max(max(exponent(si_cvt<DT>::lo(step)) + 1, exponent(si_cvt<DT>::lo(size)) - 9), kLowE), kHighE));
-            most = (uint32_t)(DT == SI_BF16 ? (E + 127) << 7 : (E + 15) << 10);
+            most = (uint32_t)(DT == SI_BF16 ? (E + 127) << 7 : (E + 15) << 10) << 16 | 0xFFFFu;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
-                    float mx = raw[nt][c];
+                    float mx = m[nt][c];
 #pragma unroll
                     for (int u = 0; u < 2; ++u) mx = fmaxf(mx, fmaxf(x[u][nt][c], x[u][nt][c + 2]));
                     mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 4));
                     mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 8));
                     mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 16));
-                    raw[nt][c] = mx;
-                    edge[nt][c] = mx + kLazy / Q.back[nt][c];
-                    mx *= Q.back[nt][c];
-                    const float to = mx == -INFINITY ? 0.f : mx + (float)(E - 6), f = m[nt][c] == -INFINITY ? 1.f : ex2(base[nt][c] - to);
+                    edge[nt][c] = mx + Q.lazy[nt][c];
+                    const float to = mx == -INFINITY ? 0.f : fmaf(mx, Q.back[nt][c], (float)(E - 6)), f = m[nt][c] == -INFINITY ? 1.f : ex2(base[nt][c] - to);
                     m[nt][c] = mx;
                     base[nt][c] = to;
                     l[nt][c] *= f;
@@ -446,110 +567,229 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
                     for (int i = 0; i < 2 * W; ++i) { o[nt][i][c] *= f; o[nt][i][c + 2] *= f; }
                 }
         };
-        for (; id < seg_end; id += kWarps) {
-            char *tile;
-            uint32_t vis;
-            int j0;
-            prepare(id, tile, vis, j0);
-            scores(tile, 0, x[0]);
-            scores(tile, 1, x[1]);
-            settle(tile, vis, j0);
-            add(tile, 0, x[0], vp[0]);
-            add(tile, 1, x[1], vp[1]);
+        for (; id < seg_end; ++id) {
+            char *tile = ring + stage * C::kStage;
+            const uint32_t vis = prepare(tile);
+            scores(tile, x);
+            settle(tile, vis);
+            add(tile, x, vp);
             __syncwarp();                      // the stage may be loaded again
-            issue();
+            issue(stage);
+            if (++stage == kStages) { stage = 0; parity ^= 1; }
         }
-        const Cursor seg = cons;
-        if (seg_end < g1) next_item<CH>(A, cons);
-        // the CTAs of this item, for the joining kernel: written by the one that has its first tile
-        if (tid == 0 && seg.start >= g0)
-            A.runs[(long long)seg.b * A.kv.H * A.GB + seg.hh] = make_int2(seg.start / per | (first_segment ? 0 : kSecondSlot), (seg.start + w.nc - 1) / per);
-        // ---- the segment's warps joined: rows scaled to the common base, summed in warp order
-        const bool whole = seg.start >= g0 && seg.start + w.nc <= g1;
-        float *po = A.part_o + ((long long)blockIdx.x * 2 + (first_segment ? 0 : 1)) * HB * D;
-        float *pml = A.part_ml + ((long long)blockIdx.x * 2 + (first_segment ? 0 : 1)) * HB * 2;
+        // ---- the item's end, or the run's: the lanes' sums joined; a result, or a part for the joining kernel
+        const bool whole = start >= g0 && end <= g1;
+        const long long slot = (long long)my_run * 2 + (first_segment ? 0 : 1), row = (long long)seq * A.Hq + h * A.G + head0;
+        if (lane == 0 && start >= g0)          // the runs of this item, for the joining kernel: by the one that has its first tile
+            A.runs[(long long)seq * A.kv.H * A.GB + item.hh] = make_int2(my_run | (first_segment ? 0 : kSecondSlot), whole ? my_run : runs.of(end - 1));
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
+                const int head = nt * 8 + head_of + c;
 #pragma unroll
-                for (int s = 4; s < 32; s <<= 1) l[nt][c] += __shfl_xor_sync(0xFFFFFFFFu, l[nt][c], s);
-                if (lane < 4) *reinterpret_cast<float2 *>(ml + (warp * HB + nt * 8 + head_of + c) * 2) = make_float2(m[nt][c] == -INFINITY ? -INFINITY : base[nt][c], l[nt][c]);
-            }
-        __syncthreads();
+                for (int s = 4; s < 32; s <<= 1) {
+                    l[nt][c] += __shfl_xor_sync(0xFFFFFFFFu, l[nt][c], s);
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            float f[2];
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                float top = -INFINITY;
-#pragma unroll
-                for (int v = 0; v < kWarps; ++v) top = fmaxf(top, ml[(v * HB + nt * 8 + head_of + c) * 2]);
-                f[c] = m[nt][c] == -INFINITY ? 1.f : ex2(base[nt][c] - top);
-#pragma unroll
-                for (int g = 0; g < L; ++g)
-#pragma unroll
-                    for (int s = 4; s < 32; s <<= 1) low[nt][g][c] += __shfl_xor_sync(0xFFFFFFFFu, low[nt][g][c], s);
-            }
-            float *mine = merge_o + warp % kMergeWarps * C::kMerge;
-#pragma unroll
-            for (int round = 0; round < kWarps; round += kMergeWarps) {
-                if (warp / kMergeWarps * kMergeWarps == round)
-#pragma unroll
-                    for (int c = 0; c < 2; ++c)
-#pragma unroll
-                        for (int i = 0; i < (PAIR ? W / 2 : W); ++i) {
-                            // the lane's words: all, or k of its own groups
-                            const int word = PAIR ? i / GW * 2 * GW + i % GW + (lt >> 1) * GW : i;
-                            const float mn = low[nt][PAIR ? i / GW : T::place_of(T::group_of(i))][c];
-                            auto of = [&](int n) { return PAIR ? (lt >> 1 ? o[nt][(4 * i + n) % (2 * W)][c + 2] : o[nt][(4 * i + n) % (2 * W)][c]) : o[nt][2 * i + n / 2][c + 2 * (n & 1)]; };
-                            float4 *to = reinterpret_cast<float4 *>(mine + (head_of + c) * C::kRow + 32 * word + 4 * lg);
-                            float4 y = round == 0 ? make_float4(0.f, 0.f, 0.f, 0.f) : *to;
-                            y.x = fmaf(fmaf(of(0), 0x1p24f, mn), f[c], y.x);
-                            y.y = fmaf(fmaf(of(1), 0x1p20f, mn), f[c], y.y);
-                            y.z = fmaf(fmaf(of(2), 0x1p24f, mn), f[c], y.z);
-                            y.w = fmaf(fmaf(of(3), 0x1p20f, mn), f[c], y.w);
-                            *to = y;
-                        }
-                __syncthreads();
-            }
-            for (int i = tid; i < (PAIR ? 4 : 8) * (D / 2); i += kThreads) {
-                const int hd = i / (D / 2), d = i % (D / 2) * 2, head = nt * 8 + hd;
+                    for (int g = 0; g < L; ++g) low[nt][g][c] += __shfl_xor_sync(0xFFFFFFFFu, low[nt][g][c], s);
+                }
                 if (head >= heads) continue;
-                float top = -INFINITY, sum = 0.f;
-#pragma unroll
-                for (int v = 0; v < kWarps; ++v) top = fmaxf(top, ml[(v * HB + head) * 2]);
-#pragma unroll
-                for (int v = 0; v < kWarps; ++v) {
-                    const float2 y = *reinterpret_cast<const float2 *>(ml + (v * HB + head) * 2);
-                    sum += y.y * (y.x == -INFINITY ? 1.f : ex2(y.x - top));     // without a maximum: 0, or NaN (NaN scores only)
-                }
-                float2 acc = make_float2(0.f, 0.f);
-#pragma unroll
-                for (int v = 0; v < kMergeWarps; ++v) {
-                    const float2 y = *reinterpret_cast<const float2 *>(merge_o + v * C::kMerge + hd * C::kRow + d);
-                    acc.x += y.x; acc.y += y.y;
-                }
-                const long long row = (long long)seg.b * A.Hq + h * A.G + head0 + head;
-                if (whole) {
-                    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-                    *reinterpret_cast<uint32_t *>(A.out + row * D + d) = pack2<DT>(acc.x * inv, acc.y * inv);
-                    if (d == 0) {
-                        const float l2 = sum == 0.f ? -INFINITY : top + log2f(sum);
-                        if (A.lse) A.lse[row] = l2 / kLog2e;
-                        if (A.acc) A.done[row] = make_float2(top == -INFINITY ? 0.f : top, inv);
+                const float sum = l[nt][c], inv = sum == 0.f ? 0.f : 1.f / sum, top = m[nt][c] == -INFINITY ? -INFINITY : base[nt][c];
+                if (lg == 0 && !(PAIR && lt >> 1)) {
+                    if (whole) {
+                        if (A.lse) A.lse[row + head] = sum == 0.f ? -INFINITY : (base[nt][c] + log2f(sum)) / kLog2e;
+                        if (A.acc) A.done[row + head] = make_float2(base[nt][c], inv);
+                    } else {
+                        *reinterpret_cast<float2 *>(A.part_ml + (slot * HB + head) * 2) = make_float2(top, sum);
                     }
-                } else {
-                    *reinterpret_cast<float2 *>(po + head * D + d) = acc;
-                    if (d == 0) { pml[head * 2] = top; pml[head * 2 + 1] = sum; }
+                }
+#pragma unroll
+                for (int i = 0; i < (PAIR ? W / 2 : W); ++i) {
+                    // the lane's words: all, or k of its own groups
+                    const int word = PAIR ? i / GW * 2 * GW + i % GW + (lt >> 1) * GW : i;
+                    const float mn = low[nt][PAIR ? i / GW : T::place_of(T::group_of(i))][c];
+                    auto of = [&](int n) { return PAIR ? (lt >> 1 ? o[nt][(4 * i + n) % (2 * W)][c + 2] : o[nt][(4 * i + n) % (2 * W)][c]) : o[nt][2 * i + n / 2][c + 2 * (n & 1)]; };
+                    const float4 y = make_float4(fmaf(of(0) - of(1), 0x1p24f, mn), fmaf(of(1), 0x1p20f, mn), fmaf(of(2) - of(3), 0x1p24f, mn), fmaf(of(3), 0x1p20f, mn));
+                    if (whole) *reinterpret_cast<uint2 *>(A.out + (row + head) * D + 32 * word + 4 * lg) = make_uint2(pack2<DT>(y.x * inv, y.y * inv), pack2<DT>(y.z * inv, y.w * inv));
+                    else *reinterpret_cast<float4 *>(A.part_o + (slot * HB + head) * D + 32 * word + 4 * lg) = y;
                 }
             }
-            __syncthreads();
-        }
         first_segment = false;
-        if (seg_end >= g1) return;
-        load_q<DT, D, NG, H>(A, cons.b, cons.hh, Q);
+        if (end >= g1) return;
+        __syncwarp();
+        if (lane == 0) { Cursor next = item; next_unit_item(A, next); sh_item[warp] = next; }
+        __syncwarp();
+        load_q<DT, D, NG, H>(A, sh_item[warp].b, sh_item[warp].hh, Q);
     }
+}
+
+// Joins the parts of items that more than one run has, and, where weights are wanted, adds them up.  The first n_out CTAs of a
+// (sequence, key head) make the output: a thread per pair of channels of a head and slice of the parts, eight parts at a time,
+// each slice relative to its own maximum; the slices are joined in order.  The others have U * 256 keys each and add their weights.
+// Chains of short dependent loads: what does not depend on another load is asked for first (scores and weights beyond the length
+// too: the memory is there, the values are not used).  GX: heads per key in `scores` at most.
+constexpr int kJoin4 = 256, kMaxSlices = 16;
+template <int DT, int D, int NT, int GX, int U>
+__global__ void __launch_bounds__(kJoin4, 3) join4_kernel(const DecodeArgs A, const int n_out) {
+    constexpr int HB = 8 * NT, CH = kTileEntries;
+    __shared__ float2 sh_done[128];
+    __shared__ float4 sh_part[kJoin4];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, h = blockIdx.y, b = blockIdx.z;
+    si_tc::pdl_wait();
+    si_tc::pdl_launch();
+    const int2 *runs = A.runs + ((long long)b * A.kv.H + h) * A.GB;
+    const long long row = (long long)b * A.Hq + h * A.G;
+    const int2 run0 = runs[0];
+    struct Parts { int first, n, slot0; };
+    auto parts_of = [&](int gb) {
+        const int2 r = gb == 0 ? run0 : runs[gb];
+        return Parts{r.x & ~kSecondSlot, r.y - (r.x & ~kSecondSlot) + 1, r.x & kSecondSlot ? 1 : 0};      // later runs begin with the item
+    };
+    auto slot = [&](const Parts &p, int i) { return (long long)(p.first + i) * 2 + (i > 0 ? 0 : p.slot0); };
+    auto part_ml = [&](const Parts &p, int i, int head) { return *reinterpret_cast<const float2 *>(A.part_ml + (slot(p, i) * HB + head) * 2); };
+    // a part without a maximum has sums of 0, or NaN (NaN scores only)
+    auto factor = [&](float v, float top) { return v == -INFINITY ? 1.f : ex2(v - top); };
+    if ((int)blockIdx.x < n_out) {
+        if (seq_work<CH>(A, b, nullptr).nc == 0) return;
+        for (int gb = 0; gb < A.GB; ++gb) {
+            const int head0 = gb * HB, heads = min(HB, A.G - head0), pairs = heads * (D / 2);
+            const Parts p = parts_of(gb);
+            if (p.n == 1) continue;                        // finished by one warp
+            int slices = 1;
+            while (slices < kMaxSlices && p.n > 8 * slices) slices *= 2;
+            const int wide = kJoin4 / slices, slice = tid / wide;
+            const int k0 = p.n * slice / slices, k1 = p.n * (slice + 1) / slices;
+            for (int u = blockIdx.x; u * wide < pairs; u += n_out) {
+                const int at = u * wide + tid % wide, head = at / (D / 2), pair = at % (D / 2);
+                float4 sum = make_float4(0.f, 0.f, -INFINITY, 0.f);        // two channels, maximum, sum of p
+                if (at < pairs)
+                    for (int k = k0; k < k1; k += 8) {
+                        float2 o[8], ml[8];
+                        float top = sum.z;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const bool in = k + i < k1;
+                            ml[i] = in ? part_ml(p, k + i, head) : make_float2(-INFINITY, 0.f);
+                            o[i] = in ? *reinterpret_cast<const float2 *>(A.part_o + (slot(p, k + i) * HB + head) * D + 2 * pair) : make_float2(0.f, 0.f);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) top = fmaxf(top, ml[i].x);
+                        const float f = factor(sum.z, top);
+                        sum = make_float4(sum.x * f, sum.y * f, top, sum.w * f);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const float g = factor(ml[i].x, top);
+                            sum.x += o[i].x * g; sum.y += o[i].y * g; sum.w += ml[i].y * g;
+                        }
+                    }
+                if (slices > 1) {
+                    __syncthreads();
+                    sh_part[tid] = sum;
+                    __syncthreads();
+                    if (slice == 0) {
+                        float top = sum.z;
+                        for (int k = 1; k < slices; ++k) top = fmaxf(top, sh_part[k * wide + tid].z);
+                        const float f = factor(sum.z, top);
+                        sum = make_float4(sum.x * f, sum.y * f, top, sum.w * f);
+                        for (int k = 1; k < slices; ++k) {
+                            const float4 t = sh_part[k * wide + tid];
+                            const float g = factor(t.z, top);
+                            sum.x += t.x * g; sum.y += t.y * g; sum.w += t.w * g;
+                        }
+                    }
+                }
+                if (slice == 0 && at < pairs) {
+                    const float inv = sum.w == 0.f ? 0.f : 1.f / sum.w;
+                    *reinterpret_cast<uint32_t *>(A.out + (row + head0 + head) * D + 2 * pair) = pack2<DT>(sum.x * inv, sum.y * inv);
+                    if (pair == 0 && A.lse) A.lse[row + head0 + head] = sum.w == 0.f ? -INFINITY : ((sum.z == -INFINITY ? 0.f : sum.z) + log2f(sum.w)) / kLog2e;
+                }
+            }
+        }
+        return;
+    }
+    const int j0 = (blockIdx.x - n_out) * (U * kJoin4);
+    float *weight = A.kv.weight + A.kv.meta(b, h);
+    const float *sc = A.scores + ((long long)b * A.kv.H + h) * A.GB * A.kv.cap * A.GS;
+    float2 x[U][GX / 2];                   // the first head block's scores
+    float old[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+        const int j = j0 + i * kJoin4 + tid;
+        if (j >= A.kv.cap) continue;
+        old[i] = weight[j];
+#pragma unroll
+        for (int g = 0; g < GX; g += 2)
+            if (g < A.GS) x[i][g / 2] = *reinterpret_cast<const float2 *>(sc + (long long)j * A.GS + g);
+    }
+    const float2 whole = tid < A.G ? A.done[row + tid] : make_float2(0.f, 0.f);
+    const SeqWork w = seq_work<CH>(A, b, nullptr);
+    if (j0 >= w.n) return;
+    if (tid < A.G) sh_done[tid] = whole;
+    __syncthreads();
+    for (int gb = 0; gb < A.GB && w.nc > 0; ++gb) {
+        const int head0 = gb * HB, heads = min(HB, A.G - head0);
+        const Parts p = parts_of(gb);
+        if (p.n == 1) continue;
+        for (int head = warp; head < heads; head += kJoin4 / 32) {      // a warp per head, a lane per part
+            float2 ml[4];                              // the first 128 parts stay in registers
+            float top = -INFINITY, sum = 0.f;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) ml[k] = k * 32 + lane < p.n ? part_ml(p, k * 32 + lane, head) : make_float2(-INFINITY, 0.f);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) top = fmaxf(top, ml[k].x);
+            for (int i = 128 + lane; i < p.n; i += 32) top = fmaxf(top, part_ml(p, i, head).x);
+#pragma unroll
+            for (int s = 16; s; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, s));
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sum += ml[k].y * factor(ml[k].x, top);
+            for (int i = 128 + lane; i < p.n; i += 32) { const float2 v = part_ml(p, i, head); sum += v.y * factor(v.x, top); }
+#pragma unroll
+            for (int s = 16; s; s >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, s);
+            if (lane == 0) sh_done[head0 + head] = make_float2(top == -INFINITY ? 0.f : top, sum == 0.f ? 0.f : 1.f / sum);
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+        const int j = j0 + i * kJoin4 + tid, c = j / CH;
+        if (j >= w.n) continue;
+        if (!(c < w.c_sink || (c >= w.c_win && c < w.c_win + w.nc - w.c_sink))) { if (j == w.n_old) weight[j] = 0.f; continue; }
+        float sum = 0.f;
+        for (int gb = 0; gb < A.GB; ++gb) {
+            const float *more = sc + ((long long)gb * A.kv.cap + j) * A.GS;
+#pragma unroll
+            for (int g = 0; g < GX; g += 2) {
+                if (g >= A.GS || gb * HB + g >= A.G) break;
+                const float2 y = gb == 0 ? x[i][g / 2] : *reinterpret_cast<const float2 *>(more + g);
+                // a hidden entry's score is -inf: it receives nothing, from a head whose sum is NaN neither
+                if (y.x != -INFINITY) sum += ex2(y.x - sh_done[gb * HB + g].x) * sh_done[gb * HB + g].y;
+                if (gb * HB + g + 1 < A.G && y.y != -INFINITY) sum += ex2(y.y - sh_done[gb * HB + g + 1].x) * sh_done[gb * HB + g + 1].y;
+            }
+        }
+        weight[j] = j == w.n_old ? sum : old[i] + sum;
+    }
+}
+
+template <int DT, int D, int NT, int GX> int launch_join4(const DecodeArgs &A, cudaStream_t st) {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &at; cfg.numAttrs = 1;
+    cfg.stream = st;
+    cfg.blockDim = dim3(kJoin4);
+    constexpr int kKeys = NT == 1 ? 4 : 2;
+    const long long items = (long long)A.kv.H * A.kv.B;
+    // CTAs for the output while they are resident at once (four per SM)
+    const long long room = 4ll * si_sm_count() / items, most = (long long)(A.G < 8 * NT ? A.G : 8 * NT) * (D / 2) * kMaxSlices / kJoin4;
+    const int n_out = (int)(room < 1 || most < 1 ? 1 : room < most ? room : most);
+    // ranges of 256 keys while all their CTAs are resident at once (three per SM): the start of a CTA costs more than its keys
+    const bool few = items * ((A.kv.cap + kJoin4 - 1) / kJoin4) <= 3ll * si_sm_count();
+    const int keys = (few ? 1 : kKeys) * kJoin4;
+    cfg.gridDim = dim3(n_out + (A.acc ? (A.kv.cap + keys - 1) / keys : 0), A.kv.H, A.kv.B);
+    if (few || !A.acc) SI_CUDA_TRY(cudaLaunchKernelEx(&cfg, join4_kernel<DT, D, NT, GX, 1>, A, n_out));
+    else SI_CUDA_TRY(cudaLaunchKernelEx(&cfg, join4_kernel<DT, D, NT, GX, kKeys>, A, n_out));
+    return SI_OK;
 }
 
 template <int DT, int D, int NG, int H> int launch(const Decode4Args &A, cudaStream_t st) {
@@ -562,12 +802,13 @@ template <int DT, int D, int NG, int H> int launch(const Decode4Args &A, cudaStr
     at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at.val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = &at; cfg.numAttrs = 1;
-    cfg.gridDim = dim3(A.d.n_cta);
+    cfg.gridDim = dim3(A.d.n_cta / kWarps);
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = C::kSmem;
     cfg.stream = st;
     SI_CUDA_TRY(cudaLaunchKernelEx(&cfg, decode4_kernel<DT, D, NG, H>, A));
-    return launch_join<DT, D, kTilesOf<H>, kTileEntries>(A.d, st);
+    if constexpr (H == 16) return launch_join4<DT, D, 2, 16>(A.d, st);
+    else return A.d.GS <= 4 ? launch_join4<DT, D, 1, 4>(A.d, st) : launch_join4<DT, D, 1, 8>(A.d, st);
 }
 template <int DT, int D, int NG> int launch_h(const Decode4Args &A, cudaStream_t st) {
     if (A.d.G > 8) return launch<DT, D, NG, 16>(A, st);
@@ -580,7 +821,7 @@ template <int DT> int launch_t(const Decode4Args &A, int NG, cudaStream_t st) {
 }
 
 Layout layout_of(const si_kv4_t *kv, int n_q_heads, bool acc) {
-    return layout_of((n_q_heads / kv->n_kv_heads > 8 ? kPerSmOf<16> : kPerSmOf<8>) * si_sm_count(), kv->n_seqs, kv->n_kv_heads, kv->head_dim, kv->capacity, n_q_heads, acc);
+    return layout_of((n_q_heads / kv->n_kv_heads > 8 ? kPerSmOf<16> : kPerSmOf<8>) * kWarps * si_sm_count(), kv->n_seqs, kv->n_kv_heads, kv->head_dim, kv->capacity, n_q_heads, acc);
 }
 
 }  // namespace
@@ -603,7 +844,7 @@ extern "C" int si_kv4_attn_decode(const si_kv4_t *kv, const void *q, long long q
         return SI_ERR_ALIGNMENT;
     const Layout L = layout_of(kv, n_q_heads, acc);
     // tiles are numbered in 32 bits
-    if ((double)kv->n_seqs * kv->n_kv_heads * L.GB * (kv->capacity / kTileEntries + 2) > 2.0e9) return SI_ERR_TOO_LARGE;
+    if ((double)kv->n_seqs * kv->n_kv_heads * L.GB * (kv->capacity / kTileEntries + 2 + kPad) > 2.0e9) return SI_ERR_TOO_LARGE;
     if (ws_bytes < L.total) return SI_ERR_NOMEM;
     if (!workspace) return SI_ERR_INVALID_ARG;
     if ((uintptr_t)workspace & 255) return SI_ERR_ALIGNMENT;

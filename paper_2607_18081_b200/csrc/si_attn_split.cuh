@@ -8,7 +8,7 @@
 namespace {
 
 constexpr int kJoinWarps = 8, kJoinThreads = kJoinWarps * 32;
-constexpr int kMaxParts = 608;             // CTAs of the main kernel at most
+constexpr int kMaxParts = 608;             // CTAs of a main kernel whose parts decode_join_kernel joins at most
 constexpr int kSecondSlot = 1 << 30;       // in the table of runs: the item's first part is in the second slot of its CTA
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLazy = 8.f;               // the running maximum moves only when a score exceeds it by 2^8: p stays below 2^8, exact to fp32 all the same
@@ -232,7 +232,7 @@ __global__ void __launch_bounds__(kJoinThreads, 3) decode_join_kernel(const Deco
 struct Layout { int n_cta, NT, GB, GS; size_t o, ml, done, scores, runs, total; };
 inline Layout layout_of(int n_cta, int n_seqs, int n_kv_heads, int head_dim, int capacity, int n_q_heads, bool acc) {
     Layout L;
-    L.n_cta = n_cta < kMaxParts ? n_cta : kMaxParts;
+    L.n_cta = n_cta;
     const int G = n_q_heads / n_kv_heads;
     L.NT = G <= 8 ? 1 : 2;
     L.GB = (G + 8 * L.NT - 1) / (8 * L.NT);

@@ -155,7 +155,7 @@ __global__ void __launch_bounds__(kThreads) load_kernel(const LoadArgs A) {
         const uint32_t v0 = *reinterpret_cast<const uint32_t *>(from + T::value_word(r, w, 2 * t)), v1 = *reinterpret_cast<const uint32_t *>(from + T::value_word(r, w, 2 * t + 1));
         const uint32_t kp = *reinterpret_cast<const uint32_t *>(from + T::kKeyPar + (r * NG + g) * 4), vp = *reinterpret_cast<const uint32_t *>(from + T::kValuePar + (r * NG + g) * 4);
         // codes come as c 2^-24 and 16 c 2^-24
-        float s = si_cvt<DT>::lo(kp), m = si_cvt<DT>::hi(kp), s0 = s * 0x1p24f, s1 = s * 0x1p20f;
+        float s = si_cvt<DT>::hi(kp), m = si_cvt<DT>::lo(kp), s0 = s * 0x1p24f, s1 = s * 0x1p20f;
         float2 x[4] = {si_q4::code_pair(si_q4::low_codes(kw)), si_q4::code_pair(si_q4::high_codes(kw)), si_q4::code_pair(si_q4::low_codes(kw >> 8)), si_q4::code_pair(si_q4::high_codes(kw >> 8))};
         uint32_t o[4];
 #pragma unroll
@@ -163,7 +163,7 @@ __global__ void __launch_bounds__(kThreads) load_kernel(const LoadArgs A) {
         const long long at = A.dst.row(b, h, e0 + r - first) + c * 8;
         *reinterpret_cast<uint4 *>(A.dst.k + at) = make_uint4(o[0], o[1], o[2], o[3]);
         const uint32_t vw = __byte_perm(v0, v1, r & 1 ? 0x7632 : 0x5410);       // elements 0 .. 3 | 4 .. 7
-        s = si_cvt<DT>::lo(vp); m = si_cvt<DT>::hi(vp); s0 = s * 0x1p24f; s1 = s * 0x1p20f;
+        s = si_cvt<DT>::hi(vp); m = si_cvt<DT>::lo(vp); s0 = s * 0x1p24f; s1 = s * 0x1p20f;
         float2 y[4] = {si_q4::code_pair(si_q4::low_codes(vw)), si_q4::code_pair(si_q4::high_codes(vw)), si_q4::code_pair(si_q4::low_codes(vw >> 8)), si_q4::code_pair(si_q4::high_codes(vw >> 8))};
 #pragma unroll
         for (int k = 0; k < 4; ++k) { y[k].x = value_of<DT>(y[k].x, k & 1 ? s1 : s0, m); y[k].y = value_of<DT>(y[k].y, k & 1 ? s1 : s0, m); }

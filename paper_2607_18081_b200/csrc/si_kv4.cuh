@@ -14,7 +14,7 @@
 //   values   from 16 D: entries in pairs, pair r / 2 of D bytes at D (r / 2); lane g of eight has elements 32 w + 4 g + i (i < 4): D / 8
 //            bytes, word w, the even entry in its lower half, the odd one in its upper half, element i in nibble i of the half.
 //            The eight cells of a pair are permuted by an XOR of g (bank conflicts).
-//   steps    from 32 D: per entry D / group words of step (lower half) and lowest value (upper half) of the keys, then of the values;
+//   steps    from 32 D: per entry D / group words of lowest value (lower half) and step (upper half) of the keys, then of the values;
 //            four groups in the order 0, 2, 1, 3 (two lanes of four work on the even groups, two on the odd ones)
 // A word masked with 0x000F000F is then a pair of f16 numbers c 2^-24 (subnormal, and exact in a product with fp32 sums): two
 // neighbouring elements of a key, or one element of two neighbouring entries; with 0x00F000F0, the next ones, times 16.
@@ -71,7 +71,7 @@ namespace si_q4 {
 __device__ __forceinline__ float min_nan(float a, float b) { float r; asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
 __device__ __forceinline__ float max_nan(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
 
-// step | lowest value << 16 of a group with these extremes; *inverse is what its codes are computed with
+// lowest value | step << 16 of a group with these extremes; *inverse is what its codes are computed with
 template <int DT> __device__ __forceinline__ uint32_t group_word(float low, float high, float *inverse) {
     const float range = high - low;
     *inverse = 0.f;
@@ -82,7 +82,7 @@ template <int DT> __device__ __forceinline__ uint32_t group_word(float low, floa
     const float sf = si_cvt<DT>::lo(s);
     if (sf < 0x1p-126f) s = 0;
     else *inverse = __frcp_rn(sf);
-    return s | (uint32_t)si_cvt<DT>::from_float(low) << 16;
+    return s << 16 | (uint32_t)si_cvt<DT>::from_float(low);
 }
 // 2^23 * 1.5 + code: the code is in the low bits
 __device__ __forceinline__ uint32_t code_bits(float x, float low, float inverse) { return __float_as_uint(__fmaf_rn(__fsub_rn(x, low), inverse, 12582912.f)); }

@@ -1,12 +1,34 @@
 // The key/value cache in 4 bits: quantising entries as they are stored, reading them back, eviction.  (Layout and format: si_kv4.cuh.)
 //
 // All three are bound by HBM: an entry is 4 D bytes in 16 bits and D + 8 D / group in 4.
+#include <type_traits>
+
 #include "si_evict.cuh"
 #include "si_tc.cuh"
 
 namespace {
 
-constexpr int kWarps = 4, kThreads = kWarps * 32;
+constexpr int kWarps = 4, kThreads = kWarps * 32, kOctet = 8;
+
+template <int DT> __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    uint32_t r;
+    if (DT == SI_BF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+// Pairs of 16-bit numbers; NaN if either is.
+template <int DT> __device__ __forceinline__ uint32_t min2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    if (DT == SI_BF16) asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    else asm("min.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+template <int DT> __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    if (DT == SI_BF16) asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    else asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
 
 struct StoreArgs {
     si_kv_view src, meta;            // meta: pos, weight, len, capacity of the cache in 4 bits
@@ -15,93 +37,79 @@ struct StoreArgs {
     int32_t *status;
 };
 
-// A warp per tile: the entries' rows come in as 16-byte pieces (eight elements: one word of a key's codes, two half words of a
-// value's), the tile is put together in shared memory and goes out in 16-byte pieces.
+// A warp per eight entries, everything it reads asked for at once: 16-byte pieces of rows, eight elements a lane, which make one word
+// of a key's codes and two half words of a value's (the two entries of a pair exchange a half each).  A warp's words of a store are
+// 128 contiguous bytes, in the tile's order.  No room for more than a warp per tile would leave a prompt's store waiting for memory
+// (8192 tokens of eight heads: 20 us with a warp per tile).
 template <int DT, int D, int NG>
 __global__ void __launch_bounds__(kThreads) store_kernel(const StoreArgs A) {
     using T = si_tile4<D, NG>;
-    constexpr int L = D / 8, ROWS = 32 / L, GL = D / NG / 8;     // lanes of a row, rows of a warp, lanes of a group
-    __shared__ __align__(16) char sh[kWarps][T::kBytes];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, h = blockIdx.y, b = blockIdx.z;
+    constexpr int L = D / 8, ROWS = 32 / L, N = kOctet / ROWS, GL = D / NG / 8;     // lanes of a row, rows of a warp at a time, times, lanes of a group
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, h = blockIdx.x % A.src.H, b = blockIdx.z;
+    const long long block = blockIdx.x / A.src.H;          // the heads of a token side by side in time: in a token-major source they share DRAM pages
     si_tc::pdl_wait();
     si_tc::pdl_launch();
-    const bool tell = h == 0 && blockIdx.x == 0 && threadIdx.x == 0;
+    const bool tell = blockIdx.x == 0 && threadIdx.x == 0;
     const int start = si_kv_len(A.meta, b, tell ? A.status : nullptr);
     int n = si_kv_len(A.src, b, tell ? A.status : nullptr);
     if (n > A.meta.cap - start) { if (tell) si_report(A.status, SI_ERR_OUT_OF_RANGE); n = A.meta.cap - start; }
-    const int tile = start / kTileEntries + blockIdx.x * kWarps + warp, e0 = tile * kTileEntries;
+    const long long e0 = (start / kOctet + block * kWarps + warp) * kOctet;
     if (n <= 0 || e0 >= start + n) return;
-    const int r0 = max(0, start - e0), r1 = min(kTileEntries, start + n - e0);
-    char *sm = sh[warp];
-    const int c = lane % L, w = c / 4, t = c % 4;
-#pragma unroll 2
-    for (int i = 0; i < kTileEntries; i += ROWS) {
-        const int r = i + lane / L;
+    const int r0 = max(0, start - (int)e0), r1 = min(kOctet, start + n - (int)e0);     // rows of the eight that are stored
+    const int c = lane % L, w = c / 4, t = c % 4, sub = lane / L;
+    uint4 raw[N][2];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int r = i * ROWS + sub;
         const bool in = r >= r0 && r < r1;
-        const long long at = A.src.row(b, h, in ? e0 + r - start : 0) + c * 8;
-        uint4 raw[2];
-        raw[0] = in ? *reinterpret_cast<const uint4 *>(A.src.k + at) : make_uint4(0, 0, 0, 0);
-        raw[1] = in ? *reinterpret_cast<const uint4 *>(A.src.v + at) : make_uint4(0, 0, 0, 0);
+        const long long at = A.src.row(b, h, in ? (int)e0 + r - start : 0) + c * 8;
+        raw[i][0] = in ? __ldcs(reinterpret_cast<const uint4 *>(A.src.k + at)) : make_uint4(0, 0, 0, 0);
+        raw[i][1] = in ? __ldcs(reinterpret_cast<const uint4 *>(A.src.v + at)) : make_uint4(0, 0, 0, 0);
+    }
+    uint8_t *tile = A.dst.row(b, h) + e0 / kTileEntries * T::kBytes;
+    const int in_tile = (int)(e0 % kTileEntries);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int row = i * ROWS + sub, r = in_tile + row, other_row = row ^ 1;
+        const bool in = row >= r0 && row < r1, both = in && other_row >= r0 && other_row < r1;
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
-            const uint32_t u[4] = {raw[which].x, raw[which].y, raw[which].z, raw[which].w};
-            float f[8];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) { f[2 * k] = si_cvt<DT>::lo(u[k]); f[2 * k + 1] = si_cvt<DT>::hi(u[k]); }
-            float low = f[0], high = f[0];
-#pragma unroll
-            for (int k = 1; k < 8; ++k) { low = si_q4::min_nan(low, f[k]); high = si_q4::max_nan(high, f[k]); }
+            const uint32_t u[4] = {raw[i][which].x, raw[i][which].y, raw[i][which].z, raw[i][which].w};
+            uint32_t lo2 = min2<DT>(min2<DT>(u[0], u[1]), min2<DT>(u[2], u[3])), hi2 = max2<DT>(max2<DT>(u[0], u[1]), max2<DT>(u[2], u[3]));
 #pragma unroll
             for (int o = 1; o < GL; o <<= 1) {
-                low = si_q4::min_nan(low, __shfl_xor_sync(0xFFFFFFFFu, low, o));
-                high = si_q4::max_nan(high, __shfl_xor_sync(0xFFFFFFFFu, high, o));
+                lo2 = min2<DT>(lo2, __shfl_xor_sync(0xFFFFFFFFu, lo2, o));
+                hi2 = max2<DT>(hi2, __shfl_xor_sync(0xFFFFFFFFu, hi2, o));
             }
+            const float low = si_q4::min_nan(si_cvt<DT>::lo(lo2), si_cvt<DT>::hi(lo2)), high = si_q4::max_nan(si_cvt<DT>::lo(hi2), si_cvt<DT>::hi(hi2));
             float inverse;
             const uint32_t par = si_q4::group_word<DT>(low, high, &inverse);
-            uint32_t code[8], word = 0;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) code[k] = si_q4::code_bits(f[k], low, inverse) & 15u;
+            // a code's bits lie above those of 2^23 * 1.5, whose sum over eight places is taken off at the end
+            auto code = [&](int k) { return si_q4::code_bits(k & 1 ? si_cvt<DT>::hi(u[k / 2]) : si_cvt<DT>::lo(u[k / 2]), low, inverse); };
+            auto joined = [&](int k7, int k6, int k5, int k4, int k3, int k2, int k1, int k0) {
+                uint32_t x = code(k7);
+                x = x * 16 + code(k6); x = x * 16 + code(k5); x = x * 16 + code(k4);
+                x = x * 16 + code(k3); x = x * 16 + code(k2); x = x * 16 + code(k1);
+                return x * 16 + code(k0) - 0x3F400000u;
+            };
             if (which == 0) {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) word |= code[k] << (4 * ((k >> 1) + (k & 1) * 4));
-                *reinterpret_cast<uint32_t *>(sm + T::key_word(r, w, t)) = word;
+                const uint32_t word = joined(7, 5, 3, 1, 6, 4, 2, 0);
+                if (in) *reinterpret_cast<uint32_t *>(tile + T::key_word(r, w, t)) = word;
             } else {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) word |= code[k] << (4 * k);
-                // elements 0 .. 3 in the lower half, 4 .. 7 in the upper: the two entries of a pair exchange a half each
+                const uint32_t word = joined(7, 6, 5, 4, 3, 2, 1, 0);      // elements 0 .. 3 in the lower half
                 const uint32_t other = __shfl_xor_sync(0xFFFFFFFFu, word, L);
-                const uint32_t both = r & 1 ? __byte_perm(other, word, 0x7632) : __byte_perm(word, other, 0x5410);
-                *reinterpret_cast<uint32_t *>(sm + T::value_word(r, w, 2 * t + (r & 1))) = both;
+                if (both) {
+                    *reinterpret_cast<uint32_t *>(tile + T::value_word(r, w, 2 * t + (r & 1))) = r & 1 ? __byte_perm(other, word, 0x7632) : __byte_perm(word, other, 0x5410);
+                } else if (in) {
+                    *reinterpret_cast<uint16_t *>(tile + T::value_word(r, w, 2 * t) + 2 * (r & 1)) = (uint16_t)word;
+                    *reinterpret_cast<uint16_t *>(tile + T::value_word(r, w, 2 * t + 1) + 2 * (r & 1)) = (uint16_t)(word >> 16);
+                }
             }
-            if (c % GL == 0) *reinterpret_cast<uint32_t *>(sm + (which ? T::kValuePar : T::kKeyPar) + (r * NG + T::place_of(c / GL)) * 4) = par;
-        }
-    }
-    __syncwarp();
-    uint8_t *to = A.dst.row(b, h) + (long long)tile * T::kBytes;
-    auto copy16 = [&](int from, int end) {
-        for (int i = from + lane * 16; i < end; i += 512) *reinterpret_cast<uint4 *>(to + i) = *reinterpret_cast<const uint4 *>(sm + i);
-    };
-    if (r0 == 0 && r1 == kTileEntries) {
-        copy16(0, T::kBytes);
-    } else {
-        copy16(r0 * (D / 2), r1 * (D / 2));
-        const int p0 = (r0 + 1) / 2, p1 = r1 / 2;                // whole pairs of values, then the single ones
-        copy16(T::kValues + p0 * D, T::kValues + p1 * D);
-        auto single = [&](int r) {
-            if (lane >= D / 4) return;
-            const int at = T::kValues + (r >> 1) * D + lane * 4 + 2 * (r & 1);
-            *reinterpret_cast<uint16_t *>(to + at) = *reinterpret_cast<const uint16_t *>(sm + at);
-        };
-        if (r0 & 1) single(r0);
-        if (r1 & 1) single(r1 - 1);
-#pragma unroll
-        for (int which = 0; which < 2; ++which) {
-            const int par = which ? T::kValuePar : T::kKeyPar;
-            for (int i = r0 * NG + lane; i < r1 * NG; i += 32) *reinterpret_cast<uint32_t *>(to + par + i * 4) = *reinterpret_cast<const uint32_t *>(sm + par + i * 4);
+            if (in && c % GL == 0) *reinterpret_cast<uint32_t *>(tile + (which ? T::kValuePar : T::kKeyPar) + (r * NG + T::place_of(c / GL)) * 4) = par;
         }
     }
     if (lane < r0 || lane >= r1) return;
-    const int e = e0 + lane, j = e - start;
+    const int e = (int)e0 + lane, j = e - start;
     if (A.meta.pos) A.meta.pos[A.meta.meta(b, h) + e] = A.src.pos ? A.src.pos[A.src.meta(b, h) + j] : A.first_pos ? A.first_pos[b] + j : e;
     if (A.meta.weight) A.meta.weight[A.meta.meta(b, h) + e] = A.src.weight ? A.src.weight[A.src.meta(b, h) + j] : 0.f;
 }
@@ -114,13 +122,6 @@ struct LoadArgs {
     int32_t *len_out, *status;
 };
 
-template <int DT> __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
-    uint32_t r;
-    if (DT == SI_BF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
-
 // m + s c.  The step is rounded up, so that the highest code may stand for a little more than the type holds: the largest number
 // then (bf16: a range of 2^94 is far from its end).
 template <int DT> __device__ __forceinline__ float value_of(float code, float step, float low) {
@@ -128,64 +129,141 @@ template <int DT> __device__ __forceinline__ float value_of(float code, float st
     return DT == SI_F16 ? si_q4::min_nan(x, 65504.f) : x;
 }
 
-// A warp per tile; a lane makes eight neighbouring elements of a row.
+// A warp per eight entries, all words asked for at once; a lane makes eight neighbouring elements of a row.
 template <int DT, int D, int NG>
 __global__ void __launch_bounds__(kThreads) load_kernel(const LoadArgs A) {
     using T = si_tile4<D, NG>;
-    constexpr int L = D / 8, ROWS = 32 / L;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, h = blockIdx.y, b = blockIdx.z;
+    constexpr int L = D / 8, ROWS = 32 / L, N = kOctet / ROWS;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, h = blockIdx.x % A.dst.H, b = blockIdx.z;
+    const long long block = blockIdx.x / A.dst.H;
     si_tc::pdl_wait();
     si_tc::pdl_launch();
-    const bool tell = h == 0 && blockIdx.x == 0 && threadIdx.x == 0;
+    const bool tell = blockIdx.x == 0 && threadIdx.x == 0;
     const int len = si_kv_len(A.meta, b, tell ? A.status : nullptr);
     int first = A.first ? A.first[b] : 0;
     if (first < 0) { if (tell) si_report(A.status, SI_ERR_OUT_OF_RANGE); first = 0; }
     const int end = first + min(A.n, max(0, len - first));
     if (tell && A.len_out) A.len_out[b] = end - first;
-    if (end <= first) return;
-    const int tile = first / kTileEntries + blockIdx.x * kWarps + warp, e0 = tile * kTileEntries;
-    if (e0 >= end) return;
-    const uint8_t *from = A.src.row(b, h) + (long long)tile * T::kBytes;
-    const int c = lane % L, w = c / 4, t = c % 4, g = T::place_of(T::group_of(w));
-#pragma unroll 4
-    for (int i = 0; i < kTileEntries; i += ROWS) {
-        const int r = i + lane / L;
-        if (e0 + r < first || e0 + r >= end) continue;
-        const uint32_t kw = *reinterpret_cast<const uint32_t *>(from + T::key_word(r, w, t));
-        const uint32_t v0 = *reinterpret_cast<const uint32_t *>(from + T::value_word(r, w, 2 * t)), v1 = *reinterpret_cast<const uint32_t *>(from + T::value_word(r, w, 2 * t + 1));
-        const uint32_t kp = *reinterpret_cast<const uint32_t *>(from + T::kKeyPar + (r * NG + g) * 4), vp = *reinterpret_cast<const uint32_t *>(from + T::kValuePar + (r * NG + g) * 4);
-        // codes come as c 2^-24 and 16 c 2^-24
-        float s = si_cvt<DT>::hi(kp), m = si_cvt<DT>::lo(kp), s0 = s * 0x1p24f, s1 = s * 0x1p20f;
-        float2 x[4] = {si_q4::code_pair(si_q4::low_codes(kw)), si_q4::code_pair(si_q4::high_codes(kw)), si_q4::code_pair(si_q4::low_codes(kw >> 8)), si_q4::code_pair(si_q4::high_codes(kw >> 8))};
-        uint32_t o[4];
+    const long long e0 = (first / kOctet + block * kWarps + warp) * kOctet;
+    if (end <= first || e0 >= end) return;
+    const int r0 = max(0, first - (int)e0), r1 = min(kOctet, end - (int)e0);
+    const uint8_t *from = A.src.row(b, h) + e0 / kTileEntries * T::kBytes;
+    const int c = lane % L, w = c / 4, t = c % 4, g = T::place_of(T::group_of(w)), sub = lane / L, in_tile = (int)(e0 % kTileEntries);
+    uint32_t kw[N], v0[N], v1[N], kp[N], vp[N];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) o[k] = pack2<DT>(value_of<DT>(x[k].x, k & 1 ? s1 : s0, m), value_of<DT>(x[k].y, k & 1 ? s1 : s0, m));
-        const long long at = A.dst.row(b, h, e0 + r - first) + c * 8;
-        *reinterpret_cast<uint4 *>(A.dst.k + at) = make_uint4(o[0], o[1], o[2], o[3]);
-        const uint32_t vw = __byte_perm(v0, v1, r & 1 ? 0x7632 : 0x5410);       // elements 0 .. 3 | 4 .. 7
-        s = si_cvt<DT>::hi(vp); m = si_cvt<DT>::lo(vp); s0 = s * 0x1p24f; s1 = s * 0x1p20f;
-        float2 y[4] = {si_q4::code_pair(si_q4::low_codes(vw)), si_q4::code_pair(si_q4::high_codes(vw)), si_q4::code_pair(si_q4::low_codes(vw >> 8)), si_q4::code_pair(si_q4::high_codes(vw >> 8))};
-#pragma unroll
-        for (int k = 0; k < 4; ++k) { y[k].x = value_of<DT>(y[k].x, k & 1 ? s1 : s0, m); y[k].y = value_of<DT>(y[k].y, k & 1 ? s1 : s0, m); }
-        *reinterpret_cast<uint4 *>(A.dst.v + at) = make_uint4(pack2<DT>(y[0].x, y[1].x), pack2<DT>(y[2].x, y[3].x), pack2<DT>(y[0].y, y[1].y), pack2<DT>(y[2].y, y[3].y));
+    for (int i = 0; i < N; ++i) {              // the eight entries lie in one tile: all of it is there to be read
+        const int r = in_tile + i * ROWS + sub;
+        auto word = [&](int at) { return __ldcs(reinterpret_cast<const uint32_t *>(from + at)); };
+        kw[i] = word(T::key_word(r, w, t));
+        v0[i] = word(T::value_word(r, w, 2 * t)); v1[i] = word(T::value_word(r, w, 2 * t + 1));
+        kp[i] = word(T::kKeyPar + (r * NG + g) * 4); vp[i] = word(T::kValuePar + (r * NG + g) * 4);
     }
-    const int e = e0 + lane;
-    if (e < first || e >= end) return;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int row = i * ROWS + sub;
+        // codes come as c 2^-24 and 16 c 2^-24
+        float2 x[4];
+        auto values = [&](uint32_t codes, uint32_t par) {
+            const float s = si_cvt<DT>::hi(par), m = si_cvt<DT>::lo(par), s0 = s * 0x1p24f, s1 = s * 0x1p20f;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                x[k] = si_q4::code_pair(k & 1 ? si_q4::high_codes(codes >> 4 * (k & 2)) : si_q4::low_codes(codes >> 4 * (k & 2)));
+                x[k].x = value_of<DT>(x[k].x, k & 1 ? s1 : s0, m); x[k].y = value_of<DT>(x[k].y, k & 1 ? s1 : s0, m);
+            }
+        };
+        if (row < r0 || row >= r1) continue;
+        const long long at = A.dst.row(b, h, (int)e0 + row - first) + c * 8;
+        values(kw[i], kp[i]);
+        __stcs(reinterpret_cast<uint4 *>(A.dst.k + at), make_uint4(pack2<DT>(x[0].x, x[0].y), pack2<DT>(x[1].x, x[1].y), pack2<DT>(x[2].x, x[2].y), pack2<DT>(x[3].x, x[3].y)));
+        values(__byte_perm(v0[i], v1[i], row & 1 ? 0x7632 : 0x5410), vp[i]);       // elements 0 .. 3 | 4 .. 7
+        __stcs(reinterpret_cast<uint4 *>(A.dst.v + at), make_uint4(pack2<DT>(x[0].x, x[1].x), pack2<DT>(x[2].x, x[3].x), pack2<DT>(x[0].y, x[1].y), pack2<DT>(x[2].y, x[3].y)));
+    }
+    if (lane < r0 || lane >= r1) return;
+    const int e = (int)e0 + lane;
     if (A.meta.pos && A.dst.pos) A.dst.pos[A.dst.meta(b, h) + e - first] = A.meta.pos[A.meta.meta(b, h) + e];
     if (A.meta.weight && A.dst.weight) A.dst.weight[A.dst.meta(b, h) + e - first] = A.meta.weight[A.meta.meta(b, h) + e];
 }
 
-// The kept entries to their slots; nothing to do for an entry that stays.
+// The kept entries to their slots; nothing to do for an entry that stays.  Sixteen lanes per pair of slots, kMovePairs pairs in flight:
+// eight lanes have the values' cells of both sources (which hold a neighbour each) and put the two halves together, eight the
+// two keys, and of these four the steps and four positions and weights.
+constexpr int kMovePairs = 4;
+template <int D, int NG>
 __global__ void __launch_bounds__(256) move4_kernel(const EvictArgs A) {
-    constexpr int kSlots = 256 / kMoveLanes4;
-    const int b = blockIdx.z, h = blockIdx.y, row = b * A.src.H + h, lane = threadIdx.x % kMoveLanes4;
+    using T = si_tile4<D, NG>;
+    constexpr int W = T::W, kGroups = 256 / 16;
+    const int h = blockIdx.x % A.src.H, b = blockIdx.z, row = b * A.src.H + h, lane = threadIdx.x % 16, group = threadIdx.x / 16;
+    const long long block = blockIdx.x / A.src.H;
     si_tc::pdl_wait();
     si_tc::pdl_launch();
-    if (h == 0 && blockIdx.x == 0 && threadIdx.x == 0 && A.len_out) A.len_out[b] = min(si_evict_entries(A, b), A.budget);
-    const int slot = blockIdx.x * kSlots + threadIdx.x / kMoveLanes4;
-    if (slot >= A.slots) return;
-    const int j = A.source[(size_t)row * A.slots + slot];
-    if (j >= 0 && !(A.in_place && j == slot)) si_move_entry4(A, b, h, j, slot, lane);
+    if (blockIdx.x == 0 && threadIdx.x == 0 && A.len_out) A.len_out[b] = min(si_evict_entries(A, b), A.budget);
+    const uint8_t *src = A.src4.row(b, h);
+    uint8_t *dst = A.dst4.row(b, h);
+    const int half = lane >> 2 & 1;                        // lanes 8 .. 15: the key of which slot; of the second round: the slot is lane % 2
+    int from[kMovePairs][2];
+#pragma unroll
+    for (int k = 0; k < kMovePairs; ++k)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const long long slot = ((block * kMovePairs + k) * kGroups + group) * 2 + i;
+            from[k][i] = slot < A.slots ? A.source[(size_t)row * A.slots + slot] : -1;
+            if (A.in_place && from[k][i] == slot) from[k][i] = -1;
+        }
+    auto tile_at = [](int j) { return (long long)(j / kTileEntries) * T::kBytes; };
+    uint32_t one[kMovePairs][W], two[kMovePairs][W > NG ? W : NG];
+#pragma unroll
+    for (int k = 0; k < kMovePairs; ++k) {
+        auto words = [&](auto &to, auto n, const uint8_t *at) {
+            constexpr int N = decltype(n)::value;
+            if constexpr (N == 4) { const uint4 v = __ldcs(reinterpret_cast<const uint4 *>(at)); to[0] = v.x; to[1] = v.y; to[2] = v.z; to[3] = v.w; }
+            else if constexpr (N == 2) { const uint2 v = __ldcs(reinterpret_cast<const uint2 *>(at)); to[0] = v.x; to[1] = v.y; }
+            else to[0] = __ldcs(reinterpret_cast<const uint32_t *>(at));
+        };
+        if (lane < 8) {
+            if (from[k][0] >= 0) words(one[k], std::integral_constant<int, W>(), src + tile_at(from[k][0]) + T::value_word(from[k][0] % kTileEntries, 0, lane));
+            if (from[k][1] >= 0) words(two[k], std::integral_constant<int, W>(), src + tile_at(from[k][1]) + T::value_word(from[k][1] % kTileEntries, 0, lane));
+        } else {
+            const int j = half ? from[k][1] : from[k][0], i = lane & 1 ? from[k][1] : from[k][0];
+            if (j >= 0) words(one[k], std::integral_constant<int, W>(), src + tile_at(j) + T::key_word(j % kTileEntries, 0, lane & 3));
+            if (i >= 0) {
+                if (lane < 12) words(two[k], std::integral_constant<int, NG>(), src + tile_at(i) + (lane & 2 ? T::kValuePar : T::kKeyPar) + i % kTileEntries * NG * 4);
+                else if (lane & 2) two[k][0] = __float_as_uint(A.src.weight[A.src.meta(b, h) + i]);
+                else two[k][0] = A.src.pos ? A.src.pos[A.src.meta(b, h) + i] : i;
+            }
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kMovePairs; ++k) {
+        const long long s0 = ((block * kMovePairs + k) * kGroups + group) * 2;
+        auto put = [&](uint8_t *at, const auto &x, auto n) {
+            constexpr int N = decltype(n)::value;
+            if constexpr (N == 4) *reinterpret_cast<uint4 *>(at) = make_uint4(x[0], x[1], x[2], x[3]);
+            else if constexpr (N == 2) *reinterpret_cast<uint2 *>(at) = make_uint2(x[0], x[1]);
+            else *reinterpret_cast<uint32_t *>(at) = x[0];
+        };
+        if (from[k][0] < 0 && from[k][1] < 0) continue;
+        uint8_t *to = dst + tile_at((int)s0);
+        const int r = (int)(s0 % kTileEntries);
+        if (lane < 8) {
+            uint8_t *at = to + T::value_word(r, 0, lane);
+            uint32_t y[W];
+#pragma unroll
+            for (int i = 0; i < W; ++i)          // the source's half into the slot's
+                y[i] = (from[k][0] & 1 ? one[k][i] >> 16 : one[k][i] & 0xFFFFu) | (from[k][1] & 1 ? two[k][i] & 0xFFFF0000u : two[k][i] << 16);
+            if (from[k][0] >= 0 && from[k][1] >= 0) put(at, y, std::integral_constant<int, W>());
+            else
+#pragma unroll
+                for (int i = 0; i < W; ++i) reinterpret_cast<uint16_t *>(at)[2 * i + (from[k][0] < 0)] = (uint16_t)(from[k][0] < 0 ? y[i] >> 16 : y[i]);
+        } else {
+            const int j = half ? from[k][1] : from[k][0], i = lane & 1 ? from[k][1] : from[k][0];
+            if (j >= 0) put(to + T::key_word(r + half, 0, lane & 3), one[k], std::integral_constant<int, W>());
+            if (i >= 0) {
+                if (lane < 12) put(to + (lane & 2 ? T::kValuePar : T::kKeyPar) + (r + (lane & 1)) * NG * 4, two[k], std::integral_constant<int, NG>());
+                else if (lane & 2) A.dst.weight[A.dst.meta(b, h) + s0 + (lane & 1)] = __uint_as_float(two[k][0]);
+                else A.dst.pos[A.dst.meta(b, h) + s0 + (lane & 1)] = (int)two[k][0];
+            }
+        }
+    }
 }
 
 cudaLaunchConfig_t config(dim3 grid, int threads, cudaStream_t st, cudaLaunchAttribute *at) {
@@ -214,8 +292,12 @@ template <int DT, int D, int NG> struct Load {
     static int go(cudaLaunchConfig_t *cfg, const LoadArgs *A) { SI_CUDA_TRY(cudaLaunchKernelEx(cfg, load_kernel<DT, D, NG>, *A)); return SI_OK; }
 };
 
-// Blocks that cover n entries, wherever in a tile the first one is.
-unsigned tile_blocks(int n) { return (unsigned)(((long long)n + kTileEntries - 2) / kTileEntries + kWarps) / kWarps; }
+template <int DT, int D, int NG> struct Move {
+    static int go(cudaLaunchConfig_t *cfg, const EvictArgs *A) { SI_CUDA_TRY(cudaLaunchKernelEx(cfg, move4_kernel<D, NG>, *A)); return SI_OK; }
+};
+
+// Blocks that cover n entries, wherever among eight the first one is, for every head.
+long long octet_blocks(int n, int heads) { return (((long long)n + kOctet - 2) / kOctet + kWarps) / kWarps * heads; }
 
 bool same_shape(const si_kv_t *a, const si_kv4_t *b) {
     return a->n_seqs == b->n_seqs && a->n_kv_heads == b->n_kv_heads && a->head_dim == b->head_dim && a->dtype == b->dtype;
@@ -251,7 +333,9 @@ extern "C" int si_kv4_store(const si_kv_t *src, const si_kv4_t *dst, const int32
     const StoreArgs A{si_kv_view_of(src), si_kv4_meta_of(dst), si_kv4_view_of(dst), first_pos, status_dev};
     si_mt_forget();
     cudaLaunchAttribute at;
-    cudaLaunchConfig_t cfg = config(dim3(tile_blocks(src->capacity), dst->n_kv_heads, dst->n_seqs), kThreads, (cudaStream_t)stream, &at);
+    const long long blocks = octet_blocks(src->capacity < dst->capacity ? src->capacity : dst->capacity, dst->n_kv_heads);
+    if (blocks > INT_MAX) return SI_ERR_TOO_LARGE;
+    cudaLaunchConfig_t cfg = config(dim3((unsigned)blocks, 1, dst->n_seqs), kThreads, (cudaStream_t)stream, &at);
     return by_shape<Store>(dst->dtype, dst->head_dim, si_kv4_groups(dst), &cfg, &A);
 }
 
@@ -267,7 +351,9 @@ extern "C" int si_kv4_load(const si_kv4_t *src, const si_kv_t *dst, const int32_
     si_mt_forget();
     const int most = n < src->capacity ? n : src->capacity;
     cudaLaunchAttribute at;
-    cudaLaunchConfig_t cfg = config(dim3(tile_blocks(most), src->n_kv_heads, src->n_seqs), kThreads, (cudaStream_t)stream, &at);
+    const long long blocks = octet_blocks(most, src->n_kv_heads);
+    if (blocks > INT_MAX) return SI_ERR_TOO_LARGE;
+    cudaLaunchConfig_t cfg = config(dim3((unsigned)blocks, 1, src->n_seqs), kThreads, (cudaStream_t)stream, &at);
     return by_shape<Load>(src->dtype, src->head_dim, si_kv4_groups(src), &cfg, &A);
 }
 
@@ -290,11 +376,13 @@ extern "C" int si_kv4_evict(const si_kv4_t *src, const si_kv4_t *dst, const int3
     if (!workspace) return SI_ERR_INVALID_ARG;
     if ((uintptr_t)workspace & 255) return SI_ERR_ALIGNMENT;
     EvictArgs A = si_evict_args(si_kv4_meta_of(src), si_kv4_meta_of(dst), in_place, q_pos, n_new, budget, n_sink, n_recent, kept, len_out, workspace, status_dev);
+    if (((long long)A.slots / 128 + 1) * src->n_kv_heads > INT_MAX) return SI_ERR_TOO_LARGE;
     A.src4 = si_kv4_view_of(src); A.dst4 = si_kv4_view_of(dst); A.groups = si_kv4_groups(src);
     si_mt_forget();
     if ((rc = si_evict_select(A, (cudaStream_t)stream)) || A.move_here) return rc;
     cudaLaunchAttribute at;
-    cudaLaunchConfig_t cfg = config(dim3((A.slots + 256 / kMoveLanes4 - 1) / (256 / kMoveLanes4), src->n_kv_heads, src->n_seqs), 256, (cudaStream_t)stream, &at);
-    SI_CUDA_TRY(cudaLaunchKernelEx(&cfg, move4_kernel, A));
-    return SI_OK;
+    constexpr int kPerBlock = 256 / 16 * 2 * kMovePairs;
+    const long long blocks = ((long long)A.slots + kPerBlock - 1) / kPerBlock * src->n_kv_heads;
+    cudaLaunchConfig_t cfg = config(dim3((unsigned)blocks, 1, src->n_seqs), 256, (cudaStream_t)stream, &at);
+    return by_shape<Move>(src->dtype, src->head_dim, A.groups, &cfg, &A);
 }

@@ -29,7 +29,9 @@ constexpr int kWarps = 4, kThreads = kWarps * 32;
 template <int H> constexpr int kPerSmOf = H == 16 ? 2 : 3;
 template <int H> constexpr int kStagesOf = H == 16 ? 4 : 3;
 constexpr int kPad = 3;                // an item's start and end take about as long as so many tiles (0: 47.7 us for 512 windows of 2052, 3: 41.7, 8: 44.4)
-constexpr int kMinUnits = 2;           // of a run: fewer would leave more parts than they save time
+// Units of a run: fewer would leave more parts than they save time (24 x 2 caches of 2049 entries and their eviction: two 28.7 us a
+// step, four 27.3), but with little work the SMs come first (one cache of 1001, 8 heads: two 17.9, four 18.6).
+constexpr int kFewUnits = 2, kManyUnits = 4;
 
 // H: query heads of a pass, 4, 8 or 16.  Eight fill the eight columns of a product; 16 are two tiles of columns beside the same
 // codes; with four the columns are two neighbouring groups side by side (a word of codes meets zeros in the columns of the
@@ -47,7 +49,7 @@ struct Decode4Args {
 
 // Runs: the tiles of all (sequence, head block) items in one row, in front of every item kPad units without a tile, which stand for
 // the time an item's start and end take (short items are then not crowded into one run); run i of n has units total * i / n up to
-// total * (i + 1) / n.  A.n_cta is the number of warps; there are fewer runs if they had less than kMinUnits.
+// total * (i + 1) / n.  A.n_cta is the number of warps; there are fewer runs if they had less than kManyUnits.
 struct Runs {
     int total, n;
     __device__ __forceinline__ int first(int i) const { return (int)((long long)total * i / n); }
@@ -74,7 +76,8 @@ __device__ __forceinline__ Runs find_runs(const DecodeArgs &A, Cursor *at, int *
         empty |= w.nc == 0;
     }
     const int before = si_block_scan<kThreads>(sum, sh);
-    const Runs r{sh[kThreads / 32], min(A.n_cta, (sh[kThreads / 32] + kMinUnits - 1) / kMinUnits)};
+    const int total = sh[kThreads / 32];
+    const Runs r{total, min(A.n_cta, max((total + kManyUnits - 1) / kManyUnits, min((total + kFewUnits - 1) / kFewUnits, (int)gridDim.x)))};
     if (r.total > 0)
         for (int i = 0; i < kWarps; ++i) {
             const int run = i * gridDim.x + blockIdx.x;

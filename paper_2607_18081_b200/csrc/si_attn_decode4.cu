@@ -3,7 +3,7 @@
 //   out_q = sum_j p_qj (s_j c_j + m_j),  p_q = softmax over the visible entries j of scale q . (s'_j c'_j + m'_j)
 //
 // with a step s and a lowest value m per entry and group of channels.  Nothing is unpacked to 16-bit values: per group,
-//   q . k_j = s'_j (q . c'_j) + m'_j sum(q)        out = sum_j (p_j s_j) c_j + sum_j p_j m_j,
+//   q . k_j = s'_j (q . c'_j) + m'_j sum(q)        out = sum_j (p_j s_j) (c_j - 8) + sum_j p_j (m_j + 8 s_j),
 // so that the matrix products run on the codes themselves and the steps are applied to few numbers: to the scores (keys x
 // heads) and to p.  A word of eight codes becomes matrix operands by one shift and four masks: a pair of nibbles in the low bits of two
 // halves is a pair of f16 numbers c 2^-24 (subnormal, which the matrix unit multiplies exactly), sixteen times that one nibble
@@ -337,10 +337,9 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
         }
         id = max(id, start);
         float *scores_to = A.scores + (((long long)seq * A.kv.H + h) * A.GB + gb) * A.kv.cap * A.GS;
-        // o: sum p s c 2^-24.  Word i: elements 4 lg + 2 n, 4 lg + 2 n + 1 (the latter times 16, the former plus the latter) in the two halves of
-        // quad 2 i + n.  H = 4: words k of an even and an odd group, in the halves of four quads, one per element; those of the lane's
-        // own groups count.
-        // low: sum p m of this lane's entries
+        // o: sum p s (c - 8) 2^-24.  Word i: elements 4 lg + 2 n, 4 lg + 2 n + 1 (the latter times 16) in the two halves of quad 2 i + n.
+        // H = 4: words k of an even and an odd group, in the halves of four quads, one per element; those of the lane's own groups count.
+        // low: sum p (m + 8 s) of this lane's entries
         float o[NT][2 * W][4] = {}, low[NT][L][2] = {};
         // the maximum and the score that moves it, both without the factor `back`; base: what p is relative to, 0 while there is none
         float m[NT][2], edge[NT][2], base[NT][2], l[NT][2];
@@ -458,17 +457,17 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
                     for (int g = 0; g < L; ++g)
 #pragma unroll
                         for (int r = 0; r < 2; ++r) {
-                            const float s = si_cvt<DT>::hi(vp[u][r][g]), mn = si_cvt<DT>::lo(vp[u][r][g]);
+                            const float s = si_cvt<DT>::hi(vp[u][r][g]), mn = fmaf(8.f, s, si_cvt<DT>::lo(vp[u][r][g]));
                             pf[u][nt][g][r] = transposed(pack2<SI_F16>(p[2 * r] * s, p[2 * r + 1] * s));
                             low[nt][g][0] = fmaf(p[2 * r], mn, low[nt][g][0]);
                             low[nt][g][1] = fmaf(p[2 * r + 1], mn, low[nt][g][1]);
                         }
                 }
-            // A byte masked as a whole (h 16 + l) and its upper nibble: two operands by one instruction each; l is the difference at the end.
-            auto codes = [&](uint32_t w, int n) {
-                const uint32_t bytes = n < 2 ? w : __byte_perm(w, 0, 0x4341);
-                return n & 1 ? si_q4::high_codes(bytes) : n < 2 ? w & 0x00FF00FFu : bytes;
-            };
+            // Every sum also gets -8 times (upper nibbles: -128 times) its p s, out of a product with constants: with codes around zero it
+            // stays small, and so do what the matrix unit cuts off of it and what the rounding of p s leaves (one of 2052 entries, f16:
+            // error 2.4e-4 instead of 4.7e-4; of 260001, bf16: 1.7e-3 instead of 4.5e-3).
+            auto codes = [&](uint32_t w, int n) { return n & 1 ? si_q4::high_codes(w >> 4 * (n & 2)) : si_q4::low_codes(w >> 4 * (n & 2)); };
+            constexpr uint32_t kLow8 = 0x80088008u, kHigh8 = 0x80808080u;          // pairs of -8 2^-24 and -128 2^-24
 #pragma unroll
             for (int u = 0; u < 2; ++u)
                 if constexpr (PAIR) {
@@ -477,7 +476,9 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
                         const int even = i / GW * 2 * GW + i % GW, odd = even + GW;
 #pragma unroll
                         for (int n = 0; n < 4; ++n) {
-                            const uint32_t a[4] = {codes(va[u][even], n), codes(va[u][odd], n), codes(vb[u][even], n), codes(vb[u][odd], n)};
+                            const uint32_t k8 = n & 1 ? kHigh8 : kLow8;
+                            const uint32_t a[4] = {codes(va[u][even], n), codes(va[u][odd], n), codes(vb[u][even], n), codes(vb[u][odd], n)}, eight[4] = {k8, k8, k8, k8};
+                            product<SI_F16>(o[0][4 * i + n], eight, pf[u][0][i / GW][0], pf[u][0][i / GW][1]);
                             product<SI_F16>(o[0][4 * i + n], a, pf[u][0][i / GW][0], pf[u][0][i / GW][1]);
                         }
                     }
@@ -486,9 +487,13 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
                     for (int i = 0; i < W; ++i)
 #pragma unroll
                         for (int half = 0; half < 2; ++half) {
-                            const uint32_t a[4] = {codes(va[u][i], 2 * half), codes(va[u][i], 2 * half + 1), codes(vb[u][i], 2 * half), codes(vb[u][i], 2 * half + 1)};
+                            const uint32_t a[4] = {codes(va[u][i], 2 * half), codes(va[u][i], 2 * half + 1), codes(vb[u][i], 2 * half), codes(vb[u][i], 2 * half + 1)}, eight[4] = {kLow8, kHigh8, kLow8, kHigh8};
 #pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) product<SI_F16>(o[nt][2 * i + half], a, pf[u][nt][T::place_of(T::group_of(i))][0], pf[u][nt][T::place_of(T::group_of(i))][1]);
+                            for (int nt = 0; nt < NT; ++nt) {
+                                const int g = T::place_of(T::group_of(i));
+                                product<SI_F16>(o[nt][2 * i + half], eight, pf[u][nt][g][0], pf[u][nt][g][1]);
+                                product<SI_F16>(o[nt][2 * i + half], a, pf[u][nt][g][0], pf[u][nt][g][1]);
+                            }
                         }
                 }
         };
@@ -612,7 +617,7 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
                     const int word = PAIR ? i / GW * 2 * GW + i % GW + (lt >> 1) * GW : i;
                     const float mn = low[nt][PAIR ? i / GW : T::place_of(T::group_of(i))][c];
                     auto of = [&](int n) { return PAIR ? (lt >> 1 ? o[nt][(4 * i + n) % (2 * W)][c + 2] : o[nt][(4 * i + n) % (2 * W)][c]) : o[nt][2 * i + n / 2][c + 2 * (n & 1)]; };
-                    const float4 y = make_float4(fmaf(of(0) - of(1), 0x1p24f, mn), fmaf(of(1), 0x1p20f, mn), fmaf(of(2) - of(3), 0x1p24f, mn), fmaf(of(3), 0x1p20f, mn));
+                    const float4 y = make_float4(fmaf(of(0), 0x1p24f, mn), fmaf(of(1), 0x1p20f, mn), fmaf(of(2), 0x1p24f, mn), fmaf(of(3), 0x1p20f, mn));
                     if (whole) *reinterpret_cast<uint2 *>(A.out + (row + head) * D + 32 * word + 4 * lg) = make_uint2(pack2<DT>(y.x * inv, y.y * inv), pack2<DT>(y.z * inv, y.w * inv));
                     else *reinterpret_cast<float4 *>(A.part_o + (slot * HB + head) * D + 32 * word + 4 * lg) = y;
                 }

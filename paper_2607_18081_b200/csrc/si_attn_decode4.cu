@@ -212,6 +212,9 @@ template <int DT> __device__ __forceinline__ void first_product(float (&c)[4], c
         asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
             : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
 }
+__device__ __forceinline__ void add2(float &a, float &b, float c, float d) {
+    asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %3};\n\tadd.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}" : "+f"(a), "+f"(b) : "f"(c), "f"(d));
+}
 __device__ __forceinline__ uint32_t transposed(uint32_t x) { uint32_t r; asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x)); return r; }
 
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint64_t *bar, uint64_t hint) {
@@ -463,11 +466,13 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
                             low[nt][g][1] = fmaf(p[2 * r + 1], mn, low[nt][g][1]);
                         }
                 }
-            // Every sum also gets -8 times (upper nibbles: -128 times) its p s, out of a product with constants: with codes around zero it
-            // stays small, and so do what the matrix unit cuts off of it and what the rounding of p s leaves (one of 2052 entries, f16:
-            // error 2.4e-4 instead of 4.7e-4; of 260001, bf16: 1.7e-3 instead of 4.5e-3).
+            // Every sum also gets -8 times (upper nibbles: -128 times) the sum of its rounded p s, which a product with constants gives: with
+            // codes around zero it stays small, and so do what the matrix unit cuts off of it and what the rounding of p s leaves
+            // (2052 entries, f16: error 2.6e-4 instead of 4.7e-4; 260001, bf16: 1.7e-3 instead of 4.5e-3).  In the products
+            // themselves, as one more each, it costs 5 us of 68 for one sequence of 260001.
             auto codes = [&](uint32_t w, int n) { return n & 1 ? si_q4::high_codes(w >> 4 * (n & 2)) : si_q4::low_codes(w >> 4 * (n & 2)); };
-            constexpr uint32_t kLow8 = 0x80088008u, kHigh8 = 0x80808080u;          // pairs of -8 2^-24 and -128 2^-24
+            constexpr uint32_t kEight = 0x80088008u;           // a pair of -8 2^-24
+            const uint32_t eight[4] = {kEight, kEight, kEight, kEight};
 #pragma unroll
             for (int u = 0; u < 2; ++u)
                 if constexpr (PAIR) {
@@ -476,9 +481,7 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
                         const int even = i / GW * 2 * GW + i % GW, odd = even + GW;
 #pragma unroll
                         for (int n = 0; n < 4; ++n) {
-                            const uint32_t k8 = n & 1 ? kHigh8 : kLow8;
-                            const uint32_t a[4] = {codes(va[u][even], n), codes(va[u][odd], n), codes(vb[u][even], n), codes(vb[u][odd], n)}, eight[4] = {k8, k8, k8, k8};
-                            product<SI_F16>(o[0][4 * i + n], eight, pf[u][0][i / GW][0], pf[u][0][i / GW][1]);
+                            const uint32_t a[4] = {codes(va[u][even], n), codes(va[u][odd], n), codes(vb[u][even], n), codes(vb[u][odd], n)};
                             product<SI_F16>(o[0][4 * i + n], a, pf[u][0][i / GW][0], pf[u][0][i / GW][1]);
                         }
                     }
@@ -487,14 +490,42 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
                     for (int i = 0; i < W; ++i)
 #pragma unroll
                         for (int half = 0; half < 2; ++half) {
-                            const uint32_t a[4] = {codes(va[u][i], 2 * half), codes(va[u][i], 2 * half + 1), codes(vb[u][i], 2 * half), codes(vb[u][i], 2 * half + 1)}, eight[4] = {kLow8, kHigh8, kLow8, kHigh8};
+                            const uint32_t a[4] = {codes(va[u][i], 2 * half), codes(va[u][i], 2 * half + 1), codes(vb[u][i], 2 * half), codes(vb[u][i], 2 * half + 1)};
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt) {
                                 const int g = T::place_of(T::group_of(i));
-                                product<SI_F16>(o[nt][2 * i + half], eight, pf[u][nt][g][0], pf[u][nt][g][1]);
                                 product<SI_F16>(o[nt][2 * i + half], a, pf[u][nt][g][0], pf[u][nt][g][1]);
                             }
                         }
+                }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int g = 0; g < L; ++g) {
+                    float e[4];
+                    first_product<SI_F16>(e, eight, pf[0][nt][g][0], pf[0][nt][g][1]);
+                    product<SI_F16>(e, eight, pf[1][nt][g][0], pf[1][nt][g][1]);
+                    const float f0 = 16.f * e[0], f1 = 16.f * e[1];
+                    if constexpr (PAIR) {
+#pragma unroll
+                        for (int i = g * GW; i < (g + 1) * GW; ++i)
+#pragma unroll
+                            for (int n = 0; n < 4; ++n) {
+                                float (&q)[4] = o[nt][4 * i + n];
+                                add2(q[0], q[1], n & 1 ? f0 : e[0], n & 1 ? f1 : e[1]);
+                                add2(q[2], q[3], n & 1 ? f0 : e[0], n & 1 ? f1 : e[1]);
+                            }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < W; ++i)
+                            if (T::place_of(T::group_of(i)) == g)
+#pragma unroll
+                                for (int half = 0; half < 2; ++half) {
+                                    float (&q)[4] = o[nt][2 * i + half];
+                                    add2(q[0], q[1], e[0], e[1]);
+                                    add2(q[2], q[3], f0, f1);
+                                }
+                    }
                 }
         };
         float x[2][NT][4];

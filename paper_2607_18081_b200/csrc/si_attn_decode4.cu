@@ -747,22 +747,25 @@ __global__ void __launch_bounds__(kJoin4, 3) join4_kernel(const DecodeArgs A, co
         return;
     }
     const int j0 = (blockIdx.x - n_out) * (U * kJoin4);
+    SeqWork w;
+    // few keys a thread: everything at once; many: not before it is known that the range has entries
+    if (U > 1) { w = seq_work<CH>(A, b, nullptr); if (j0 >= w.n) return; }
     float *weight = A.kv.weight + A.kv.meta(b, h);
     const float *sc = A.scores + ((long long)b * A.kv.H + h) * A.GB * A.kv.cap * A.GS;
     float2 x[U][GX / 2];                   // the first head block's scores
     float old[U];
+    const int most = U > 1 ? w.n : A.kv.cap;
 #pragma unroll
     for (int i = 0; i < U; ++i) {
         const int j = j0 + i * kJoin4 + tid;
-        if (j >= A.kv.cap) continue;
+        if (j >= most) continue;
         old[i] = weight[j];
 #pragma unroll
         for (int g = 0; g < GX; g += 2)
             if (g < A.GS) x[i][g / 2] = *reinterpret_cast<const float2 *>(sc + (long long)j * A.GS + g);
     }
     const float2 whole = tid < A.G ? A.done[row + tid] : make_float2(0.f, 0.f);
-    const SeqWork w = seq_work<CH>(A, b, nullptr);
-    if (j0 >= w.n) return;
+    if (U == 1) { w = seq_work<CH>(A, b, nullptr); if (j0 >= w.n) return; }
     if (tid < A.G) sh_done[tid] = whole;
     __syncthreads();
     for (int gb = 0; gb < A.GB && w.nc > 0; ++gb) {
@@ -788,23 +791,29 @@ __global__ void __launch_bounds__(kJoin4, 3) join4_kernel(const DecodeArgs A, co
         }
     }
     __syncthreads();
+    // the first block's heads: a hidden entry's score is -inf; it receives nothing, from a head whose sum is NaN neither
+    float add[U] = {};
+#pragma unroll
+    for (int g = 0; g < GX; ++g) {
+        if (g >= A.G) break;
+        const float2 done = sh_done[g];
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const float y = g & 1 ? x[i][g / 2].y : x[i][g / 2].x;
+            if (y != -INFINITY) add[i] = fmaf(ex2(y - done.x), done.y, add[i]);
+        }
+    }
 #pragma unroll
     for (int i = 0; i < U; ++i) {
         const int j = j0 + i * kJoin4 + tid, c = j / CH;
         if (j >= w.n) continue;
         if (!(c < w.c_sink || (c >= w.c_win && c < w.c_win + w.nc - w.c_sink))) { if (j == w.n_old) weight[j] = 0.f; continue; }
-        float sum = 0.f;
-        for (int gb = 0; gb < A.GB; ++gb) {
-            const float *more = sc + ((long long)gb * A.kv.cap + j) * A.GS;
-#pragma unroll
-            for (int g = 0; g < GX; g += 2) {
-                if (g >= A.GS || gb * HB + g >= A.G) break;
-                const float2 y = gb == 0 ? x[i][g / 2] : *reinterpret_cast<const float2 *>(more + g);
-                // a hidden entry's score is -inf: it receives nothing, from a head whose sum is NaN neither
-                if (y.x != -INFINITY) sum += ex2(y.x - sh_done[gb * HB + g].x) * sh_done[gb * HB + g].y;
-                if (gb * HB + g + 1 < A.G && y.y != -INFINITY) sum += ex2(y.y - sh_done[gb * HB + g + 1].x) * sh_done[gb * HB + g + 1].y;
+        float sum = add[i];
+        for (int gb = 1; gb < A.GB; ++gb)
+            for (int g = gb * HB; g < min(A.G, gb * HB + HB); ++g) {
+                const float y = sc[((long long)gb * A.kv.cap + j) * A.GS + g - gb * HB];
+                if (y != -INFINITY) sum = fmaf(ex2(y - sh_done[g].x), sh_done[g].y, sum);
             }
-        }
         weight[j] = j == w.n_old ? sum : old[i] + sum;
     }
 }

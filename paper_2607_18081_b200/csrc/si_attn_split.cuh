@@ -1,6 +1,6 @@
-// What the single-token kernels over a key/value cache share, whatever its entries are held in: the chunks of all (sequence, head)
-// items in one row, cut into equal runs, one per CTA; the parts of items that cross CTAs; the kernel that joins the parts in
-// the order of the CTAs and adds up the weights.  CH: entries of a chunk.
+// What the single-token kernels over a key/value cache share, whatever its entries are held in: a call's arguments, the chunks of a
+// sequence that hold visible entries, the workspace; and for 16-bit entries the row of all chunks, cut into equal runs, one per CTA, and
+// the kernel that joins the parts of items that cross CTAs in their order and adds up the weights.  CH: entries of a chunk.
 #pragma once
 #include "si_kv.cuh"
 #include "si_tc.cuh"

@@ -69,46 +69,62 @@ __global__ void __launch_bounds__(kThreads) store_kernel(const StoreArgs A) {
         raw[i][0] = in ? __ldcs(reinterpret_cast<const uint4 *>(A.src.k + at)) : make_uint4(0, 0, 0, 0);
         raw[i][1] = in ? __ldcs(reinterpret_cast<const uint4 *>(A.src.v + at)) : make_uint4(0, 0, 0, 0);
     }
-    uint8_t *tile = A.dst.row(b, h) + e0 / kTileEntries * T::kBytes;
-    const int in_tile = (int)(e0 % kTileEntries);
+    // the eight entries' part of the tile, and of the steps
+    uint8_t *tile = A.dst.row(b, h) + e0 / kTileEntries * T::kBytes + (int)(e0 % kTileEntries) * (D / 2);
+    uint8_t *steps = A.dst.row(b, h) + e0 / kTileEntries * T::kBytes + (int)(e0 % kTileEntries) * NG * 4;
+    // The extremes of every group, of keys then of values, are with all of its lanes; its step and reciprocal are found by one of them.
+    constexpr int I = 2 * N, CALLS = (I + GL - 1) / GL;
+    uint32_t lo2[I], hi2[I];
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const int row = i * ROWS + sub, r = in_tile + row, other_row = row ^ 1;
+    for (int k = 0; k < I; ++k) {
+        const uint4 u = raw[k % N][k / N];
+        lo2[k] = min2<DT>(min2<DT>(u.x, u.y), min2<DT>(u.z, u.w));
+        hi2[k] = max2<DT>(max2<DT>(u.x, u.y), max2<DT>(u.z, u.w));
+#pragma unroll
+        for (int o = 1; o < GL; o <<= 1) {
+            lo2[k] = min2<DT>(lo2[k], __shfl_xor_sync(0xFFFFFFFFu, lo2[k], o));
+            hi2[k] = max2<DT>(hi2[k], __shfl_xor_sync(0xFFFFFFFFu, hi2[k], o));
+        }
+    }
+    uint32_t par[CALLS];
+    float inverse[CALLS];
+#pragma unroll
+    for (int q = 0; q < CALLS; ++q) {
+        const int mine = q * GL + c % GL;
+        uint32_t lo = lo2[0], hi = hi2[0];
+#pragma unroll
+        for (int k = 1; k < I; ++k) if (mine == k) { lo = lo2[k]; hi = hi2[k]; }
+        par[q] = si_q4::group_word<DT>(si_q4::min_nan(si_cvt<DT>::lo(lo), si_cvt<DT>::hi(lo)), si_q4::max_nan(si_cvt<DT>::lo(hi), si_cvt<DT>::hi(hi)), &inverse[q]);
+        const int row = mine % N * ROWS + sub;
+        if (mine < I && row >= r0 && row < r1)
+            *reinterpret_cast<uint32_t *>(steps + (mine / N ? T::kValuePar : T::kKeyPar) + (row * NG + T::place_of(c / GL)) * 4) = par[q];
+    }
+#pragma unroll
+    for (int k = 0; k < I; ++k) {
+        const int i = k % N, row = i * ROWS + sub, other_row = row ^ 1, from = lane / GL * GL + k % GL;
         const bool in = row >= r0 && row < r1, both = in && other_row >= r0 && other_row < r1;
-#pragma unroll
-        for (int which = 0; which < 2; ++which) {
-            const uint32_t u[4] = {raw[i][which].x, raw[i][which].y, raw[i][which].z, raw[i][which].w};
-            uint32_t lo2 = min2<DT>(min2<DT>(u[0], u[1]), min2<DT>(u[2], u[3])), hi2 = max2<DT>(max2<DT>(u[0], u[1]), max2<DT>(u[2], u[3]));
-#pragma unroll
-            for (int o = 1; o < GL; o <<= 1) {
-                lo2 = min2<DT>(lo2, __shfl_xor_sync(0xFFFFFFFFu, lo2, o));
-                hi2 = max2<DT>(hi2, __shfl_xor_sync(0xFFFFFFFFu, hi2, o));
+        const float low = si_cvt<DT>::lo(__shfl_sync(0xFFFFFFFFu, par[k / GL], from)), inv = __shfl_sync(0xFFFFFFFFu, inverse[k / GL], from);
+        const uint32_t u[4] = {raw[i][k / N].x, raw[i][k / N].y, raw[i][k / N].z, raw[i][k / N].w};
+        // a code's bits lie above those of 2^23 * 1.5, whose sum over eight places is taken off at the end
+        auto code = [&](int e) { return si_q4::code_bits(e & 1 ? si_cvt<DT>::hi(u[e / 2]) : si_cvt<DT>::lo(u[e / 2]), low, inv); };
+        auto joined = [&](int k7, int k6, int k5, int k4, int k3, int k2, int k1, int k0) {
+            uint32_t x = code(k7);
+            x = x * 16 + code(k6); x = x * 16 + code(k5); x = x * 16 + code(k4);
+            x = x * 16 + code(k3); x = x * 16 + code(k2); x = x * 16 + code(k1);
+            return x * 16 + code(k0) - 0x3F400000u;
+        };
+        if (k < N) {
+            const uint32_t word = joined(7, 5, 3, 1, 6, 4, 2, 0);
+            if (in) *reinterpret_cast<uint32_t *>(tile + T::key_word(row, w, t)) = word;
+        } else {
+            const uint32_t word = joined(7, 6, 5, 4, 3, 2, 1, 0);      // elements 0 .. 3 in the lower half
+            const uint32_t other = __shfl_xor_sync(0xFFFFFFFFu, word, L);
+            if (both) {
+                *reinterpret_cast<uint32_t *>(tile + T::value_word(row, w, 2 * t + (row & 1))) = row & 1 ? __byte_perm(other, word, 0x7632) : __byte_perm(word, other, 0x5410);
+            } else if (in) {
+                *reinterpret_cast<uint16_t *>(tile + T::value_word(row, w, 2 * t) + 2 * (row & 1)) = (uint16_t)word;
+                *reinterpret_cast<uint16_t *>(tile + T::value_word(row, w, 2 * t + 1) + 2 * (row & 1)) = (uint16_t)(word >> 16);
             }
-            const float low = si_q4::min_nan(si_cvt<DT>::lo(lo2), si_cvt<DT>::hi(lo2)), high = si_q4::max_nan(si_cvt<DT>::lo(hi2), si_cvt<DT>::hi(hi2));
-            float inverse;
-            const uint32_t par = si_q4::group_word<DT>(low, high, &inverse);
-            // a code's bits lie above those of 2^23 * 1.5, whose sum over eight places is taken off at the end
-            auto code = [&](int k) { return si_q4::code_bits(k & 1 ? si_cvt<DT>::hi(u[k / 2]) : si_cvt<DT>::lo(u[k / 2]), low, inverse); };
-            auto joined = [&](int k7, int k6, int k5, int k4, int k3, int k2, int k1, int k0) {
-                uint32_t x = code(k7);
-                x = x * 16 + code(k6); x = x * 16 + code(k5); x = x * 16 + code(k4);
-                x = x * 16 + code(k3); x = x * 16 + code(k2); x = x * 16 + code(k1);
-                return x * 16 + code(k0) - 0x3F400000u;
-            };
-            if (which == 0) {
-                const uint32_t word = joined(7, 5, 3, 1, 6, 4, 2, 0);
-                if (in) *reinterpret_cast<uint32_t *>(tile + T::key_word(r, w, t)) = word;
-            } else {
-                const uint32_t word = joined(7, 6, 5, 4, 3, 2, 1, 0);      // elements 0 .. 3 in the lower half
-                const uint32_t other = __shfl_xor_sync(0xFFFFFFFFu, word, L);
-                if (both) {
-                    *reinterpret_cast<uint32_t *>(tile + T::value_word(r, w, 2 * t + (r & 1))) = r & 1 ? __byte_perm(other, word, 0x7632) : __byte_perm(word, other, 0x5410);
-                } else if (in) {
-                    *reinterpret_cast<uint16_t *>(tile + T::value_word(r, w, 2 * t) + 2 * (r & 1)) = (uint16_t)word;
-                    *reinterpret_cast<uint16_t *>(tile + T::value_word(r, w, 2 * t + 1) + 2 * (r & 1)) = (uint16_t)(word >> 16);
-                }
-            }
-            if (in && c % GL == 0) *reinterpret_cast<uint32_t *>(tile + (which ? T::kValuePar : T::kKeyPar) + (r * NG + T::place_of(c / GL)) * 4) = par;
         }
     }
     if (lane < r0 || lane >= r1) return;

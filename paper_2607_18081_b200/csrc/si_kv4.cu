@@ -206,7 +206,7 @@ __global__ void __launch_bounds__(kThreads) load_kernel(const LoadArgs A) {
 // The kept entries to their slots; nothing to do for an entry that stays.  Sixteen lanes per pair of slots, kMovePairs pairs in flight:
 // eight lanes have the values' cells of both sources (which hold a neighbour each) and put the two halves together, eight the
 // two keys, and of these four the steps and four positions and weights.
-constexpr int kMovePairs = 4;
+constexpr int kMovePairs = 2;
 template <int D, int NG>
 __global__ void __launch_bounds__(256) move4_kernel(const EvictArgs A) {
     using T = si_tile4<D, NG>;

@@ -540,7 +540,9 @@ def si_attn_weights(cache: KVCache, q, window: int, n_sink: int, scale: float, l
                                 _on(stream, cache)), "si_attn_weights")
 
 
-def _decode(call, name, cache, q, q_pos, k_new, v_new, window, n_sink, scale, out, lse, flags, workspace, status, stream):
+def si_attn_decode(cache: KVCache, q, q_pos, k_new, v_new, window: int, n_sink: int, scale: float, out, lse, flags: int,
+                   workspace, status=None, stream=None) -> None:
+    """q, out: [n_seqs, n_q_heads, head_dim]; k_new, v_new: [n_seqs, n_kv_heads, head_dim] of equal strides, or both None."""
     _, hq, _ = shape = q.shape
     kp = vp = None
     new_stride = 0
@@ -550,32 +552,23 @@ def _decode(call, name, cache, q, q_pos, k_new, v_new, window, n_sink, scale, ou
         kp, vp = _heads(k_new, "k_new", cache, cache.n_kv_heads), _heads(v_new, "v_new", cache, cache.n_kv_heads)
         new_stride = k_new.stride(0)
     ws, ws_bytes = _ws(workspace, cache)
-    _check(call(cache.ref, _heads(q, "q", cache, hq), q.stride(0), hq, _ptr(q_pos, "q_pos", cache, (cache.n_seqs,), torch.int32),
-                kp, vp, new_stride, window, n_sink, scale, _ptr(out, "out", cache, shape, q.dtype),
-                _ptr(lse, "lse", cache, shape[:2], torch.float32), flags, ws, ws_bytes,
-                _ptr(status, "status", cache, (1,), torch.int32), _on(stream, cache)), name)
-
-
-def si_attn_decode(cache: KVCache, q, q_pos, k_new, v_new, window: int, n_sink: int, scale: float, out, lse, flags: int,
-                   workspace, status=None, stream=None) -> None:
-    """q, out: [n_seqs, n_q_heads, head_dim]; k_new, v_new: [n_seqs, n_kv_heads, head_dim] of equal strides, or both None."""
-    _decode(_lib.si_attn_decode, "si_attn_decode", cache, q, q_pos, k_new, v_new, window, n_sink, scale, out, lse, flags, workspace, status, stream)
-
-
-def _evict(call, name, src, dst, q_pos, n_new, budget, n_sink, n_recent, kept, len_out, workspace, status, stream):
-    _one_device(src, dst)
-    seqs = (src.n_seqs,)
-    ws, ws_bytes = _ws(workspace, src)
-    _check(call(src.ref, dst.ref, _ptr(q_pos, "q_pos", src, seqs, torch.int32), n_new, budget, n_sink, n_recent,
-                _ptr(kept, "kept", src, (src.n_seqs, src.n_kv_heads, budget), torch.int32),
-                _ptr(len_out, "len_out", src, seqs, torch.int32), ws, ws_bytes,
-                _ptr(status, "status", src, (1,), torch.int32), _on(stream, src)), name)
+    _check(_lib.si_attn_decode(cache.ref, _heads(q, "q", cache, hq), q.stride(0), hq, _ptr(q_pos, "q_pos", cache, (cache.n_seqs,), torch.int32),
+                               kp, vp, new_stride, window, n_sink, scale, _ptr(out, "out", cache, shape, q.dtype),
+                               _ptr(lse, "lse", cache, shape[:2], torch.float32), flags, ws, ws_bytes,
+                               _ptr(status, "status", cache, (1,), torch.int32), _on(stream, cache)), "si_attn_decode")
 
 
 def si_kv_evict(src: KVCache, dst: KVCache, q_pos, n_new: int, budget: int, n_sink: int, n_recent: int, kept, len_out,
                 workspace, status=None, stream=None) -> None:
     """dst is src: in place.  kept: int32 [n_seqs, n_kv_heads, budget] or None; len_out: int32 [n_seqs] or None."""
-    _evict(_lib.si_kv_evict, "si_kv_evict", src, dst, q_pos, n_new, budget, n_sink, n_recent, kept, len_out, workspace, status, stream)
+    if dst.device != src.device:
+        raise ValueError("both caches have to be on one device")
+    seqs = (src.n_seqs,)
+    ws, ws_bytes = _ws(workspace, src)
+    _check(_lib.si_kv_evict(src.ref, dst.ref, _ptr(q_pos, "q_pos", src, seqs, torch.int32), n_new, budget, n_sink, n_recent,
+                            _ptr(kept, "kept", src, (src.n_seqs, src.n_kv_heads, budget), torch.int32),
+                            _ptr(len_out, "len_out", src, seqs, torch.int32), ws, ws_bytes,
+                            _ptr(status, "status", src, (1,), torch.int32), _on(stream, src)), "si_kv_evict")
 
 
 # ------------------------------------------------------------------------- a key/value cache held in 4 bits
@@ -660,13 +653,31 @@ def si_kv4_load(src: KV4Cache, dst: KVCache, first, n: int, len_out, status=None
 def si_kv4_attn_decode(cache: KV4Cache, q, q_pos, k_new, v_new, window: int, n_sink: int, scale: float, out, lse, flags: int,
                        workspace, status=None, stream=None) -> None:
     """As si_attn_decode."""
-    _decode(_lib.si_kv4_attn_decode, "si_kv4_attn_decode", cache, q, q_pos, k_new, v_new, window, n_sink, scale, out, lse, flags, workspace, status, stream)
+    _, hq, _ = shape = q.shape
+    kp = vp = None
+    new_stride = 0
+    if k_new is not None or v_new is not None:
+        if k_new is None or v_new is None or k_new.stride() != v_new.stride():
+            raise ValueError("k_new and v_new: [n_seqs, n_kv_heads, head_dim] of equal strides, both or neither")
+        kp, vp = _heads(k_new, "k_new", cache, cache.n_kv_heads), _heads(v_new, "v_new", cache, cache.n_kv_heads)
+        new_stride = k_new.stride(0)
+    ws, ws_bytes = _ws(workspace, cache)
+    _check(_lib.si_kv4_attn_decode(cache.ref, _heads(q, "q", cache, hq), q.stride(0), hq, _ptr(q_pos, "q_pos", cache, (cache.n_seqs,), torch.int32),
+                                   kp, vp, new_stride, window, n_sink, scale, _ptr(out, "out", cache, shape, q.dtype),
+                                   _ptr(lse, "lse", cache, shape[:2], torch.float32), flags, ws, ws_bytes,
+                                   _ptr(status, "status", cache, (1,), torch.int32), _on(stream, cache)), "si_kv4_attn_decode")
 
 
 def si_kv4_evict(src: KV4Cache, dst: KV4Cache, q_pos, n_new: int, budget: int, n_sink: int, n_recent: int, kept, len_out,
                  workspace, status=None, stream=None) -> None:
     """As si_kv_evict."""
-    _evict(_lib.si_kv4_evict, "si_kv4_evict", src, dst, q_pos, n_new, budget, n_sink, n_recent, kept, len_out, workspace, status, stream)
+    _one_device(src, dst)
+    seqs = (src.n_seqs,)
+    ws, ws_bytes = _ws(workspace, src)
+    _check(_lib.si_kv4_evict(src.ref, dst.ref, _ptr(q_pos, "q_pos", src, seqs, torch.int32), n_new, budget, n_sink, n_recent,
+                             _ptr(kept, "kept", src, (src.n_seqs, src.n_kv_heads, budget), torch.int32),
+                             _ptr(len_out, "len_out", src, seqs, torch.int32), ws, ws_bytes,
+                             _ptr(status, "status", src, (1,), torch.int32), _on(stream, src)), "si_kv4_evict")
 
 
 # ------------------------------------------------------------------------- owner object

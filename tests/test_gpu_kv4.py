@@ -249,6 +249,41 @@ def test_decode(api, B, lens, Hq, Hkv, window, n_sink, given, new, D, group, dty
     _decode_case(api, made, B, lens, Hq, Hkv, window, n_sink, given, new, acc, 1.0 / math.sqrt(D))
 
 
+@pytest.mark.parametrize("B,Hq,Hkv,D,group,dtype,given", [(300, 4, 2, 64, 32, "bf16", False), (260, 12, 1, 128, 64, "f16", False), (140, 6, 1, 64, 64, "bf16", True)])
+def test_decode_of_many_short_sequences(api, B, Hq, Hkv, D, group, dtype, given):
+    """More sequences than a CTA has threads, empty ones among them; twelve and six query heads to a key head."""
+    lens = [(37 * b) % 71 if b % 5 else 0 for b in range(B)]
+    made = k4.Made(api, B, Hkv, D, 96, group, dtype, lens, seed=B)
+    _decode_case(api, made, B, lens, Hq, Hkv, 0 if given else 20, 2, given, True, True, 0.1, seed=B)
+    made = k4.Made(api, B, Hkv, D, 96, group, dtype, lens, seed=B + 1)
+    _decode_case(api, made, B, lens, Hq, Hkv, 0, 0, False, False, True, 0.1, seed=B)
+
+
+@pytest.mark.parametrize("Hq,Hkv,window,n_sink", [(16, 1, 1, 0), (12, 1, 500, 700), (3, 1, 33, 1), (2, 2, 64, 64)])
+def test_decode_at_the_edges_of_windows(api, Hq, Hkv, window, n_sink):
+    """A window of one entry, more first positions than entries, windows that end inside a tile and on its boundary."""
+    for D, group, dtype in ((128, 32, "f16"), (64, 64, "bf16")):
+        lens = [639, 640, 641, 33]
+        made = k4.Made(api, 4, Hkv, D, 672, group, dtype, lens, seed=window)
+        _decode_case(api, made, 4, lens, Hq, Hkv, window, n_sink, False, True, True, 0.1)
+
+
+def test_a_query_before_every_entry_sees_nothing(api):
+    made = k4.Made(api, 2, 2, 64, 64, 32, "bf16", [40, 3], seed=1)
+    q, kn, vn = (torch.randn(2, h, 64, device="cuda").to(torch.bfloat16) for h in (4, 2, 2))
+    out, lse = torch.full_like(q, 7.0), torch.full((2, 4), 7.0, device="cuda")
+    weight = torch.full((2, 2, 64), 0.5, device="cuda")
+    cache = api.KV4Cache(made.cache.data, 64, 32, made.dt, made.length, None, weight)
+    api.si_kv4_attn_decode(cache, q, torch.tensor([-1, -5], **I32), kn, vn, 0, 0, 0.1, out, lse, api.SI_FLAG_ACC_WEIGHT, cache.workspace(4))
+    assert (out == 0).all() and torch.isneginf(lse).all()
+    for b, n in enumerate([40, 3]):
+        made.set(b, n, kn[b], vn[b])
+        assert (weight[b, :, n] == 0).all() and (weight[b, :, :n] == 0.5).all() and (weight[b, :, n + 1:] == 0.5).all()
+    for x, y in zip(made.read(torch.tensor([41, 4], **I32)), (made.kq, made.vq)):
+        for b, n in enumerate([41, 4]):
+            assert same(x[b, :, :n], ko.read_back(*y, "bf16")[b, :, :n])
+
+
 @pytest.mark.parametrize("dtype,scale,spread", [("bf16", 2.0, 4.0), ("f16", -0.7, 3.0), ("bf16", 1e-3, 2.0 ** -40), ("f16", 0.1, 2.0 ** -12), ("bf16", 2.0 ** -40, 2.0 ** 40), ("f16", 1.0, 0.0)])
 def test_decode_with_scores_far_apart_and_queries_of_any_size(api, dtype, scale, spread):
     """Maxima that keep growing, a negative scale, queries far below and above one, all of them zero."""

@@ -1,9 +1,9 @@
 // The key/value cache in 4 bits: quantising entries as they are stored, reading them back, eviction.  (Layout and format: si_kv4.cuh.)
 //
 // All three are bound by HBM: an entry is 4 D bytes in 16 bits and D + 8 D / group in 4.  Measured: 65000 entries of eight heads of 128 read
-// back in 58 us (6.0 TB/s of the two sides together); a prompt of 8192 tokens stored in 12 us (3.6 TB/s; 150 instructions for
-// the eight values of a lane and two rows keep the issue slots two thirds busy); 2048 of 16384 entries of 128 heads moved in 24 us (a
-// value's cell holds its neighbour too, so 256 bytes are read for 160).
+// back in 58 us (6.0 TB/s of the two sides together); a prompt of 8192 tokens stored in 9 us (4.9 TB/s; the issue slots are two
+// thirds busy, half of it the codes); 2048 of 16384 entries of 128 heads moved in 21 us (a value's cell holds its neighbour too, so
+// 256 bytes are read for 160).
 #include <type_traits>
 
 #include "si_evict.cuh"
@@ -43,7 +43,8 @@ struct StoreArgs {
 // A warp per eight entries, everything it reads asked for at once: 16-byte pieces of rows, eight elements a lane, which make one word
 // of a key's codes and two half words of a value's (the two entries of a pair exchange a half each).  A warp's words of a store are
 // 128 contiguous bytes, in the tile's order.  (A warp per tile, with the tile put together in shared memory, has a quarter of the
-// loads in flight: 8192 tokens of eight heads 20 us instead of 12.)
+// loads in flight: 8192 tokens of eight heads 20 us instead of 12; 9 since the steps of the eight groups that a lane takes part in
+// are dealt to the groups' lanes.)
 template <int DT, int D, int NG>
 __global__ void __launch_bounds__(kThreads) store_kernel(const StoreArgs A) {
     using T = si_tile4<D, NG>;
@@ -203,7 +204,8 @@ __global__ void __launch_bounds__(kThreads) load_kernel(const LoadArgs A) {
     if (A.meta.weight && A.dst.weight) A.dst.weight[A.dst.meta(b, h) + e - first] = A.meta.weight[A.meta.meta(b, h) + e];
 }
 
-// The kept entries to their slots; nothing to do for an entry that stays.  Sixteen lanes per pair of slots, kMovePairs pairs in flight:
+// The kept entries to their slots; nothing to do for an entry that stays.  Sixteen lanes per pair of slots, kMovePairs pairs in flight
+// (one, two, three, four: 64.9, 65.2, 66.2, 67.6 us for 2048 of 16384 entries of 128 heads with selection and read-back):
 // eight lanes have the values' cells of both sources (which hold a neighbour each) and put the two halves together, eight the
 // two keys, and of these four the steps and four positions and weights.
 constexpr int kMovePairs = 2;

@@ -2,10 +2,8 @@
 //
 // All three are bound by HBM: an entry is 4 D bytes in 16 bits and D + 8 D / group in 4.  Measured: 65000 entries of eight heads of 128 read
 // back in 58 us (6.0 TB/s of the two sides together); a prompt of 8192 tokens stored in 9 us (4.9 TB/s; the issue slots are two
-// thirds busy, half of it the codes); 2048 of 16384 entries of 128 heads moved in 21 us (a value's cell holds its neighbour too, so
+// thirds busy, half of it the codes); 2048 of 16384 entries of 128 heads moved in 19 us (a value's cell holds its neighbour too, so
 // 256 bytes are read for 160).
-#include <type_traits>
-
 #include "si_evict.cuh"
 #include "si_tc.cuh"
 
@@ -204,86 +202,76 @@ __global__ void __launch_bounds__(kThreads) load_kernel(const LoadArgs A) {
     if (A.meta.weight && A.dst.weight) A.dst.weight[A.dst.meta(b, h) + e - first] = A.meta.weight[A.meta.meta(b, h) + e];
 }
 
-// The kept entries to their slots; nothing to do for an entry that stays.  Sixteen lanes per pair of slots, kMovePairs pairs in flight
-// (one, two, three, four: 64.9, 65.2, 66.2, 67.6 us for 2048 of 16384 entries of 128 heads with selection and read-back):
-// eight lanes have the values' cells of both sources (which hold a neighbour each) and put the two halves together, eight the
-// two keys, and of these four the steps and four positions and weights.
-constexpr int kMovePairs = 2;
+// The kept entries to their slots; nothing to do for an entry that stays.  A warp per sixteen slots, everything asked for before anything is
+// written: eight lanes have the values' cells of both sources of a pair of slots (which hold a neighbour each) and put the two halves
+// together, four the cells of a key, two the steps of an entry, two its position and weight.  (Sixteen lanes per pair with these
+// roles side by side: a warp's lanes part ways, 21 us instead of 19 for 2048 of 16384 entries of 128 heads.)
+constexpr int kMoveSlots = 16;                // of a warp
 template <int D, int NG>
 __global__ void __launch_bounds__(256) move4_kernel(const EvictArgs A) {
     using T = si_tile4<D, NG>;
-    constexpr int W = T::W, kGroups = 256 / 16;
-    const int h = blockIdx.x % A.src.H, b = blockIdx.z, row = b * A.src.H + h, lane = threadIdx.x % 16, group = threadIdx.x / 16;
-    const long long block = blockIdx.x / A.src.H;
+    constexpr int W = T::W;
+    const int h = blockIdx.x % A.src.H, b = blockIdx.z, lane = threadIdx.x % 32;
+    const long long row = (long long)b * A.src.H + h, s0 = ((long long)(blockIdx.x / A.src.H) * 8 + threadIdx.x / 32) * kMoveSlots;
     si_tc::pdl_wait();
     si_tc::pdl_launch();
     if (blockIdx.x == 0 && threadIdx.x == 0 && A.len_out) A.len_out[b] = min(si_evict_entries(A, b), A.budget);
+    if (s0 >= A.slots) return;
+    int mine = -1;                            // the source of slot s0 + lane
+    if (lane < kMoveSlots && s0 + lane < A.slots) mine = A.source[row * A.slots + s0 + lane];
+    if (A.in_place && mine == s0 + lane) mine = -1;
+    if (!__any_sync(0xFFFFFFFFu, mine >= 0)) return;
     const uint8_t *src = A.src4.row(b, h);
-    uint8_t *dst = A.dst4.row(b, h);
-    const int half = lane >> 2 & 1;                        // lanes 8 .. 15: the key of which slot; of the second round: the slot is lane % 2
-    int from[kMovePairs][2];
+    uint8_t *dst = A.dst4.row(b, h) + s0 / kTileEntries * T::kBytes;             // sixteen slots lie in one tile
+    const int r0 = (int)(s0 % kTileEntries);
+    auto from = [&](int slot) { return __shfl_sync(0xFFFFFFFFu, mine, slot); };
+    auto tile_of = [&](int j) { return src + (long long)(j / kTileEntries) * T::kBytes; };
+    auto load = [](auto &to, const uint8_t *at) {
+        constexpr int N = sizeof(to) / 4;
+        if constexpr (N == 4) { const uint4 v = __ldcs(reinterpret_cast<const uint4 *>(at)); to[0] = v.x; to[1] = v.y; to[2] = v.z; to[3] = v.w; }
+        else if constexpr (N == 2) { const uint2 v = __ldcs(reinterpret_cast<const uint2 *>(at)); to[0] = v.x; to[1] = v.y; }
+        else to[0] = __ldcs(reinterpret_cast<const uint32_t *>(at));
+    };
+    auto store = [](uint8_t *at, const auto &x) {
+        constexpr int N = sizeof(x) / 4;
+        if constexpr (N == 4) *reinterpret_cast<uint4 *>(at) = make_uint4(x[0], x[1], x[2], x[3]);
+        else if constexpr (N == 2) *reinterpret_cast<uint2 *>(at) = make_uint2(x[0], x[1]);
+        else *reinterpret_cast<uint32_t *>(at) = x[0];
+    };
+    uint32_t even[2][W], odd[2][W], key[2][W], step[NG], word = 0;
+    int v0[2], v1[2], k0[2];
 #pragma unroll
-    for (int k = 0; k < kMovePairs; ++k)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const long long slot = ((block * kMovePairs + k) * kGroups + group) * 2 + i;
-            from[k][i] = slot < A.slots ? A.source[(size_t)row * A.slots + slot] : -1;
-            if (A.in_place && from[k][i] == slot) from[k][i] = -1;
-        }
-    auto tile_at = [](int j) { return (long long)(j / kTileEntries) * T::kBytes; };
-    uint32_t one[kMovePairs][W], two[kMovePairs][W > NG ? W : NG];
-#pragma unroll
-    for (int k = 0; k < kMovePairs; ++k) {
-        auto words = [&](auto &to, auto n, const uint8_t *at) {
-            constexpr int N = decltype(n)::value;
-            if constexpr (N == 4) { const uint4 v = __ldcs(reinterpret_cast<const uint4 *>(at)); to[0] = v.x; to[1] = v.y; to[2] = v.z; to[3] = v.w; }
-            else if constexpr (N == 2) { const uint2 v = __ldcs(reinterpret_cast<const uint2 *>(at)); to[0] = v.x; to[1] = v.y; }
-            else to[0] = __ldcs(reinterpret_cast<const uint32_t *>(at));
-        };
-        if (lane < 8) {
-            if (from[k][0] >= 0) words(one[k], std::integral_constant<int, W>(), src + tile_at(from[k][0]) + T::value_word(from[k][0] % kTileEntries, 0, lane));
-            if (from[k][1] >= 0) words(two[k], std::integral_constant<int, W>(), src + tile_at(from[k][1]) + T::value_word(from[k][1] % kTileEntries, 0, lane));
-        } else {
-            const int j = half ? from[k][1] : from[k][0], i = lane & 1 ? from[k][1] : from[k][0];
-            if (j >= 0) words(one[k], std::integral_constant<int, W>(), src + tile_at(j) + T::key_word(j % kTileEntries, 0, lane & 3));
-            if (i >= 0) {
-                if (lane < 12) words(two[k], std::integral_constant<int, NG>(), src + tile_at(i) + (lane & 2 ? T::kValuePar : T::kKeyPar) + i % kTileEntries * NG * 4);
-                else if (lane & 2) two[k][0] = __float_as_uint(A.src.weight[A.src.meta(b, h) + i]);
-                else two[k][0] = A.src.pos ? A.src.pos[A.src.meta(b, h) + i] : i;
-            }
-        }
+    for (int i = 0; i < 2; ++i) {
+        const int pair = i * 4 + lane / 8;
+        v0[i] = from(2 * pair); v1[i] = from(2 * pair + 1); k0[i] = from(i * 8 + lane / 4);
+        if (v0[i] >= 0) load(even[i], tile_of(v0[i]) + T::value_word(v0[i] % kTileEntries, 0, lane % 8));
+        if (v1[i] >= 0) load(odd[i], tile_of(v1[i]) + T::value_word(v1[i] % kTileEntries, 0, lane % 8));
+        if (k0[i] >= 0) load(key[i], tile_of(k0[i]) + T::key_word(k0[i] % kTileEntries, 0, lane % 4));
+    }
+    const int p0 = from(lane / 2), m0 = from(lane % 16), par = lane & 1 ? T::kValuePar : T::kKeyPar;
+    if (p0 >= 0) load(step, tile_of(p0) + par + p0 % kTileEntries * NG * 4);
+    if (m0 >= 0) {
+        if (lane >= 16) word = __float_as_uint(A.src.weight[A.src.meta(b, h) + m0]);
+        else word = A.src.pos ? A.src.pos[A.src.meta(b, h) + m0] : m0;
     }
 #pragma unroll
-    for (int k = 0; k < kMovePairs; ++k) {
-        const long long s0 = ((block * kMovePairs + k) * kGroups + group) * 2;
-        auto put = [&](uint8_t *at, const auto &x, auto n) {
-            constexpr int N = decltype(n)::value;
-            if constexpr (N == 4) *reinterpret_cast<uint4 *>(at) = make_uint4(x[0], x[1], x[2], x[3]);
-            else if constexpr (N == 2) *reinterpret_cast<uint2 *>(at) = make_uint2(x[0], x[1]);
-            else *reinterpret_cast<uint32_t *>(at) = x[0];
-        };
-        if (from[k][0] < 0 && from[k][1] < 0) continue;
-        uint8_t *to = dst + tile_at((int)s0);
-        const int r = (int)(s0 % kTileEntries);
-        if (lane < 8) {
-            uint8_t *at = to + T::value_word(r, 0, lane);
-            uint32_t y[W];
+    for (int i = 0; i < 2; ++i) {
+        uint8_t *at = dst + T::value_word(r0 + 2 * (i * 4 + lane / 8), 0, lane % 8);
+        uint32_t both[W];
 #pragma unroll
-            for (int i = 0; i < W; ++i)          // the source's half into the slot's
-                y[i] = (from[k][0] & 1 ? one[k][i] >> 16 : one[k][i] & 0xFFFFu) | (from[k][1] & 1 ? two[k][i] & 0xFFFF0000u : two[k][i] << 16);
-            if (from[k][0] >= 0 && from[k][1] >= 0) put(at, y, std::integral_constant<int, W>());
-            else
+        for (int w = 0; w < W; ++w)            // the source's half into the slot's
+            both[w] = (v0[i] & 1 ? even[i][w] >> 16 : even[i][w] & 0xFFFFu) | (v1[i] & 1 ? odd[i][w] & 0xFFFF0000u : odd[i][w] << 16);
+        if (v0[i] >= 0 && v1[i] >= 0) store(at, both);
+        else if (v0[i] >= 0 || v1[i] >= 0)
 #pragma unroll
-                for (int i = 0; i < W; ++i) reinterpret_cast<uint16_t *>(at)[2 * i + (from[k][0] < 0)] = (uint16_t)(from[k][0] < 0 ? y[i] >> 16 : y[i]);
-        } else {
-            const int j = half ? from[k][1] : from[k][0], i = lane & 1 ? from[k][1] : from[k][0];
-            if (j >= 0) put(to + T::key_word(r + half, 0, lane & 3), one[k], std::integral_constant<int, W>());
-            if (i >= 0) {
-                if (lane < 12) put(to + (lane & 2 ? T::kValuePar : T::kKeyPar) + (r + (lane & 1)) * NG * 4, two[k], std::integral_constant<int, NG>());
-                else if (lane & 2) A.dst.weight[A.dst.meta(b, h) + s0 + (lane & 1)] = __uint_as_float(two[k][0]);
-                else A.dst.pos[A.dst.meta(b, h) + s0 + (lane & 1)] = (int)two[k][0];
-            }
-        }
+            for (int w = 0; w < W; ++w) reinterpret_cast<uint16_t *>(at)[2 * w + (v0[i] < 0)] = (uint16_t)(v0[i] < 0 ? both[w] >> 16 : both[w]);
+        if (k0[i] >= 0) store(dst + T::key_word(r0 + i * 8 + lane / 4, 0, lane % 4), key[i]);
+    }
+    if (p0 >= 0) store(dst + par + (r0 + lane / 2) * NG * 4, step);
+    if (m0 >= 0) {
+        const long long to = A.dst.meta(b, h) + s0 + lane % 16;
+        if (lane >= 16) A.dst.weight[to] = __uint_as_float(word);
+        else A.dst.pos[to] = (int)word;
     }
 }
 
@@ -402,7 +390,7 @@ extern "C" int si_kv4_evict(const si_kv4_t *src, const si_kv4_t *dst, const int3
     si_mt_forget();
     if ((rc = si_evict_select(A, (cudaStream_t)stream)) || A.move_here) return rc;
     cudaLaunchAttribute at;
-    constexpr int kPerBlock = 256 / 16 * 2 * kMovePairs;
+    constexpr int kPerBlock = 8 * kMoveSlots;
     const long long blocks = ((long long)A.slots + kPerBlock - 1) / kPerBlock * src->n_kv_heads;
     cudaLaunchConfig_t cfg = config(dim3((unsigned)blocks, 1, src->n_seqs), 256, (cudaStream_t)stream, &at);
     return by_shape<Move>(src->dtype, src->head_dim, A.groups, &cfg, &A);

@@ -90,7 +90,7 @@ enum {
                                      persistent bulk-copy kernel (kept for cross-checking) */
     SI_FLAG_PRENORM = 512u,      /* si_decode_chain_forward: the FFN sees its input scaled to unit root mean
                                     square, as the FFN of a pre-norm transformer block does */
-    SI_FLAG_ACC_WEIGHT = 1024u   /* si_attn_decode: add the attention every entry receives to kv->weight */
+    SI_FLAG_ACC_WEIGHT = 1024u   /* si_attn_decode, si_kv4_attn_decode: add the attention every entry receives to kv->weight */
 };
 
 /* selection modes for si_select */
@@ -568,7 +568,8 @@ int si_kv4_store(const si_kv_t *src, const si_kv4_t *dst, const int32_t *first_p
 
 /* Read entries back to 16 bits: entries first[b] .. min(src->len[b], first[b] + n) - 1 of src (first: device int32 [n_seqs], NULL: 0;
  * a negative one is SI_ERR_OUT_OF_RANGE and taken as 0) become entries 0, 1, .. of the 16-bit cache dst, rounded once to dtype (f16: at most its
- * largest number, since s was rounded up), with their pos and weight where both sides have them.  dst->len is not read; other rows of dst stay as they were.  n <= dst->capacity.
+ * largest number, since s was rounded up), with their pos and weight where both sides have them.  dst->len is not read; other
+ * rows of dst stay as they were.  n <= dst->capacity.
  *   len_out      device int32 [n_seqs] or NULL: entries read back; may be dst->len
  * This is how the next chunk of a prompt is prefilled on such a cache: into a scratch cache, the chunk's own keys and values
  * behind, si_attn_prefill. */
@@ -577,7 +578,8 @@ int si_kv4_load(const si_kv4_t *src, const si_kv_t *dst, const int32_t *first, i
 
 /* si_attn_decode on a cache in 4 bits; all arguments as there.  A new entry is quantised, stored, and attended to as it is stored.  The
  * stored values are not rounded in between: out is the attention over m + s * c.  Scores, softmax and sums are fp32; p * s is
- * rounded to 11 bits for the product with the codes; out has the cache's type.  A query that holds a NaN or an infinity has NaN as result. */
+ * rounded to 11 bits for the product with the codes (fewer where all steps of the values are below 2^-110: bf16 values below some
+ * 1e-32); out has the cache's type.  A query that holds a NaN or an infinity has NaN as result. */
 int si_kv4_attn_decode(const si_kv4_t *kv, const void *q, long long q_seq_stride, int n_q_heads, const int32_t *q_pos,
                        const void *k_new, const void *v_new, long long new_seq_stride, int window, int n_sink, float scale,
                        void *out, float *lse, unsigned flags, void *workspace, size_t ws_bytes, int32_t *status_dev, void *stream);

@@ -580,14 +580,17 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
                         }
             }
             if (!__any_sync(0xFFFFFFFFu, grow)) return;
-            uint32_t low16 = 0;
+            // groups that are NaN (no other step's word is as large) do not count: they would drive all others' p s out of f16
+            constexpr uint32_t kNotFinite = DT == SI_BF16 ? 0x7F800000u : 0x7C000000u;
+            uint32_t step16 = 0, low16 = 0;
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int r = 0; r < 2; ++r)
 #pragma unroll
-                    for (int g = 0; g < L; ++g) low16 = max(low16, vp[u][r][g] & 0x7FFFu);
-            const uint32_t step = __reduce_max_sync(0xFFFFFFFFu, top) >> 16, size = __reduce_max_sync(0xFFFFFFFFu, low16);
+                    for (int g = 0; g < L; ++g)
+                        if (vp[u][r][g] < kNotFinite) { step16 = max(step16, vp[u][r][g]); low16 = max(low16, vp[u][r][g] & 0x7FFFu); }
+            const uint32_t step = __reduce_max_sync(0xFFFFFFFFu, step16) >> 16, size = __reduce_max_sync(0xFFFFFFFFu, low16);
             // above every step, and p m stays in fp32
             E = max(E, min(max(max(exponent(si_cvt<DT>::lo(step)) + 1, exponent(si_cvt<DT>::lo(size)) - 9), kLowE), kHighE));
             most = (uint32_t)(DT == SI_BF16 ? (E + 127) << 7 : (E + 15) << 10) << 16 | 0xFFFFu;

@@ -1,0 +1,113 @@
+"""Single-token attention over the cache in 4 bits where the values' steps differ by many orders of magnitude: between the groups of
+an entry, between entries that matter and entries that do not, from one tile to the next, beside NaN.
+
+Bounds (e = 2^-24, u the unit roundoff of the type; p softmax weights, s c the step and code of value j, m its lowest value), per
+query head and channel, the channel's own group only:
+  p s      rounded to 11 bits for the products with codes shifted to -8 .. 7: 8 * 2^-11 sum_j p_j s_j.  The scale that f16 is given follows the
+           largest p s of the head and group and holds it above 2^7, so below 2^-14 a rounding is 2^-25 at most, 2^-32 of the largest: 8 n 2^-32 max_j p_j s_j
+  sums     (2 delta + (n + 32) e) sum_j p_j (|m_j| + 16 s_j): partial sums hold the codes without the shift
+  weights  below 2^-110 of the largest count as 0: 2^-108 sum_j (|m_j| + 16 s_j)
+  result   u |out|, f16 2^-25
+delta and the bounds of lse and of the weights as in kv4_utils."""
+import numpy as np
+import pytest
+import torch
+
+from tests import attn_utils as au
+from tests import kv4_utils as k4
+
+pytestmark = pytest.mark.gpu
+I32 = dict(dtype=torch.int32, device="cuda")
+E = au.E
+
+# head_dim, group, query heads per key head: every way of laying heads and groups out in the matrix products
+FORMS = [(128, 32, 4), (128, 64, 3), (64, 32, 4), (64, 64, 4), (128, 32, 8), (128, 64, 6), (64, 32, 5), (128, 32, 16), (128, 64, 9), (64, 64, 12), (64, 32, 20)]
+
+
+@pytest.fixture(scope="module")
+def api():
+    from paper_2607_18081_b200 import api as _api
+    return _api
+
+
+def statement(made, q, n, scale):
+    """float64: results of the first n entries of sequence 0 for queries q [Hq, D], and what the bounds need."""
+    qn, H = au.f64(q), made.k.shape[1]
+    G = len(qn) // H
+    k = made.values("k")
+    (km, ks, kc), (vm, vs, vc) = made.kq, made.vq
+    r = {x: [] for x in ("out", "ps", "peak", "reach", "all", "lse", "size", "p")}
+    with np.errstate(invalid="ignore", over="ignore"):
+        for hq in range(len(qn)):
+            h = hq // G
+            x = k[0, h, :n] @ qn[hq] * scale
+            p = np.exp(x - x.max())
+            r["lse"].append(x.max() + np.log(p.sum()))
+            r["size"].append(((np.abs(km[0, h, :n]) + ks[0, h, :n] * kc[0, h, :n]) @ np.abs(qn[hq])).max() * abs(scale))
+            p /= p.sum()
+            m, s, c = vm[0, h, :n], vs[0, h, :n], vc[0, h, :n]
+            r["p"].append(p)
+            r["out"].append(p @ (m + s * c))
+            r["ps"].append(p @ s)
+            r["peak"].append((p[:, None] * s).max(0))
+            r["reach"].append(p @ (np.abs(m) + 16 * s))
+            r["all"].append((np.abs(m) + 16 * s).sum(0))
+    return {x: np.array(y) for x, y in r.items()} | {"n": n}
+
+
+def attend(api, made, q, n, scale, rows):
+    """q [Hq, D] over sequence 0, `rows` times as sequences that share its memory: out [rows, Hq, D], lse, weights [rows, H, cap]."""
+    c, Hq = made.cache, len(q)
+    cache = api.KV4Cache(c.data[:1].expand(rows, -1, -1, -1), made.D, made.group, made.dt, torch.full((rows,), n, **I32), None,
+                         torch.zeros(rows, c.n_kv_heads, c.capacity, device="cuda"))
+    out, lse = torch.full((rows, Hq, made.D), 7.0, dtype=made.dt, device="cuda"), torch.full((rows, Hq), 7.0, device="cuda")
+    status, ws = torch.zeros(1, **I32), cache.workspace(Hq)
+    ws.fill_(0xFF)
+    api.si_kv4_attn_decode(cache, q.expand(rows, -1, -1).contiguous(), None, None, None, 0, 0, scale, out, lse, api.SI_FLAG_ACC_WEIGHT, ws, status)
+    assert status.item() == 0
+    return out, lse, cache.weight
+
+
+def check(made, got, ref):
+    """Every row against the statement; NaN exactly where the statement has it."""
+    out, lse, weight = (au.f64(x) for x in got)
+    n, H = ref["n"], weight.shape[1]
+    d = (2 * made.D + 16) * E * ref["size"] + E * (4 * (np.abs(ref["lse"]) + ref["size"]) + 128)
+    rel = (2 * d + (n + 32) * E)[:, None]
+    bound = 1.01 * (au.U[made.dtype] * np.abs(ref["out"]) + 8 * 2.0 ** -11 * ref["ps"] + 8 * n * 2.0 ** -32 * ref["peak"] + rel * ref["reach"] + 2.0 ** -108 * ref["all"])
+    bound = bound + (2.0 ** -25 if made.dtype == "f16" else 0.0)
+    nan = np.isnan(ref["out"])
+    assert np.array_equal(np.isnan(out), np.broadcast_to(nan, out.shape))
+    err = np.where(nan, 0.0, np.abs(out - ref["out"]))
+    bound = np.where(nan, 1.0, bound)
+    assert np.all(err <= bound), f"out: {np.max(err / np.maximum(bound, 1e-300)):.3f} of the bound"
+    bound = d + 4 * E * (np.abs(ref["lse"]) + 128) + n * E
+    assert np.all(np.abs(lse - ref["lse"]) <= bound), np.max(np.abs(lse - ref["lse"]) / bound)
+    want = ref["p"].reshape(H, -1, n).sum(1)
+    bound = (4 * d.max() + (n + len(d) // H + 16) * E) * want + 2 * E * want + 1e-30
+    assert np.all(np.abs(weight[:, :, :n] - want) <= bound) and (weight[:, :, n:] == 0).all()
+
+
+def case(api, D, group, G, dtype, v, k=None, q=None, n=1000, scale=0.1, seed=0, H=2):
+    g = torch.Generator().manual_seed(seed + G)
+    cap = (n + 31) // 32 * 32
+    k = torch.randn(1, H, cap, D, generator=g) * 0.3 if k is None else k
+    made = k4.Made(api, 1, H, D, cap, group, dtype, [n], k=k, v=v)
+    q = (torch.randn(G * H, D, generator=g) if q is None else q).to(made.dt).cuda()
+    ref = statement(made, q, n, scale)
+    for rows in (1, 400):                     # a run of tiles per warp: one or two tiles of one item, and many
+        check(made, attend(api, made, q, n, scale, rows), ref)
+
+
+def noise(D, n=1000, H=2, seed=1):
+    return torch.randn(1, H, (n + 31) // 32 * 32, D, generator=torch.Generator().manual_seed(seed))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("D,group,G", FORMS)
+def test_nan_and_infinity_stay_in_their_group(api, D, group, G, dtype):
+    """One group of one value, in the first tile or a later one: the other groups' results are what they are without it."""
+    for at, special in ((3, float("inf")), (700, float("nan")), (999, float("-inf"))):
+        v = noise(D)
+        v[0, 1, at, D - 5] = special
+        case(api, D, group, G, dtype, v)

@@ -11,8 +11,9 @@
 // m16n8k16 operands as they lie there.
 //   - q enters as f16, scaled per head by the power of two that brings its largest element to 2^14 .. 2^15 (exact but for elements below
 //     2^-31 of it).
-//   - p enters as f16(p s) relative to a base 2^(m + E - 6): m the running maximum of the scores, 2^E above all steps so far.  So p s is
-//     below 2^14 and the largest of all is around 2^5, far from both ends of f16: rounded to 11 bits for every type.
+//   - p is relative to 2^(m + 12), m the running maximum of the scores: whatever the values are, its sum and the weights do not depend
+//     on them, and 2^12 below 1 it leaves room for sums of p times the largest bf16 numbers.  It enters as f16(p s 2^(18 - E)), 2^E above all
+//     steps so far.
 // Everything else is fp32.
 //
 // D + 8 D / group bytes per entry, key head (and 16 query heads) have to come from HBM, a third of what 16 bits take, and that is no
@@ -34,6 +35,7 @@ namespace {
 constexpr int kWarps = 4, kThreads = kWarps * 32;
 template <int H> constexpr int kPerSmOf = H == 16 ? 2 : 3;
 template <int H> constexpr int kStagesOf = H == 16 ? 4 : 3;
+constexpr int kRoom = 12;              // p is at most 2^-12, but for scores that have not moved the maximum yet
 constexpr int kPad = 3;                // an item's start and end take about as long as so many tiles (0: 47.7 us for 512 windows of 2052, 3: 41.7, 8: 44.4)
 // Units of a run: fewer would leave more parts than they save time (24 x 2 caches of 2049 entries and their eviction: two 28.7 us a
 // step, four 27.3), but with little work the SMs come first (one cache of 1001, 8 heads: two 17.9, four 18.6).
@@ -236,7 +238,7 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
     constexpr int L = PAIR ? NG / 2 : NG, GW = W / NG;      // groups of a lane (H = 4: the even or the odd ones), words of a group
     using C = Cfg<D, NG, H>;
     constexpr int kStages = kStagesOf<H>;
-    constexpr int kLowE = DT == SI_BF16 ? -90 : -14, kHighE = DT == SI_BF16 ? 90 : 16;
+    constexpr int kLowE = DT == SI_BF16 ? -90 : -14, kHighE = DT == SI_BF16 ? 92 : 16;
     const DecodeArgs &A = A4.d;
     extern __shared__ __align__(128) char smem[];
     __shared__ int sh_scan[kThreads / 32 + 1];
@@ -352,7 +354,8 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
         float o[NT][2 * W][4] = {}, low[NT][L][2] = {};
         // the maximum and the score that moves it, both without the factor `back`; base: what p is relative to, 0 while there is none
         float m[NT][2], edge[NT][2], base[NT][2], l[NT][2];
-        int E = -1000;
+        int E = kLowE;
+        float up = pow2(kRoom + 6 - kLowE);                // what p s is scaled with for f16
         uint32_t most = 0;                                 // 2^E in the place of a step: no word of a value so far is above
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) { m[nt][0] = m[nt][1] = edge[nt][0] = edge[nt][1] = -INFINITY; base[nt][0] = base[nt][1] = l[nt][0] = l[nt][1] = 0.f; }
@@ -467,7 +470,7 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
 #pragma unroll
                         for (int r = 0; r < 2; ++r) {
                             const float s = si_cvt<DT>::hi(vp[u][r][g]), mn = fmaf(8.f, s, si_cvt<DT>::lo(vp[u][r][g]));
-                            pf[u][nt][g][r] = transposed(pack2<SI_F16>(p[2 * r] * s, p[2 * r + 1] * s));
+                            pf[u][nt][g][r] = transposed(pack2<SI_F16>(p[2 * r] * s * up, p[2 * r + 1] * s * up));
                             low[nt][g][0] = fmaf(p[2 * r], mn, low[nt][g][0]);
                             low[nt][g][1] = fmaf(p[2 * r + 1], mn, low[nt][g][1]);
                         }
@@ -582,17 +585,18 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
             if (!__any_sync(0xFFFFFFFFu, grow)) return;
             // groups that are NaN (no other step's word is as large) do not count: they would drive all others' p s out of f16
             constexpr uint32_t kNotFinite = DT == SI_BF16 ? 0x7F800000u : 0x7C000000u;
-            uint32_t step16 = 0, low16 = 0;
+            uint32_t step16 = 0;
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int r = 0; r < 2; ++r)
 #pragma unroll
                     for (int g = 0; g < L; ++g)
-                        if (vp[u][r][g] < kNotFinite) { step16 = max(step16, vp[u][r][g]); low16 = max(low16, vp[u][r][g] & 0x7FFFu); }
-            const uint32_t step = __reduce_max_sync(0xFFFFFFFFu, step16) >> 16, size = __reduce_max_sync(0xFFFFFFFFu, low16);
-            // above every step, and p m stays in fp32
-            E = max(E, min(max(max(exponent(si_cvt<DT>::lo(step)) + 1, exponent(si_cvt<DT>::lo(size)) - 9), kLowE), kHighE));
+                        if (vp[u][r][g] < kNotFinite) step16 = max(step16, vp[u][r][g]);
+            const int was = E;
+            E = max(E, min(exponent(si_cvt<DT>::lo(__reduce_max_sync(0xFFFFFFFFu, step16) >> 16)) + 1, kHighE));      // above every step
+            up = pow2(kRoom + 6 - E);
+            const float down0 = pow2((was - E) / 2), down1 = pow2(was - E - (was - E) / 2);       // one factor may be below fp32
             most = (uint32_t)(DT == SI_BF16 ? (E + 127) << 7 : (E + 15) << 10) << 16 | 0xFFFFu;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
@@ -605,14 +609,14 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
                     mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 8));
                     mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 16));
                     edge[nt][c] = mx + Q.lazy[nt][c];
-                    const float to = mx == -INFINITY ? 0.f : fmaf(mx, Q.back[nt][c], (float)(E - 6)), f = m[nt][c] == -INFINITY ? 1.f : ex2(base[nt][c] - to);
+                    const float to = mx == -INFINITY ? 0.f : fmaf(mx, Q.back[nt][c], (float)kRoom), f = m[nt][c] == -INFINITY ? 1.f : ex2(base[nt][c] - to);
                     m[nt][c] = mx;
                     base[nt][c] = to;
                     l[nt][c] *= f;
 #pragma unroll
                     for (int g = 0; g < L; ++g) low[nt][g][c] *= f;
 #pragma unroll
-                    for (int i = 0; i < 2 * W; ++i) { o[nt][i][c] *= f; o[nt][i][c + 2] *= f; }
+                    for (int i = 0; i < 2 * W; ++i) { o[nt][i][c] *= f * down0; o[nt][i][c] *= down1; o[nt][i][c + 2] *= f * down0; o[nt][i][c + 2] *= down1; }
                 }
         };
         for (; id < seg_end; ++id) {
@@ -642,7 +646,7 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
                     for (int g = 0; g < L; ++g) low[nt][g][c] += __shfl_xor_sync(0xFFFFFFFFu, low[nt][g][c], s);
                 }
                 if (head >= heads) continue;
-                const float sum = l[nt][c], inv = sum == 0.f ? 0.f : 1.f / sum, top = m[nt][c] == -INFINITY ? -INFINITY : base[nt][c];
+                const float f0 = pow2(24 - (kRoom + 6 - E)), f1 = f0 * 0.0625f, sum = l[nt][c], inv = sum == 0.f ? 0.f : 1.f / sum, top = m[nt][c] == -INFINITY ? -INFINITY : base[nt][c];
                 if (lg == 0 && !(PAIR && lt >> 1)) {
                     if (whole) {
                         if (A.lse) A.lse[row + head] = sum == 0.f ? -INFINITY : (base[nt][c] + log2f(sum)) / kLog2e;
@@ -657,7 +661,7 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
                     const int word = PAIR ? i / GW * 2 * GW + i % GW + (lt >> 1) * GW : i;
                     const float mn = low[nt][PAIR ? i / GW : T::place_of(T::group_of(i))][c];
                     auto of = [&](int n) { return PAIR ? (lt >> 1 ? o[nt][(4 * i + n) % (2 * W)][c + 2] : o[nt][(4 * i + n) % (2 * W)][c]) : o[nt][2 * i + n / 2][c + 2 * (n & 1)]; };
-                    const float4 y = make_float4(fmaf(of(0), 0x1p24f, mn), fmaf(of(1), 0x1p20f, mn), fmaf(of(2), 0x1p24f, mn), fmaf(of(3), 0x1p20f, mn));
+                    const float4 y = make_float4(fmaf(of(0), f0, mn), fmaf(of(1), f1, mn), fmaf(of(2), f0, mn), fmaf(of(3), f1, mn));
                     if (whole) *reinterpret_cast<uint2 *>(A.out + (row + head) * D + 32 * word + 4 * lg) = make_uint2(pack2<DT>(y.x * inv, y.y * inv), pack2<DT>(y.z * inv, y.w * inv));
                     else *reinterpret_cast<float4 *>(A.part_o + (slot * HB + head) * D + 32 * word + 4 * lg) = y;
                 }

@@ -111,3 +111,32 @@ def test_nan_and_infinity_stay_in_their_group(api, D, group, G, dtype):
         v = noise(D)
         v[0, 1, at, D - 5] = special
         case(api, D, group, G, dtype, v)
+
+
+FAR = ["apart", "zeros_large", "zeros_constant", "zeros_nan", "constant_small"]
+
+
+@pytest.mark.parametrize("kind", FAR)
+@pytest.mark.parametrize("D,group,G", FORMS)
+def test_steps_that_jump_do_not_touch_the_softmax(api, D, group, G, kind):
+    """bf16 values whose size changes at once by more than fp32 has exponents: with equal scores lse is log n and every weight 1 / n,
+    whatever the values are."""
+    v, n = noise(D), 1000
+    first = torch.arange(v.shape[2])[:, None] < 500
+    one = torch.ones_like(v)
+    v = {"apart": torch.where(first, v * 2.0 ** -70, v * 2.0 ** 70), "zeros_large": torch.where(first, 0.0, v * 2.0 ** 60),
+         "zeros_constant": torch.where(first, 0.0, one * 2.0 ** 100), "zeros_nan": torch.where(first, 0.0, v),
+         "constant_small": torch.where(first, one * 2.0 ** 30, v * 2.0 ** -60)}[kind]
+    if kind == "zeros_nan":
+        v[0, 0, 600, 1], v[0, 1, 999, D - 1] = float("nan"), float("inf")
+    case(api, D, group, G, "bf16", v, n=n)
+    case(api, D, group, G, "bf16", v, k=torch.zeros_like(v), n=n)
+
+
+def test_every_entry_of_a_constant_group_counts(api):
+    """Groups without a step, zeros first: 2^30, and the largest number of bf16."""
+    for top in (2.0 ** 30, 3.3e38):
+        v = torch.zeros(1, 2, 320, 128)
+        v[:, :, 200:] = top
+        case(api, 128, 32, 4, "bf16", v, n=300)
+        case(api, 64, 64, 12, "bf16", v[..., :64].contiguous(), n=300)

@@ -36,6 +36,7 @@ constexpr int kWarps = 4, kThreads = kWarps * 32;
 template <int H> constexpr int kPerSmOf = H == 16 ? 2 : 3;
 template <int H> constexpr int kStagesOf = H == 16 ? 4 : 3;
 constexpr int kRoom = 12;              // p is at most 2^-12, but for scores that have not moved the maximum yet
+constexpr float kOne = 1 << kRoom;
 constexpr int kPad = 3;                // an item's start and end take about as long as so many tiles (0: 47.7 us for 512 windows of 2052, 3: 41.7, 8: 44.4)
 // Units of a run: fewer would leave more parts than they save time (24 x 2 caches of 2049 entries and their eviction: two 28.7 us a
 // step, four 27.3), but with little work the SMs come first (one cache of 1001, 8 heads: two 17.9, four 18.6).
@@ -352,13 +353,14 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
         // H = 4: words k of an even and an odd group, in the halves of four quads, one per element; those of the lane's own groups count.
         // low: sum p (m + 8 s) of this lane's entries
         float o[NT][2 * W][4] = {}, low[NT][L][2] = {};
-        // the maximum and the score that moves it, both without the factor `back`; base: what p is relative to, 0 while there is none
-        float m[NT][2], edge[NT][2], base[NT][2], l[NT][2];
+        // the maximum (0 while there is none) and the score that moves it, both without the factor `back`.  p is 2^((x - m) back - 12), the
+        // difference taken first: with m back rounded, scores beyond 2^24 would lose the 12, and at 2^30 p would be anything
+        float m[NT][2], edge[NT][2], l[NT][2];
         int E = kLowE;
         float up = pow2(kRoom + 6 - kLowE);                // what p s is scaled with for f16
         uint32_t most = 0;                                 // 2^E in the place of a step: no word of a value so far is above
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) { m[nt][0] = m[nt][1] = edge[nt][0] = edge[nt][1] = -INFINITY; base[nt][0] = base[nt][1] = l[nt][0] = l[nt][1] = 0.f; }
+        for (int nt = 0; nt < NT; ++nt) { edge[nt][0] = edge[nt][1] = -INFINITY; m[nt][0] = m[nt][1] = l[nt][0] = l[nt][1] = 0.f; }
         // The next tile in the ring: waits for it, clears the steps of hidden entries (they must not meet the products: 0 * NaN), puts the
         // new entry in its place.  Which entries are visible.
         auto first_of = [&]() { const int t = id - start; return (t < c_sink ? t : t + c_skip) * CH; };
@@ -462,7 +464,7 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
                     float p[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        p[e] = ex2(fmaf(x[u][nt][e], Q.back[nt][e & 1], -base[nt][e & 1]));
+                        p[e] = ex2(fmaf(x[u][nt][e] - m[nt][e & 1], Q.back[nt][e & 1], (float)-kRoom));
                         l[nt][e & 1] += p[e];
                     }
 #pragma unroll
@@ -602,16 +604,17 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
-                    float mx = m[nt][c];
+                    const bool none = edge[nt][c] == -INFINITY;
+                    float mx = none ? -INFINITY : m[nt][c];
 #pragma unroll
                     for (int u = 0; u < 2; ++u) mx = fmaxf(mx, fmaxf(x[u][nt][c], x[u][nt][c + 2]));
                     mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 4));
                     mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 8));
                     mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 16));
-                    edge[nt][c] = mx + Q.lazy[nt][c];
-                    const float to = mx == -INFINITY ? 0.f : fmaf(mx, Q.back[nt][c], (float)kRoom), f = m[nt][c] == -INFINITY ? 1.f : ex2(base[nt][c] - to);
+                    if (mx == -INFINITY) continue;         // all hidden or NaN
+                    const float f = none ? 1.f : ex2((m[nt][c] - mx) * Q.back[nt][c]);
                     m[nt][c] = mx;
-                    base[nt][c] = to;
+                    edge[nt][c] = mx + Q.lazy[nt][c];
                     l[nt][c] *= f;
 #pragma unroll
                     for (int g = 0; g < L; ++g) low[nt][g][c] *= f;
@@ -646,13 +649,15 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
                     for (int g = 0; g < L; ++g) low[nt][g][c] += __shfl_xor_sync(0xFFFFFFFFu, low[nt][g][c], s);
                 }
                 if (head >= heads) continue;
-                const float f0 = pow2(24 - (kRoom + 6 - E)), f1 = f0 * 0.0625f, sum = l[nt][c], inv = sum == 0.f ? 0.f : 1.f / sum, top = m[nt][c] == -INFINITY ? -INFINITY : base[nt][c];
+                const float f0 = pow2(24 - (kRoom + 6 - E)), f1 = f0 * 0.0625f, sum = l[nt][c], inv = sum == 0.f ? 0.f : 1.f / sum;
+                // what the maximum loses as a score of its own goes into the sums (where a score has less than whole numbers, nothing is known of it)
+                const float top = m[nt][c] * Q.back[nt][c], lost = fmaf(m[nt][c], Q.back[nt][c], -top), rest = fabsf(lost) < 1.f ? lost : 0.f, grow = ex2(rest);
                 if (lg == 0 && !(PAIR && lt >> 1)) {
                     if (whole) {
-                        if (A.lse) A.lse[row + head] = sum == 0.f ? -INFINITY : (base[nt][c] + log2f(sum)) / kLog2e;
-                        if (A.acc) A.done[row + head] = make_float2(base[nt][c], inv);
+                        if (A.lse) A.lse[row + head] = sum == 0.f ? -INFINITY : (top + (rest + log2f(sum * kOne))) / kLog2e;
+                        if (A.acc) A.done[row + head] = make_float2(top, inv == 0.f ? 0.f : 1.f / (sum * grow * kOne));
                     } else {
-                        *reinterpret_cast<float2 *>(A.part_ml + (slot * HB + head) * 2) = make_float2(top, sum);
+                        *reinterpret_cast<float2 *>(A.part_ml + (slot * HB + head) * 2) = make_float2(edge[nt][c] == -INFINITY ? -INFINITY : top, sum * grow);
                     }
                 }
 #pragma unroll
@@ -663,7 +668,7 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
                     auto of = [&](int n) { return PAIR ? (lt >> 1 ? o[nt][(4 * i + n) % (2 * W)][c + 2] : o[nt][(4 * i + n) % (2 * W)][c]) : o[nt][2 * i + n / 2][c + 2 * (n & 1)]; };
                     const float4 y = make_float4(fmaf(of(0), f0, mn), fmaf(of(1), f1, mn), fmaf(of(2), f0, mn), fmaf(of(3), f1, mn));
                     if (whole) *reinterpret_cast<uint2 *>(A.out + (row + head) * D + 32 * word + 4 * lg) = make_uint2(pack2<DT>(y.x * inv, y.y * inv), pack2<DT>(y.z * inv, y.w * inv));
-                    else *reinterpret_cast<float4 *>(A.part_o + (slot * HB + head) * D + 32 * word + 4 * lg) = y;
+                    else *reinterpret_cast<float4 *>(A.part_o + (slot * HB + head) * D + 32 * word + 4 * lg) = make_float4(y.x * grow, y.y * grow, y.z * grow, y.w * grow);
                 }
             }
         first_segment = false;
@@ -753,7 +758,7 @@ __global__ void __launch_bounds__(kJoin4, 3) join4_kernel(const DecodeArgs A, co
                 if (slice == 0 && at < pairs) {
                     const float inv = sum.w == 0.f ? 0.f : 1.f / sum.w;
                     *reinterpret_cast<uint32_t *>(A.out + (row + head0 + head) * D + 2 * pair) = pack2<DT>(sum.x * inv, sum.y * inv);
-                    if (pair == 0 && A.lse) A.lse[row + head0 + head] = sum.w == 0.f ? -INFINITY : ((sum.z == -INFINITY ? 0.f : sum.z) + log2f(sum.w)) / kLog2e;
+                    if (pair == 0 && A.lse) A.lse[row + head0 + head] = sum.w == 0.f ? -INFINITY : ((sum.z == -INFINITY ? 0.f : sum.z) + log2f(sum.w * kOne)) / kLog2e;
                 }
             }
         }
@@ -800,7 +805,7 @@ __global__ void __launch_bounds__(kJoin4, 3) join4_kernel(const DecodeArgs A, co
             for (int i = 128 + lane; i < p.n; i += 32) { const float2 v = part_ml(p, i, head); sum += v.y * factor(v.x, top); }
 #pragma unroll
             for (int s = 16; s; s >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, s);
-            if (lane == 0) sh_done[head0 + head] = make_float2(top == -INFINITY ? 0.f : top, sum == 0.f ? 0.f : 1.f / sum);
+            if (lane == 0) sh_done[head0 + head] = make_float2(top == -INFINITY ? 0.f : top, sum == 0.f ? 0.f : 1.f / (sum * kOne));
         }
     }
     __syncthreads();

@@ -140,3 +140,20 @@ def test_every_entry_of_a_constant_group_counts(api):
         v[:, :, 200:] = top
         case(api, 128, 32, 4, "bf16", v, n=300)
         case(api, 64, 64, 12, "bf16", v[..., :64].contiguous(), n=300)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_the_largest_of_scores_beyond_2_to_24(api, dtype):
+    """Scores that are exact and so far apart that one entry has all the weight: its value comes back."""
+    n, D, H = 300, 64, 1
+    g = torch.Generator().manual_seed(3)
+    k = torch.ones(1, H, 320, D) * torch.randperm(320, generator=g).float()[:, None] / 64
+    v = torch.randn(1, H, 320, D, generator=g) * (2.0 ** 40 if dtype == "bf16" else 64.0)
+    for G, group in ((4, 32), (8, 64), (16, 32)):
+        made = k4.Made(api, 1, H, D, 320, group, dtype, [n], k=k, v=v)
+        q = torch.full((G, D), 8.0 if dtype == "f16" else 2.0 ** 24, dtype=made.dt, device="cuda")
+        m, s, c = (x[0, 0, int(made.values("k")[0, 0, :n, 0].argmax())] for x in made.vq)
+        for rows in (1, 400):
+            out = au.f64(attend(api, made, q, n, 1.0 if dtype == "bf16" else 2.0 ** 20, rows)[0])
+            want = m + s * c
+            assert np.all(np.abs(out - want) <= 1.01 * (au.U[dtype] * np.abs(want) + 8 * 2.0 ** -11 * s) + (2.0 ** -25 if dtype == "f16" else 0.0))

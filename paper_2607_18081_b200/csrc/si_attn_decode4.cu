@@ -11,9 +11,10 @@
 // m16n8k16 operands as they lie there.
 //   - q enters as f16, scaled per head by the power of two that brings its largest element to 2^14 .. 2^15 (exact but for elements below
 //     2^-31 of it).
-//   - p is relative to 2^(m + 12), m the running maximum of the scores: whatever the values are, its sum and the weights do not depend
-//     on them, and 2^12 below 1 it leaves room for sums of p times the largest bf16 numbers.  It enters as f16(p s 2^(18 - E)), 2^E above all
-//     steps so far.
+//   - p is 2^(score - m - 12), m the running maximum of the scores: whatever the values are, its sum and the weights do not depend
+//     on them, and 2^12 below 1 it leaves room for sums of p times the largest bf16 numbers.  It enters as f16(p s up), `up` a scale per head and
+//     group of channels that follows the largest p s so far and keeps it at 2^7 .. 2^15: rounded to 11 bits down to 2^-20 of that one, however
+//     far apart the steps of groups, or of entries that matter and entries that do not, may be.
 // Everything else is fp32.
 //
 // D + 8 D / group bytes per entry, key head (and 16 query heads) have to come from HBM, a third of what 16 bits take, and that is no
@@ -37,6 +38,7 @@ template <int H> constexpr int kPerSmOf = H == 16 ? 2 : 3;
 template <int H> constexpr int kStagesOf = H == 16 ? 4 : 3;
 constexpr int kRoom = 12;              // p is at most 2^-12, but for scores that have not moved the maximum yet
 constexpr float kOne = 1 << kRoom;
+constexpr float kMostUp = 0x1p126f;    // scale of p s before anything was seen
 constexpr int kPad = 3;                // an item's start and end take about as long as so many tiles (0: 47.7 us for 512 windows of 2052, 3: 41.7, 8: 44.4)
 // Units of a run: fewer would leave more parts than they save time (24 x 2 caches of 2049 entries and their eviction: two 28.7 us a
 // step, four 27.3), but with little work the SMs come first (one cache of 1001, 8 heads: two 17.9, four 18.6).
@@ -237,14 +239,15 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
     constexpr int NT = kTilesOf<H>, CH = kTileEntries, HB = 8 * NT, W = T::W;
     constexpr bool PAIR = H == 4;
     constexpr int L = PAIR ? NG / 2 : NG, GW = W / NG;      // groups of a lane (H = 4: the even or the odd ones), words of a group
+    constexpr bool kUpShared = NT * L >= 4, kShort = NT == 1 && L == 4;
     using C = Cfg<D, NG, H>;
     constexpr int kStages = kStagesOf<H>;
-    constexpr int kLowE = DT == SI_BF16 ? -90 : -14, kHighE = DT == SI_BF16 ? 92 : 16;
     const DecodeArgs &A = A4.d;
     extern __shared__ __align__(128) char smem[];
     __shared__ int sh_scan[kThreads / 32 + 1];
     __shared__ Cursor sh_item[kWarps], sh_load[kWarps];        // every warp's item to work on and to load from
     __shared__ uint64_t full[kWarps][kStages];
+    __shared__ float2 sh_up[kUpShared ? kWarps : 1][NT * L][4];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, lg = lane >> 2, lt = lane & 3;
     const int head_of = PAIR ? 2 * (lt & 1) : 2 * lt, par_of = PAIR ? (lt >> 1) * L * 4 : 0;      // the lane's first head, where its groups' words are
     char *ring = smem + warp * kStages * C::kStage;
@@ -356,11 +359,25 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
         // the maximum (0 while there is none) and the score that moves it, both without the factor `back`.  p is 2^((x - m) back - 12), the
         // difference taken first: with m back rounded, scores beyond 2^24 would lose the 12, and at 2^30 p would be anything
         float m[NT][2], edge[NT][2], l[NT][2];
-        int E = kLowE;
-        float up = pow2(kRoom + 6 - kLowE);                // what p s is scaled with for f16
-        uint32_t most = 0;                                 // 2^E in the place of a step: no word of a value so far is above
+        // what p s is scaled with for f16, per group and the lane's heads; in shared memory where registers are short
+        float2 up_reg[kUpShared ? 1 : NT * L] = {};
+        auto up_of = [&](int nt, int g) { if constexpr (kUpShared) return sh_up[warp][nt * L + g][lt]; else return up_reg[nt * L + g]; };
+        auto set_up = [&](int nt, int g, float2 y) {       // the eight lanes of these heads have the same
+            if constexpr (kUpShared) { __syncwarp(); if (lg == 0) sh_up[warp][nt * L + g][lt] = y; __syncwarp(); }
+            else up_reg[nt * L + g] = y;
+        };
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) { edge[nt][0] = edge[nt][1] = -INFINITY; m[nt][0] = m[nt][1] = l[nt][0] = l[nt][1] = 0.f; }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int g = 0; g < L; ++g) set_up(nt, g, make_float2(kMostUp, kMostUp));
+        // o of a group and head times f
+        auto scale_o = [&](int nt, int g, int c, float f) {
+#pragma unroll
+            for (int i = 0; i < 2 * W; ++i)
+                if ((PAIR ? i / 4 / GW : T::place_of(T::group_of(i / 2))) == g) { o[nt][i][c] *= f; o[nt][i][c + 2] *= f; }
+        };
         // The next tile in the ring: waits for it, clears the steps of hidden entries (they must not meet the products: 0 * NaN), puts the
         // new entry in its place.  Which entries are visible.
         auto first_of = [&]() { const int t = id - start; return (t < c_sink ? t : t + c_skip) * CH; };
@@ -449,34 +466,117 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
                         x[u][nt][e] = PAIR ? y + __shfl_xor_sync(0xFFFFFFFFu, y, 2) : y;
                     }
         };
-        // p of the same entries, and their share of the sums.
+        // p of the same entries, and their share of the sums.  One vote for all that seldom happens: the maximum and the scales move.
         auto add = [&](const char *tile, const float (&x)[2][NT][4], const uint32_t (&vp)[2][2][L]) {
             uint32_t va[2][W], vb[2][W], pf[2][NT][L][2];
+            auto times_step = [&](float2 y, uint32_t word) { const float s = si_cvt<DT>::hi(word); return __fmul2_rn(y, make_float2(s, s)); };
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                bool grow = false;
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) grow |= x[u][nt][e] > edge[nt][e & 1];
+                float2 p[2][2];                            // entries 16 u + 8 r + lg, the lane's heads
+                auto make_p = [&]() {
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int r = 0; r < 2; ++r) {
+                            const float2 d = __fadd2_rn(make_float2(x[u][nt][2 * r], x[u][nt][2 * r + 1]), make_float2(-m[nt][0], -m[nt][1]));
+                            const float2 y = __ffma2_rn(d, make_float2(Q.back[nt][0], Q.back[nt][1]), make_float2(-kRoom, -kRoom));
+                            p[u][r] = make_float2(ex2(y.x), ex2(y.y));
+                        }
+                };
+                make_p();
+                auto pack = [&]() {
+                    uint32_t top = 0;                      // the largest of each half (NaN above all)
+#pragma unroll
+                    for (int g = 0; g < L; ++g) {
+                        const float2 f = up_of(nt, g);
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            uint32_t ps[2];
+#pragma unroll
+                            for (int r = 0; r < 2; ++r) {
+                                const float2 y = __fmul2_rn(times_step(p[u][r], vp[u][r][g]), f);
+                                ps[r] = pack2<SI_F16>(y.x, y.y);
+                                pf[u][nt][g][r] = transposed(ps[r]);
+                            }
+                            top = __vimax3_u16x2(top, ps[0], ps[1]);
+                        }
+                    }
+                    return ((top + 0x08000800u) & 0x80008000u) != 0;
+                };
+                if (__builtin_expect(__any_sync(0xFFFFFFFFu, pack() | grow), 0)) {
+                    float f[2] = {1.f, 1.f};
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        const bool none = edge[nt][c] == -INFINITY;
+                        float mx = none ? -INFINITY : m[nt][c];
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) mx = fmaxf(mx, fmaxf(x[u][nt][c], x[u][nt][c + 2]));
+                        mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 4));
+                        mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 8));
+                        mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 16));
+                        if (mx == -INFINITY) continue;         // all hidden or NaN
+                        if (!none) f[c] = ex2((m[nt][c] - mx) * Q.back[nt][c]);
+                        m[nt][c] = mx;
+                        edge[nt][c] = mx + Q.lazy[nt][c];
+                        l[nt][c] *= f[c];
+                    }
+                    make_p();
+                    // a score far above the maximum, or a p s of 2^15 or more: the maximum moves, and the scale of every group and head
+                    // whose largest p s is above 2^14 then goes down, so that it is 2^7 again
+#pragma unroll
+                    for (int g = 0; g < L; ++g) {
+                        float2 most = make_float2(0.f, 0.f);
+                        const float2 was = up_of(nt, g);
+#pragma unroll
+                        for (int u = 0; u < 2; ++u)
+#pragma unroll
+                            for (int r = 0; r < 2; ++r) {
+                                const float2 y = times_step(p[u][r], vp[u][r][g]);
+                                most = make_float2(fmaxf(most.x, y.x), fmaxf(most.y, y.y));      // NaN does not count
+                            }
+#pragma unroll
+                        for (int s = 4; s < 32; s <<= 1) most = make_float2(fmaxf(most.x, __shfl_xor_sync(0xFFFFFFFFu, most.x, s)), fmaxf(most.y, __shfl_xor_sync(0xFFFFFFFFu, most.y, s)));
+                        float2 now;
+                        auto move = [&](int c, float ps, float from, float &to) {
+                            // p has fallen by f, so its scale rises by as much; but p s is to fit
+                            to = f[c] == 1.f ? from : fminf(__fdividef(from, f[c]), kMostUp);
+                            if (ps * to > 16384.f) to = __fdividef(128.f, ps);
+                            if (f[c] != 1.f || to != from) scale_o(nt, g, c, __fdividef(f[c] * to, from));
+                            low[nt][g][c] *= f[c];
+                        };
+                        move(0, most.x, was.x, now.x);
+                        move(1, most.y, was.y, now.y);
+                        set_up(nt, g, now);
+                    }
+                    pack();
+                }
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        const float2 y = p[u][r];
+                        uint32_t word[L];                  // once more where registers are short
+                        if constexpr (kShort) load_words(word, tile + T::kValuePar + (u * 16 + r * 8 + lg) * NG * 4 + par_of);
+                        add2(l[nt][0], l[nt][1], y.x, y.y);
+#pragma unroll
+                        for (int g = 0; g < L; ++g) {
+                            const uint32_t v = kShort ? word[g] : vp[u][r][g];
+                            const float mn = fmaf(8.f, si_cvt<DT>::hi(v), si_cvt<DT>::lo(v));
+                            const float2 z = __ffma2_rn(y, make_float2(mn, mn), make_float2(low[nt][g][0], low[nt][g][1]));
+                            low[nt][g][0] = z.x; low[nt][g][1] = z.y;
+                        }
+                    }
+            }
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 load_words(va[u], tile + T::kValues + u * 8 * D + lt * D + (lg ^ T::swizzle(lt)) * T::kCell);
                 load_words(vb[u], tile + T::kValues + u * 8 * D + 4 * D + lt * D + (lg ^ T::swizzle(lt)) * T::kCell);
             }
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    float p[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        p[e] = ex2(fmaf(x[u][nt][e] - m[nt][e & 1], Q.back[nt][e & 1], (float)-kRoom));
-                        l[nt][e & 1] += p[e];
-                    }
-#pragma unroll
-                    for (int g = 0; g < L; ++g)
-#pragma unroll
-                        for (int r = 0; r < 2; ++r) {
-                            const float s = si_cvt<DT>::hi(vp[u][r][g]), mn = fmaf(8.f, s, si_cvt<DT>::lo(vp[u][r][g]));
-                            pf[u][nt][g][r] = transposed(pack2<SI_F16>(p[2 * r] * s * up, p[2 * r + 1] * s * up));
-                            low[nt][g][0] = fmaf(p[2 * r], mn, low[nt][g][0]);
-                            low[nt][g][1] = fmaf(p[2 * r + 1], mn, low[nt][g][1]);
-                        }
-                }
             // Every sum also gets -8 times (upper nibbles: -128 times) the sum of its rounded p s, which a product with constants gives: with
             // codes around zero it stays small, and so do what the matrix unit cuts off of it and what the rounding of p s leaves
             // (2052 entries, f16: error 2.6e-4 instead of 4.7e-4; 260001, bf16: 1.7e-3 instead of 4.5e-3).  In the products
@@ -541,7 +641,7 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
         };
         float x[2][NT][4];
         uint32_t vp[2][2][L];
-        // Hidden entries out of the scores; the scores out for the weights; steps of the values; whether the base has to move first.
+        // Hidden entries out of the scores; the scores out for the weights; steps of the values.
         auto settle = [&](const char *tile, uint32_t vis) {
             if (vis != 0xFFFFFFFFu) {
 #pragma unroll
@@ -552,22 +652,10 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
                         for (int e = 0; e < 4; ++e)
                             if (!(vis >> (u * 16 + lg + (e >> 1) * 8) & 1)) x[u][nt][e] = -INFINITY;
             }
-            uint32_t top = 0;
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    load_words(vp[u][r], tile + T::kValuePar + (u * 16 + r * 8 + lg) * NG * 4 + par_of);
-#pragma unroll
-                    for (int g = 0; g < L; ++g) top = max(top, vp[u][r][g]);
-                }
-            bool grow = top > most;
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) grow |= x[u][nt][e] > edge[nt][e & 1];
+                for (int r = 0; r < 2; ++r) load_words(vp[u][r], tile + T::kValuePar + (u * 16 + r * 8 + lg) * NG * 4 + par_of);
             if (A.acc) {
                 const int j0 = first_of();
                 float *sc = scores_to + (long long)j0 * A.GS;
@@ -584,43 +672,6 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
                                              ::"l"(sc + key * A.GS + head), "f"(x[u][nt][e] * Q.back[nt][0]), "f"(x[u][nt][e + 1] * Q.back[nt][1]), "l"(stay) : "memory");
                         }
             }
-            if (!__any_sync(0xFFFFFFFFu, grow)) return;
-            // groups that are NaN (no other step's word is as large) do not count: they would drive all others' p s out of f16
-            constexpr uint32_t kNotFinite = DT == SI_BF16 ? 0x7F800000u : 0x7C000000u;
-            uint32_t step16 = 0;
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int r = 0; r < 2; ++r)
-#pragma unroll
-                    for (int g = 0; g < L; ++g)
-                        if (vp[u][r][g] < kNotFinite) step16 = max(step16, vp[u][r][g]);
-            const int was = E;
-            E = max(E, min(exponent(si_cvt<DT>::lo(__reduce_max_sync(0xFFFFFFFFu, step16) >> 16)) + 1, kHighE));      // above every step
-            up = pow2(kRoom + 6 - E);
-            const float down0 = pow2((was - E) / 2), down1 = pow2(was - E - (was - E) / 2);       // one factor may be below fp32
-            most = (uint32_t)(DT == SI_BF16 ? (E + 127) << 7 : (E + 15) << 10) << 16 | 0xFFFFu;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    const bool none = edge[nt][c] == -INFINITY;
-                    float mx = none ? -INFINITY : m[nt][c];
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) mx = fmaxf(mx, fmaxf(x[u][nt][c], x[u][nt][c + 2]));
-                    mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 4));
-                    mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 8));
-                    mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 16));
-                    if (mx == -INFINITY) continue;         // all hidden or NaN
-                    const float f = none ? 1.f : ex2((m[nt][c] - mx) * Q.back[nt][c]);
-                    m[nt][c] = mx;
-                    edge[nt][c] = mx + Q.lazy[nt][c];
-                    l[nt][c] *= f;
-#pragma unroll
-                    for (int g = 0; g < L; ++g) low[nt][g][c] *= f;
-#pragma unroll
-                    for (int i = 0; i < 2 * W; ++i) { o[nt][i][c] *= f * down0; o[nt][i][c] *= down1; o[nt][i][c + 2] *= f * down0; o[nt][i][c + 2] *= down1; }
-                }
         };
         for (; id < seg_end; ++id) {
             char *tile = ring + stage * C::kStage;
@@ -649,13 +700,13 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
                     for (int g = 0; g < L; ++g) low[nt][g][c] += __shfl_xor_sync(0xFFFFFFFFu, low[nt][g][c], s);
                 }
                 if (head >= heads) continue;
-                const float f0 = pow2(24 - (kRoom + 6 - E)), f1 = f0 * 0.0625f, sum = l[nt][c], inv = sum == 0.f ? 0.f : 1.f / sum;
+                const float sum = l[nt][c], inv = sum == 0.f ? 0.f : 1.f / sum;
                 // what the maximum loses as a score of its own goes into the sums (where a score has less than whole numbers, nothing is known of it)
                 const float top = m[nt][c] * Q.back[nt][c], lost = fmaf(m[nt][c], Q.back[nt][c], -top), rest = fabsf(lost) < 1.f ? lost : 0.f, grow = ex2(rest);
                 if (lg == 0 && !(PAIR && lt >> 1)) {
                     if (whole) {
                         if (A.lse) A.lse[row + head] = sum == 0.f ? -INFINITY : (top + (rest + log2f(sum * kOne))) / kLog2e;
-                        if (A.acc) A.done[row + head] = make_float2(top, inv == 0.f ? 0.f : 1.f / (sum * grow * kOne));
+                        if (A.acc) A.done[row + head] = make_float2(top, inv * ex2(-rest - (float)kRoom));
                     } else {
                         *reinterpret_cast<float2 *>(A.part_ml + (slot * HB + head) * 2) = make_float2(edge[nt][c] == -INFINITY ? -INFINITY : top, sum * grow);
                     }
@@ -664,7 +715,8 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
                 for (int i = 0; i < (PAIR ? W / 2 : W); ++i) {
                     // the lane's words: all, or k of its own groups
                     const int word = PAIR ? i / GW * 2 * GW + i % GW + (lt >> 1) * GW : i;
-                    const float mn = low[nt][PAIR ? i / GW : T::place_of(T::group_of(i))][c];
+                    const int g = PAIR ? i / GW : T::place_of(T::group_of(i));
+                    const float mn = low[nt][g][c], f0 = __fdividef(0x1p24f, c ? up_of(nt, g).y : up_of(nt, g).x), f1 = f0 * 0.0625f;
                     auto of = [&](int n) { return PAIR ? (lt >> 1 ? o[nt][(4 * i + n) % (2 * W)][c + 2] : o[nt][(4 * i + n) % (2 * W)][c]) : o[nt][2 * i + n / 2][c + 2 * (n & 1)]; };
                     const float4 y = make_float4(fmaf(of(0), f0, mn), fmaf(of(1), f1, mn), fmaf(of(2), f0, mn), fmaf(of(3), f1, mn));
                     if (whole) *reinterpret_cast<uint2 *>(A.out + (row + head) * D + 32 * word + 4 * lg) = make_uint2(pack2<DT>(y.x * inv, y.y * inv), pack2<DT>(y.z * inv, y.w * inv));

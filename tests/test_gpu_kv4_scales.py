@@ -157,3 +157,49 @@ def test_the_largest_of_scores_beyond_2_to_24(api, dtype):
             out = au.f64(attend(api, made, q, n, 1.0 if dtype == "bf16" else 2.0 ** 20, rows)[0])
             want = m + s * c
             assert np.all(np.abs(out - want) <= 1.01 * (au.U[dtype] * np.abs(want) + 8 * 2.0 ** -11 * s) + (2.0 ** -25 if dtype == "f16" else 0.0))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("D,group,G", FORMS)
+def test_groups_of_very_different_sizes(api, D, group, G, dtype):
+    """Channels of an entry 2^30 (f16: 2^22) apart, alone and with one entry that has most of the weight."""
+    v, groups = noise(D), D // group
+    reach = 30 if dtype == "bf16" else 22
+    up = torch.arange(D) // group * (reach / max(groups - 1, 1)) - (15 if dtype == "bf16" else 12)
+    case(api, D, group, G, dtype, v * 2.0 ** up)
+    base = torch.randn(1, D, generator=torch.Generator().manual_seed(5))
+    q = base + 0.1 * torch.randn(2 * G, D, generator=torch.Generator().manual_seed(6))
+    k = noise(D, seed=7) * 0.1
+    k[0, :, 450] = base * (4.2 / (0.1 * base.pow(2).sum()))
+    case(api, D, group, G, dtype, v * 2.0 ** up.flip(0), k=k, q=q)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("D,group,G", FORMS)
+@pytest.mark.parametrize("at", [0, 33, 620])
+def test_one_large_entry_of_no_weight(api, D, group, G, dtype, at):
+    """An entry whose steps are far above all others and whose weight is 0: the others keep their bits."""
+    v, base = noise(D), torch.randn(1, D, generator=torch.Generator().manual_seed(5))
+    q = base + 0.1 * torch.randn(2 * G, D, generator=torch.Generator().manual_seed(6))
+    k = noise(D, seed=7) * 0.1
+    k[0, :, at] = -base * (200.0 / (0.1 * base.pow(2).sum()))
+    if dtype == "f16":
+        v = v * 2.0 ** -10
+    v[0, :, at] = v[0, :, at] * (2.0 ** 70 if dtype == "bf16" else 2.0 ** 23)
+    case(api, D, group, G, dtype, v, k=k, q=q)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("D,group,G", FORMS)
+def test_scores_grow_while_steps_shrink(api, D, group, G, dtype):
+    """What is large comes first and loses its weight little by little, and at once; and the other way round."""
+    base = torch.randn(1, D, generator=torch.Generator().manual_seed(5))
+    q = base + 0.05 * torch.randn(2 * G, D, generator=torch.Generator().manual_seed(6))
+    along = torch.linspace(0.0, 1.0, 1024)[:, None]
+    unit = base / (0.1 * base.pow(2).sum())
+    range2 = 40.0 if dtype == "bf16" else 20.0
+    for shape in (along, torch.floor(along * 4) / 4):
+        size = 2.0 ** (range2 * (0.5 - shape))
+        for steps in (size, 1 / size):
+            k = unit * shape * 25.0 + noise(D, seed=7) * 0.05
+            case(api, D, group, G, dtype, noise(D) * steps, k=k, q=q)

@@ -9,8 +9,8 @@
 // halves is a pair of f16 numbers c 2^-24 (subnormal, which the matrix unit multiplies exactly), sixteen times that one nibble
 // further up, which the other operand (q / 16) or the end (out / 16) takes back.  The layout of a tile (si_kv4.cuh) makes them
 // m16n8k16 operands as they lie there.
-//   - q enters as f16, scaled per head by the power of two that brings its largest element to 2^14 .. 2^15 (exact but for elements below
-//     2^-31 of it).
+//   - q enters as f16, scaled per head by the power of two that brings its largest element to 2^14 .. 2^15.  Half of its elements are divided by
+//     16 on top of it: exact but for elements below 2^-27 (bf16) or 2^-24 (f16) of the largest.
 //   - p is 2^(score - m - 12), m the running maximum of the scores: whatever the values are, its sum and the weights do not depend
 //     on them, and 2^12 below 1 it leaves room for sums of p times the largest bf16 numbers.  It enters as f16(p s up), `up` a scale per head and
 //     group of channels that follows the largest p s so far and keeps it at 2^7 .. 2^15: rounded to 11 bits down to 2^-20 of that one, however
@@ -155,14 +155,16 @@ template <int DT, int D, int NG, int H> __device__ __forceinline__ void load_q(c
         }
         top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
         top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-        const int e = top == 0.f ? 0 : min(exponent(top), 117), up = 14 - e;
-        const float f0 = pow2(up / 2), f1 = copysignf(pow2(up - up / 2), A.scale2);      // 2^up may be beyond fp32
+        const int e = exponent(top), up = 14 - e;
+        auto back = [&](int n) { return fabsf(A.scale2) * pow2(n / 2) * pow2(n - n / 2); };      // 2^n may be beyond fp32
+        // where `back` is below fp32 its rest goes into the query; where it is beyond, the scores are NaN
+        const float f0 = pow2(up / 2) * fminf(back(min(e + 136, 200)), 1.f), f1 = copysignf(pow2(up - up / 2), A.scale2), most = back(e + 10) <= 3.4e38f ? 3.4e38f : -1.f;
         float sum[NG] = {};
 #pragma unroll
         for (int w = 0; w < T::W; ++w) {
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                x[w][k] = fabsf(x[w][k]) <= 3.4e38f ? x[w][k] * f0 * f1 : NAN;      // infinity times a code of zero, minus itself: NaN in any case
+                x[w][k] = fabsf(x[w][k]) <= most ? x[w][k] * f0 * f1 : NAN;      // infinity times a code of zero, minus itself: NaN in any case
                 sum[T::group_of(w)] += x[w][k];
             }
 #pragma unroll
@@ -199,7 +201,7 @@ template <int DT, int D, int NG, int H> __device__ __forceinline__ void load_q(c
                 Q.sum[nt][i][r] = v;
             }
 #pragma unroll
-        for (int c = 0; c < 2; ++c) Q.back[nt][c] = fminf(fmaxf(fabsf(A.scale2) * pow2(__shfl_sync(0xFFFFFFFFu, e, 8 * (PAIR ? t & 1 : t) + 4 * c) + 10), 1.2e-38f), 3.4e38f);
+        for (int c = 0; c < 2; ++c) Q.back[nt][c] = fminf(fmaxf(back(__shfl_sync(0xFFFFFFFFu, e, 8 * (PAIR ? t & 1 : t) + 4 * c) + 10), 0x1p-126f), 3.4e38f);
 #pragma unroll
         for (int c = 0; c < 2; ++c) Q.lazy[nt][c] = kLazy / Q.back[nt][c];
     }

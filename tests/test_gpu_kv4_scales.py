@@ -203,3 +203,28 @@ def test_scores_grow_while_steps_shrink(api, D, group, G, dtype):
         for steps in (size, 1 / size):
             k = unit * shape * 25.0 + noise(D, seed=7) * 0.05
             case(api, D, group, G, dtype, noise(D) * steps, k=k, q=q)
+
+
+@pytest.mark.parametrize("D,group,G", FORMS)
+def test_queries_near_the_largest_number(api, D, group, G):
+    """Finite bf16 queries of up to 2^127 with a scale that brings the scores back; a query and a scale of zero."""
+    q = torch.randn(2 * G, D, generator=torch.Generator().manual_seed(4))
+    q[0] = 0.0
+    case(api, D, group, G, "bf16", noise(D), q=q.clamp(-1.9, 1.9) * 2.0 ** 126, scale=0.1 * 2.0 ** -126)
+    one = torch.where(torch.arange(D) % 7 == 2, 1.9, 0.0) * 2.0 ** 126 * torch.ones(2 * G, 1)
+    case(api, D, group, G, "bf16", noise(D), q=one, scale=0.1 * 2.0 ** -126)
+    case(api, D, group, G, "bf16", noise(D), q=q, k=torch.sign(noise(D, seed=2)[..., :1]).expand(-1, -1, -1, D) * 3.0e38, scale=0.0)
+    case(api, D, group, G, "bf16", noise(D), q=torch.zeros(2 * G, D), scale=1.9e38)
+
+
+def test_scores_beyond_the_largest_number_are_nan(api):
+    """Never finite and wrong: |scale q| of 2^130 is refused by NaN, and the other heads keep their results."""
+    for D, group, G in FORMS:
+        q = torch.randn(2 * G, D, generator=torch.Generator().manual_seed(4)) * 2.0 ** -20
+        k = noise(D, seed=7)
+        made = k4.Made(api, 1, 2, D, 1024, group, "bf16", [1000], k=k * 2.0 ** -100, v=noise(D))
+        q[G - 1] = 2.0 ** 105
+        q = q.to(made.dt).cuda()
+        out, lse, _ = attend(api, made, q, 1000, 2.0 ** 25, 1)
+        assert out[0, G - 1].isnan().all() and lse[0, G - 1].isnan()
+        assert not out[0, :G - 1].isnan().any() and not out[0, G:].isnan().any()

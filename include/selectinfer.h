@@ -580,7 +580,8 @@ int si_kv4_load(const si_kv4_t *src, const si_kv_t *dst, const int32_t *first, i
  * stored values are not rounded in between: out is the attention over m + s * c.  Scores, softmax and sums are fp32; p * s is
  * rounded to 11 bits for the product with the codes: for every query head and group of channels on its own, whatever the steps of other
  * groups are, down to 2^-20 of the largest p * s of that head and group and to an absolute 2^-32 of it below (fewer bits where all
- * steps are below 2^-110: bf16 values below some 1e-32).  Weights below 2^-110 of the largest count as 0.  out has the cache's type.
+ * steps are below 2^-110: bf16 values below some 1e-32).  Weights below 2^-110 of the largest count as 0.  out has the cache's type
+ * (f16: at most its largest number, as in si_kv4_load).
  * A query that holds a NaN or an infinity has NaN as result, and so may one whose largest element times scale is beyond 2^117. */
 int si_kv4_attn_decode(const si_kv4_t *kv, const void *q, long long q_seq_stride, int n_q_heads, const int32_t *q_pos,
                        const void *k_new, const void *v_new, long long new_seq_stride, int window, int n_sink, float scale,

@@ -207,6 +207,12 @@ template <int DT, int D, int NG, int H> __device__ __forceinline__ void load_q(c
     }
 }
 
+// Two results.  Steps are rounded up, so that the highest code may stand for a little more than f16 holds: the largest number then,
+// as when it is read back.
+template <int DT> __device__ __forceinline__ uint32_t result2(float a, float b) {
+    return DT == SI_F16 ? pack2<DT>(si_q4::min_nan(a, 65504.f), si_q4::min_nan(b, 65504.f)) : pack2<DT>(a, b);
+}
+
 // One product of 16 x 16 by 16 x 8.  Not volatile: the compiler may interleave those of different tiles.
 template <int DT> __device__ __forceinline__ void product(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     if (DT == SI_BF16)
@@ -721,7 +727,7 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
                     const float mn = low[nt][g][c], f0 = __fdividef(0x1p24f, c ? up_of(nt, g).y : up_of(nt, g).x), f1 = f0 * 0.0625f;
                     auto of = [&](int n) { return PAIR ? (lt >> 1 ? o[nt][(4 * i + n) % (2 * W)][c + 2] : o[nt][(4 * i + n) % (2 * W)][c]) : o[nt][2 * i + n / 2][c + 2 * (n & 1)]; };
                     const float4 y = make_float4(fmaf(of(0), f0, mn), fmaf(of(1), f1, mn), fmaf(of(2), f0, mn), fmaf(of(3), f1, mn));
-                    if (whole) *reinterpret_cast<uint2 *>(A.out + (row + head) * D + 32 * word + 4 * lg) = make_uint2(pack2<DT>(y.x * inv, y.y * inv), pack2<DT>(y.z * inv, y.w * inv));
+                    if (whole) *reinterpret_cast<uint2 *>(A.out + (row + head) * D + 32 * word + 4 * lg) = make_uint2(result2<DT>(y.x * inv, y.y * inv), result2<DT>(y.z * inv, y.w * inv));
                     else *reinterpret_cast<float4 *>(A.part_o + (slot * HB + head) * D + 32 * word + 4 * lg) = make_float4(y.x * grow, y.y * grow, y.z * grow, y.w * grow);
                 }
             }
@@ -811,7 +817,7 @@ __global__ void __launch_bounds__(kJoin4, 3) join4_kernel(const DecodeArgs A, co
                 }
                 if (slice == 0 && at < pairs) {
                     const float inv = sum.w == 0.f ? 0.f : 1.f / sum.w;
-                    *reinterpret_cast<uint32_t *>(A.out + (row + head0 + head) * D + 2 * pair) = pack2<DT>(sum.x * inv, sum.y * inv);
+                    *reinterpret_cast<uint32_t *>(A.out + (row + head0 + head) * D + 2 * pair) = result2<DT>(sum.x * inv, sum.y * inv);
                     if (pair == 0 && A.lse) A.lse[row + head0 + head] = sum.w == 0.f ? -INFINITY : ((sum.z == -INFINITY ? 0.f : sum.z) + log2f(sum.w * kOne)) / kLog2e;
                 }
             }

@@ -228,3 +228,18 @@ def test_scores_beyond_the_largest_number_are_nan(api):
         out, lse, _ = attend(api, made, q, 1000, 2.0 ** 25, 1)
         assert out[0, G - 1].isnan().all() and lse[0, G - 1].isnan()
         assert not out[0, :G - 1].isnan().any() and not out[0, G:].isnan().any()
+
+
+@pytest.mark.parametrize("D,group,G", FORMS)
+def test_results_end_where_f16_ends(api, D, group, G):
+    """-65504 and 65504 in one group: the step is rounded up and m + 15 s is 65536.  The largest number comes back, from attention as from
+    reading back; one entry (a result of one run of tiles) and many (parts that are joined)."""
+    for n in (1, 900):
+        v = torch.where(torch.arange(D) % 2 == 0, 65504.0, -65504.0) * torch.ones(1, 2, (n + 31) // 32 * 32, 1)
+        made = k4.Made(api, 1, 2, D, v.shape[2], group, "f16", [n], k=torch.zeros_like(v), v=v)
+        q = torch.randn(2 * G, D, device="cuda").half()
+        back = made.read()[1][0, 0, 0]
+        assert back.tolist() == [65504.0, -65504.0] * (D // 2)
+        for rows in (1, 400):
+            out, _, _ = attend(api, made, q, n, 0.1, rows)
+            assert torch.equal(out, back.expand_as(out))

@@ -570,7 +570,8 @@ int si_kv4_store(const si_kv_t *src, const si_kv4_t *dst, const int32_t *first_p
  * a negative one is SI_ERR_OUT_OF_RANGE and taken as 0) become entries 0, 1, .. of the 16-bit cache dst, rounded once to dtype (f16: at most its
  * largest number, since s was rounded up), with their pos and weight where both sides have them.  dst->len is not read; other
  * rows of dst stay as they were.  n <= dst->capacity.
- *   len_out      device int32 [n_seqs] or NULL: entries read back; may be dst->len
+ *   len_out      device int32 [n_seqs] or NULL: entries read back; may be dst->len, src->len or first (written after they were
+ *                read; another overlap with the latter two is SI_ERR_INVALID_ARG)
  * This is how the next chunk of a prompt is prefilled on such a cache: into a scratch cache, the chunk's own keys and values
  * behind, si_attn_prefill. */
 int si_kv4_load(const si_kv4_t *src, const si_kv_t *dst, const int32_t *first, int n, int32_t *len_out, int32_t *status_dev,

@@ -147,6 +147,14 @@ template <int DT> __device__ __forceinline__ float value_of(float code, float st
     return DT == SI_F16 ? si_q4::min_nan(x, 65504.f) : x;
 }
 
+// The entries of sequence b that are read back: from *first up to the returned end.
+__device__ __forceinline__ int load_span(const LoadArgs &A, int b, int32_t *status, int *first) {
+    const int len = si_kv_len(A.meta, b, status), f = A.first ? A.first[b] : 0;
+    if (f < 0) si_report(status, SI_ERR_OUT_OF_RANGE);
+    *first = max(0, f);
+    return *first + min(A.n, max(0, len - *first));
+}
+
 // A warp per eight entries, all words asked for at once; a lane makes eight neighbouring elements of a row.
 template <int DT, int D, int NG>
 __global__ void __launch_bounds__(kThreads) load_kernel(const LoadArgs A) {
@@ -157,10 +165,8 @@ __global__ void __launch_bounds__(kThreads) load_kernel(const LoadArgs A) {
     si_tc::pdl_wait();
     si_tc::pdl_launch();
     const bool tell = blockIdx.x == 0 && threadIdx.x == 0;
-    const int len = si_kv_len(A.meta, b, tell ? A.status : nullptr);
-    int first = A.first ? A.first[b] : 0;
-    if (first < 0) { if (tell) si_report(A.status, SI_ERR_OUT_OF_RANGE); first = 0; }
-    const int end = first + min(A.n, max(0, len - first));
+    int first;
+    const int end = load_span(A, b, tell ? A.status : nullptr, &first);
     if (tell && A.len_out) A.len_out[b] = end - first;
     const long long e0 = (first / kOctet + block * kWarps + warp) * kOctet;
     if (end <= first || e0 >= end) return;
@@ -200,6 +206,15 @@ __global__ void __launch_bounds__(kThreads) load_kernel(const LoadArgs A) {
     const int e = (int)e0 + lane;
     if (A.meta.pos && A.dst.pos) A.dst.pos[A.dst.meta(b, h) + e - first] = A.meta.pos[A.meta.meta(b, h) + e];
     if (A.meta.weight && A.dst.weight) A.dst.weight[A.dst.meta(b, h) + e - first] = A.meta.weight[A.meta.meta(b, h) + e];
+}
+
+// Numbers of entries that go where the lengths or the first entries are.
+__global__ void load_len_kernel(const LoadArgs A) {
+    const int b = blockIdx.x * blockDim.x + threadIdx.x;
+    if (b >= A.dst.B) return;
+    int first;
+    const int end = load_span(A, b, nullptr, &first);
+    A.len_out[b] = end - first;
 }
 
 // The kept entries to their slots; nothing to do for an entry that stays.  A warp per sixteen slots, everything asked for before anything is
@@ -356,14 +371,23 @@ extern "C" int si_kv4_load(const si_kv4_t *src, const si_kv_t *dst, const int32_
     if (src->n_seqs == 0) return SI_OK;
     if (si_kv_shared(dst)) return SI_ERR_INVALID_ARG;
     if (!si_aligned4(first, len_out, status_dev)) return SI_ERR_ALIGNMENT;
-    const LoadArgs A{si_kv4_meta_of(src), si_kv_view_of(dst), si_kv4_view_of(src), first, n, len_out, status_dev};
+    // all blocks read the lengths and the first entries: a result in their place is written behind them
+    const bool len_after = len_out && (len_out == src->len || len_out == first);
+    for (const int32_t *in : {src->len, first})
+        if (len_out && in && len_out != in && len_out < in + src->n_seqs && in < len_out + src->n_seqs) return SI_ERR_INVALID_ARG;
+    LoadArgs A{si_kv4_meta_of(src), si_kv_view_of(dst), si_kv4_view_of(src), first, n, len_after ? nullptr : len_out, status_dev};
     si_mt_forget();
     const int most = n < src->capacity ? n : src->capacity;
     cudaLaunchAttribute at;
     const long long blocks = octet_blocks(most, src->n_kv_heads);
     if (blocks > INT_MAX) return SI_ERR_TOO_LARGE;
     cudaLaunchConfig_t cfg = config(dim3((unsigned)blocks, 1, src->n_seqs), kThreads, (cudaStream_t)stream, &at);
-    return by_shape<Load>(src->dtype, src->head_dim, si_kv4_groups(src), &cfg, &A);
+    rc = by_shape<Load>(src->dtype, src->head_dim, si_kv4_groups(src), &cfg, &A);
+    if (rc || !len_after) return rc;
+    A.len_out = len_out;
+    load_len_kernel<<<(src->n_seqs + 127) / 128, 128, 0, (cudaStream_t)stream>>>(A);
+    SI_CUDA_TRY(cudaGetLastError());
+    return SI_OK;
 }
 
 extern "C" int si_kv4_evict(const si_kv4_t *src, const si_kv4_t *dst, const int32_t *q_pos, int n_new, int budget, int n_sink, int n_recent,

@@ -124,8 +124,9 @@ class Decoder:
 
 def main():
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
-    for name, value in (("prompt", 600), ("steps", 32), ("budget", 256), ("layers", 4), ("bits", 16)):
+    for name, value in (("prompt", 600), ("steps", 32), ("budget", 256), ("layers", 4)):
         ap.add_argument("--" + name, type=int, default=value)
+    ap.add_argument("--bits", type=int, default=16, choices=(4, 16))
     a = ap.parse_args()
     model = Decoder(layers=a.layers, budget=a.budget, bits=a.bits)
     g = torch.Generator(device="cuda").manual_seed(1)

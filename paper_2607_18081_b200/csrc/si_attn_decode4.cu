@@ -207,10 +207,11 @@ template <int DT, int D, int NG, int H> __device__ __forceinline__ void load_q(c
     }
 }
 
-// Two results.  Steps are rounded up, so that the highest code may stand for a little more than f16 holds: the largest number then,
-// as when it is read back.
+// Two results.  Steps are rounded up, so that the highest code may stand for a little more than f16 holds: the largest number then, as
+// when it is read back.  The lowest one too: what p s loses in rounding may lie beyond it.
 template <int DT> __device__ __forceinline__ uint32_t result2(float a, float b) {
-    return DT == SI_F16 ? pack2<DT>(si_q4::min_nan(a, 65504.f), si_q4::min_nan(b, 65504.f)) : pack2<DT>(a, b);
+    auto in = [](float x) { return DT == SI_F16 ? si_q4::max_nan(si_q4::min_nan(x, 65504.f), -65504.f) : x; };
+    return pack2<DT>(in(a), in(b));
 }
 
 // One product of 16 x 16 by 16 x 8.  Not volatile: the compiler may interleave those of different tiles.

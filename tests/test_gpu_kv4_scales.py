@@ -243,3 +243,14 @@ def test_results_end_where_f16_ends(api, D, group, G):
         for rows in (1, 400):
             out, _, _ = attend(api, made, q, n, 0.1, rows)
             assert torch.equal(out, back.expand_as(out))
+
+
+@pytest.mark.parametrize("D,group,G", FORMS)
+def test_roundings_beyond_the_ends_of_f16(api, D, group, G):
+    """The same values, one entry ahead of the others by 2 / (1 + 1.05 * 2^-11): p s of the others lies just above the middle of two f16 numbers and is
+    rounded up, by 30 in what the lowest number comes out as.  Still a finite result."""
+    v = torch.where(torch.arange(D) % 2 == 0, 65504.0, -65504.0) * torch.ones(1, 2, 32, 1)
+    k = torch.zeros_like(v)
+    k[:, :, 0] = 1.0
+    scale = -float(np.log(0.5 * (1.0 + 1.05 * 2.0 ** -11))) / D
+    case(api, D, group, G, "f16", v, k=k, q=torch.ones(2 * G, D), n=32, scale=scale)

@@ -17,11 +17,14 @@
 //     far apart the steps of groups, or of entries that matter and entries that do not, may be.
 // Everything else is fp32.
 //
-// D + 8 D / group bytes per entry, key head (and 16 query heads) have to come from HBM, a third of what 16 bits take, and that is no
-// longer what binds: some 450 instructions per tile of 32 entries and four heads, 144 of them to unpack, 36 to 40 products.  A tile of
-// groups of 64 takes an SM 0.11 us (loads alone 0.10, work alone 0.11, and they overlap), more warps or two tiles in turn in
-// a warp change nothing.  One sequence of 260001 entries, 32/8 heads: 63 us, 4.7 TB/s; 512 windows of 2052: 44 us, 3.9 TB/s; a
-// call takes 9 us without any work (two kernels).
+// D + 8 D / group bytes per entry, key head (and 16 query heads) have to come from HBM, a third of what 16 bits take.  Neither they nor the
+// issue slots bind: with some 650 instructions per tile of 32 entries and four heads (all included) half of the slots are used, a quarter of
+// the matrix unit, 45 % of HBM.  Each of a scheduler's three warps waits for its own chain from shared memory through a product, the
+// exponent, a pack, a transposition and a product (most stalls: fixed latencies, then loads and the busy matrix unit).  One sequence of
+// 260001 entries, 32/8 heads, groups of 64: 63 us, 4.7 TB/s; 512 windows of 2052: 46 us, 3.7 TB/s; a call takes 9 us without any work (two
+// kernels).  8 sequences of 15000 with two key heads: 8 query heads each 25 us (groups of 64: 22), 12 and 16 36 and 38 (groups of 64: 32).
+// The scales per head and group cost 1 to 2 % of long caches, 5 % of the windows and 7 % of the step of 24 caches, whose runs of four tiles set
+// them anew.
 //
 // A warp keeps kStages - 1 tiles in flight, one bulk copy each.  Work is cut into equal runs of tiles, one per warp, whatever the
 // lengths; items that more than one run has leave parts that a second kernel joins in order: no atomics, the same bits every time.
@@ -30,16 +33,18 @@
 
 namespace {
 
-// Three CTAs of four warps per SM (registers allow no more without spills: two 71 us for one sequence of 260001 entries, three 63,
-// four 66), two for sixteen heads; three (four) tiles per warp in flight.  Every warp has a run of tiles of its own: joining the
-// warps of a CTA at an item's end cost more than the additional parts do.
+// Three CTAs of four warps per SM, two for sixteen heads; three (four) tiles per warp in flight.  (Two 71 us for one sequence of 260001 entries,
+// three 63, four 66, where 128 registers were too few and spilled; taken before the codes were shifted.)  168 and 255 registers are
+// enough but for heads of 128 in four groups: with 5 to 8 query heads a thread spills 44 to 64 bytes, with more than 8 72 to 104, and in two
+// groups with 5 to 8 8 bytes.  Every warp has a run of tiles of its own: joining the warps of a CTA at an item's end cost more than the
+// additional parts do.
 constexpr int kWarps = 4, kThreads = kWarps * 32;
 template <int H> constexpr int kPerSmOf = H == 16 ? 2 : 3;
 template <int H> constexpr int kStagesOf = H == 16 ? 4 : 3;
 constexpr int kRoom = 12;              // p is at most 2^-12, but for scores that have not moved the maximum yet
 constexpr float kOne = 1 << kRoom;
 constexpr float kMostUp = 0x1p126f;    // scale of p s before anything was seen
-constexpr int kPad = 3;                // an item's start and end take about as long as so many tiles (0: 47.7 us for 512 windows of 2052, 3: 41.7, 8: 44.4)
+constexpr int kPad = 3;                // an item's start and end take about as long as so many tiles (0: 47.7 us for 512 windows of 2052, 3: 41.7, 8: 44.4, before the codes were shifted)
 // Units of a run: fewer would leave more parts than they save time (24 x 2 caches of 2049 entries and their eviction: two 28.7 us a
 // step, four 27.3), but with little work the SMs come first (one cache of 1001, 8 heads: two 17.9, four 18.6).
 constexpr int kFewUnits = 2, kManyUnits = 4;
@@ -589,7 +594,7 @@ __global__ void __launch_bounds__(kThreads, kPerSmOf<H>) decode4_kernel(const De
             // Every sum also gets -8 times (upper nibbles: -128 times) the sum of its rounded p s, which a product with constants gives: with
             // codes around zero it stays small, and so do what the matrix unit cuts off of it and what the rounding of p s leaves
             // (2052 entries, f16: error 2.6e-4 instead of 4.7e-4; 260001, bf16: 1.7e-3 instead of 4.5e-3).  In the products
-            // themselves, as one more each, it costs 5 us of 68 for one sequence of 260001.
+            // themselves, as one more each, it cost 5 us of 68 for one sequence of 260001.
             auto codes = [&](uint32_t w, int n) { return n & 1 ? si_q4::high_codes(w >> 4 * (n & 2)) : si_q4::low_codes(w >> 4 * (n & 2)); };
             constexpr uint32_t kEight = 0x80088008u;           // a pair of -8 2^-24
             const uint32_t eight[4] = {kEight, kEight, kEight, kEight};

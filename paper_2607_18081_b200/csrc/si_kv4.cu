@@ -1,9 +1,9 @@
 // The key/value cache in 4 bits: quantising entries as they are stored, reading them back, eviction.  (Layout and format: si_kv4.cuh.)
 //
-// All three are bound by HBM: an entry is 4 D bytes in 16 bits and D + 8 D / group in 4.  Measured: 65000 entries of eight heads of 128 read
-// back in 58 us (6.0 TB/s of the two sides together); a prompt of 8192 tokens stored in 9 us (4.9 TB/s; the issue slots are two
-// thirds busy, half of it the codes); 2048 of 16384 entries of 128 heads moved in 19 us (a value's cell holds its neighbour too, so
-// 256 bytes are read for 160).
+// An entry is 4 D bytes in 16 bits and D + 8 D / group in 4.  Measured: 65000 entries of eight heads of 128 read back in 58 us (6.0 TB/s of the
+// two sides together: bound by HBM); a prompt of 8192 tokens stored in 9 us (4.9 TB/s; the issue slots are two thirds busy, half of it the
+// codes, and the warps are a wave and a half); 2048 of 16384 entries of 128 heads moved in 19 us (bound by the latency of scattered
+// reads: a value's cell holds its neighbour too, so 256 bytes are read for 160).
 #include "si_evict.cuh"
 #include "si_tc.cuh"
 
